@@ -346,9 +346,102 @@ int mxq_linear_batch_info(const mxq_linear_desc *descs, int count, int M, int32_
  * tiles that CTA had not finished are NaN.  unit = -1, wait_us = 0 cancels. */
 int mxq_debug_batch_fault(int unit, unsigned wait_us);
 
+/* ---- a 4-bit key/value cache --------------------------------------------------------------------------------------------
+ * What a decoder step needs beside its linear layers: attention over what was decoded so far, with K and V held as MXFP4
+ * pairs (the cast of mxq_quantize along the head dimension, 4.25 bits per element) in pages that sequences share, branch
+ * and give back as speculation goes (Sec. III-A: tokens after the first mismatch are dropped; the paper names the
+ * quantised key/value cache as work to come).
+ *
+ * The cache is a pool of `num_pages` pages of `page_tokens` tokens, owned by the caller:
+ *   pages  uint8 [layers][num_pages][page_tokens / 32][kv_heads][tile]  (mxq_kv_page_bytes per layer and page)
+ *   refs   int32 [num_pages]: how many sequences hold the page; 0 = free.  Zero it once; only mxq_kv_resize and mxq_kv_fork
+ *          write it
+ *   tile   32 tokens of one head, nb = head_dim / 32 blocks per row:
+ *            K codes [32][head_dim / 2]  byte c*4*nb + 4*j + i of a row = byte 16*j + 4*c + i of the row in natural order
+ *            V codes [32][head_dim / 2]  byte g*2*nb + 2*j + i of a row = byte 16*j + 2*g + i of the row in natural order
+ *            K scales [32][nb]
+ *            V scales [32 * nb]          token 16*u + tig + 4*e + 8*h, block j at 16*nb*u + 4*nb*tig + 2*nb*h + 2*j + e
+ *          (the natural order, and the values, are those of `codes` and `scales` above; mxq_kv_read gives them back)
+ * A page is the same in every layer: one page table serves all of them.  The cache needs no initialisation but refs.
+ *
+ * The sequences of a call, all in device memory:
+ *   tables int32 [B][W]: page of tokens w*page_tokens .. of sequence b; -1 = none.  Tokens on an entry that is no page of
+ *          the pool are left out by every call
+ *   lens   int32 [B]: tokens of the sequence, those of this call's rows included (values outside 0..W*page_tokens count
+ *          as the nearest end)
+ *   rows   int32 [B] or NULL: how many of the call's M token rows sequence b has (NULL: all M); row i of sequence b is the
+ *          token at position lens[b] - rows[b] + i.  Rows beyond rows[b] are ignored as input and zero as output
+ * 1 <= B <= MXQ_KV_MAX_SEQS, W >= 1, B * W <= 2^30, head_dim 64 or 128, page_tokens 32, 64, 128 or 256 (MXQ_ERR_SHAPE
+ * otherwise).  `cache` is a HOST struct read during the call; int32 and float arrays need their own alignment only,
+ * everything else 16 bytes. */
+#define MXQ_KV_MAX_SEQS 4096
+#define MXQ_KV_MAX_HEADS 256
+#define MXQ_KV_MAX_PAGES (1 << 24)
+typedef struct mxq_kv_cache {
+    void *pages;
+    int32_t *refs;
+    int64_t num_pages;
+    int32_t layers, kv_heads, head_dim, page_tokens;
+} mxq_kv_cache;
+
+/* Bytes of one page of one layer (32-token tiles of 34 * head_dim bytes); 0 if the shape is invalid. */
+size_t mxq_kv_page_bytes(int kv_heads, int head_dim, int page_tokens);
+
+/* Casts the M new K and V rows of every sequence into their places in one layer.  K_bf16, V_bf16 [B][M][kv_heads][head_dim]
+ * BF16, token rows k_stride / v_stride elements apart (>= kv_heads * head_dim, a multiple of 8: a column slice of a fused
+ * projection's output will do).  Same cast as mxq_quantize (a block with an Inf or NaN becomes scale 0xFF, codes 0).  The
+ * pages written must not be shared (mxq_kv_fork copies the one that would be).  B * M * kv_heads <= 2^29. */
+int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int64_t k_stride, const void *V_bf16, int64_t v_stride,
+                  int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows, void *stream);
+
+/* The inverse: K_bf16, V_bf16 [B][M][kv_heads][head_dim] receive what the cache holds for those rows, exactly (zero for a
+ * row that is not there).  For tools, tests, and for handing a cached prefix to something else. */
+int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16, int B, int M, const int32_t *tables, int W,
+                const int32_t *lens, const int32_t *rows, void *stream);
+
+/* Attention of M token rows per sequence over one layer of the cache, whose last rows[b] tokens are these rows:
+ *     O[b][i][h] = sum_t w_t v^[t][h / g] / sum_t w_t,   w_t = exp(scale * Q[b][i][h] . k^[t][h / g]),   g = q_heads / kv_heads,
+ * over the tokens row i sees: with tree == NULL those up to its own (t <= lens[b] - rows[b] + i); with tree, uint64 [B][M]
+ * (M <= 64), all tokens before the rows and those rows j whose bit j is set in tree[b][i].
+ *   Q_bf16  [B][M][q_heads][head_dim] BF16, token rows q_stride elements apart (as in mxq_kv_append)
+ *   O_bf16  [B][M][q_heads][head_dim] BF16;  lse  float [B][M][q_heads], ln of the sum of w_t, or NULL
+ * A row that sees no token gives O = 0 and lse = -inf; tokens a row does not see do not touch it, whatever they hold.
+ * Scores, maxima, sums and the accumulators are FP32; each weight is rounded to 11 bits before it meets V, so that
+ * |O - exact| <= 2^-10 * sum_t w_t |v^_t| / sum_t w_t + BF16's rounding.  Bit-reproducible run to run for given lengths.
+ *   workspace  device memory, >= mxq_kv_attention_workspace_bytes, 16-byte aligned; zero its first 4096 bytes once before
+ *              the first use, every call leaves them zero again; one per stream. */
+size_t mxq_kv_attention_workspace_bytes(int B, int M, int q_heads, int kv_heads, int head_dim);
+int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, int64_t q_stride, int B, int M, int q_heads,
+                     const int32_t *tables, int W, const int32_t *lens, const int32_t *rows, const uint64_t *tree, float scale,
+                     void *O_bf16, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gives and takes pages so that sequence b holds new_lens[b] tokens, and sets lens[b] to it: growth before the append,
+ * rollback after the verification, 0 to free the sequence.  Pages behind the new end lose this sequence's reference
+ * (entry -1); then the pages wanted are taken in order of (sequence, place) from the free pages in order of their index, the
+ * ones just released among them.  From the first sequence on whose pages do not fit any more, no sequence gets pages: one
+ * that wants some keeps its old length and pages (lens[b] != new_lens[b] tells).  The same for a new length outside
+ * 0..W*page_tokens. */
+int mxq_kv_resize(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_t *lens, const int32_t *new_lens, void *stream);
+
+/* Makes slots dst[0..n) copies of the sequences in slots src[0..n) (int32, device; slots of tables / lens): whole pages are
+ * shared, a last page that is partly filled is copied in every layer to the lowest free page, in order of i.  A slot dst[i]
+ * that is not empty (lens != 0), a pair out of range, or a child whose page is not there any more is left out (lens of
+ * the slot stays).  All dst must be distinct and none may be a src of the same call.
+ *   workspace  device memory, >= mxq_kv_fork_workspace_bytes(n), 16-byte aligned, no initialisation; one per stream. */
+size_t mxq_kv_fork_workspace_bytes(int n);
+int mxq_kv_fork(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_t *lens, int n, const int32_t *src, const int32_t *dst,
+                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Cuts the last rows[b] tokens of every sequence (a verified token tree) down to its accepted path: the token of row
+ * keep[b][j] moves to the place of row j, j < kept[b], in all layers and heads.  keep int32 [B][M], ascending in each row,
+ * 0 <= keep < rows[b]; kept int32 [B]; 1 <= M <= 64.  lens_out[b] (an array of its own) = lens[b] - rows[b] + kept[b]; lens stays, so that
+ * mxq_kv_resize(lens, lens_out) then gives back the pages behind it.  The pages of the rows must not be shared. */
+int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows,
+                   const int32_t *keep, const int32_t *kept, int32_t *lens_out, void *stream);
+
 /* The bounds-checked build (the library compiled with -DMXQ_DEBUG_BOUNDS; python -m paper_2503_13565_b200.build
  * --checked writes it to libmxq_checked.so): in the linear kernels (mxq_linear with every kernel choice, the layer
- * epilogues, mxq_lm_head_accept, mxq_linear_batch, mxq_linear_bf16) every plain load and store of global memory whose
+ * epilogues, mxq_lm_head_accept, mxq_linear_batch, mxq_linear_bf16) and those of the key/value cache every plain load and store of global memory whose
  * address is formed from an index -- X, codes, scales, Y, residual, workspace images, partial sums, correction lists,
  * tickets -- is tested against its buffer first.  An access outside it is counted, the first one recorded, and the
  * access itself redirected to a scratch area: a wrong index shows as a report, never as a fault.  (TMA copies are
@@ -356,7 +449,8 @@ int mxq_debug_batch_fault(int unit, unsigned wait_us);
  * ragged-shape tests where no memory checker is at hand.
  * mxq_debug_bounds_report: report[0] = 1 if this library is the checked build (else 0 and the rest stays 0);
  *   report[1] = accesses refused since the last call; of the first one: report[2] = source file (0 mxq_linear.cu, 1
- *   mxq_linear_umma.cu, 2 mxq_linear_fp4.cu, 3 mxq_linear_mma.cu, 4 mxq_linear_batch.cu, 5 mxq_linear_bf16.cu),
+ *   mxq_linear_umma.cu, 2 mxq_linear_fp4.cu, 3 mxq_linear_mma.cu, 4 mxq_linear_batch.cu, 5 mxq_linear_bf16.cu, 6 mxq_kv_cache.cu,
+ *   7 mxq_kv_pages.cu, 8 mxq_kv_attention.cu),
  *   report[3] = source line, report[4] = byte offset from the buffer's base (modulo 2^64), report[5] = the buffer's size.
  *   Reading clears the record.  Synchronises with the device.
  * mxq_debug_bounds_selftest: checked build only (otherwise MXQ_ERR_SHAPE): one kernel stores 4 bytes at offset 100

@@ -99,6 +99,24 @@ def lib() -> ctypes.CDLL:
             L.mxq_debug_bounds_report.argtypes = [vp]
             L.mxq_debug_bounds_selftest.restype = i32
             L.mxq_debug_bounds_selftest.argtypes = [vp]
+            L.mxq_kv_page_bytes.restype = sz
+            L.mxq_kv_page_bytes.argtypes = [i32, i32, i32]
+            L.mxq_kv_append.restype = i32
+            L.mxq_kv_append.argtypes = [vp, i32, vp, i64, vp, i64, i32, i32, vp, i32, vp, vp, vp]
+            L.mxq_kv_read.restype = i32
+            L.mxq_kv_read.argtypes = [vp, i32, vp, vp, i32, i32, vp, i32, vp, vp, vp]
+            L.mxq_kv_attention_workspace_bytes.restype = sz
+            L.mxq_kv_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+            L.mxq_kv_attention.restype = i32
+            L.mxq_kv_attention.argtypes = [vp, i32, vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz, vp]
+            L.mxq_kv_resize.restype = i32
+            L.mxq_kv_resize.argtypes = [vp, i32, vp, i32, vp, vp, vp]
+            L.mxq_kv_fork_workspace_bytes.restype = sz
+            L.mxq_kv_fork_workspace_bytes.argtypes = [i32]
+            L.mxq_kv_fork.restype = i32
+            L.mxq_kv_fork.argtypes = [vp, i32, vp, i32, vp, i32, vp, vp, vp, sz, vp]
+            L.mxq_kv_compact.restype = i32
+            L.mxq_kv_compact.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
             L.mxq_debug_batch_fault.restype = i32
             L.mxq_debug_batch_fault.argtypes = [i32, ctypes.c_uint]
             _lib = L
@@ -545,11 +563,177 @@ class IndependentBatches:
             cur.wait_event(join)
 
 
+# ---- a 4-bit key/value cache --------------------------------------------------------------------
+
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("layers", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
+def mxq_kv_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    return int(lib().mxq_kv_page_bytes(kv_heads, head_dim, page_tokens))
+
+
+class KVCache:
+    """A pool of 4-bit key/value pages (layout: mxq_kv_cache in mxq.h) and their reference counts, marshalled once.
+    ``pages`` uint8 [layers, num_pages, page bytes] and ``refs`` int32 [num_pages] (zero = free) are the caller's tensors;
+    ``KVCache.new`` makes both.  Page tables int32 [B, W] (-1 = none) and lengths int32 [B] are passed to the calls:
+    ``new_sequences`` makes empty ones."""
+
+    def __init__(self, pages: torch.Tensor, refs: torch.Tensor, kv_heads: int, head_dim: int, page_tokens: int):
+        if pages.dim() != 3 or pages.shape[2] != mxq_kv_page_bytes(kv_heads, head_dim, page_tokens):
+            raise ValueError("pages must be [layers, num_pages, mxq_kv_page_bytes(kv_heads, head_dim, page_tokens)]")
+        if tuple(refs.shape) != (pages.shape[1],):
+            raise ValueError("refs must be [num_pages]")
+        self.pages, self.refs = pages, refs
+        self.layers, self.num_pages = int(pages.shape[0]), int(pages.shape[1])
+        self.kv_heads, self.head_dim, self.page_tokens = int(kv_heads), int(head_dim), int(page_tokens)
+        self._struct = _KvCacheStruct(_dev(pages, torch.uint8, "pages"), _dev(refs, torch.int32, "refs"), self.num_pages, self.layers,
+                                      self.kv_heads, self.head_dim, self.page_tokens)
+        self.ptr = ctypes.addressof(self._struct)
+
+    @classmethod
+    def new(cls, layers: int, num_pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, device="cuda") -> "KVCache":
+        nbytes = mxq_kv_page_bytes(kv_heads, head_dim, page_tokens)
+        if nbytes == 0:
+            raise ValueError("no such page: kv_heads %d, head_dim %d, page_tokens %d" % (kv_heads, head_dim, page_tokens))
+        return cls(torch.empty((layers, num_pages, nbytes), dtype=torch.uint8, device=device),
+                   torch.zeros(num_pages, dtype=torch.int32, device=device), kv_heads, head_dim, page_tokens)
+
+    def new_sequences(self, batch: int, max_tokens: int):
+        """Page tables [batch, pages for max_tokens] and lengths [batch] of empty sequences."""
+        width = max(1, -(-int(max_tokens) // self.page_tokens))
+        return (torch.full((batch, width), -1, dtype=torch.int32, device=self.pages.device),
+                torch.zeros(batch, dtype=torch.int32, device=self.pages.device))
+
+
+def _kv_seqs(tables, lens):
+    """(B, tables, W, lens) for a call, shapes checked."""
+    b, w = tables.shape
+    if tuple(lens.shape) != (b,):
+        raise ValueError("tables must be [B, W] and lens [B]")
+    return b, _dev(tables, torch.int32, "tables"), w, _dev(lens, torch.int32, "lens")
+
+
+def _kv_ints(t, shape, what: str) -> int:
+    if t is None:
+        return 0
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must be %s" % (what, list(shape)))
+    return _dev(t, torch.int32, what)
+
+
+def _token_rows(t: torch.Tensor, shape, what: str):
+    """Pointer and token-row stride (elements) of a BF16 [B, M, heads, D] tensor whose heads lie together: contiguous, or a
+    column slice of a fused projection's output."""
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must be %s" % (what, list(shape)))
+    b, m, h, d = shape
+    sb, sm, sh, sd = t.stride()
+    stride = sm if m > 1 else (sb if b > 1 else h * d)
+    if not t.is_cuda or t.dtype != torch.bfloat16 or sd != 1 or (h > 1 and sh != d) or (b > 1 and sb != m * stride):
+        raise TypeError("%s must be a CUDA tensor of dtype torch.bfloat16 with contiguous heads and one stride between token rows" % what)
+    return t.data_ptr(), stride
+
+
+def mxq_kv_append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor,
+                  rows: torch.Tensor = None, stream=None) -> None:
+    """Cast the new rows k, v [B, M, kv_heads, D] BF16 into one layer of the cache: row i of sequence b is the token at
+    position lens[b] - rows[b] + i (rows None: all M).  ``lens`` counts the new rows (mxq_kv_resize has made the room)."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    m = k.shape[1]
+    shape = (b, m, cache.kv_heads, cache.head_dim)
+    kp, ks = _token_rows(k, shape, "k")
+    vp, vs = _token_rows(v, shape, "v")
+    _check(lib().mxq_kv_append(cache.ptr, layer, kp, ks, vp, vs, b, m, tp, w, lp, _kv_ints(rows, (b,), "rows"), _stream(stream)), "mxq_kv_append")
+
+
+def mxq_kv_read(cache: KVCache, layer: int, tables: torch.Tensor, lens: torch.Tensor, m: int, rows: torch.Tensor = None, stream=None):
+    """What one layer of the cache holds for the last ``m`` (or rows[b]) tokens of every sequence: K, V [B, m, kv_heads, D]
+    BF16, exactly; zero where there is no such token."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    k = torch.empty((b, m, cache.kv_heads, cache.head_dim), dtype=torch.bfloat16, device=tables.device)
+    v = torch.empty_like(k)
+    _check(lib().mxq_kv_read(cache.ptr, layer, k.data_ptr(), v.data_ptr(), b, m, tp, w, lp, _kv_ints(rows, (b,), "rows"), _stream(stream)), "mxq_kv_read")
+    return k, v
+
+
+def mxq_kv_attention_workspace_bytes(b: int, m: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().mxq_kv_attention_workspace_bytes(b, m, q_heads, kv_heads, head_dim))
+
+
+def mxq_kv_attention(q: torch.Tensor, cache: KVCache, layer: int, tables: torch.Tensor, lens: torch.Tensor, rows: torch.Tensor = None,
+                     tree: torch.Tensor = None, scale: float = None, out: torch.Tensor = None, lse: torch.Tensor = None,
+                     workspace: torch.Tensor = None, with_lse: bool = False, stream=None):
+    """Attention of the rows q [B, M, q_heads, D] BF16 over one layer of the cache, whose last rows[b] tokens they are (see
+    mxq.h).  ``tree`` int64 [B, M] (bits as uint64): which of the rows each row sees, itself included; None: causal.
+    ``scale`` defaults to D ** -0.5.  Returns O [B, M, q_heads, D] BF16, with ``with_lse`` also lse [B, M, q_heads] FP32.
+    ``workspace``: from ``new_workspace(mxq_kv_attention_workspace_bytes(...))``, zero-filled once, one per stream."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    m, hq, d = q.shape[1], q.shape[2], cache.head_dim
+    qp, qs = _token_rows(q, (b, m, hq, d), "q")
+    if out is None:
+        out = torch.empty((b, m, hq, d), dtype=torch.bfloat16, device=q.device)
+    elif tuple(out.shape) != (b, m, hq, d):
+        raise ValueError("out must be [B, M, q_heads, D]")
+    if with_lse and lse is None:
+        lse = torch.empty((b, m, hq), dtype=torch.float32, device=q.device)
+    if lse is not None and tuple(lse.shape) != (b, m, hq):
+        raise ValueError("lse must be [B, M, q_heads]")
+    if tree is not None and tuple(tree.shape) != (b, m):
+        raise ValueError("tree must be [B, M]")
+    if workspace is None:
+        workspace = new_workspace(mxq_kv_attention_workspace_bytes(b, m, hq, cache.kv_heads, d), q.device)
+    _check(lib().mxq_kv_attention(cache.ptr, layer, qp, qs, b, m, hq, tp, w, lp, _kv_ints(rows, (b,), "rows"),
+                                  0 if tree is None else _dev(tree, torch.int64, "tree"), d ** -0.5 if scale is None else scale,
+                                  _dev(out, torch.bfloat16, "out"), 0 if lse is None else _dev(lse, torch.float32, "lse"),
+                                  _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_kv_attention")
+    return (out, lse) if with_lse else out
+
+
+def mxq_kv_resize(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, new_lens: torch.Tensor, stream=None) -> None:
+    """Give and take pages so that every sequence holds new_lens[b] tokens (0 frees it); ``tables``, ``lens`` and the cache's
+    ``refs`` are updated.  Where the pool has no room lens[b] stays (see mxq.h)."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    _check(lib().mxq_kv_resize(cache.ptr, b, tp, w, lp, _kv_ints(new_lens, (b,), "new_lens"), _stream(stream)), "mxq_kv_resize")
+
+
+def mxq_kv_fork_workspace_bytes(n: int) -> int:
+    return int(lib().mxq_kv_fork_workspace_bytes(n))
+
+
+def mxq_kv_fork(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, src: torch.Tensor, dst: torch.Tensor,
+                workspace: torch.Tensor = None, stream=None) -> None:
+    """Make the empty slots dst [n] int32 copies of the sequences in slots src [n]: whole pages are shared, a partly filled
+    last page is copied in every layer (see mxq.h)."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    n = int(src.shape[0])
+    if workspace is None:
+        workspace = new_workspace(mxq_kv_fork_workspace_bytes(n), tables.device)
+    _check(lib().mxq_kv_fork(cache.ptr, b, tp, w, lp, n, _kv_ints(src, (n,), "src"), _kv_ints(dst, (n,), "dst"),
+                             _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_kv_fork")
+
+
+def mxq_kv_compact(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, rows: torch.Tensor, keep: torch.Tensor, kept: torch.Tensor,
+                   lens_out: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Cut the last rows[b] tokens (None: all keep.shape[1]) down to the rows keep[b][0..kept[b]) (int32 [B, M], ascending) in
+    every layer; returns lens_out [B] = lens - rows + kept for the mxq_kv_resize that follows."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    m = int(keep.shape[1])
+    if lens_out is None:
+        lens_out = torch.empty(b, dtype=torch.int32, device=tables.device)
+    _check(lib().mxq_kv_compact(cache.ptr, b, m, tp, w, lp, _kv_ints(rows, (b,), "rows"), _kv_ints(keep, (b, m), "keep"),
+                                _kv_ints(kept, (b,), "kept"), _kv_ints(lens_out, (b,), "lens_out"), _stream(stream)), "mxq_kv_compact")
+    return lens_out
+
+
 def mxq_debug_bounds_report() -> dict:
     """What the bounds-checked build has refused since the last call (see mxq.h); ``checked`` is False for the ordinary build."""
     r = (ctypes.c_uint64 * 6)()
     _check(lib().mxq_debug_bounds_report(ctypes.cast(r, ctypes.c_void_p)), "mxq_debug_bounds_report")
-    files = ("mxq_linear.cu", "mxq_linear_umma.cu", "mxq_linear_fp4.cu", "mxq_linear_mma.cu", "mxq_linear_batch.cu", "mxq_linear_bf16.cu")
+    files = ("mxq_linear.cu", "mxq_linear_umma.cu", "mxq_linear_fp4.cu", "mxq_linear_mma.cu", "mxq_linear_batch.cu", "mxq_linear_bf16.cu",
+             "mxq_kv_cache.cu", "mxq_kv_pages.cu", "mxq_kv_attention.cu")
     out = {"checked": bool(r[0]), "refused": int(r[1])}
     if r[1]:
         out.update(file=files[int(r[2])], line=int(r[3]), offset=int(r[4]), extent=int(r[5]))

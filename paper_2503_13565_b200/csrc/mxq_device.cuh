@@ -124,6 +124,44 @@ __device__ __forceinline__ uint32_t float2_to_e2m1x2(float lo, float hi) {
     return out;
 }
 
+// ---- the direct cast ---------------------------------------------------------------------
+// Cast the 8 BF16 values of one chunk given the block's scale byte; returns 8 packed codes.
+// The kernels that cast are streams of 2.5 bytes per weight, so the integer pipe must not spend more than a few
+// instructions per weight: the conversion instruction takes the sign along (a negative value that rounds to zero gives the
+// code of -0, as the cast requires).
+__device__ __forceinline__ uint32_t cast_chunk(const uint4 &v, float inv_x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float lo[4], hi[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        lo[j] = __uint_as_float(w[j] << 16) * inv_x;            // element 2j
+        hi[j] = __uint_as_float(w[j] & 0xFFFF0000u) * inv_x;    // element 2j+1
+    }
+    // round-to-nearest-even, clamp, sign kept; the bytes are packed with multiply-adds, which run on the other pipe
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = float2_to_e2m1x2(lo[j], hi[j]);
+    uint32_t out;
+    asm("{\n\t.reg .u32 t;\n\tmad.lo.u32 t, %2, 256, %1;\n\tmad.lo.u32 t, %3, 65536, t;\n\tmad.lo.u32 %0, %4, 16777216, t;\n\t}"
+        : "=r"(out)
+        : "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
+    return out;
+}
+
+// largest magnitude pattern (15 bits, in both halves of the result's halves) among the 8 BF16 values of a chunk: for
+// finite BF16 the magnitude bits order like the values; two values per instruction
+__device__ __forceinline__ uint32_t chunk_max2(const uint4 &v) {
+    const uint32_t m = 0x7FFF7FFFu;
+    return __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
+}
+
+// scale byte of a block whose largest magnitude pattern (15 bits) is `a`: floor(log2 max) - 2 + 127, clamped at 0 (also
+// covers subnormal and zero maxima); 0xFF if the block holds an Inf or a NaN (they sort above every finite pattern)
+__device__ __forceinline__ uint32_t scale_byte(uint32_t a) {
+    const uint32_t efield = a >> 7;   // biased exponent of the block maximum
+    return efield == 0xFFu ? 0xFFu : (efield > 2u ? efield - 2u : 0u);
+}
+
 __device__ __forceinline__ float bf16_bits_to_float(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
 
 __device__ __forceinline__ float warp_sum(float v) {

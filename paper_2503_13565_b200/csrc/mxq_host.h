@@ -78,7 +78,7 @@ int linear_mma_take_status(uint32_t *out);    // the mma.sync kernel (mxq_linear
 int linear_batch_take_status(uint32_t *out);  // the persistent multi-layer kernel (mxq_linear_batch.cu)
 int linear_bf16_take_status(uint32_t *out);   // the BF16-weight comparison kernel (mxq_linear_bf16.cu)
 
-// Bounds-checked build (-DMXQ_DEBUG_BOUNDS): every translation unit with linear kernels keeps a record of global accesses
+// Bounds-checked build (-DMXQ_DEBUG_BOUNDS): every translation unit with linear or cache kernels keeps a record of global accesses
 // that fell outside their buffer (out[0] = how many; of the first: out[1] source line, out[2] byte offset, out[3] extent);
 // reading clears it.  In the ordinary build the functions report zeros.
 int bounds_take_linear(unsigned long long *out);        // mxq_linear.cu
@@ -87,5 +87,8 @@ int bounds_take_linear_fp4(unsigned long long *out);    // mxq_linear_fp4.cu
 int bounds_take_linear_mma(unsigned long long *out);    // mxq_linear_mma.cu
 int bounds_take_linear_batch(unsigned long long *out);  // mxq_linear_batch.cu
 int bounds_take_linear_bf16(unsigned long long *out);   // mxq_linear_bf16.cu
+int bounds_take_kv_cache(unsigned long long *out);      // mxq_kv_cache.cu
+int bounds_take_kv_pages(unsigned long long *out);      // mxq_kv_pages.cu
+int bounds_take_kv_attention(unsigned long long *out);  // mxq_kv_attention.cu
 
 }  // namespace mxq

@@ -1,0 +1,250 @@
+// mxq_kv_append / mxq_kv_read: the direct cast of new K and V rows into the pages of a 4-bit cache, and its inverse.
+//
+// Both are streams: 2 bytes of BF16 against 0.53 bytes of codes and scales per element, in opposite directions.  Four
+// lanes share a row: lane c takes elements 8c..8c+7 of every MX block (16-byte accesses, 64 consecutive bytes per quad),
+// the quad agrees on the blocks' maxima with two exchanges (two blocks per register), and the permutation of the layout
+// (mxq_kv.cuh) makes the lane's codes of the row ONE store: K wants word c of every block side by side, V its halfwords.
+#include "mxq_kv.cuh"
+
+namespace mxq {
+
+constexpr int kKvThreads = 128;
+
+struct RowPlace {
+    uint8_t *tile;   // nullptr: no such row
+    int slot;        // token in the tile
+};
+
+// where row i of sequence b lives: position len - rows + i
+template <int D>
+__device__ __forceinline__ RowPlace row_place(const KvView &c, const KvSeqs &s, int b, int i, int head) {
+    RowPlace p = {nullptr, 0};
+    const int rows = s.nrows(b), pos = s.len(b) - rows + i;
+    if (i >= rows || pos < 0) return p;
+    const int page = s.page(b, pos >> c.page_shift);
+    if (!kv_page_ok(c, page)) return p;
+    const int slot = pos & ((1 << c.page_shift) - 1);
+    p.tile = kv_tile<D>(c, page, slot, head);
+    p.slot = slot & (kTileTokens - 1);
+    return p;
+}
+
+struct KvRows {   // the BF16 side: [B][M][heads][D], token rows `stride` elements apart
+    const uint16_t *k, *v;
+    int64_t k_stride, v_stride;
+};
+
+// grid.x covers (sequence, row, head, quarter); grid.y: 0 = K, 1 = V
+template <int D>
+__global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs s, KvRows in, uint32_t total) {
+    using T = KvTile<D>;
+    constexpr int kNb = T::kNb;
+    pdl_trigger();
+    const uint32_t idx = blockIdx.x * kKvThreads + threadIdx.x;
+    const uint32_t q = idx & 3u, rowhead = idx >> 2, row = rowhead / (uint32_t)c.heads, head = rowhead - row * (uint32_t)c.heads;
+    const bool value = blockIdx.y != 0;
+    const bool live = idx < total;   // (the quads of a warp leave together: total is a multiple of 4)
+    const int b = live ? (int)(row / (uint32_t)s.m) : 0, i = live ? (int)(row - (uint32_t)b * (uint32_t)s.m) : 0;
+    pdl_wait();
+    RowPlace at = {nullptr, 0};
+    uint4 x[kNb];
+    if (live) {
+        const int64_t stride = value ? in.v_stride : in.k_stride;
+        const uint16_t *base = value ? in.v : in.k;
+        const uint16_t *src = base + (int64_t)row * stride + (int64_t)head * D;
+#pragma unroll
+        for (int j = 0; j < kNb; ++j)
+            x[j] = ld_dep_u4(MXQ_AT(src + 32 * j + 8 * q, 16, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
+        at = row_place<D>(c, s, b, i, (int)head);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) x[j] = make_uint4(0, 0, 0, 0);
+    }
+    // maxima of blocks 2p and 2p + 1 in the halves of one register
+    uint32_t top[kNb / 2];
+#pragma unroll
+    for (int p = 0; p < kNb / 2; ++p) {
+        const uint32_t a = chunk_max2(x[2 * p]), d = chunk_max2(x[2 * p + 1]);
+        top[p] = __vmaxu2(__byte_perm(a, d, 0x5410), __byte_perm(a, d, 0x7632));
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) top[p] = __vmaxu2(top[p], __shfl_xor_sync(0xffffffffu, top[p], o));
+    }
+    uint32_t w[kNb], scale = 0;
+#pragma unroll
+    for (int j = 0; j < kNb; ++j) {
+        const uint32_t byte = scale_byte((top[j / 2] >> (16 * (j & 1))) & 0xFFFFu);
+        w[j] = byte == 0xFFu ? 0u : cast_chunk(x[j], __uint_as_float((254u - byte) << 23));
+        scale |= byte << (8 * j);
+    }
+    if (at.tile == nullptr) return;
+    uint32_t out[kNb];
+    if (!value) {
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) out[j] = w[j];
+    } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
+#pragma unroll
+        for (int p = 0; p < kNb / 2; ++p) {
+            out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
+            out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
+        }
+    }
+    uint8_t *dst = at.tile + (value ? T::kV : 0) + at.slot * T::kRow + q * 4 * kNb;
+    dst = MXQ_AT(dst, 4 * kNb, c.pool, c.pool_bytes);
+    if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+    else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
+    if (!value) {
+        if (q == 0) {
+            uint8_t *sc = MXQ_AT(at.tile + T::kKs + at.slot * kNb, kNb, c.pool, c.pool_bytes);
+            if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
+            else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
+        }
+    } else if (q < kNb) {
+        *MXQ_AT(at.tile + T::vs(at.slot, (int)q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * q));
+    }
+}
+
+// eight codes (natural order) under one scale -> eight BF16 values
+__device__ __forceinline__ uint4 codes_to_bf16(uint32_t w, float s) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(e2m1x2_to_half2((w >> (8 * i)) & 0xFFu));
+        // at most two significant bits times a power of two: the FP32 product is exact and its upper half is the BF16 number
+        o[i] = (__float_as_uint(f.x * s) >> 16) | (__float_as_uint(f.y * s) & 0xFFFF0000u);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kKvThreads) kv_read_kernel(KvView c, KvSeqs s, uint16_t *K, uint16_t *V, uint32_t total) {
+    using T = KvTile<D>;
+    constexpr int kNb = T::kNb;
+    pdl_trigger();
+    const uint32_t idx = blockIdx.x * kKvThreads + threadIdx.x;
+    if (idx >= total) return;
+    const uint32_t q = idx & 3u, rowhead = idx >> 2, row = rowhead / (uint32_t)c.heads, head = rowhead - row * (uint32_t)c.heads;
+    const bool value = blockIdx.y != 0;
+    const int b = (int)(row / (uint32_t)s.m), i = (int)(row - (uint32_t)b * (uint32_t)s.m);
+    pdl_wait();
+    const RowPlace at = row_place<D>(c, s, b, i, (int)head);
+    uint4 out[kNb];
+    if (at.tile == nullptr) {
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) out[j] = make_uint4(0, 0, 0, 0);
+    } else {
+        const uint8_t *src = at.tile + (value ? T::kV : 0) + at.slot * T::kRow + q * 4 * kNb;
+        src = MXQ_AT(src, 4 * kNb, c.pool, c.pool_bytes);
+        uint32_t w[kNb], n[kNb];
+        if constexpr (kNb == 4) {
+            const uint4 r = ld_dep_u4(src);
+            w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;
+        } else {
+            w[0] = ld_dep_u32(src), w[1] = ld_dep_u32(src + 4);
+        }
+#pragma unroll
+        for (int p = 0; p < kNb / 2; ++p) {
+            n[2 * p] = value ? __byte_perm(w[p], w[kNb / 2 + p], 0x5410) : w[2 * p];
+            n[2 * p + 1] = value ? __byte_perm(w[p], w[kNb / 2 + p], 0x7632) : w[2 * p + 1];
+        }
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) {
+            const uint8_t *sc = at.tile + (value ? T::vs(at.slot, j) : T::kKs + at.slot * kNb + j);
+            unsigned short sb;
+            asm volatile("ld.global.cg.u8 %0, [%1];" : "=h"(sb) : "l"(MXQ_AT(sc, 1, c.pool, c.pool_bytes)) : "memory");
+            out[j] = codes_to_bf16(n[j], e8m0_to_float(sb));
+        }
+    }
+    uint16_t *base = value ? V : K;
+#pragma unroll
+    for (int j = 0; j < kNb; ++j)
+        *reinterpret_cast<uint4 *>(MXQ_AT(base + (int64_t)rowhead * D + 32 * j + 8 * q, 16, base, (int64_t)total / 4 * D * 2)) = out[j];
+}
+
+MXQ_BOUNDS_TU(bounds_take_kv_cache)
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+
+static int log2_pages(int tokens) {
+    for (int s = 5; s <= 8; ++s)
+        if (tokens == 1 << s) return s;
+    return -1;
+}
+
+static size_t tile_bytes(int D) { return D == 128 ? KvTile<128>::kBytes : D == 64 ? KvTile<64>::kBytes : 0; }
+
+int kv_check_cache(const mxq_kv_cache *c, int layer) {
+    if (!c || !c->pages || !c->refs) return MXQ_ERR_NULL;
+    if (mxq_kv_page_bytes(c->kv_heads, c->head_dim, c->page_tokens) == 0 || c->num_pages < 1 || c->num_pages > MXQ_KV_MAX_PAGES ||
+        c->layers < 1 || layer < 0 || layer >= c->layers)
+        return MXQ_ERR_SHAPE;
+    if (!aligned16(c->pages) || !aligned_to(c->refs, 16)) return MXQ_ERR_ALIGN;
+    return MXQ_OK;
+}
+
+int kv_check_seqs(int B, int W, const int32_t *tables, const int32_t *lens) {
+    if (!tables || !lens) return MXQ_ERR_NULL;
+    if (B < 1 || B > MXQ_KV_MAX_SEQS || W < 1 || (int64_t)B * W > ((int64_t)1 << 30)) return MXQ_ERR_SHAPE;
+    if (!aligned_to(tables, 4) || !aligned_to(lens, 4)) return MXQ_ERR_ALIGN;
+    return MXQ_OK;
+}
+
+KvView kv_view(const mxq_kv_cache *c, int layer) {
+    KvView v;
+    v.page_bytes = (int64_t)mxq_kv_page_bytes(c->kv_heads, c->head_dim, c->page_tokens);
+    v.pool = (const uint8_t *)c->pages;
+    v.pool_bytes = v.page_bytes * c->num_pages * c->layers;
+    v.base = (uint8_t *)c->pages + v.page_bytes * c->num_pages * layer;
+    v.num_pages = (int32_t)c->num_pages;
+    v.heads = c->kv_heads;
+    v.page_shift = log2_pages(c->page_tokens);
+    return v;
+}
+
+// rows of one call: at most 2^29 (row, head) pairs, so that a lane's index fits 32 bits
+static bool rows_ok(const mxq_kv_cache *c, int B, int M) { return M >= 1 && (int64_t)B * M <= ((int64_t)1 << 29) / c->kv_heads; }
+
+}  // namespace mxq
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+size_t mxq_kv_page_bytes(int kv_heads, int head_dim, int page_tokens) {
+    const size_t tile = mxq::tile_bytes(head_dim);
+    if (tile == 0 || kv_heads < 1 || kv_heads > MXQ_KV_MAX_HEADS || mxq::log2_pages(page_tokens) < 0) return 0;
+    return tile * (size_t)kv_heads * (size_t)(page_tokens / mxq::kTileTokens);
+}
+
+int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int64_t k_stride, const void *V_bf16, int64_t v_stride,
+                  int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows, void *stream) {
+    if (!K_bf16 || !V_bf16) return MXQ_ERR_NULL;
+    int rc = mxq::kv_check_cache(cache, layer);
+    if (rc == MXQ_OK) rc = mxq::kv_check_seqs(B, W, tables, lens);
+    if (rc != MXQ_OK) return rc;
+    const int64_t width = (int64_t)cache->kv_heads * cache->head_dim;
+    if (!mxq::rows_ok(cache, B, M) || k_stride < width || v_stride < width) return MXQ_ERR_SHAPE;
+    if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || k_stride % 8 || v_stride % 8 || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
+    const uint32_t total = (uint32_t)B * (uint32_t)M * (uint32_t)cache->kv_heads * 4u;
+    const mxq::KvRows in = {(const uint16_t *)K_bf16, (const uint16_t *)V_bf16, k_stride, v_stride};
+    const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
+    const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
+    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_append_kernel<128> : mxq::kv_append_kernel<64>, grid, mxq::kKvThreads, 0,
+                          (cudaStream_t)stream, mxq::kv_view(cache, layer), s, in, total);
+}
+
+int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16, int B, int M, const int32_t *tables, int W,
+                const int32_t *lens, const int32_t *rows, void *stream) {
+    if (!K_bf16 || !V_bf16) return MXQ_ERR_NULL;
+    int rc = mxq::kv_check_cache(cache, layer);
+    if (rc == MXQ_OK) rc = mxq::kv_check_seqs(B, W, tables, lens);
+    if (rc != MXQ_OK) return rc;
+    if (!mxq::rows_ok(cache, B, M)) return MXQ_ERR_SHAPE;
+    if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
+    const uint32_t total = (uint32_t)B * (uint32_t)M * (uint32_t)cache->kv_heads * 4u;
+    const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
+    const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
+    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_read_kernel<128> : mxq::kv_read_kernel<64>, grid, mxq::kKvThreads, 0,
+                          (cudaStream_t)stream, mxq::kv_view(cache, layer), s, (uint16_t *)K_bf16, (uint16_t *)V_bf16, total);
+}
+
+#pragma GCC visibility pop
+}  // extern "C"

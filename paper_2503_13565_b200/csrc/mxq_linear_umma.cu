@@ -857,9 +857,10 @@ int mxq_debug_bounds_report(uint64_t *report) {
 #ifdef MXQ_DEBUG_BOUNDS
     report[0] = 1;
 #endif
-    int (*const take[6])(unsigned long long *) = {mxq::bounds_take_linear,     mxq::bounds_take_linear_umma,  mxq::bounds_take_linear_fp4,
-                                                 mxq::bounds_take_linear_mma, mxq::bounds_take_linear_batch, mxq::bounds_take_linear_bf16};
-    for (int u = 0; u < 6; ++u) {
+    int (*const take[9])(unsigned long long *) = {mxq::bounds_take_linear,     mxq::bounds_take_linear_umma,  mxq::bounds_take_linear_fp4,
+                                                 mxq::bounds_take_linear_mma, mxq::bounds_take_linear_batch, mxq::bounds_take_linear_bf16,
+                                                 mxq::bounds_take_kv_cache,   mxq::bounds_take_kv_pages,     mxq::bounds_take_kv_attention};
+    for (int u = 0; u < 9; ++u) {
         unsigned long long r[4] = {0, 0, 0, 0};
         const int rc = take[u](r);
         if (rc != MXQ_OK) return rc;

@@ -17,36 +17,6 @@ namespace mxq {
 constexpr int kQuantThreads = 256;
 constexpr int kQuantUnroll = 2;  // blocks (64 bytes each) in flight per lane
 
-// Cast the 8 BF16 values of one chunk given the block's scale byte; returns 8 packed codes.
-// The kernel is a stream of 2.5 bytes per weight, so the integer pipe must not spend more than a few instructions
-// per weight: the conversion instruction takes the sign along (a negative value that rounds to zero gives the
-// code of -0, as the cast requires).
-__device__ __forceinline__ uint32_t cast_chunk(const uint4 &v, float inv_x) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float lo[4], hi[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        lo[j] = __uint_as_float(w[j] << 16) * inv_x;            // element 2j
-        hi[j] = __uint_as_float(w[j] & 0xFFFF0000u) * inv_x;    // element 2j+1
-    }
-    // round-to-nearest-even, clamp, sign kept; the bytes are packed with multiply-adds, which run on the other pipe
-    uint32_t c[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = float2_to_e2m1x2(lo[j], hi[j]);
-    uint32_t out;
-    asm("{\n\t.reg .u32 t;\n\tmad.lo.u32 t, %2, 256, %1;\n\tmad.lo.u32 t, %3, 65536, t;\n\tmad.lo.u32 %0, %4, 16777216, t;\n\t}"
-        : "=r"(out)
-        : "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
-    return out;
-}
-
-// largest magnitude pattern (15 bits, in both halves of the result's halves) among the 8 BF16 values of a chunk: for
-// finite BF16 the magnitude bits order like the values; two values per instruction
-__device__ __forceinline__ uint32_t chunk_max2(const uint4 &v) {
-    const uint32_t m = 0x7FFF7FFFu;
-    return __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
-}
-
 __device__ __forceinline__ uint4 ld_nc_u4(const uint4 *p) {   // (cached in L1: the four loads of a lane share sectors with its neighbours')
     uint4 v;
     asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
@@ -77,10 +47,8 @@ quantize_kernel(const uint4 *__restrict__ W, uint4 *__restrict__ codes, uint8_t 
             if (idx[u] < nblocks) {
                 const uint32_t a2 = __vmaxu2(__vmaxu2(chunk_max2(v[u][0]), chunk_max2(v[u][1])), __vmaxu2(chunk_max2(v[u][2]), chunk_max2(v[u][3])));
                 const uint32_t a = max(a2 & 0xFFFFu, a2 >> 16);
-                const uint32_t efield = a >> 7;               // biased exponent of the block maximum
-                const bool nonfinite = efield == 0xFFu;       // Inf/NaN sort above every finite pattern
-                // floor(log2 max) - 2 + 127 = efield - 2; clamped at 0 (also covers subnormal and zero maxima)
-                const uint32_t byte = nonfinite ? 0xFFu : (efield > 2u ? efield - 2u : 0u);
+                const uint32_t byte = scale_byte(a);
+                const bool nonfinite = byte == 0xFFu;
                 // v / X with X = 2^(byte-127): multiply by 2^(127-byte), exact (a power of two; results stay below 8 in
                 // magnitude, and anything that underflows is far below the first rounding boundary)
                 const float inv_x = __uint_as_float((254u - byte) << 23);
