@@ -1,7 +1,31 @@
 // mxq_kv_attention: softmax(scale * q . K^T) . V over the pages of a 4-bit cache.
 //
-// Plain form: one warp per (sequence, token row, query head) walks the tokens with a running maximum and sum in FP32; a lane
-// decodes D / 32 consecutive elements of every K and V row.
+// The mathematics.  A step reads every K and V row of the cache once (D + D / 16 bytes per token and kv head) for a handful
+// of query rows, so the cache's bytes bound it as long as decoding 4-bit codes and the two products keep up with them.
+//   - One pass with a running maximum m and sum l per row (base 2: the softmax scale times log2 e multiplies the score).
+//     The maximum only moves when a score exceeds it by 2^8, so that the warp-wide reduction and the rescaling of the
+//     accumulators happen a few times per sequence, not per tile; weights up to 2^8 are accounted for in the ranges below.
+//   - Both products run on m16n8k16 with the TOKENS (K) or the head dimension (V) as the 16 rows and eight query rows as the
+//     8 columns: a decode step with few rows wastes no half of a 16-row tile.  Codes become FP16 with the conversion
+//     instruction, exactly, without their scales.
+//   - K: S^T[16 tokens][8 rows] += K[16][16 d] . Q^T.  A block of 32 d is two instructions; their sum is scaled per token in
+//     FP32 (the product of codes and q is exact, q being normalised per row by a power of two into FP16, which holds BF16's
+//     8 bits over 2^28 of range below the row's largest element).
+//   - V: O^T[16 d][8 rows] += V^T[16 d][16 tokens] . P^T.  V's scale varies along the contracted tokens and per block of
+//     32 d, so it goes into P: one multiplication of the packed weights per block, shared by the block's two instructions.
+//     FP16 holds P * scale at 11 bits over 2^24 (kHalfRange) between the largest weight times the largest scale met so far (`ref`, an
+//     exponent common to the warp's accumulators) and the smallest.  Weights below that are still right to 11 bits: a tile that has any
+//     adds them in a second product over accumulators scaled up by the width of the first (two tiers).  A tile with weights
+//     or scales spread even wider, or a NaN scale, takes the step in BF16, whose range holds any, with the weights as a sum of two
+//     BF16 numbers.
+//   - S^T leaves the tensor core with a lane holding one token and two rows; the second product wants one row and two
+//     tokens: one 8x8 transposition (movmatrix) per packed register.
+//
+// The split.  Lengths live on the device, so the grid is fixed (as many CTAs as fit) and every CTA takes an equal share
+// of the steps of all (sequence, kv head, row tile) segments, a step being 128 tokens, 32 for each of its four warps.  A warp
+// keeps its own m, l, O and a ring of tiles filled by 16-byte asynchronous copies (no warp waits for another until the segment ends).
+// A segment cut over several CTAs is joined by the last of them to arrive (a ticket; nobody waits), in order of the CTAs:
+// the result does not depend on scheduling.
 #include <math.h>
 
 #include "mxq_kv.cuh"
@@ -16,65 +40,789 @@ struct KvQuery {
     float *lse;              // [B][M][heads] or nullptr
     int32_t heads, group;    // query heads, query heads per kv head
     float scale_log2;        // scale * log2(e)
+    float *partials;         // workspace: two slots per CTA
+    unsigned *tickets;       // one per CTA
 };
 
-template <int D>
-__global__ void __launch_bounds__(128) kv_attention_plain_kernel(KvView c, KvSeqs s, KvQuery a) {
+constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
+constexpr int kAttStages = 2;                  // tiles in a warp's ring
+constexpr int kAttMaxCtas = 1024;              // tickets in the workspace's first 4096 bytes
+constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
+constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
+constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
+constexpr int kHalfRange = kScaleBias + 14;    // a normal number while P * 2^(scale - ref) >= 2^-24
+constexpr int kScaleSpread = 14;               // scales this far below ref still take the FP16 step
+
+// rows of the flattened (token row, head of the group) index per tile of NT column blocks
+template <int NT>
+constexpr int kAttRows = 8 * NT;
+constexpr int kAttRegisterQ = 2;               // up to this NT the query fragments stay in registers
+
+template <int NT>
+constexpr int kAttCtasPerSm = NT == 1 ? 4 : NT == 2 ? 3 : 2;
+template <int D, int NT>
+constexpr size_t kAttSlotFloats = (size_t)kAttRows<NT> * (D + 2);
+template <int D, int NT>
+constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * KvTile<D>::kBytes + (NT > kAttRegisterQ ? (size_t)(D / 32) * NT * 32 * 16 : 0);
+
+// ---- fragments ------------------------------------------------------------------------------------------------------------
+
+// four code bytes -> four pairs of halves
+__device__ __forceinline__ void decode4(uint32_t w, uint32_t (&h)[4]) {
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+}
+template <bool kBf16>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (kBf16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t o;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(o) : "r"(v));
+    return o;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+    uint32_t o;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
+    return o;
+}
+__device__ __forceinline__ uint32_t pack_bf162(float lo, float hi) {
+    uint32_t o;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
+    return o;
+}
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+    uint32_t o;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+__device__ __forceinline__ uint32_t mul_bf162(uint32_t a, uint32_t b) {
+    uint32_t o;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// two scale bytes -> 2^(b - 127) each (0xFF: NaN), exactly
+__device__ __forceinline__ float2 scales2(uint32_t half) {
+    uint32_t o;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.bf16x2.ue8m0x2 %0, l;\n\t}" : "=r"(o) : "r"(half));
+    return make_float2(__uint_as_float(o << 16), __uint_as_float(o & 0xFFFF0000u));
+}
+// x * 2^e for e <= 127 (below -252 as -252) in two steps
+__device__ __forceinline__ float scale_by_power(float x, int e) {
+    const int first = max(e, -126);
+    return x * __uint_as_float((uint32_t)(first + 127) << 23) * __uint_as_float((uint32_t)(max(e - first, -126) + 127) << 23);
+}
+__device__ __forceinline__ uint32_t lds_u32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[N]) {
+    static_assert(N == 1 || N == 2 || N == 4, "");
+    if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
+    else w[0] = lds_u32(a);
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// ---- one segment, as its CTA sees it ----------------------------------------------------------------------------------------
+
+struct Segment {
+    int b, head, r0;         // sequence, kv head, first flattened row of the tile
+    int len, base;           // tokens; tokens before the rows
+    int rows_total;          // flattened rows of the sequence (token rows * group)
+};
+
+// A warp's state of a segment.  Column c of column block nt is flattened row r0 + 8 * nt + c; a lane (g = lane / 4, tig = lane % 4) holds
+// columns 2 * tig and 2 * tig + 1.
+template <int D, int NT>
+struct WarpState {
+    float o[D / 16][NT][4];   // rows of block j: d = 32 j + 4 g + {0, 1} in o[2j], + {2, 3} in o[2j + 1]; [d][column]: 00 01 10 11
+    float m[NT][2], l[NT][2];
+    int ref;
+};
+
+__device__ __forceinline__ bool row_sees(const KvSeqs &s, const KvQuery &a, const Segment &g, int r, int t) {
+    if (r >= g.rows_total || t >= g.len) return false;
+    const int i = r / a.group, d = t - g.base;
+    if (a.tree == nullptr) return d <= i;
+    if (d < 0) return true;
+    const uint64_t *p = MXQ_AT(a.tree + (int64_t)g.b * s.m + i, 8, a.tree, (size_t)s.B * s.m * 8);
+    uint32_t lo = ld_dep_u32(p), hi = ld_dep_u32(reinterpret_cast<const uint32_t *>(p) + 1);
+    return d < 64 && ((((uint64_t)hi << 32 | lo) >> d) & 1) != 0;
+}
+
+template <int D, int NT>
+__device__ __forceinline__ void rescale(WarpState<D, NT> &w, const float (&f)[NT][2]) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.o[i][n][e] *= f[n][e & 1];
+}
+
+// bytes 2y and 2y + 1 of a word -> two pairs of halves
+__device__ __forceinline__ void decode2(uint32_t w, int y, uint32_t (&h)[2]) {
+    asm("{\n\t.reg .b16 l, u;\n\t.reg .b8 b0, b1;\n\tmov.b32 {l, u}, %2;\n\tmov.b16 {b0, b1}, l;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t}"
+        : "=r"(h[0]), "=r"(h[1])
+        : "r"(y ? w >> 16 : w));
+}
+
+// O += P . V for a whole tile, in FP16.  p[u][n][h]: packed weights of row g of column block n, tokens 16 u + tig + 8 h (low half) and
+// + 4 (high half).  kTiers == 2: deep[..] are the weights too small for p, scaled up by `up`.
+template <int D, int NT, int kTiers>
+__device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, int g, int tig, const uint32_t (&p)[2][NT][2],
+                                           const uint32_t (&deep)[2][NT][2], float up, float down) {
     using T = KvTile<D>;
-    constexpr int kE = D / 32, kBytes = kE / 2;   // elements and code bytes of a row per lane
-    pdl_trigger();
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int64_t row = unit / a.heads;
-    const int hq = (int)(unit - row * a.heads), hk = hq / a.group;
-    const int b = (int)(row / s.m), i = (int)(row - (int64_t)b * s.m);
-    if (b >= s.B) return;
-    pdl_wait();
-    const int len = s.len(b), rows = s.nrows(b), base = len - rows;
-    const int e0 = lane * kE, j = e0 / 32, nat = lane * kBytes - 16 * j;   // natural byte within the block
-    float q[kE], o[kE], m = -INFINITY, l = 0.f;
+    constexpr int kNb = T::kNb, kW = kNb / 2;   // words of V codes per lane and token
+    uint32_t sw[2][kNb];                        // scales: [group][h, block pair] words of (A.j, B.j, A.j+1, B.j+1)
+    uint32_t ev[2][2][kW], od[2][2][kW];        // bytes (element of token A, element of token B): even elements, odd elements
 #pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = 0.f, q[e] = ld_dep_bf16(a.q + row * a.q_stride + (int64_t)hq * D + e0 + e);
-    const uint64_t tree = a.tree != nullptr && i < rows ? a.tree[row] : 0;
-    for (int t = 0; t < (i < rows ? len : 0); ++t) {
-        const int d = t - base;
-        if (a.tree != nullptr ? (d >= 0 && !((tree >> d) & 1)) : d > i) continue;
-        const int page = s.page(b, t >> c.page_shift);
-        if (!kv_page_ok(c, page)) continue;
-        const uint8_t *tile = kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), hk);
-        const int ts = t & 31;
-        float kv[2][kE];
+    for (int u = 0; u < 2; ++u) {
+        lds_words<kNb>(tile + T::kVs + 16 * kNb * u + 4 * kNb * tig, sw[u]);
+        const uint32_t row = tile + T::kV + (16 * u + tig) * T::kRow + 2 * kNb * g;
+        uint32_t v[4][kW];
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const float sc = e8m0_to_float(__ldcg(tile + (w ? T::vs(ts, j) : T::kKs + ts * T::kNb + j)));
+        for (int k = 0; k < 4; ++k) lds_words<kW>(row + 4 * k * T::kRow, v[k]);
 #pragma unroll
-            for (int y = 0; y < kBytes; ++y) {
-                const int n = nat + y, p = w ? (n / 2) * 2 * T::kNb + 2 * j + n % 2 : (n / 4) * 4 * T::kNb + 4 * j + n % 4;
-                const float2 f = __half22float2(e2m1x2_to_half2(__ldcg(tile + (w ? T::kV : 0) + ts * T::kRow + p)));
-                kv[w][2 * y] = f.x * sc, kv[w][2 * y + 1] = f.y * sc;
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < kW; ++x) {
+                const uint32_t A = v[2 * h][x], B = v[2 * h + 1][x];
+                ev[u][h][x] = (A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u);
+                od[u][h][x] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
+            }
+    }
+    const uint32_t bias = ((uint32_t)(15 + kScaleBias - w.ref) & 0xFFFFu) * 0x10001u;
+#pragma unroll
+    for (int j = 0; j < kNb; ++j) {
+        const int x = j / 2, y = j & 1;
+        uint32_t e[2][2][2], o[2][2][2], sc[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                decode2(ev[u][h][x], y, e[u][h]);
+                decode2(od[u][h][x], y, o[u][h]);
+                // the two tokens' scales as 16-bit numbers -> exponent fields (none below zero) -> halves
+                sc[u][h] = __viaddmax_s16x2(__byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140), bias, 0u) << 10;
+            }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float(&o0)[4] = w.o[2 * j][n], (&o1)[4] = w.o[2 * j + 1][n];
+            if constexpr (kTiers == 2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o0[i] *= up, o1[i] *= up;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t b0 = mul_half2(deep[u][n][0], sc[u][0]), b1 = mul_half2(deep[u][n][1], sc[u][1]);
+                    mma16816<false>(o0, e[u][0][0], o[u][0][0], e[u][1][0], o[u][1][0], b0, b1);
+                    mma16816<false>(o1, e[u][0][1], o[u][0][1], e[u][1][1], o[u][1][1], b0, b1);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o0[i] *= down, o1[i] *= down;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t b0 = mul_half2(p[u][n][0], sc[u][0]), b1 = mul_half2(p[u][n][1], sc[u][1]);
+                mma16816<false>(o0, e[u][0][0], o[u][0][0], e[u][1][0], o[u][1][0], b0, b1);
+                mma16816<false>(o1, e[u][0][1], o[u][0][1], e[u][1][1], o[u][1][1], b0, b1);
             }
         }
-        float dot = 0.f;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) dot += q[e] * kv[0][e];
-        const float x = warp_sum(dot) * a.scale_log2;
-        const float top = fmaxf(m, x), use = top == -INFINITY ? 0.f : top;
-        const float alpha = exp2f(m - use), p = exp2f(x - use);
-        l = l * alpha + p;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) o[e] = o[e] * alpha + p * kv[1][e];
-        m = top;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+}
+
+// The same for the 16 tokens of group u, in BF16: any spread of weights and scales; NaN scales count only where the row sees the token.
+template <int D, int NT, class Sees>
+__device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t tile, int u, int g, int tig, const uint32_t (&p)[NT][2], Sees sees) {
+    using T = KvTile<D>;
+    constexpr int kNb = T::kNb, kW = kNb / 2;
+    uint32_t sw[kNb];
+    lds_words<kNb>(tile + T::kVs + 16 * kNb * u + 4 * kNb * tig, sw);
+    const uint32_t row = tile + T::kV + (16 * u + tig) * T::kRow + 2 * kNb * g;
+    const uint32_t bias = ((uint32_t)(127 + kScaleBias - w.ref) & 0xFFFFu) * 0x10001u;
+    auto widen = [](uint32_t h) {
+        const float2 f = __half22float2(*reinterpret_cast<__half2 *>(&h));
+        return pack_bf162(f.x, f.y);
+    };
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-        const __nv_bfloat16 r = __float2bfloat16(o[e] * inv);
-        a.o[(row * a.heads + hq) * D + e0 + e] = *reinterpret_cast<const uint16_t *>(&r);
+    for (int x = 0; x < kW; ++x) {
+        uint32_t ev[2][4], od[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t A = lds_u32(row + 8 * h * T::kRow + 4 * x), B = lds_u32(row + (8 * h + 4) * T::kRow + 4 * x);
+            decode4((A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u), ev[h]);
+            decode4(((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u), od[h]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ev[h][i] = widen(ev[h][i]), od[h][i] = widen(od[h][i]);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int j = 2 * x + y;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                uint32_t b[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t word = sw[h * kW + x];
+                    uint32_t f = __viaddmax_s16x2(__byte_perm(word, 0, y ? 0x4342 : 0x4140), bias, 0u) << 7;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (((word >> (16 * y + 8 * e)) & 0xFFu) == 0xFFu)
+                            f = (f & ~(0xFFFFu << (16 * e))) | ((sees(n, 16 * u + tig + 8 * h + 4 * e) ? 0x7FC0u : 0u) << (16 * e));
+                    b[h] = mul_bf162(p[n][h], f);
+                }
+                mma16816<true>(w.o[2 * j][n], ev[0][2 * y], od[0][2 * y], ev[1][2 * y], od[1][2 * y], b[0], b[1]);
+                mma16816<true>(w.o[2 * j + 1][n], ev[0][2 * y + 1], od[0][2 * y + 1], ev[1][2 * y + 1], od[1][2 * y + 1], b[0], b[1]);
+            }
+        }
     }
-    if (lane == 0 && a.lse != nullptr) a.lse[row * a.heads + hq] = (m == -INFINITY ? 0.f : m * 0.69314718f) + logf(l);
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_kernel(KvView c, KvSeqs s, KvQuery a) {
+    using T = KvTile<D>;
+    constexpr int kNb = T::kNb;
+    extern __shared__ __align__(128) uint8_t att_smem_raw[];
+    __shared__ int64_t sh_scan[kAttWarps + 3];
+    __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
+    __shared__ int sh_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, tig = lane & 3;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * T::kBytes;
+    uint4 *const sh_q = reinterpret_cast<uint4 *>(att_smem_raw + kAttWarps * kAttStages * T::kBytes);
+    float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][8][D + 4], between segments
+    constexpr int kMergeRow = D + 4;
+    static_assert(kAttWarps * 8 * kMergeRow * 4 <= kAttWarps * kAttStages * T::kBytes, "the merge buffer lies over the rings");
+
+    pdl_trigger();
+    pdl_wait();
+
+    // ---- this CTA's share of all steps ----
+    auto shape_of = [&](int b, int &len, int &rows, int64_t &n, int64_t &tiles) {
+        len = s.len(b), rows = s.nrows(b);
+        n = max(1, (len + kAttWarps * kTileTokens - 1) / (kAttWarps * kTileTokens));
+        tiles = max(1, (rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
+    };
+    int64_t first, left;      // global index of the CTA's next step; steps left
+    int64_t b_start;          // global index of the first step of sequence b
+    int b;
+    int64_t total, grid;
+    {
+        const int per = (s.B + kAttThreads - 1) / kAttThreads;
+        int64_t mine = 0;
+        for (int i = tid * per; i < min(s.B, (tid + 1) * per); ++i) {
+            int len, rows;
+            int64_t n, tiles;
+            shape_of(i, len, rows, n, tiles);
+            mine += n * tiles * c.heads;
+        }
+        int64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += up;
+        }
+        if (lane == 31) sh_scan[warp] = upto;
+        __syncthreads();
+        total = 0;
+        for (int w = 0; w < kAttWarps; ++w) {
+            if (w < warp) upto += sh_scan[w];
+            total += sh_scan[w];
+        }
+        grid = min((int64_t)gridDim.x, total);      // no CTA without a step among those that share a segment
+        if (blockIdx.x >= grid) return;
+        first = total * blockIdx.x / grid;
+        left = total * (blockIdx.x + 1) / grid - first;
+        if (upto - mine <= first && first < upto) {
+            int64_t at = upto - mine;
+            int i = tid * per;
+            for (;; ++i) {
+                int len, rows;
+                int64_t n, tiles;
+                shape_of(i, len, rows, n, tiles);
+                if (at + n * tiles * c.heads > first) break;
+                at += n * tiles * c.heads;
+            }
+            sh_scan[kAttWarps] = i;
+            sh_scan[kAttWarps + 1] = at;
+        }
+        __syncthreads();
+        b = (int)sh_scan[kAttWarps];
+        b_start = sh_scan[kAttWarps + 1];
+    }
+
+    while (left > 0) {
+        int len, rows;
+        int64_t n, tiles;
+        shape_of(b, len, rows, n, tiles);
+        const int64_t seg = (first - b_start) / n, seg_start = b_start + seg * n;
+        const int step0 = (int)(first - seg_start), steps = (int)min(left, n - step0);
+        Segment sg;
+        sg.b = b, sg.head = (int)(seg / tiles), sg.r0 = (int)(seg % tiles) * kAttRows<NT>;
+        sg.len = len, sg.base = len - rows, sg.rows_total = rows * a.group;
+        const int nrows = min(max(sg.rows_total - sg.r0, 0), kAttRows<NT>);
+
+        // ---- the warp's tiles: number k is tile (step0 + k) * kAttWarps + warp of the sequence ----
+        const int last_tile = (len + kTileTokens - 1) / kTileTokens;
+        const int first_tile = step0 * kAttWarps + warp;
+        const int count = nrows > 0 && first_tile < last_tile ? min(steps, (last_tile - first_tile + kAttWarps - 1) / kAttWarps) : 0;
+        int window = 0, ids = -1;          // page ids of tiles window + lane
+        uint32_t there = 0;                // bit per ring slot: the tile's page exists
+        auto load_ids = [&](int k) {
+            window = k;
+            const int t = first_tile + (k + lane) * kAttWarps;
+            ids = k + lane < count ? s.page(b, (t * kTileTokens) >> c.page_shift) : -1;
+        };
+        auto issue = [&](int k) {
+            if (k < count) {
+                if (k - window >= 32) load_ids(k);
+                const int page = __shfl_sync(0xffffffffu, ids, k - window);
+                const uint32_t slot = (uint32_t)(k % kAttStages);
+                const bool ok = kv_page_ok(c, page);
+                there = (there & ~(1u << slot)) | ((uint32_t)ok << slot);
+                if (ok) {
+                    const int t = (first_tile + k * kAttWarps) * kTileTokens;
+                    const uint8_t *src = kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), sg.head);
+                    const uint32_t dst = ring + slot * T::kBytes;
+#pragma unroll
+                    for (int i = 0; i < (T::kBytes + 511) / 512; ++i) {
+                        const int off = i * 512 + lane * 16;
+                        if (off < T::kBytes) copy16(dst + off, MXQ_AT(src + off, 16, c.pool, c.pool_bytes));
+                    }
+                }
+            }
+            copy_commit();
+        };
+        if (count > 0) load_ids(0);
+#pragma unroll
+        for (int k = 0; k < kAttStages; ++k) issue(k);
+
+        // ---- query fragments: elements 32 j + 8 tig .. + 7 of row g, normalised by a power of two ----
+        uint4 qf[NT > kAttRegisterQ ? 1 : NT][kNb];
+        float factor[NT][2];               // score -> log2 domain, for the lane's two columns
+        int limit[NT][2];                  // first token (causally) hidden from the column's row; 0: no such row
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = sg.r0 + 8 * nt + g;
+            uint4 x[kNb];
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < kNb; ++j) {
+                x[j] = make_uint4(0, 0, 0, 0);
+                if (r < sg.rows_total) {
+                    const uint16_t *src = a.q + ((int64_t)b * s.m + r / a.group) * a.q_stride + (int64_t)(sg.head * a.group + r % a.group) * D + 32 * j + 8 * tig;
+                    x[j] = ld_dep_u4(MXQ_AT(src, 16, a.q, (((int64_t)s.B * s.m - 1) * a.q_stride + (int64_t)a.heads * D) * 2));
+                }
+                top = __vmaxu2(top, chunk_max2(x[j]));
+            }
+            top = max(top & 0xFFFFu, top >> 16);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // exponent field e of the largest element -> 2^14 (rows with an Inf or NaN as they are: their scores are NaN or infinite)
+            const int e = (int)(top >> 7), up = e == 255 ? 127 : min(268 - e, 254);
+            const float mul = __uint_as_float((uint32_t)up << 23);
+            const float back = up == 254 ? __uint_as_float(0x00400000u) : __uint_as_float((uint32_t)(254 - up) << 23);
+#pragma unroll
+            for (int j = 0; j < kNb; ++j) {
+                const uint32_t in[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+                uint32_t out[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i] = pack_half2(__uint_as_float(in[i] << 16) * mul, __uint_as_float(in[i] & 0xFFFF0000u) * mul);
+                const uint4 f = make_uint4(out[0], out[1], out[2], out[3]);
+                if constexpr (NT > kAttRegisterQ) {
+                    if (warp == 0) sh_q[(j * NT + nt) * 32 + lane] = f;
+                } else {
+                    qf[nt][j] = f;
+                }
+            }
+#pragma unroll
+            for (int e2 = 0; e2 < 2; ++e2) {
+                const int rc = sg.r0 + 8 * nt + 2 * tig + e2;
+                factor[nt][e2] = a.scale_log2 * __shfl_sync(0xffffffffu, back, (2 * tig + e2) * 4);
+                limit[nt][e2] = rc < sg.rows_total ? min(sg.base + rc / a.group + 1, len) : 0;
+            }
+        }
+        if constexpr (NT > kAttRegisterQ) __syncthreads();
+
+        WarpState<D, NT> w;
+        w.ref = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) w.m[nt][e] = -INFINITY, w.l[nt][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w.o[i][nt][e] = 0.f;
+        }
+
+        for (int k = 0; k < count; ++k) {
+            const uint32_t slot = (uint32_t)(k % kAttStages), tile = ring + slot * T::kBytes;
+            const int t0 = (first_tile + k * kAttWarps) * kTileTokens;
+            copy_wait<kAttStages - 1>();
+            __syncwarp();
+            if ((there >> slot) & 1u) {
+                // ---- scores ----
+                float x[2][NT][4];
+                const int tok = (g >> 1) + 4 * (g & 1);      // row g of the product is this token of the group, row g + 8 the one 8 further
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t k0[kNb], k1[kNb];
+                    const uint32_t row = tile + (16 * u + tok) * T::kRow + 4 * kNb * tig;
+                    lds_words<kNb>(row, k0);
+                    lds_words<kNb>(row + 8 * T::kRow, k1);
+                    uint32_t s0, s1;
+                    const uint32_t sa = tile + T::kKs + (16 * u + tok) * kNb;
+                    if constexpr (kNb == 4) {
+                        s0 = lds_u32(sa), s1 = lds_u32(sa + 8 * kNb);
+                    } else {
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s0) : "r"(sa));
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s1) : "r"(sa + 8 * kNb));
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[u][nt][e] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < kNb; ++j) {
+                        uint32_t h0[4], h1[4];
+                        decode4(k0[j], h0);
+                        decode4(k1[j], h1);
+                        const float2 f0 = scales2(s0 >> (16 * (j / 2))), f1 = scales2(s1 >> (16 * (j / 2)));
+                        const float c0 = j & 1 ? f0.y : f0.x, c1 = j & 1 ? f1.y : f1.x;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            uint4 q;
+                            if constexpr (NT > kAttRegisterQ) q = sh_q[(j * NT + nt) * 32 + lane];
+                            else q = qf[nt][j];
+                            float d[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
+                            mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
+                            x[u][nt][0] += d[0] * c0, x[u][nt][1] += d[1] * c0;
+                            x[u][nt][2] += d[2] * c1, x[u][nt][3] += d[3] * c1;
+                        }
+                    }
+                }
+                // ---- mask, running maximum ----
+                float top[NT][2];
+                const bool edge = t0 + kTileTokens > sg.base;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    top[nt][0] = top[nt][1] = -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float v = x[u][nt][e] * factor[nt][e & 1];
+                            if (edge) {
+                                const int t = t0 + 16 * u + tok + 8 * (e >> 1);
+                                if (a.tree == nullptr ? t >= limit[nt][e & 1] : !row_sees(s, a, sg, sg.r0 + 8 * nt + 2 * tig + (e & 1), t)) v = -INFINITY;
+                            }
+                            x[u][nt][e] = v;
+                            top[nt][e & 1] = fmaxf(top[nt][e & 1], v);
+                        }
+                }
+                bool over = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) over |= top[nt][e] > w.m[nt][e] + kMaxSlack;
+                if (__any_sync(0xffffffffu, over)) {
+                    float f[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float v = top[nt][e];
+#pragma unroll
+                            for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+                            const float m = fmaxf(w.m[nt][e], v);
+                            f[nt][e] = m == -INFINITY ? 1.f : exp2_fast(w.m[nt][e] - m);
+                            w.m[nt][e] = m;
+                            w.l[nt][e] *= f[nt][e];
+                        }
+                    rescale(w, f);
+                }
+                // ---- weights ----
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float m = w.m[nt][e] == -INFINITY ? 0.f : w.m[nt][e];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float &v = x[u][nt][2 * h + e];
+                                v = exp2_fast(v - m);
+                                w.l[nt][e] += v;
+                            }
+                    }
+                // ---- V scales: tokens behind the end count as zero; largest, smallest non-zero ----
+                uint32_t sv = 0;
+                const uint32_t sv_at = tile + T::kVs + 4 * lane;
+                if (lane < 8 * kNb) {
+                    sv = lds_u32(sv_at);
+                    if (t0 + kTileTokens > len) {
+                        const int at = 4 * lane, t = t0 + 16 * (at / (16 * kNb)) + (at / (4 * kNb)) % 4 + 8 * ((at / (2 * kNb)) % 2);
+                        sv &= (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"(sv) : "memory");
+                    }
+                }
+                uint32_t hi = 0, lo = 255;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t v = (sv >> (8 * i)) & 0xFFu;
+                    hi = max(hi, v), lo = min(lo, v == 0 ? 255u : v);
+                }
+                hi = __reduce_max_sync(0xffffffffu, hi);      // (also orders the stores above before the loads below)
+                lo = __reduce_min_sync(0xffffffffu, lo);
+                __syncwarp();
+                const bool nan = hi == 255u;
+                if (nan) {       // the largest that is a number
+                    hi = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t v = (sv >> (8 * i)) & 0xFFu;
+                        if (v != 255u) hi = max(hi, v);
+                    }
+                    hi = __reduce_max_sync(0xffffffffu, hi);
+                }
+                if ((int)hi > w.ref + kScaleHeadroom) {
+                    const float f = scale_by_power(1.f, w.ref - (int)hi);
+                    float ff[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = f;
+                    rescale(w, ff);
+                    w.ref = (int)hi;
+                }
+                // ---- O += P V: which form holds this tile's weights? ----
+                const int range = kHalfRange - (w.ref - min((int)lo, w.ref));      // binades of weight the tile's scales leave
+                const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23), tiny = small * small;
+                float least = 1.f;             // the smallest weight that is not zero
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) least = fminf(least, x[u][nt][e] == 0.f ? 1.f : x[u][nt][e]);
+                uint32_t p[2][NT][2];
+                if (nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, least < tiny)) {
+                    auto sees = [&](int nt, int t) { return row_sees(s, a, sg, sg.r0 + 8 * nt + g, t0 + t); };
+#pragma unroll 1
+                    for (int part = 0; part < 2; ++part)       // the weights' upper and lower eight bits
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    float &x0 = x[u][nt][2 * h], &x1 = x[u][nt][2 * h + 1];
+                                    const uint32_t b = pack_bf162(x0, x1);
+                                    x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xFFFF0000u);
+                                    p[u][nt][h] = transpose8x8(b);
+                                }
+                            add_values_wide<D, NT>(w, tile, u, g, tig, p[u], sees);
+                        }
+                } else if (__any_sync(0xffffffffu, least < small)) {
+                    const float up = __uint_as_float((uint32_t)(127 + range) << 23);
+                    uint32_t deep[2][NT][2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float x0 = x[u][nt][2 * h], x1 = x[u][nt][2 * h + 1];
+                                p[u][nt][h] = transpose8x8(pack_half2(x0 < small ? 0.f : x0, x1 < small ? 0.f : x1));
+                                deep[u][nt][h] = transpose8x8(pack_half2(x0 < small ? x0 * up : 0.f, x1 < small ? x1 * up : 0.f));
+                            }
+                    add_values<D, NT, 2>(w, tile, g, tig, p, deep, up, small);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(pack_half2(x[u][nt][2 * h], x[u][nt][2 * h + 1]));
+                    add_values<D, NT, 1>(w, tile, g, tig, p, p, 1.f, 1.f);
+                }
+            }
+            __syncwarp();
+            issue(k + kAttStages);
+        }
+
+        // ---- join the warps: each as (maximum, sum, average), eight rows at a time over the drained rings ----
+        copy_wait<0>();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
+                if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
+            }
+        const bool whole = steps == n;
+        const int64_t seg_end = seg_start + n;
+        float *slot = a.partials + (2 * (int64_t)blockIdx.x + (step0 == 0)) * kAttSlotFloats<D, NT>;   // 1: starts here, 0: began earlier
+        [[maybe_unused]] const size_t ws_bytes = 2 * (size_t)gridDim.x * kAttSlotFloats<D, NT> * 4;
+
+        auto store_row = [&](int r, int d, const float4 &v, float m, float l) {   // final result: flattened row r of the sequence, 4 elements, by one warp
+            const int64_t at = ((int64_t)b * s.m + r / a.group) * a.heads + sg.head * a.group + r % a.group;
+            [[maybe_unused]] const size_t o_bytes = (size_t)s.B * s.m * a.heads * D * 2;
+            if (d < D) *reinterpret_cast<uint2 *>(MXQ_AT(a.o + at * D + d, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
+            if (d == 0 && a.lse != nullptr) *MXQ_AT(a.lse + at, 4, a.lse, o_bytes / D * 2) = (m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f);
+        };
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (8 * nt >= nrows && nt > 0) break;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float inv = w.l[nt][e] == 0.f ? 0.f : 1.f / w.l[nt][e];
+                float *dst = merge + (warp * 8 + 2 * tig + e) * kMergeRow + 4 * g;
+#pragma unroll
+                for (int j = 0; j < kNb; ++j) {
+                    float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127 - kScaleBias);
+                    *reinterpret_cast<float4 *>(dst + 32 * j) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            }
+            __syncthreads();
+            for (int r = warp; r < min(nrows - 8 * nt, 8); r += kAttWarps) {
+                float m = -INFINITY, l = 0.f;
+#pragma unroll
+                for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][8 * nt + r][0]);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < kAttWarps; ++i) {
+                    const float li = sh_ml[i][8 * nt + r][1], f = li == 0.f ? 0.f : li * exp2_fast(sh_ml[i][8 * nt + r][0] - m);
+                    l += f;
+                    if (4 * lane < D && li != 0.f) {
+                        const float4 x = *reinterpret_cast<const float4 *>(merge + (i * 8 + r) * kMergeRow + 4 * lane);
+                        v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
+                    }
+                }
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+                if (whole) {
+                    store_row(sg.r0 + 8 * nt + r, 4 * lane, v, m, l);
+                } else {
+                    if (4 * lane < D) *reinterpret_cast<float4 *>(MXQ_AT(slot + (8 * nt + r) * D + 4 * lane, 16, a.partials, ws_bytes)) = v;
+                    if (lane == 0) *reinterpret_cast<float2 *>(MXQ_AT(slot + kAttRows<NT> * D + 2 * (8 * nt + r), 8, a.partials, ws_bytes)) = make_float2(m, l);
+                }
+            }
+        }
+
+        // ---- join the CTAs of a cut segment: the last to arrive adds the parts in order ----
+        bool finish = whole;
+        if (!whole) {
+            // CTA i starts at total * i / grid: step x belongs to the last i whose start is not above it
+            const int64_t i0 = ((seg_start + 1) * grid - 1) / total, i1 = (seg_end * grid - 1) / total;
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                unsigned *ticket = MXQ_AT(a.tickets + i0, 4, a.tickets, kAttMaxCtas * 4);
+                sh_last = atomicAdd(ticket, 1u) == (unsigned)(i1 - i0);
+                if (sh_last) *ticket = 0;
+            }
+            __syncthreads();
+            if (sh_last) {
+                finish = true;
+                __threadfence();
+                for (int r = warp; r < nrows; r += kAttWarps) {
+                    auto part = [&](int64_t i) {     // (the first contributor's part starts the segment, or is a share that begins exactly there)
+                        return a.partials + (2 * i + (total * i / grid <= seg_start)) * kAttSlotFloats<D, NT>;
+                    };
+                    float m = -INFINITY, l = 0.f;
+                    for (int64_t i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(part(i) + kAttRows<NT> * D + 2 * r));
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int64_t i = i0; i <= i1; ++i) {
+                        const float *p = part(i);
+                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
+                        const float f = ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - m);
+                        l += f;
+                        if (4 * lane < D) {
+                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p + r * D + 4 * lane, 16, a.partials, ws_bytes)));
+                            v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
+                        }
+                    }
+                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    store_row(sg.r0 + r, 4 * lane, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv), m, l);
+                }
+            }
+        }
+        // rows the sequence does not have
+        if (finish && sg.r0 == 0)
+            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) store_row(r, 4 * lane, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+        __syncthreads();      // the rings, sh_ml and sh_q are free again
+        first += steps;
+        left -= steps;
+        if (first == b_start + n * tiles * c.heads) b_start = first, ++b;
+    }
 }
 
 MXQ_BOUNDS_TU(bounds_take_kv_attention)
+
+// ---- host -------------------------------------------------------------------------------------------------------------------
+
+// Column blocks per tile: as many as the rows of one kv head fill, so that K and V are decoded once for all of them; 32 rows
+// are what a lane's registers hold.
+static int att_column_blocks(int M, int group) {
+    const int64_t rows = (int64_t)M * group;
+    return rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+}
+template <int D>
+static size_t att_workspace(int nt) {
+    const size_t sms = (size_t)sm_count();
+    auto bytes = [&](size_t per_sm, size_t slot) { return 4096 + 2 * (sms * per_sm < kAttMaxCtas ? sms * per_sm : (size_t)kAttMaxCtas) * slot * 4; };
+    return nt == 1 ? bytes(kAttCtasPerSm<1>, kAttSlotFloats<D, 1>) : nt == 2 ? bytes(kAttCtasPerSm<2>, kAttSlotFloats<D, 2>) : bytes(kAttCtasPerSm<4>, kAttSlotFloats<D, 4>);
+}
+
+template <int D, int NT>
+static int att_launch(const KvView &c, const KvSeqs &s, const KvQuery &a, cudaStream_t stream) {
+    constexpr size_t smem = kAttSmem<D, NT>;
+    static bool configured[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return MXQ_ERR_CUDA;
+    if (!configured[dev]) {
+        if (cudaFuncSetAttribute(kv_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+            cudaFuncSetAttribute(kv_attention_kernel<D, NT>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return MXQ_ERR_CUDA;
+        }
+        configured[dev] = true;
+    }
+    int grid = sm_count() * kAttCtasPerSm<NT>;
+    if (grid > kAttMaxCtas) grid = kAttMaxCtas;
+    return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)grid), kAttThreads, smem, stream, c, s, a);
+}
 
 }  // namespace mxq
 
@@ -85,7 +833,9 @@ size_t mxq_kv_attention_workspace_bytes(int B, int M, int q_heads, int kv_heads,
     if (B < 1 || B > MXQ_KV_MAX_SEQS || M < 1 || kv_heads < 1 || kv_heads > MXQ_KV_MAX_HEADS || q_heads < kv_heads || q_heads % kv_heads ||
         mxq_kv_page_bytes(kv_heads, head_dim, 32) == 0)
         return 0;
-    return 4096;
+    if ((int64_t)M * (q_heads / kv_heads) > (1 << 24)) return 0;
+    const int nt = mxq::att_column_blocks(M, q_heads / kv_heads);
+    return head_dim == 128 ? mxq::att_workspace<128>(nt) : mxq::att_workspace<64>(nt);
 }
 
 int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, int64_t q_stride, int B, int M, int q_heads,
@@ -101,12 +851,16 @@ int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, i
         !mxq::aligned_to(rows, 4) || !mxq::aligned16(workspace))
         return MXQ_ERR_ALIGN;
     if (!workspace || workspace_bytes < need) return MXQ_ERR_WORKSPACE;
-    const mxq::KvQuery a = {(const uint16_t *)Q_bf16, q_stride, tree, (uint16_t *)O_bf16, lse, q_heads, q_heads / cache->kv_heads,
-                            scale * 1.44269504f};
+    const int group = q_heads / cache->kv_heads;
+    const mxq::KvQuery a = {(const uint16_t *)Q_bf16, q_stride, tree, (uint16_t *)O_bf16, lse, q_heads, group, scale * 1.44269504f,
+                            (float *)((char *)workspace + 4096), (unsigned *)workspace};
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
-    const int64_t units = (int64_t)B * M * q_heads;
-    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_attention_plain_kernel<128> : mxq::kv_attention_plain_kernel<64>,
-                          dim3((unsigned)((units + 3) / 4)), 128, 0, (cudaStream_t)stream, mxq::kv_view(cache, layer), s, a);
+    const mxq::KvView c = mxq::kv_view(cache, layer);
+    cudaStream_t st = (cudaStream_t)stream;
+    const int nt = mxq::att_column_blocks(M, group);
+    if (cache->head_dim == 128)
+        return nt == 1 ? mxq::att_launch<128, 1>(c, s, a, st) : nt == 2 ? mxq::att_launch<128, 2>(c, s, a, st) : mxq::att_launch<128, 4>(c, s, a, st);
+    return nt == 1 ? mxq::att_launch<64, 1>(c, s, a, st) : nt == 2 ? mxq::att_launch<64, 2>(c, s, a, st) : mxq::att_launch<64, 4>(c, s, a, st);
 }
 
 #pragma GCC visibility pop
