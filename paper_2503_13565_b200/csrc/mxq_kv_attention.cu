@@ -52,6 +52,9 @@ constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may e
 constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
 constexpr int kHalfRange = kScaleBias + 14;    // a normal number while P * 2^(scale - ref) >= 2^-24
 constexpr int kScaleSpread = 14;               // scales this far below ref still take the FP16 step
+constexpr int kScaleSlack = 3;                 // how far (log2) a tile's largest scale may lie below ref
+constexpr int kScaleDrop = 12;                 // how far ref may fall below its highest: accumulators are below 2^18 per token, and
+                                               // the deepest of the tiers below scales them by up to 2^72
 
 // rows of the flattened (token row, head of the group) index per tile of NT column blocks
 template <int NT>
@@ -110,6 +113,19 @@ __device__ __forceinline__ uint32_t mul_bf162(uint32_t a, uint32_t b) {
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
     return o;
 }
+__device__ __forceinline__ uint32_t max_half2(uint32_t a, uint32_t b) {   // (NaN wins)
+    uint32_t o;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+__device__ __forceinline__ uint32_t min_half2(uint32_t a, uint32_t b) {
+    uint32_t o;
+    asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+__device__ __forceinline__ bool all_le_half2(uint32_t a, uint32_t b) {
+    return __hble2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -159,7 +175,7 @@ template <int D, int NT>
 struct WarpState {
     float o[D / 16][NT][4];   // rows of block j: d = 32 j + 4 g + {0, 1} in o[2j], + {2, 3} in o[2j + 1]; [d][column]: 00 01 10 11
     float m[NT][2], l[NT][2];
-    int ref;
+    int ref, ref_max;
 };
 
 __device__ __forceinline__ bool row_sees(const KvSeqs &s, const KvQuery &a, const Segment &g, int r, int t) {
@@ -211,11 +227,12 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
 #pragma unroll
             for (int x = 0; x < kW; ++x) {
                 const uint32_t A = v[2 * h][x], B = v[2 * h + 1][x];
-                ev[u][h][x] = (A & 0x0F0F0F0Fu) | ((B << 4) & 0xF0F0F0F0u);
+                ev[u][h][x] = (A & 0x0F0F0F0Fu) | ((B * 16u) & 0xF0F0F0F0u);
                 od[u][h][x] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
             }
     }
-    const uint32_t bias = ((uint32_t)(15 + kScaleBias - w.ref) & 0xFFFFu) * 0x10001u;
+    // exponent field of 2^(scale - ref + kScaleBias): never below 1 here, so both halves fit one 32-bit multiply-add
+    const uint32_t bias = (uint32_t)(15 + kScaleBias - w.ref) * (0x10001u << 10);
 #pragma unroll
     for (int j = 0; j < kNb; ++j) {
         const int x = j / 2, y = j & 1;
@@ -226,8 +243,7 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
             for (int h = 0; h < 2; ++h) {
                 decode2(ev[u][h][x], y, e[u][h]);
                 decode2(od[u][h][x], y, o[u][h]);
-                // the two tokens' scales as 16-bit numbers -> exponent fields (none below zero) -> halves
-                sc[u][h] = __viaddmax_s16x2(__byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140), bias, 0u) << 10;
+                sc[u][h] = __byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140) * 1024u + bias;   // (the two tokens' scales as 16-bit numbers)
             }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -467,7 +483,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
         if constexpr (NT > kAttRegisterQ) __syncthreads();
 
         WarpState<D, NT> w;
-        w.ref = 0;
+        w.ref = w.ref_max = 0;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -525,149 +541,183 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                         }
                     }
                 }
-                // ---- mask, running maximum ----
-                float top[NT][2];
-                const bool edge = t0 + kTileTokens > sg.base;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    top[nt][0] = top[nt][1] = -INFINITY;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float v = x[u][nt][e] * factor[nt][e & 1];
-                            if (edge) {
-                                const int t = t0 + 16 * u + tok + 8 * (e >> 1);
-                                if (a.tree == nullptr ? t >= limit[nt][e & 1] : !row_sees(s, a, sg, sg.r0 + 8 * nt + 2 * tig + (e & 1), t)) v = -INFINITY;
-                            }
-                            x[u][nt][e] = v;
-                            top[nt][e & 1] = fmaxf(top[nt][e & 1], v);
-                        }
-                }
-                bool over = false;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) over |= top[nt][e] > w.m[nt][e] + kMaxSlack;
-                if (__any_sync(0xffffffffu, over)) {
-                    float f[NT][2];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float v = top[nt][e];
-#pragma unroll
-                            for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-                            const float m = fmaxf(w.m[nt][e], v);
-                            f[nt][e] = m == -INFINITY ? 1.f : exp2_fast(w.m[nt][e] - m);
-                            w.m[nt][e] = m;
-                            w.l[nt][e] *= f[nt][e];
-                        }
-                    rescale(w, f);
-                }
-                // ---- weights ----
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float m = w.m[nt][e] == -INFINITY ? 0.f : w.m[nt][e];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                float &v = x[u][nt][2 * h + e];
-                                v = exp2_fast(v - m);
-                                w.l[nt][e] += v;
-                            }
-                    }
-                // ---- V scales: tokens behind the end count as zero; largest, smallest non-zero ----
-                uint32_t sv = 0;
+                // ---- V scales of the tile: largest and smallest ----
+                uint32_t sv = 0, in = 0;       // a word of them per lane, and the bytes of tokens that are there
                 const uint32_t sv_at = tile + T::kVs + 4 * lane;
+                const bool tail = t0 + kTileTokens > len;
                 if (lane < 8 * kNb) {
                     sv = lds_u32(sv_at);
-                    if (t0 + kTileTokens > len) {
-                        const int at = 4 * lane, t = t0 + 16 * (at / (16 * kNb)) + (at / (4 * kNb)) % 4 + 8 * ((at / (2 * kNb)) % 2);
-                        sv &= (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
-                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"(sv) : "memory");
+                    in = 0xFFFFFFFFu;
+                    if (tail) {
+                        const int t = t0 + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
+                        in = (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
                     }
                 }
-                uint32_t hi = 0, lo = 255;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t v = (sv >> (8 * i)) & 0xFFu;
-                    hi = max(hi, v), lo = min(lo, v == 0 ? 255u : v);
-                }
-                hi = __reduce_max_sync(0xffffffffu, hi);      // (also orders the stores above before the loads below)
-                lo = __reduce_min_sync(0xffffffffu, lo);
-                __syncwarp();
-                const bool nan = hi == 255u;
+                const uint32_t hi2 = __vmaxu2(sv & in & 0x00FF00FFu, ((sv & in) >> 8) & 0x00FF00FFu);
+                const uint32_t lo2 = __vminu2((sv | ~in) & 0x00FF00FFu, ((sv | ~in) >> 8) & 0x00FF00FFu);
+                int hi = (int)__reduce_max_sync(0xffffffffu, max(hi2 & 0xFFFFu, hi2 >> 16));
+                const int lo = (int)__reduce_min_sync(0xffffffffu, min(lo2 & 0xFFFFu, lo2 >> 16));
+                const bool nan = hi == 255;
                 if (nan) {       // the largest that is a number
                     hi = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t v = (sv >> (8 * i)) & 0xFFu;
-                        if (v != 255u) hi = max(hi, v);
+                        const int v = (int)(((sv & in) >> (8 * i)) & 0xFFu);
+                        if (v != 255) hi = max(hi, v);
                     }
-                    hi = __reduce_max_sync(0xffffffffu, hi);
+                    hi = (int)__reduce_max_sync(0xffffffffu, (uint32_t)hi);
                 }
-                if ((int)hi > w.ref + kScaleHeadroom) {
-                    const float f = scale_by_power(1.f, w.ref - (int)hi);
+                // ref follows the tiles' largest scale up and (within what FP32 accumulators bear) down
+                if (hi > w.ref + kScaleHeadroom || hi + kScaleSlack < w.ref) {
+                    w.ref_max = max(w.ref_max, hi);
+                    const int ref = max(hi, w.ref_max - kScaleDrop);
+                    const float f = scale_by_power(1.f, w.ref - ref);
                     float ff[NT][2];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = f;
                     rescale(w, ff);
-                    w.ref = (int)hi;
+                    w.ref = ref;
                 }
-                // ---- O += P V: which form holds this tile's weights? ----
-                const int range = kHalfRange - (w.ref - min((int)lo, w.ref));      // binades of weight the tile's scales leave
-                const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23), tiny = small * small;
-                float least = 1.f;             // the smallest weight that is not zero
+                if (tail) {      // tokens behind the end carry no weight: any scale that fits will do
+                    if (lane < 8 * kNb) asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"((sv & in) | ((uint32_t)w.ref * 0x01010101u & ~in)) : "memory");
+                    __syncwarp();
+                }
+                const int range = kHalfRange - max(w.ref - lo, 0);      // binades of weight the tile's scales leave to FP16
+                const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
+
+                // ---- weights, under the maximum as it stands ----
+                const bool edge = t0 + kTileTokens > sg.base;
+                uint32_t pk[2][NT][2];
+                uint32_t most = 0, least = 0x7C007C00u;
+                float l[NT][2];
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int nt = 0; nt < NT; ++nt) {
+                    l[nt][0] = w.l[nt][0], l[nt][1] = w.l[nt][1];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float p0 = exp2_fast(fmaf(x[u][nt][2 * h], factor[nt][0], -w.m[nt][0]));
+                            const float p1 = exp2_fast(fmaf(x[u][nt][2 * h + 1], factor[nt][1], -w.m[nt][1]));
+                            l[nt][0] += p0, l[nt][1] += p1;
+                            pk[u][nt][h] = pack_half2(p0, p1);
+                            most = max_half2(most, pk[u][nt][h]);
+                            least = min_half2(least, pk[u][nt][h]);
+                        }
+                }
+                // (NaN compares false)
+                const bool plain = !edge && all_le_half2(most, 0x4C004C00u) && all_le_half2(pack_half2(small, small), least);
+                if (__all_sync(0xffffffffu, plain) && range >= kHalfRange - kScaleSpread) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        w.l[nt][0] = l[nt][0], w.l[nt][1] = l[nt][1];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) pk[u][nt][h] = transpose8x8(pk[u][nt][h]);
+                    }
+                    add_values<D, NT, 1>(w, tile, g, tig, pk, pk, 1.f, 1.f);
+                } else {
+                    // ---- mask, new maximum, weights again ----
+                    float top[NT][2];
+                    bool over = false;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        top[nt][0] = top[nt][1] = -INFINITY;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float v = x[u][nt][e] * factor[nt][e & 1];
+                                if (edge) {
+                                    const int t = t0 + 16 * u + tok + 8 * (e >> 1);
+                                    if (a.tree == nullptr ? t >= limit[nt][e & 1] : !row_sees(s, a, sg, sg.r0 + 8 * nt + 2 * tig + (e & 1), t)) v = -INFINITY;
+                                }
+                                x[u][nt][e] = v;
+                                top[nt][e & 1] = fmaxf(top[nt][e & 1], v);
+                            }
+                        over |= top[nt][0] > w.m[nt][0] + kMaxSlack || top[nt][1] > w.m[nt][1] + kMaxSlack;
+                    }
+                    if (__any_sync(0xffffffffu, over)) {
+                        float f[NT][2];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float v = top[nt][e];
+#pragma unroll
+                                for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+                                const float m = fmaxf(w.m[nt][e], v);
+                                f[nt][e] = m == -INFINITY ? 1.f : exp2_fast(w.m[nt][e] - m);
+                                w.m[nt][e] = m;
+                                w.l[nt][e] *= f[nt][e];
+                            }
+                        rescale(w, f);
+                    }
+                    float low = 1.f;             // the smallest weight that is not zero
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) least = fminf(least, x[u][nt][e] == 0.f ? 1.f : x[u][nt][e]);
-                uint32_t p[2][NT][2];
-                if (nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, least < tiny)) {
-                    auto sees = [&](int nt, int t) { return row_sees(s, a, sg, sg.r0 + 8 * nt + g, t0 + t); };
-#pragma unroll 1
-                    for (int part = 0; part < 2; ++part)       // the weights' upper and lower eight bits
+                        for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    float &x0 = x[u][nt][2 * h], &x1 = x[u][nt][2 * h + 1];
-                                    const uint32_t b = pack_bf162(x0, x1);
-                                    x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xFFFF0000u);
-                                    p[u][nt][h] = transpose8x8(b);
-                                }
-                            add_values_wide<D, NT>(w, tile, u, g, tig, p[u], sees);
-                        }
-                } else if (__any_sync(0xffffffffu, least < small)) {
-                    const float up = __uint_as_float((uint32_t)(127 + range) << 23);
-                    uint32_t deep[2][NT][2];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float x0 = x[u][nt][2 * h], x1 = x[u][nt][2 * h + 1];
-                                p[u][nt][h] = transpose8x8(pack_half2(x0 < small ? 0.f : x0, x1 < small ? 0.f : x1));
-                                deep[u][nt][h] = transpose8x8(pack_half2(x0 < small ? x0 * up : 0.f, x1 < small ? x1 * up : 0.f));
+                            for (int e = 0; e < 4; ++e) {
+                                float &v = x[u][nt][e];
+                                v = exp2_fast(v - (w.m[nt][e & 1] == -INFINITY ? 0.f : w.m[nt][e & 1]));
+                                w.l[nt][e & 1] += v;
+                                low = fminf(low, v == 0.f ? 1.f : v);
                             }
-                    add_values<D, NT, 2>(w, tile, g, tig, p, deep, up, small);
-                } else {
+                    // ---- O += P V: which form holds this tile's weights? ----
+                    const float tiny = small * small;
+                    if (nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, low < tiny * tiny)) {
+                        auto sees = [&](int nt, int t) { return row_sees(s, a, sg, sg.r0 + 8 * nt + g, t0 + t); };
+#pragma unroll 1
+                        for (int part = 0; part < 2; ++part)       // the weights' upper and lower eight bits
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                            for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(pack_half2(x[u][nt][2 * h], x[u][nt][2 * h + 1]));
-                    add_values<D, NT, 1>(w, tile, g, tig, p, p, 1.f, 1.f);
+                                    for (int h = 0; h < 2; ++h) {
+                                        float &x0 = x[u][nt][2 * h], &x1 = x[u][nt][2 * h + 1];
+                                        const uint32_t b = pack_bf162(x0, x1);
+                                        x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xFFFF0000u);
+                                        pk[u][nt][h] = transpose8x8(b);
+                                    }
+                                add_values_wide<D, NT>(w, tile, u, g, tig, pk[u], sees);
+                            }
+                    } else {
+                        // tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in small^(i+1) .. small^i
+                        const float up = __uint_as_float((uint32_t)(127 + range) << 23);
+                        const bool four = __any_sync(0xffffffffu, low < tiny);
+#pragma unroll 1
+                        for (int pass = four ? 0 : 1; pass < 2; ++pass) {
+                            const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part = pass == 0 ? tiny * small : small;
+                            const float floor_ = pass == 0 ? 0.f : (four ? tiny : 0.f);
+                            uint32_t deep[2][NT][2];
+#pragma unroll
+                            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h) {
+                                        float main_[2], deep_[2];
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e) {
+                                            const float v = x[u][nt][2 * h + e];
+                                            const bool here = !(v < floor_) && !(v >= bound);
+                                            main_[e] = here && !(v < part) ? v * gain : 0.f;
+                                            deep_[e] = here && v < part ? v * gain * up : 0.f;
+                                        }
+                                        pk[u][nt][h] = transpose8x8(pack_half2(main_[0], main_[1]));
+                                        deep[u][nt][h] = transpose8x8(pack_half2(deep_[0], deep_[1]));
+                                    }
+                            float ff[NT][2];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
+                            if (four) rescale(w, ff);
+                            add_values<D, NT, 2>(w, tile, g, tig, pk, deep, up, small);
+                        }
+                    }
                 }
             }
             __syncwarp();
