@@ -76,6 +76,7 @@ cudaError_t linear_fp4_launch(const Fp4Plan &plan, const void *X, const uint8_t 
 int linear_fp4_take_status(uint32_t *out);
 int linear_mma_take_status(uint32_t *out);    // the mma.sync kernel (mxq_linear_mma.cu)
 int linear_batch_take_status(uint32_t *out);  // the persistent multi-layer kernel (mxq_linear_batch.cu)
+int kv_take_status(uint32_t *out);            // the attention kernel over 4-bit pages (mxq_kv_attention.cu)
 int linear_bf16_take_status(uint32_t *out);   // the BF16-weight comparison kernel (mxq_linear_bf16.cu)
 
 // Bounds-checked build (-DMXQ_DEBUG_BOUNDS): every translation unit with linear or cache kernels keeps a record of global accesses

@@ -29,6 +29,7 @@
 #include <math.h>
 
 #include "mxq_kv.cuh"
+#include "mxq_tcgen05.cuh"
 
 namespace mxq {
 
@@ -52,7 +53,8 @@ constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may e
 constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
 constexpr int kHalfRange = kScaleBias + 14;    // a normal number while P * 2^(scale - ref) >= 2^-24
 constexpr int kScaleSpread = 14;               // scales this far below ref still take the FP16 step
-constexpr int kScaleSlack = 3;                 // how far (log2) a tile's largest scale may lie below ref
+constexpr int kScaleSlack = 8;                 // scales no further below ref need no closer look
+constexpr int kScaleLag = 3;                   // how far (log2) a tile's largest scale may lie below ref when it is looked at
 constexpr int kScaleDrop = 12;                 // how far ref may fall below its highest: accumulators are below 2^18 per token, and
                                                // the deepest of the tiers below scales them by up to 2^72
 
@@ -131,12 +133,39 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// two scale bytes -> 2^(b - 127) each (0xFF: NaN), exactly
-__device__ __forceinline__ float2 scales2(uint32_t half) {
-    uint32_t o;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.bf16x2.ue8m0x2 %0, l;\n\t}" : "=r"(o) : "r"(half));
-    return make_float2(__uint_as_float(o << 16), __uint_as_float(o & 0xFFFF0000u));
+// Scale byte j of a word as a factor: the byte in the exponent's place.  The lowest mantissa bit is set so that 0xFF is a NaN (the
+// factor is then 1 + 2^-23 of the power of two, the same for every score); byte 0 becomes 2^-149: blocks scaled by 2^-127 count as zero.
+template <int J>
+__device__ __forceinline__ float scale_factor(uint32_t w) {
+    return __uint_as_float(((J == 3 ? w >> 1 : w * (1u << (23 - 8 * (J & 3)))) & 0x7F800000u) | 1u);
 }
+__device__ __forceinline__ float scale_factor(uint32_t w, int j) {   // (j a constant after unrolling)
+    return j == 0 ? scale_factor<0>(w) : j == 1 ? scale_factor<1>(w) : j == 2 ? scale_factor<2>(w) : scale_factor<3>(w);
+}
+// pairs of FP32 operations in one instruction
+__device__ __forceinline__ uint64_t pair2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ void scale4(float (&o)[4], float f01, float f23) {   // o[0..1] *= f01, o[2..3] *= f23
+    uint64_t a, b;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a) : "l"(pair2(o[0], o[1])), "l"(pair2(f01, f01)));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(b) : "l"(pair2(o[2], o[3])), "l"(pair2(f23, f23)));
+    split2(a, o[0], o[1]), split2(b, o[2], o[3]);
+}
+
 // x * 2^e for e <= 127 (below -252 as -252) in two steps
 __device__ __forceinline__ float scale_by_power(float x, int e) {
     const int first = max(e, -126);
@@ -154,13 +183,6 @@ __device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[N]) {
     else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
     else w[0] = lds_u32(a);
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // ---- one segment, as its CTA sees it ----------------------------------------------------------------------------------------
 
 struct Segment {
@@ -171,6 +193,8 @@ struct Segment {
 
 // A warp's state of a segment.  Column c of column block nt is flattened row r0 + 8 * nt + c; a lane (g = lane / 4, tig = lane % 4) holds
 // columns 2 * tig and 2 * tig + 1.
+__device__ unsigned int g_kv_status = 0;   // sticky: bit 0 a requested tile never arrived
+
 template <int D, int NT>
 struct WarpState {
     float o[D / 16][NT][4];   // rows of block j: d = 32 j + 4 g + {0, 1} in o[2j], + {2, 3} in o[2j + 1]; [d][column]: 00 01 10 11
@@ -194,16 +218,14 @@ __device__ __forceinline__ void rescale(WarpState<D, NT> &w, const float (&f)[NT
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w.o[i][n][e] *= f[n][e & 1];
-}
-
-// bytes 2y and 2y + 1 of a word -> two pairs of halves
-__device__ __forceinline__ void decode2(uint32_t w, int y, uint32_t (&h)[2]) {
-    asm("{\n\t.reg .b16 l, u;\n\t.reg .b8 b0, b1;\n\tmov.b32 {l, u}, %2;\n\tmov.b16 {b0, b1}, l;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t}"
-        : "=r"(h[0]), "=r"(h[1])
-        : "r"(y ? w >> 16 : w));
+        {
+            const uint64_t ff = pair2(f[n][0], f[n][1]);
+            float(&o)[4] = w.o[i][n];
+            uint64_t a, b;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a) : "l"(pair2(o[0], o[1])), "l"(ff));
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(b) : "l"(pair2(o[2], o[3])), "l"(ff));
+            split2(a, o[0], o[1]), split2(b, o[2], o[3]);
+        }
 }
 
 // O += P . V for a whole tile, in FP16.  p[u][n][h]: packed weights of row g of column block n, tokens 16 u + tig + 8 h (low half) and
@@ -234,37 +256,40 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
     // exponent field of 2^(scale - ref + kScaleBias): never below 1 here, so both halves fit one 32-bit multiply-add
     const uint32_t bias = (uint32_t)(15 + kScaleBias - w.ref) * (0x10001u << 10);
 #pragma unroll
-    for (int j = 0; j < kNb; ++j) {
-        const int x = j / 2, y = j & 1;
-        uint32_t e[2][2][2], o[2][2][2], sc[2][2];
+    for (int x = 0; x < kW; ++x) {
+        uint32_t e[2][2][4], o[2][2][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                decode2(ev[u][h][x], y, e[u][h]);
-                decode2(od[u][h][x], y, o[u][h]);
-                sc[u][h] = __byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140) * 1024u + bias;   // (the two tokens' scales as 16-bit numbers)
-            }
+            for (int h = 0; h < 2; ++h) decode4(ev[u][h][x], e[u][h]), decode4(od[u][h][x], o[u][h]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float(&o0)[4] = w.o[2 * j][n], (&o1)[4] = w.o[2 * j + 1][n];
-            if constexpr (kTiers == 2) {
+        for (int y = 0; y < 2; ++y) {
+            const int j = 2 * x + y;
+            uint32_t sc[2][2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o0[i] *= up, o1[i] *= up;
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t b0 = mul_half2(deep[u][n][0], sc[u][0]), b1 = mul_half2(deep[u][n][1], sc[u][1]);
-                    mma16816<false>(o0, e[u][0][0], o[u][0][0], e[u][1][0], o[u][1][0], b0, b1);
-                    mma16816<false>(o1, e[u][0][1], o[u][0][1], e[u][1][1], o[u][1][1], b0, b1);
+                for (int h = 0; h < 2; ++h)     // (the two tokens' scales as 16-bit numbers)
+                    sc[u][h] = __byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140) * 1024u + bias;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float(&o0)[4] = w.o[2 * j][n], (&o1)[4] = w.o[2 * j + 1][n];
+                if constexpr (kTiers == 2) {
+                    scale4(o0, up, up), scale4(o1, up, up);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t b0 = mul_half2(deep[u][n][0], sc[u][0]), b1 = mul_half2(deep[u][n][1], sc[u][1]);
+                        mma16816<false>(o0, e[u][0][2 * y], o[u][0][2 * y], e[u][1][2 * y], o[u][1][2 * y], b0, b1);
+                        mma16816<false>(o1, e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
+                    }
+                    scale4(o0, down, down), scale4(o1, down, down);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o0[i] *= down, o1[i] *= down;
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t b0 = mul_half2(p[u][n][0], sc[u][0]), b1 = mul_half2(p[u][n][1], sc[u][1]);
-                mma16816<false>(o0, e[u][0][0], o[u][0][0], e[u][1][0], o[u][1][0], b0, b1);
-                mma16816<false>(o1, e[u][0][1], o[u][0][1], e[u][1][1], o[u][1][1], b0, b1);
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t b0 = mul_half2(p[u][n][0], sc[u][0]), b1 = mul_half2(p[u][n][1], sc[u][1]);
+                    mma16816<false>(o0, e[u][0][2 * y], o[u][0][2 * y], e[u][1][2 * y], o[u][1][2 * y], b0, b1);
+                    mma16816<false>(o1, e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
+                }
             }
         }
     }
@@ -325,6 +350,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
     __shared__ int64_t sh_scan[kAttWarps + 3];
     __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
     __shared__ int sh_last;
+    __shared__ __align__(8) uint64_t sh_bars[kAttWarps][kAttStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, tig = lane & 3;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * T::kBytes;
     uint4 *const sh_q = reinterpret_cast<uint4 *>(att_smem_raw + kAttWarps * kAttStages * T::kBytes);
@@ -332,8 +358,15 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
     constexpr int kMergeRow = D + 4;
     static_assert(kAttWarps * 8 * kMergeRow * 4 <= kAttWarps * kAttStages * T::kBytes, "the merge buffer lies over the rings");
 
+    const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
+    uint32_t issued = 0;      // tiles the warp has requested before this segment: ring slots and phases run on
+    if (lane == 0) {
+        for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     pdl_trigger();
     pdl_wait();
+    asm volatile("fence.proxy.async;" ::: "memory");      // tiles may have been written by the kernel before, with ordinary stores
 
     // ---- this CTA's share of all steps ----
     auto shape_of = [&](int b, int &len, int &rows, int64_t &n, int64_t &tiles) {
@@ -405,31 +438,28 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
         const int first_tile = step0 * kAttWarps + warp;
         const int count = nrows > 0 && first_tile < last_tile ? min(steps, (last_tile - first_tile + kAttWarps - 1) / kAttWarps) : 0;
         int window = 0, ids = -1;          // page ids of tiles window + lane
-        uint32_t there = 0;                // bit per ring slot: the tile's page exists
         auto load_ids = [&](int k) {
             window = k;
             const int t = first_tile + (k + lane) * kAttWarps;
             ids = k + lane < count ? s.page(b, (t * kTileTokens) >> c.page_shift) : -1;
         };
-        auto issue = [&](int k) {
-            if (k < count) {
-                if (k - window >= 32) load_ids(k);
-                const int page = __shfl_sync(0xffffffffu, ids, k - window);
-                const uint32_t slot = (uint32_t)(k % kAttStages);
-                const bool ok = kv_page_ok(c, page);
-                there = (there & ~(1u << slot)) | ((uint32_t)ok << slot);
+        uint32_t there = 0;                // bit per ring slot: the tile's page exists
+        auto issue = [&](int k) {          // one lane requests the whole tile; a tile without a page completes at once
+            if (k >= count) return;
+            if (k - window >= 32) load_ids(k);
+            const int page = __shfl_sync(0xffffffffu, ids, k - window);
+            const uint32_t slot = (issued + (uint32_t)k) % kAttStages;
+            const bool ok = kv_page_ok(c, page);
+            there = (there & ~(1u << slot)) | ((uint32_t)ok << slot);
+            if (lane == 0) {
+                const uint32_t bar = bars + 8 * slot;
+                mbar_expect_tx(bar, ok ? T::kBytes : 0);
                 if (ok) {
                     const int t = (first_tile + k * kAttWarps) * kTileTokens;
-                    const uint8_t *src = kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), sg.head);
-                    const uint32_t dst = ring + slot * T::kBytes;
-#pragma unroll
-                    for (int i = 0; i < (T::kBytes + 511) / 512; ++i) {
-                        const int off = i * 512 + lane * 16;
-                        if (off < T::kBytes) copy16(dst + off, MXQ_AT(src + off, 16, c.pool, c.pool_bytes));
-                    }
+                    bulk_load(ring + slot * T::kBytes, MXQ_AT(kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), sg.head), T::kBytes, c.pool, c.pool_bytes),
+                              T::kBytes, bar);
                 }
             }
-            copy_commit();
         };
         if (count > 0) load_ids(0);
 #pragma unroll
@@ -494,11 +524,14 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                 for (int e = 0; e < 4; ++e) w.o[i][nt][e] = 0.f;
         }
 
+        bool arrived = true;
         for (int k = 0; k < count; ++k) {
-            const uint32_t slot = (uint32_t)(k % kAttStages), tile = ring + slot * T::kBytes;
+            const uint32_t at = issued + (uint32_t)k, slot = at % kAttStages, tile = ring + slot * T::kBytes;
             const int t0 = (first_tile + k * kAttWarps) * kTileTokens;
-            copy_wait<kAttStages - 1>();
-            __syncwarp();
+            if (!mbar_wait(bars + 8 * slot, (at / kAttStages) & 1u)) {      // (never in normal operation; the segment's rows become NaN)
+                if (lane == 0) atomicOr(&g_kv_status, 1u);
+                arrived = false;
+            }
             if ((there >> slot) & 1u) {
                 // ---- scores ----
                 float x[2][NT][4];
@@ -526,8 +559,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                         uint32_t h0[4], h1[4];
                         decode4(k0[j], h0);
                         decode4(k1[j], h1);
-                        const float2 f0 = scales2(s0 >> (16 * (j / 2))), f1 = scales2(s1 >> (16 * (j / 2)));
-                        const float c0 = j & 1 ? f0.y : f0.x, c1 = j & 1 ? f1.y : f1.x;
+                        const float c0 = scale_factor(s0, j), c1 = scale_factor(s1, j);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             uint4 q;
@@ -536,53 +568,59 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                             float d[4] = {0.f, 0.f, 0.f, 0.f};
                             mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
                             mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
-                            x[u][nt][0] += d[0] * c0, x[u][nt][1] += d[1] * c0;
-                            x[u][nt][2] += d[2] * c1, x[u][nt][3] += d[3] * c1;
+                            float(&v)[4] = x[u][nt];
+                            split2(fma2(pair2(d[0], d[1]), pair2(c0, c0), pair2(v[0], v[1])), v[0], v[1]);
+                            split2(fma2(pair2(d[2], d[3]), pair2(c1, c1), pair2(v[2], v[3])), v[2], v[3]);
                         }
                     }
                 }
-                // ---- V scales of the tile: largest and smallest ----
-                uint32_t sv = 0, in = 0;       // a word of them per lane, and the bytes of tokens that are there
+                // ---- V scales of the tile: within kScaleSlack .. kScaleHeadroom of ref, or looked at closely ----
+                uint32_t sv = (uint32_t)w.ref * 0x01010101u;       // a word of them per lane
                 const uint32_t sv_at = tile + T::kVs + 4 * lane;
                 const bool tail = t0 + kTileTokens > len;
-                if (lane < 8 * kNb) {
-                    sv = lds_u32(sv_at);
-                    in = 0xFFFFFFFFu;
-                    if (tail) {
-                        const int t = t0 + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
-                        in = (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
+                if (8 * kNb == 32 || lane < 8 * kNb) sv = lds_u32(sv_at);
+                int range = kHalfRange - kScaleSlack;              // binades of weight the tile's scales leave to FP16
+                bool nan = false;
+                {
+                    const uint32_t low = (uint32_t)(w.ref - kScaleSlack) * 0x10001u, high = (uint32_t)(w.ref + kScaleHeadroom) * 0x10001u;
+                    const uint32_t ev = __byte_perm(sv, 0, 0x4240), od = __byte_perm(sv, 0, 0x4341);
+                    const bool close = __vminu2(ev, od) == __vmaxu2(__vminu2(ev, od), low) && __vmaxu2(ev, od) == __vminu2(__vmaxu2(ev, od), high);
+                    if (!__all_sync(0xffffffffu, close) || tail || w.ref < kScaleSlack) {
+                        uint32_t in = 0;                           // the bytes of tokens that are there
+                        if (lane < 8 * kNb) {
+                            const int t = t0 + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
+                            in = (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
+                        }
+                        int hi = 0, lo = 255;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int v = (int)((sv >> (8 * i)) & 0xFFu);
+                            if (((in >> (8 * i)) & 1u) == 0) continue;
+                            if (v == 255) nan = true;
+                            else hi = max(hi, v);
+                            lo = min(lo, v);
+                        }
+                        nan = __any_sync(0xffffffffu, nan);
+                        hi = (int)__reduce_max_sync(0xffffffffu, (uint32_t)hi);
+                        lo = (int)__reduce_min_sync(0xffffffffu, (uint32_t)lo);
+                        // ref follows the tiles' largest scale up and (within what FP32 accumulators bear) down
+                        if (hi > w.ref + kScaleHeadroom || hi + kScaleLag < w.ref) {
+                            w.ref_max = max(w.ref_max, hi);
+                            const int ref = max(hi, w.ref_max - kScaleDrop);
+                            const float f = scale_by_power(1.f, w.ref - ref);
+                            float ff[NT][2];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = f;
+                            rescale(w, ff);
+                            w.ref = ref;
+                        }
+                        if (tail) {      // tokens behind the end carry no weight: any scale that fits will do
+                            if (lane < 8 * kNb) asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"((sv & in) | ((uint32_t)w.ref * 0x01010101u & ~in)) : "memory");
+                            __syncwarp();
+                        }
+                        range = kHalfRange - max(w.ref - lo, 0);
                     }
                 }
-                const uint32_t hi2 = __vmaxu2(sv & in & 0x00FF00FFu, ((sv & in) >> 8) & 0x00FF00FFu);
-                const uint32_t lo2 = __vminu2((sv | ~in) & 0x00FF00FFu, ((sv | ~in) >> 8) & 0x00FF00FFu);
-                int hi = (int)__reduce_max_sync(0xffffffffu, max(hi2 & 0xFFFFu, hi2 >> 16));
-                const int lo = (int)__reduce_min_sync(0xffffffffu, min(lo2 & 0xFFFFu, lo2 >> 16));
-                const bool nan = hi == 255;
-                if (nan) {       // the largest that is a number
-                    hi = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int v = (int)(((sv & in) >> (8 * i)) & 0xFFu);
-                        if (v != 255) hi = max(hi, v);
-                    }
-                    hi = (int)__reduce_max_sync(0xffffffffu, (uint32_t)hi);
-                }
-                // ref follows the tiles' largest scale up and (within what FP32 accumulators bear) down
-                if (hi > w.ref + kScaleHeadroom || hi + kScaleSlack < w.ref) {
-                    w.ref_max = max(w.ref_max, hi);
-                    const int ref = max(hi, w.ref_max - kScaleDrop);
-                    const float f = scale_by_power(1.f, w.ref - ref);
-                    float ff[NT][2];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = f;
-                    rescale(w, ff);
-                    w.ref = ref;
-                }
-                if (tail) {      // tokens behind the end carry no weight: any scale that fits will do
-                    if (lane < 8 * kNb) asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"((sv & in) | ((uint32_t)w.ref * 0x01010101u & ~in)) : "memory");
-                    __syncwarp();
-                }
-                const int range = kHalfRange - max(w.ref - lo, 0);      // binades of weight the tile's scales leave to FP16
                 const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
 
                 // ---- weights, under the maximum as it stands ----
@@ -592,22 +630,25 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                 float l[NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    l[nt][0] = w.l[nt][0], l[nt][1] = w.l[nt][1];
+                    uint64_t sum = pair2(w.l[nt][0], w.l[nt][1]);
+                    const uint64_t f = pair2(factor[nt][0], factor[nt][1]), m = pair2(-w.m[nt][0], -w.m[nt][1]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const float p0 = exp2_fast(fmaf(x[u][nt][2 * h], factor[nt][0], -w.m[nt][0]));
-                            const float p1 = exp2_fast(fmaf(x[u][nt][2 * h + 1], factor[nt][1], -w.m[nt][1]));
-                            l[nt][0] += p0, l[nt][1] += p1;
+                            float p0, p1;
+                            split2(fma2(pair2(x[u][nt][2 * h], x[u][nt][2 * h + 1]), f, m), p0, p1);
+                            p0 = exp2_fast(p0), p1 = exp2_fast(p1);
+                            sum = add2(sum, pair2(p0, p1));
                             pk[u][nt][h] = pack_half2(p0, p1);
                             most = max_half2(most, pk[u][nt][h]);
                             least = min_half2(least, pk[u][nt][h]);
                         }
+                    split2(sum, l[nt][0], l[nt][1]);
                 }
                 // (NaN compares false)
                 const bool plain = !edge && all_le_half2(most, 0x4C004C00u) && all_le_half2(pack_half2(small, small), least);
-                if (__all_sync(0xffffffffu, plain) && range >= kHalfRange - kScaleSpread) {
+                if (__all_sync(0xffffffffu, plain) && range >= kHalfRange - kScaleSpread && !nan) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         w.l[nt][0] = l[nt][0], w.l[nt][1] = l[nt][1];
@@ -725,11 +766,12 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
         }
 
         // ---- join the warps: each as (maximum, sum, average), eight rows at a time over the drained rings ----
-        copy_wait<0>();
+        issued += (uint32_t)count;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
+                if (!arrived) w.l[nt][e] = NAN;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
                 if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
@@ -831,6 +873,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
         // rows the sequence does not have
         if (finish && sg.r0 == 0)
             for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) store_row(r, 4 * lane, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+        fence_async_proxy();  // (the rings held ordinary stores; bulk copies come next)
         __syncthreads();      // the rings, sh_ml and sh_q are free again
         first += steps;
         left -= steps;
@@ -839,6 +882,15 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
 }
 
 MXQ_BOUNDS_TU(bounds_take_kv_attention)
+
+// returns and clears this kernel's sticky status word (see mxq_linear_device_status)
+int kv_take_status(uint32_t *out) {
+    unsigned int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_kv_status, sizeof v) != cudaSuccess) return MXQ_ERR_CUDA;
+    if (v != 0 && cudaMemcpyToSymbol(g_kv_status, &zero, sizeof zero) != cudaSuccess) return MXQ_ERR_CUDA;
+    *out = v;
+    return MXQ_OK;
+}
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
 
