@@ -46,29 +46,31 @@ struct KvQuery {
 };
 
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
-constexpr int kAttStages = 2;                  // tiles in a warp's ring
+constexpr int kAttStages = 2;                  // units in a warp's ring
 constexpr int kAttMaxCtas = 1024;              // tickets in the workspace's first 4096 bytes
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
 constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
 constexpr int kHalfRange = kScaleBias + 14;    // a normal number while P * 2^(scale - ref) >= 2^-24
 constexpr int kScaleSpread = 14;               // scales this far below ref still take the FP16 step
-constexpr int kScaleSlack = 8;                 // scales no further below ref need no closer look
-constexpr int kScaleLag = 3;                   // how far (log2) a tile's largest scale may lie below ref when it is looked at
+constexpr int kScaleLag = 3;                   // how far (log2) a tile's largest scale may lie below ref
 constexpr int kScaleDrop = 12;                 // how far ref may fall below its highest: accumulators are below 2^18 per token, and
                                                // the deepest of the tiers below scales them by up to 2^72
 
 // rows of the flattened (token row, head of the group) index per tile of NT column blocks
 template <int NT>
 constexpr int kAttRows = 8 * NT;
+template <int NT>
+constexpr int kAttTiles = NT == 1 ? 2 : 1;     // tiles a warp takes at a time (a unit): with few rows the checks and the ring's upkeep
+                                               // cost as much as a product, and two tiles share them
 constexpr int kAttRegisterQ = 2;               // up to this NT the query fragments stay in registers
 
-template <int NT>
-constexpr int kAttCtasPerSm = NT == 1 ? 4 : NT == 2 ? 3 : 2;
+template <int D, int NT>
+constexpr int kAttCtasPerSm = NT == 1 ? (D == 128 ? 3 : 4) : NT == 2 ? (D == 128 ? 2 : 3) : 2;
 template <int D, int NT>
 constexpr size_t kAttSlotFloats = (size_t)kAttRows<NT> * (D + 2);
 template <int D, int NT>
-constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * KvTile<D>::kBytes + (NT > kAttRegisterQ ? (size_t)(D / 32) * NT * 32 * 16 : 0);
+constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes + (NT > kAttRegisterQ ? (size_t)(D / 32) * NT * 32 * 16 : 0);
 
 // ---- fragments ------------------------------------------------------------------------------------------------------------
 
@@ -198,7 +200,8 @@ __device__ unsigned int g_kv_status = 0;   // sticky: bit 0 a requested tile nev
 template <int D, int NT>
 struct WarpState {
     float o[D / 16][NT][4];   // rows of block j: d = 32 j + 4 g + {0, 1} in o[2j], + {2, 3} in o[2j + 1]; [d][column]: 00 01 10 11
-    float m[NT][2], l[NT][2];
+    float m[NT][2], l[NT][2];     // maximum and sum; m = 0 while over = -inf
+    float over[NT][2];            // how far a score may exceed m: kMaxSlack, or -inf before the first token the row sees
     int ref, ref_max;
 };
 
@@ -295,9 +298,9 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
     }
 }
 
-// The same for the 16 tokens of group u, in BF16: any spread of weights and scales; NaN scales count only where the row sees the token.
+// The same for the 16 tokens of group u (from token t0 of the sequence on), in BF16: any spread of weights and scales; NaN scales count only where the row sees the token.
 template <int D, int NT, class Sees>
-__device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t tile, int u, int g, int tig, const uint32_t (&p)[NT][2], Sees sees) {
+__device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t tile, int u, int t0, int g, int tig, const uint32_t (&p)[NT][2], Sees sees) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb, kW = kNb / 2;
     uint32_t sw[kNb];
@@ -332,7 +335,7 @@ __device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t ti
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
                         if (((word >> (16 * y + 8 * e)) & 0xFFu) == 0xFFu)
-                            f = (f & ~(0xFFFFu << (16 * e))) | ((sees(n, 16 * u + tig + 8 * h + 4 * e) ? 0x7FC0u : 0u) << (16 * e));
+                            f = (f & ~(0xFFFFu << (16 * e))) | ((sees(n, t0 + tig + 8 * h + 4 * e) ? 0x7FC0u : 0u) << (16 * e));
                     b[h] = mul_bf162(p[n][h], f);
                 }
                 mma16816<true>(w.o[2 * j][n], ev[0][2 * y], od[0][2 * y], ev[1][2 * y], od[1][2 * y], b[0], b[1]);
@@ -343,7 +346,7 @@ __device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t ti
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_kernel(KvView c, KvSeqs s, KvQuery a) {
+__global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attention_kernel(KvView c, KvSeqs s, KvQuery a) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb;
     extern __shared__ __align__(128) uint8_t att_smem_raw[];
@@ -352,16 +355,17 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
     __shared__ int sh_last;
     __shared__ __align__(8) uint64_t sh_bars[kAttWarps][kAttStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, tig = lane & 3;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * T::kBytes;
-    uint4 *const sh_q = reinterpret_cast<uint4 *>(att_smem_raw + kAttWarps * kAttStages * T::kBytes);
+    constexpr int kU = kAttTiles<NT>, kUnitTokens = kU * kTileTokens, kUnitBytes = kU * T::kBytes;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * kUnitBytes;
+    uint4 *const sh_q = reinterpret_cast<uint4 *>(att_smem_raw + kAttWarps * kAttStages * kUnitBytes);
     float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][8][D + 4], between segments
     constexpr int kMergeRow = D + 4;
-    static_assert(kAttWarps * 8 * kMergeRow * 4 <= kAttWarps * kAttStages * T::kBytes, "the merge buffer lies over the rings");
+    static_assert(kAttWarps * 8 * kMergeRow * 4 <= kAttWarps * kAttStages * kUnitBytes, "the merge buffer lies over the rings");
 
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
-    uint32_t issued = 0;      // tiles the warp has requested before this segment: ring slots and phases run on
+    uint32_t issued = 0;      // units the warp has requested before this segment: ring slots and phases run on
     if (lane == 0) {
-        for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, 1);
+        for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, kU);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_trigger();
@@ -371,7 +375,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
     // ---- this CTA's share of all steps ----
     auto shape_of = [&](int b, int &len, int &rows, int64_t &n, int64_t &tiles) {
         len = s.len(b), rows = s.nrows(b);
-        n = max(1, (len + kAttWarps * kTileTokens - 1) / (kAttWarps * kTileTokens));
+        n = max(1, (len + kAttWarps * kUnitTokens - 1) / (kAttWarps * kUnitTokens));
         tiles = max(1, (rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
     int64_t first, left;      // global index of the CTA's next step; steps left
@@ -433,35 +437,32 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
         sg.len = len, sg.base = len - rows, sg.rows_total = rows * a.group;
         const int nrows = min(max(sg.rows_total - sg.r0, 0), kAttRows<NT>);
 
-        // ---- the warp's tiles: number k is tile (step0 + k) * kAttWarps + warp of the sequence ----
-        const int last_tile = (len + kTileTokens - 1) / kTileTokens;
-        const int first_tile = step0 * kAttWarps + warp;
-        const int count = nrows > 0 && first_tile < last_tile ? min(steps, (last_tile - first_tile + kAttWarps - 1) / kAttWarps) : 0;
-        int window = 0, ids = -1;          // page ids of tiles window + lane
-        auto load_ids = [&](int k) {
-            window = k;
-            const int t = first_tile + (k + lane) * kAttWarps;
-            ids = k + lane < count ? s.page(b, (t * kTileTokens) >> c.page_shift) : -1;
-        };
-        uint32_t there = 0;                // bit per ring slot: the tile's page exists
-        auto issue = [&](int k) {          // one lane requests the whole tile; a tile without a page completes at once
+        // ---- the warp's units: number k is unit (step0 + k) * kAttWarps + warp of the sequence ----
+        const int last_unit = (len + kUnitTokens - 1) / kUnitTokens, first_unit = step0 * kAttWarps + warp;
+        const int count = nrows > 0 && first_unit < last_unit ? min(steps, (last_unit - first_unit + kAttWarps - 1) / kAttWarps) : 0;
+        const uint8_t *source = nullptr;   // lane i: where tile i of the next 32 tiles of the warp's lies (nullptr: nowhere)
+        uint32_t exist = 0, there = 0;     // bit i: that tile exists; the units requested so far, kU bits each, the newest lowest
+        auto issue = [&](int k) {
+            there <<= kU;
             if (k >= count) return;
-            if (k - window >= 32) load_ids(k);
-            const int page = __shfl_sync(0xffffffffu, ids, k - window);
-            const uint32_t slot = (issued + (uint32_t)k) % kAttStages;
-            const bool ok = kv_page_ok(c, page);
-            there = (there & ~(1u << slot)) | ((uint32_t)ok << slot);
-            if (lane == 0) {
-                const uint32_t bar = bars + 8 * slot;
-                mbar_expect_tx(bar, ok ? T::kBytes : 0);
-                if (ok) {
-                    const int t = (first_tile + k * kAttWarps) * kTileTokens;
-                    bulk_load(ring + slot * T::kBytes, MXQ_AT(kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), sg.head), T::kBytes, c.pool, c.pool_bytes),
-                              T::kBytes, bar);
+            const int at = (k * kU) & 31;
+            if (at == 0) {
+                const int t = ((first_unit + (k + lane / kU) * kAttWarps) * kU + lane % kU) * kTileTokens;
+                source = nullptr;
+                if (k + lane / kU < count && t < len) {
+                    const int page = s.page(b, t >> c.page_shift);
+                    if (kv_page_ok(c, page)) source = kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), sg.head);
                 }
+                exist = __ballot_sync(0xffffffffu, source != nullptr);
+            }
+            there |= (exist >> at) & ((1u << kU) - 1);
+            if ((unsigned)(lane - at) < (unsigned)kU) {      // the lane that knows a tile requests it; one that is not there completes at once
+                const uint32_t slot = (issued + (uint32_t)k) % kAttStages, bar = bars + 8 * slot;
+                mbar_expect_tx(bar, source != nullptr ? T::kBytes : 0);
+                if (source != nullptr)
+                    bulk_load(ring + slot * kUnitBytes + (uint32_t)(lane - at) * T::kBytes, MXQ_AT(source, T::kBytes, c.pool, c.pool_bytes), T::kBytes, bar);
             }
         };
-        if (count > 0) load_ids(0);
 #pragma unroll
         for (int k = 0; k < kAttStages; ++k) issue(k);
 
@@ -517,7 +518,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) w.m[nt][e] = -INFINITY, w.l[nt][e] = 0.f;
+            for (int e = 0; e < 2; ++e) w.m[nt][e] = 0.f, w.over[nt][e] = -INFINITY, w.l[nt][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -526,34 +527,32 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
 
         bool arrived = true;
         for (int k = 0; k < count; ++k) {
-            const uint32_t at = issued + (uint32_t)k, slot = at % kAttStages, tile = ring + slot * T::kBytes;
-            const int t0 = (first_tile + k * kAttWarps) * kTileTokens;
+            const uint32_t at = issued + (uint32_t)k, slot = at % kAttStages, unit = ring + slot * kUnitBytes;
+            const int t0 = (first_unit + k * kAttWarps) * kUnitTokens;
             if (!mbar_wait(bars + 8 * slot, (at / kAttStages) & 1u)) {      // (never in normal operation; the segment's rows become NaN)
                 if (lane == 0) atomicOr(&g_kv_status, 1u);
                 arrived = false;
             }
-            if ((there >> slot) & 1u) {
-                // ---- scores ----
-                float x[2][NT][4];
+            const uint32_t here = (there >> (kU * (kAttStages - 1))) & ((1u << kU) - 1);
+            if (here != 0) {
+                constexpr int kG = 2 * kU;                   // groups of 16 tokens
                 const int tok = (g >> 1) + 4 * (g & 1);      // row g of the product is this token of the group, row g + 8 the one 8 further
+                // ---- scores ----
+                float x[kG][NT][4];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < kG; ++u) {
+                    const uint32_t tile = unit + (u / 2) * T::kBytes, row = tile + (16 * (u & 1) + tok) * T::kRow + 4 * kNb * tig;
                     uint32_t k0[kNb], k1[kNb];
-                    const uint32_t row = tile + (16 * u + tok) * T::kRow + 4 * kNb * tig;
                     lds_words<kNb>(row, k0);
                     lds_words<kNb>(row + 8 * T::kRow, k1);
                     uint32_t s0, s1;
-                    const uint32_t sa = tile + T::kKs + (16 * u + tok) * kNb;
+                    const uint32_t sa = tile + T::kKs + (16 * (u & 1) + tok) * kNb;
                     if constexpr (kNb == 4) {
                         s0 = lds_u32(sa), s1 = lds_u32(sa + 8 * kNb);
                     } else {
                         asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s0) : "r"(sa));
                         asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s1) : "r"(sa + 8 * kNb));
                     }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[u][nt][e] = 0.f;
 #pragma unroll
                     for (int j = 0; j < kNb; ++j) {
                         uint32_t h0[4], h1[4];
@@ -569,152 +568,167 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                             mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
                             mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
                             float(&v)[4] = x[u][nt];
-                            split2(fma2(pair2(d[0], d[1]), pair2(c0, c0), pair2(v[0], v[1])), v[0], v[1]);
-                            split2(fma2(pair2(d[2], d[3]), pair2(c1, c1), pair2(v[2], v[3])), v[2], v[3]);
+                            if (j == 0) v[0] = d[0] * c0, v[1] = d[1] * c0, v[2] = d[2] * c1, v[3] = d[3] * c1;
+                            else v[0] += d[0] * c0, v[1] += d[1] * c0, v[2] += d[2] * c1, v[3] += d[3] * c1;
                         }
                     }
                 }
-                // ---- V scales of the tile: within kScaleSlack .. kScaleHeadroom of ref, or looked at closely ----
-                uint32_t sv = (uint32_t)w.ref * 0x01010101u;       // a word of them per lane
-                const uint32_t sv_at = tile + T::kVs + 4 * lane;
-                const bool tail = t0 + kTileTokens > len;
-                if (8 * kNb == 32 || lane < 8 * kNb) sv = lds_u32(sv_at);
-                int range = kHalfRange - kScaleSlack;              // binades of weight the tile's scales leave to FP16
-                bool nan = false;
-                {
-                    const uint32_t low = (uint32_t)(w.ref - kScaleSlack) * 0x10001u, high = (uint32_t)(w.ref + kScaleHeadroom) * 0x10001u;
-                    const uint32_t ev = __byte_perm(sv, 0, 0x4240), od = __byte_perm(sv, 0, 0x4341);
-                    const bool close = __vminu2(ev, od) == __vmaxu2(__vminu2(ev, od), low) && __vmaxu2(ev, od) == __vminu2(__vmaxu2(ev, od), high);
-                    if (!__all_sync(0xffffffffu, close) || tail || w.ref < kScaleSlack) {
-                        uint32_t in = 0;                           // the bytes of tokens that are there
-                        if (lane < 8 * kNb) {
-                            const int t = t0 + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
-                            in = (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
-                        }
-                        int hi = 0, lo = 255;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int v = (int)((sv >> (8 * i)) & 0xFFu);
-                            if (((in >> (8 * i)) & 1u) == 0) continue;
-                            if (v == 255) nan = true;
-                            else hi = max(hi, v);
-                            lo = min(lo, v);
-                        }
-                        nan = __any_sync(0xffffffffu, nan);
-                        hi = (int)__reduce_max_sync(0xffffffffu, (uint32_t)hi);
-                        lo = (int)__reduce_min_sync(0xffffffffu, (uint32_t)lo);
-                        // ref follows the tiles' largest scale up and (within what FP32 accumulators bear) down
-                        if (hi > w.ref + kScaleHeadroom || hi + kScaleLag < w.ref) {
-                            w.ref_max = max(w.ref_max, hi);
-                            const int ref = max(hi, w.ref_max - kScaleDrop);
-                            const float f = scale_by_power(1.f, w.ref - ref);
-                            float ff[NT][2];
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = f;
-                            rescale(w, ff);
-                            w.ref = ref;
-                        }
-                        if (tail) {      // tokens behind the end carry no weight: any scale that fits will do
-                            if (lane < 8 * kNb) asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"((sv & in) | ((uint32_t)w.ref * 0x01010101u & ~in)) : "memory");
-                            __syncwarp();
-                        }
-                        range = kHalfRange - max(w.ref - lo, 0);
-                    }
-                }
-                const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
-
-                // ---- weights, under the maximum as it stands ----
-                const bool edge = t0 + kTileTokens > sg.base;
-                uint32_t pk[2][NT][2];
-                uint32_t most = 0, least = 0x7C007C00u;
-                float l[NT][2];
+                // ---- relative to the running maximum; what a row does not see; a new maximum ----
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    uint64_t sum = pair2(w.l[nt][0], w.l[nt][1]);
                     const uint64_t f = pair2(factor[nt][0], factor[nt][1]), m = pair2(-w.m[nt][0], -w.m[nt][1]);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < kG; ++u)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            float p0, p1;
-                            split2(fma2(pair2(x[u][nt][2 * h], x[u][nt][2 * h + 1]), f, m), p0, p1);
-                            p0 = exp2_fast(p0), p1 = exp2_fast(p1);
-                            sum = add2(sum, pair2(p0, p1));
-                            pk[u][nt][h] = pack_half2(p0, p1);
-                            most = max_half2(most, pk[u][nt][h]);
-                            least = min_half2(least, pk[u][nt][h]);
+                            float(&v)[4] = x[u][nt];
+                            split2(fma2(pair2(v[2 * h], v[2 * h + 1]), f, m), v[2 * h], v[2 * h + 1]);
                         }
-                    split2(sum, l[nt][0], l[nt][1]);
                 }
-                // (NaN compares false)
-                const bool plain = !edge && all_le_half2(most, 0x4C004C00u) && all_le_half2(pack_half2(small, small), least);
-                if (__all_sync(0xffffffffu, plain) && range >= kHalfRange - kScaleSpread && !nan) {
+                if (t0 + kUnitTokens > sg.base || here != (1u << kU) - 1) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        w.l[nt][0] = l[nt][0], w.l[nt][1] = l[nt][1];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) pk[u][nt][h] = transpose8x8(pk[u][nt][h]);
-                    }
-                    add_values<D, NT, 1>(w, tile, g, tig, pk, pk, 1.f, 1.f);
-                } else {
-                    // ---- mask, new maximum, weights again ----
-                    float top[NT][2];
-                    bool over = false;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        top[nt][0] = top[nt][1] = -INFINITY;
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                float v = x[u][nt][e] * factor[nt][e & 1];
-                                if (edge) {
-                                    const int t = t0 + 16 * u + tok + 8 * (e >> 1);
-                                    if (a.tree == nullptr ? t >= limit[nt][e & 1] : !row_sees(s, a, sg, sg.r0 + 8 * nt + 2 * tig + (e & 1), t)) v = -INFINITY;
-                                }
-                                x[u][nt][e] = v;
-                                top[nt][e & 1] = fmaxf(top[nt][e & 1], v);
-                            }
-                        over |= top[nt][0] > w.m[nt][0] + kMaxSlack || top[nt][1] > w.m[nt][1] + kMaxSlack;
-                    }
-                    if (__any_sync(0xffffffffu, over)) {
-                        float f[NT][2];
+                    for (int u = 0; u < kG; ++u)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float v = top[nt][e];
-#pragma unroll
-                                for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-                                const float m = fmaxf(w.m[nt][e], v);
-                                f[nt][e] = m == -INFINITY ? 1.f : exp2_fast(w.m[nt][e] - m);
-                                w.m[nt][e] = m;
-                                w.l[nt][e] *= f[nt][e];
+                            for (int e = 0; e < 4; ++e) {
+                                const int t = t0 + 16 * u + tok + 8 * (e >> 1);
+                                const bool seen = a.tree == nullptr ? t < limit[nt][e & 1] : row_sees(s, a, sg, sg.r0 + 8 * nt + 2 * tig + (e & 1), t);
+                                if (!seen || ((here >> (u / 2)) & 1u) == 0) x[u][nt][e] = -INFINITY;
                             }
-                        rescale(w, f);
+                }
+                bool over = false;
+                float top[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float v = fmaxf(x[0][nt][e], x[0][nt][2 + e]);
+#pragma unroll
+                        for (int u = 1; u < kG; ++u) v = fmaxf(v, fmaxf(x[u][nt][e], x[u][nt][2 + e]));
+                        top[nt][e] = v;
+                        over |= v > w.over[nt][e];
                     }
-                    float low = 1.f;             // the smallest weight that is not zero
+                if (__any_sync(0xffffffffu, over)) {
+                    float f[NT][2];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float v = top[nt][e];
+#pragma unroll
+                            for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+                            const bool none = w.over[nt][e] == -INFINITY;      // no token seen before: m is 0 for want of a better
+                            float up = none ? v : fmaxf(v, 0.f);               // how far the maximum rises
+                            f[nt][e] = none ? 1.f : exp2_fast(-up);
+                            if (v == -INFINITY) up = 0.f;
+                            else w.over[nt][e] = kMaxSlack;
+                            w.m[nt][e] += up;
+                            w.l[nt][e] *= f[nt][e];
+#pragma unroll
+                            for (int u = 0; u < kG; ++u) x[u][nt][e] -= up, x[u][nt][2 + e] -= up;
+                        }
+                    rescale(w, f);
+                }
+                // ---- weights ----
+                uint32_t pk[kG][NT][2], least = 0x7C007C00u;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    uint64_t sum = pair2(w.l[nt][0], w.l[nt][1]);
+#pragma unroll
+                    for (int u = 0; u < kG; ++u)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float &p0 = x[u][nt][2 * h], &p1 = x[u][nt][2 * h + 1];
+                            p0 = exp2_fast(p0), p1 = exp2_fast(p1);
+                            sum = add2(sum, pair2(p0, p1));
+                            pk[u][nt][h] = pack_half2(p0, p1);
+                            least = min_half2(least, pk[u][nt][h]);
+                        }
+                    split2(sum, w.l[nt][0], w.l[nt][1]);
+                }
+                // ---- V scales: largest and smallest ----
+                const bool tail = t0 + kUnitTokens > len || here != (1u << kU) - 1;
+                const uint32_t sv_at = unit + T::kVs + 4 * lane;
+                uint32_t sv[kU], in[kU], hi2 = 0, lo2 = 0x00FF00FFu;     // a word of a tile's scales per lane, and the bytes of tokens that are there
+#pragma unroll
+                for (int i = 0; i < kU; ++i) {
+                    sv[i] = 0, in[i] = 0xFFFFFFFFu;
+                    if (8 * kNb < 32 && lane >= 8 * kNb) in[i] = 0;
+                    else sv[i] = lds_u32(sv_at + i * T::kBytes);
+                    if (tail && in[i] != 0) {
+                        const int t = t0 + 32 * i + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
+                        in[i] = ((here >> i) & 1u) == 0 ? 0u : (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
+                    }
+                    const uint32_t up = sv[i] & in[i], dn = sv[i] | ~in[i];
+                    hi2 = __vmaxu2(hi2, __vmaxu2(__byte_perm(up, 0, 0x4240), __byte_perm(up, 0, 0x4341)));
+                    lo2 = __vminu2(lo2, __vminu2(__byte_perm(dn, 0, 0x4240), __byte_perm(dn, 0, 0x4341)));
+                }
+                hi2 = __vmaxu2(hi2, __byte_perm(hi2, 0, 0x1032)), lo2 = __vminu2(lo2, __byte_perm(lo2, 0, 0x1032));
+                int hi = (int)(__reduce_max_sync(0xffffffffu, hi2) & 0xFFFFu);
+                const int lo = (int)(__reduce_min_sync(0xffffffffu, lo2) & 0xFFFFu);
+                bool nan = false;
+                if (hi > w.ref + kScaleHeadroom || hi + kScaleLag < w.ref || tail) {
+                    nan = hi == 255;
+                    if (nan) {       // the largest that is a number
+                        hi = 0;
+#pragma unroll
+                        for (int i = 0; i < 4 * kU; ++i) {
+                            const int v = (int)(((sv[i / 4] & in[i / 4]) >> (8 * (i & 3))) & 0xFFu);
+                            if (v != 255) hi = max(hi, v);
+                        }
+                        hi = (int)__reduce_max_sync(0xffffffffu, (uint32_t)hi);
+                    }
+                    // ref follows the tiles' largest scale up and (within what FP32 accumulators bear) down
+                    if (hi > w.ref + kScaleHeadroom || hi + kScaleLag < w.ref) {
+                        w.ref_max = max(w.ref_max, hi);
+                        const int ref = max(hi, w.ref_max - kScaleDrop);
+                        const float f = scale_by_power(1.f, w.ref - ref);
+                        float ff[NT][2];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = f;
+                        rescale(w, ff);
+                        w.ref = ref;
+                    }
+                    if (tail) {      // tokens that are not there carry no weight: any scale that fits will do
+#pragma unroll
+                        for (int i = 0; i < kU; ++i)
+                            if (lane < 8 * kNb)
+                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at + i * T::kBytes), "r"((sv[i] & in[i]) | ((uint32_t)w.ref * 0x01010101u & ~in[i])) : "memory");
+                        __syncwarp();
+                    }
+                }
+                // ---- O += P V: which form holds these weights? ----
+                const int range = kHalfRange - max(w.ref - lo, 0);      // binades of weight the scales leave to FP16
+                const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
+                if (__all_sync(0xffffffffu, all_le_half2(pack_half2(small, small), least)) && range >= kHalfRange - kScaleSpread && !nan) {   // (NaN compares false)
+#pragma unroll
+                    for (int i = 0; i < kU; ++i) {
+                        uint32_t p[2][NT][2];
+#pragma unroll
                         for (int u = 0; u < 2; ++u)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                float &v = x[u][nt][e];
-                                v = exp2_fast(v - (w.m[nt][e & 1] == -INFINITY ? 0.f : w.m[nt][e & 1]));
-                                w.l[nt][e & 1] += v;
-                                low = fminf(low, v == 0.f ? 1.f : v);
-                            }
-                    // ---- O += P V: which form holds this tile's weights? ----
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(pk[2 * i + u][nt][h]);
+                        add_values<D, NT, 1>(w, unit + i * T::kBytes, g, tig, p, p, 1.f, 1.f);
+                    }
+                } else {
+                    float low = 1.f;             // the smallest weight that is not zero
+#pragma unroll
+                    for (int u = 0; u < kG; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) low = fminf(low, x[u][nt][e] == 0.f ? 1.f : x[u][nt][e]);
                     const float tiny = small * small;
                     if (nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, low < tiny * tiny)) {
-                        auto sees = [&](int nt, int t) { return row_sees(s, a, sg, sg.r0 + 8 * nt + g, t0 + t); };
+                        auto sees = [&](int nt, int t) { return row_sees(s, a, sg, sg.r0 + 8 * nt + g, t); };
 #pragma unroll 1
                         for (int part = 0; part < 2; ++part)       // the weights' upper and lower eight bits
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
+                            for (int u = 0; u < kG; ++u) {
+                                uint32_t p[NT][2];
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -722,9 +736,9 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                                         float &x0 = x[u][nt][2 * h], &x1 = x[u][nt][2 * h + 1];
                                         const uint32_t b = pack_bf162(x0, x1);
                                         x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xFFFF0000u);
-                                        pk[u][nt][h] = transpose8x8(b);
+                                        p[nt][h] = transpose8x8(b);
                                     }
-                                add_values_wide<D, NT>(w, tile, u, g, tig, pk[u], sees);
+                                add_values_wide<D, NT>(w, unit + (u / 2) * T::kBytes, u & 1, t0 + 16 * u, g, tig, p, sees);
                             }
                     } else {
                         // tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in small^(i+1) .. small^i
@@ -733,30 +747,34 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
 #pragma unroll 1
                         for (int pass = four ? 0 : 1; pass < 2; ++pass) {
                             const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part = pass == 0 ? tiny * small : small;
-                            const float floor_ = pass == 0 ? 0.f : (four ? tiny : 0.f);
-                            uint32_t deep[2][NT][2];
+                            const float from = pass == 1 && four ? tiny : 0.f;
+                            if (four) {
+                                float ff[NT][2];
 #pragma unroll
-                            for (int u = 0; u < 2; ++u)
+                                for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
+                                rescale(w, ff);
+                            }
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
+                            for (int i = 0; i < kU; ++i) {
+                                uint32_t p[2][NT][2], deep[2][NT][2];
 #pragma unroll
-                                    for (int h = 0; h < 2; ++h) {
-                                        float main_[2], deep_[2];
+                                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                                        for (int e = 0; e < 2; ++e) {
-                                            const float v = x[u][nt][2 * h + e];
-                                            const bool here = !(v < floor_) && !(v >= bound);
-                                            main_[e] = here && !(v < part) ? v * gain : 0.f;
-                                            deep_[e] = here && v < part ? v * gain * up : 0.f;
+                                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                        for (int h = 0; h < 2; ++h) {
+                                            float lo_[2], hi_[2];
+#pragma unroll
+                                            for (int e = 0; e < 2; ++e) {
+                                                const float v = x[2 * i + u][nt][2 * h + e], in_ = v < from || v >= bound ? 0.f : v * gain;
+                                                lo_[e] = v < part ? in_ * up : 0.f;
+                                                hi_[e] = v < part ? 0.f : in_;
+                                            }
+                                            p[u][nt][h] = transpose8x8(pack_half2(hi_[0], hi_[1]));
+                                            deep[u][nt][h] = transpose8x8(pack_half2(lo_[0], lo_[1]));
                                         }
-                                        pk[u][nt][h] = transpose8x8(pack_half2(main_[0], main_[1]));
-                                        deep[u][nt][h] = transpose8x8(pack_half2(deep_[0], deep_[1]));
-                                    }
-                            float ff[NT][2];
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
-                            if (four) rescale(w, ff);
-                            add_values<D, NT, 2>(w, tile, g, tig, pk, deep, up, small);
+                                add_values<D, NT, 2>(w, unit + i * T::kBytes, g, tig, p, deep, up, small);
+                            }
                         }
                     }
                 }
@@ -774,7 +792,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttCtasPerSm<NT>) kv_attention_k
                 if (!arrived) w.l[nt][e] = NAN;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
-                if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
+                if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.over[nt][e] == -INFINITY ? -INFINITY : w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
             }
         const bool whole = steps == n;
         const int64_t seg_end = seg_start + n;
@@ -904,7 +922,7 @@ template <int D>
 static size_t att_workspace(int nt) {
     const size_t sms = (size_t)sm_count();
     auto bytes = [&](size_t per_sm, size_t slot) { return 4096 + 2 * (sms * per_sm < kAttMaxCtas ? sms * per_sm : (size_t)kAttMaxCtas) * slot * 4; };
-    return nt == 1 ? bytes(kAttCtasPerSm<1>, kAttSlotFloats<D, 1>) : nt == 2 ? bytes(kAttCtasPerSm<2>, kAttSlotFloats<D, 2>) : bytes(kAttCtasPerSm<4>, kAttSlotFloats<D, 4>);
+    return nt == 1 ? bytes(kAttCtasPerSm<D, 1>, kAttSlotFloats<D, 1>) : nt == 2 ? bytes(kAttCtasPerSm<D, 2>, kAttSlotFloats<D, 2>) : bytes(kAttCtasPerSm<D, 4>, kAttSlotFloats<D, 4>);
 }
 
 template <int D, int NT>
@@ -921,7 +939,7 @@ static int att_launch(const KvView &c, const KvSeqs &s, const KvQuery &a, cudaSt
         }
         configured[dev] = true;
     }
-    int grid = sm_count() * kAttCtasPerSm<NT>;
+    int grid = sm_count() * (kAttCtasPerSm<D, NT>);
     if (grid > kAttMaxCtas) grid = kAttMaxCtas;
     return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)grid), kAttThreads, smem, stream, c, s, a);
 }
