@@ -402,7 +402,7 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
 
 /* Attention of M token rows per sequence over one layer of the cache, whose last rows[b] tokens are these rows:
  *     O[b][i][h] = sum_t w_t v^[t][h / g] / sum_t w_t,   w_t = exp(scale * Q[b][i][h] . k^[t][h / g]),   g = q_heads / kv_heads,
- * over the tokens row i sees: with tree == NULL those up to its own (t <= lens[b] - rows[b] + i); with tree, uint64 [B][M]
+ * over the tokens row i sees (M * g <= 65536): with tree == NULL those up to its own (t <= lens[b] - rows[b] + i); with tree, uint64 [B][M]
  * (M <= 64), all tokens before the rows and those rows j whose bit j is set in tree[b][i].
  *   Q_bf16  [B][M][q_heads][head_dim] BF16, token rows q_stride elements apart (as in mxq_kv_append)
  *   O_bf16  [B][M][q_heads][head_dim] BF16;  lse  float [B][M][q_heads], ln of the sum of w_t, or NULL

@@ -28,6 +28,8 @@
 // the result does not depend on scheduling.
 #include <math.h>
 
+#include <type_traits>
+
 #include "mxq_kv.cuh"
 #include "mxq_tcgen05.cuh"
 
@@ -40,14 +42,18 @@ struct KvQuery {
     uint16_t *o;             // [B][M][heads][D]
     float *lse;              // [B][M][heads] or nullptr
     int32_t heads, group;    // query heads, query heads per kv head
+    uint32_t group_magic;    // floor(2^32 / group) + 1 (0: group = 1): r / group = umulhi(r, group_magic) for r * group < 2^32
+    int32_t max_tiles;       // row tiles of a sequence with all its rows
     float scale_log2;        // scale * log2(e)
-    float *partials;         // workspace: two slots per CTA
-    unsigned *tickets;       // one per CTA
+    unsigned *counter;       // workspace: next item, one ticket per segment (both zero between calls), slots of partial results
+    unsigned *tickets;
+    float *partials;
+    uint32_t slots;
 };
 
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;                  // units in a warp's ring
-constexpr int kAttMaxCtas = 1024;              // tickets in the workspace's first 4096 bytes
+constexpr int kAttItemsPerCta = 6;             // items the work is cut into, per CTA
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
 constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
@@ -205,14 +211,29 @@ struct WarpState {
     int ref, ref_max;
 };
 
-__device__ __forceinline__ bool row_sees(const KvSeqs &s, const KvQuery &a, const Segment &g, int r, int t) {
-    if (r >= g.rows_total || t >= g.len) return false;
-    const int i = r / a.group, d = t - g.base;
-    if (a.tree == nullptr) return d <= i;
-    if (d < 0) return true;
+// token row of a flattened row
+__device__ __forceinline__ int token_row(const KvQuery &a, int r) { return a.group_magic ? (int)__umulhi((uint32_t)r, a.group_magic) : r; }
+
+// what a flattened row sees: tokens before `until`, and token base + j (of at most 64 rows) if bit j is set
+struct Sight {
+    int until, base;
+    uint64_t bits;
+    __device__ __forceinline__ bool sees(int t) const { return t < until || (t >= base && t < base + 64 && ((bits >> (t - base)) & 1) != 0); }
+};
+__device__ __noinline__ Sight sight_of(const KvSeqs &s, const KvQuery &a, const Segment &g, int r) {
+    Sight v = {0, g.len, 0};                    // (no such row: nothing)
+    if (r >= g.rows_total) return v;
+    const int i = token_row(a, r);
+    if (a.tree == nullptr) {
+        v.until = min(g.base + i + 1, g.len);
+        return v;
+    }
     const uint64_t *p = MXQ_AT(a.tree + (int64_t)g.b * s.m + i, 8, a.tree, (size_t)s.B * s.m * 8);
-    uint32_t lo = ld_dep_u32(p), hi = ld_dep_u32(reinterpret_cast<const uint32_t *>(p) + 1);
-    return d < 64 && ((((uint64_t)hi << 32 | lo) >> d) & 1) != 0;
+    const uint32_t lo = ld_dep_u32(p), hi = ld_dep_u32(reinterpret_cast<const uint32_t *>(p) + 1);
+    const int rows = g.len - g.base;
+    v.until = v.base = g.base;
+    v.bits = ((uint64_t)hi << 32 | lo) & (rows >= 64 ? ~0ull : (1ull << rows) - 1);
+    return v;
 }
 
 template <int D, int NT>
@@ -232,39 +253,34 @@ __device__ __forceinline__ void rescale(WarpState<D, NT> &w, const float (&f)[NT
 }
 
 // O += P . V for a whole tile, in FP16.  p[u][n][h]: packed weights of row g of column block n, tokens 16 u + tig + 8 h (low half) and
-// + 4 (high half).  kTiers == 2: deep[..] are the weights too small for p, scaled up by `up`.
-template <int D, int NT, int kTiers>
+// + 4 (high half).  With `two`, deep[..] are the weights too small for p, scaled up by `up`; `down` = 1 / up.  (One body for both: the
+// kernel's loop has to stay in the instruction cache.)
+template <int D, int NT>
 __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, int g, int tig, const uint32_t (&p)[2][NT][2],
-                                           const uint32_t (&deep)[2][NT][2], float up, float down) {
+                                           const uint32_t (&deep)[2][NT][2], bool two, float up, float down) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb, kW = kNb / 2;   // words of V codes per lane and token
     uint32_t sw[2][kNb];                        // scales: [group][h, block pair] words of (A.j, B.j, A.j+1, B.j+1)
-    uint32_t ev[2][2][kW], od[2][2][kW];        // bytes (element of token A, element of token B): even elements, odd elements
+    uint32_t v[2][4][kW];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         lds_words<kNb>(tile + T::kVs + 16 * kNb * u + 4 * kNb * tig, sw[u]);
-        const uint32_t row = tile + T::kV + (16 * u + tig) * T::kRow + 2 * kNb * g;
-        uint32_t v[4][kW];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) lds_words<kW>(row + 4 * k * T::kRow, v[k]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int x = 0; x < kW; ++x) {
-                const uint32_t A = v[2 * h][x], B = v[2 * h + 1][x];
-                ev[u][h][x] = (A & 0x0F0F0F0Fu) | ((B * 16u) & 0xF0F0F0F0u);
-                od[u][h][x] = ((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u);
-            }
+        for (int k = 0; k < 4; ++k) lds_words<kW>(tile + T::kV + (16 * u + tig + 4 * k) * T::kRow + 2 * kNb * g, v[u][k]);
     }
     // exponent field of 2^(scale - ref + kScaleBias): never below 1 here, so both halves fit one 32-bit multiply-add
     const uint32_t bias = (uint32_t)(15 + kScaleBias - w.ref) * (0x10001u << 10);
 #pragma unroll
     for (int x = 0; x < kW; ++x) {
-        uint32_t e[2][2][4], o[2][2][4];
+        uint32_t e[2][2][4], o[2][2][4];        // pairs (token A, token B) of even and odd elements
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) decode4(ev[u][h][x], e[u][h]), decode4(od[u][h][x], o[u][h]);
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t A = v[u][2 * h][x], B = v[u][2 * h + 1][x];
+                decode4((A & 0x0F0F0F0Fu) | ((B * 16u) & 0xF0F0F0F0u), e[u][h]);
+                decode4(((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u), o[u][h]);
+            }
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             const int j = 2 * x + y;
@@ -274,26 +290,24 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
 #pragma unroll
                 for (int h = 0; h < 2; ++h)     // (the two tokens' scales as 16-bit numbers)
                     sc[u][h] = __byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140) * 1024u + bias;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float(&o0)[4] = w.o[2 * j][n], (&o1)[4] = w.o[2 * j + 1][n];
-                if constexpr (kTiers == 2) {
-                    scale4(o0, up, up), scale4(o1, up, up);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t b0 = mul_half2(deep[u][n][0], sc[u][0]), b1 = mul_half2(deep[u][n][1], sc[u][1]);
-                        mma16816<false>(o0, e[u][0][2 * y], o[u][0][2 * y], e[u][1][2 * y], o[u][1][2 * y], b0, b1);
-                        mma16816<false>(o1, e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
-                    }
-                    scale4(o0, down, down), scale4(o1, down, down);
-                }
+            auto product = [&](int n, const uint32_t(&q)[2][NT][2]) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const uint32_t b0 = mul_half2(p[u][n][0], sc[u][0]), b1 = mul_half2(p[u][n][1], sc[u][1]);
-                    mma16816<false>(o0, e[u][0][2 * y], o[u][0][2 * y], e[u][1][2 * y], o[u][1][2 * y], b0, b1);
-                    mma16816<false>(o1, e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
+                    const uint32_t b0 = mul_half2(q[u][n][0], sc[u][0]), b1 = mul_half2(q[u][n][1], sc[u][1]);
+                    mma16816<false>(w.o[2 * j][n], e[u][0][2 * y], o[u][0][2 * y], e[u][1][2 * y], o[u][1][2 * y], b0, b1);
+                    mma16816<false>(w.o[2 * j + 1][n], e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
+                }
+            };
+            if (two) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    scale4(w.o[2 * j][n], up, up), scale4(w.o[2 * j + 1][n], up, up);
+                    product(n, deep);
+                    scale4(w.o[2 * j][n], down, down), scale4(w.o[2 * j + 1][n], down, down);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) product(n, p);
         }
     }
 }
@@ -350,7 +364,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     using T = KvTile<D>;
     constexpr int kNb = T::kNb;
     extern __shared__ __align__(128) uint8_t att_smem_raw[];
-    __shared__ int64_t sh_scan[kAttWarps + 3];
+    __shared__ uint64_t sh_scan[kAttWarps];
+    __shared__ int sh_item[7];
+    __shared__ uint32_t sh_next;
     __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
     __shared__ int sh_last;
     __shared__ __align__(8) uint64_t sh_bars[kAttWarps][kAttStages];
@@ -372,74 +388,101 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     pdl_wait();
     asm volatile("fence.proxy.async;" ::: "memory");      // tiles may have been written by the kernel before, with ordinary stores
 
-    // ---- this CTA's share of all steps ----
-    auto shape_of = [&](int b, int &len, int &rows, int64_t &n, int64_t &tiles) {
-        len = s.len(b), rows = s.nrows(b);
-        n = max(1, (len + kAttWarps * kUnitTokens - 1) / (kAttWarps * kUnitTokens));
-        tiles = max(1, (rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
+    // ---- the items: every segment (sequence, kv head, row tile) is cut into parts of at most `item_units` units ----
+    auto shape_of = [&](int len, int rows, uint32_t &n, uint32_t &tiles) {      // units of a segment, segments per kv head
+        n = max(1u, ((uint32_t)len + kUnitTokens - 1) / kUnitTokens);
+        tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
-    int64_t first, left;      // global index of the CTA's next step; steps left
-    int64_t b_start;          // global index of the first step of sequence b
-    int b;
-    int64_t total, grid;
+    const int each = (s.B + kAttThreads - 1) / kAttThreads, b_first = tid * each, b_last = min(s.B, b_first + each);
+    int len0 = 0, rows0 = 0;                       // the first of this thread's sequences
+    uint32_t item_units, item_lo, item_hi, part_lo, items;
     {
-        const int per = (s.B + kAttThreads - 1) / kAttThreads;
-        int64_t mine = 0;
-        for (int i = tid * per; i < min(s.B, (tid + 1) * per); ++i) {
-            int len, rows;
-            int64_t n, tiles;
-            shape_of(i, len, rows, n, tiles);
-            mine += n * tiles * c.heads;
+        uint64_t units = 0;
+        for (int i = b_first; i < b_last; ++i) {
+            const int len = s.len(i), rows = s.nrows(i);
+            if (i == b_first) len0 = len, rows0 = rows;
+            uint32_t n, tiles;
+            shape_of(len, rows, n, tiles);
+            units += (uint64_t)n * (tiles * (uint32_t)c.heads);
         }
-        int64_t upto = mine;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
+        if (lane == 0) sh_scan[warp] = units;
+        __syncthreads();
+        units = 0;
+        for (int w = 0; w < kAttWarps; ++w) units += sh_scan[w];
+        const uint64_t want = units / (kAttItemsPerCta * gridDim.x) + 1;
+        item_units = (uint32_t)((want + kAttWarps - 1) / kAttWarps) * kAttWarps;
+        uint64_t mine = 0;                         // items, and above them the items of segments that are cut
+        for (int i = b_first; i < b_last; ++i) {
+            uint32_t n, tiles;
+            shape_of(i == b_first ? len0 : s.len(i), i == b_first ? rows0 : s.nrows(i), n, tiles);
+            const uint32_t parts = (n + item_units - 1) / item_units, k = parts * tiles * (uint32_t)c.heads;
+            mine += k | (uint64_t)(parts > 1 ? k : 0) << 32;
+        }
+        uint64_t upto = mine, total = 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, upto, o);
+            const uint64_t up = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += up;
         }
+        __syncthreads();
         if (lane == 31) sh_scan[warp] = upto;
         __syncthreads();
-        total = 0;
         for (int w = 0; w < kAttWarps; ++w) {
             if (w < warp) upto += sh_scan[w];
             total += sh_scan[w];
         }
-        grid = min((int64_t)gridDim.x, total);      // no CTA without a step among those that share a segment
-        if (blockIdx.x >= grid) return;
-        first = total * blockIdx.x / grid;
-        left = total * (blockIdx.x + 1) / grid - first;
-        if (upto - mine <= first && first < upto) {
-            int64_t at = upto - mine;
-            int i = tid * per;
-            for (;; ++i) {
-                int len, rows;
-                int64_t n, tiles;
-                shape_of(i, len, rows, n, tiles);
-                if (at + n * tiles * c.heads > first) break;
-                at += n * tiles * c.heads;
-            }
-            sh_scan[kAttWarps] = i;
-            sh_scan[kAttWarps + 1] = at;
-        }
-        __syncthreads();
-        b = (int)sh_scan[kAttWarps];
-        b_start = sh_scan[kAttWarps + 1];
+        item_hi = (uint32_t)upto, item_lo = (uint32_t)(upto - mine), part_lo = (uint32_t)((upto - mine) >> 32), items = (uint32_t)total;
     }
 
-    while (left > 0) {
-        int len, rows;
-        int64_t n, tiles;
-        shape_of(b, len, rows, n, tiles);
-        const int64_t seg = (first - b_start) / n, seg_start = b_start + seg * n;
-        const int step0 = (int)(first - seg_start), steps = (int)min(left, n - step0);
+    // Items are taken in turn as CTAs become free; which CTA computes an item does not matter to its result.
+    for (uint32_t item = blockIdx.x; item < items;) {
+        uint32_t next = items;
+        if (tid == 0 && items > gridDim.x) {
+            const uint32_t taken = atomicAdd(MXQ_AT(a.counter, 4, a.counter, 4), 1u);
+            next = gridDim.x + taken;
+            if (taken == items - 1) *a.counter = 0;       // one draw per item: this was the last
+        }
+        if (item_lo <= item && item < item_hi) {
+            uint32_t at = item_lo, part = part_lo, n, tiles, parts;
+            int i = b_first, len = len0, rows = rows0;
+            for (;;) {
+                shape_of(len, rows, n, tiles);
+                parts = (n + item_units - 1) / item_units;
+                const uint32_t k = parts * tiles * (uint32_t)c.heads;
+                if (at + k > item) break;
+                at += k, part += parts > 1 ? k : 0, ++i;
+                len = s.len(i), rows = s.nrows(i);
+            }
+            sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)(item - at), sh_item[4] = (int)part, sh_item[5] = (int)parts, sh_item[6] = (int)tiles;
+        }
+        __syncthreads();
+        const int b = sh_item[0], len = sh_item[1], rows = sh_item[2];
+        const uint32_t parts = (uint32_t)sh_item[5], tiles = (uint32_t)sh_item[6], seg = (uint32_t)sh_item[3] / parts, part = (uint32_t)sh_item[3] - seg * parts;
+        const uint32_t slot0 = (uint32_t)sh_item[4] + seg * parts;      // slot of the segment's first part, if it is cut
+        const uint32_t head = tiles == 1 ? seg : seg / tiles, row_tile = tiles == 1 ? 0u : seg - head * tiles;
         Segment sg;
-        sg.b = b, sg.head = (int)(seg / tiles), sg.r0 = (int)(seg % tiles) * kAttRows<NT>;
+        sg.b = b, sg.head = (int)head, sg.r0 = (int)row_tile * kAttRows<NT>;
         sg.len = len, sg.base = len - rows, sg.rows_total = rows * a.group;
         const int nrows = min(max(sg.rows_total - sg.r0, 0), kAttRows<NT>);
 
-        // ---- the warp's units: number k is unit (step0 + k) * kAttWarps + warp of the sequence ----
-        const int last_unit = (len + kUnitTokens - 1) / kUnitTokens, first_unit = step0 * kAttWarps + warp;
-        const int count = nrows > 0 && first_unit < last_unit ? min(steps, (last_unit - first_unit + kAttWarps - 1) / kAttWarps) : 0;
+        // ---- the rows' queries: on their way while the first tiles are looked up ----
+        uint4 qx[NT][kNb];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = sg.r0 + 8 * nt + g, i = token_row(a, r);
+            const uint16_t *src = a.q + ((int64_t)b * s.m + i) * a.q_stride + (int64_t)(sg.head * a.group + r - i * a.group) * D + 8 * tig;
+#pragma unroll
+            for (int j = 0; j < kNb; ++j) {
+                qx[nt][j] = make_uint4(0, 0, 0, 0);
+                if (r < sg.rows_total) qx[nt][j] = ld_dep_u4(MXQ_AT(src + 32 * j, 16, a.q, (((int64_t)s.B * s.m - 1) * a.q_stride + (int64_t)a.heads * D) * 2));
+            }
+        }
+
+        // ---- the warp's units: number k is the segment's unit first_unit + k * kAttWarps ----
+        const int last_unit = (int)min(((uint32_t)len + kUnitTokens - 1) / kUnitTokens, (part + 1) * item_units), first_unit = (int)(part * item_units) + warp;
+        const int count = nrows > 0 && first_unit < last_unit ? (last_unit - first_unit + kAttWarps - 1) / kAttWarps : 0;
         const uint8_t *source = nullptr;   // lane i: where tile i of the next 32 tiles of the warp's lies (nullptr: nowhere)
         uint32_t exist = 0, there = 0;     // bit i: that tile exists; the units requested so far, kU bits each, the newest lowest
         auto issue = [&](int k) {
@@ -469,21 +512,12 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         // ---- query fragments: elements 32 j + 8 tig .. + 7 of row g, normalised by a power of two ----
         uint4 qf[NT > kAttRegisterQ ? 1 : NT][kNb];
         float factor[NT][2];               // score -> log2 domain, for the lane's two columns
-        int limit[NT][2];                  // first token (causally) hidden from the column's row; 0: no such row
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = sg.r0 + 8 * nt + g;
-            uint4 x[kNb];
+            const uint4(&x)[kNb] = qx[nt];
             uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < kNb; ++j) {
-                x[j] = make_uint4(0, 0, 0, 0);
-                if (r < sg.rows_total) {
-                    const uint16_t *src = a.q + ((int64_t)b * s.m + r / a.group) * a.q_stride + (int64_t)(sg.head * a.group + r % a.group) * D + 32 * j + 8 * tig;
-                    x[j] = ld_dep_u4(MXQ_AT(src, 16, a.q, (((int64_t)s.B * s.m - 1) * a.q_stride + (int64_t)a.heads * D) * 2));
-                }
-                top = __vmaxu2(top, chunk_max2(x[j]));
-            }
+            for (int j = 0; j < kNb; ++j) top = __vmaxu2(top, chunk_max2(x[j]));
             top = max(top & 0xFFFFu, top >> 16);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -506,9 +540,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             }
 #pragma unroll
             for (int e2 = 0; e2 < 2; ++e2) {
-                const int rc = sg.r0 + 8 * nt + 2 * tig + e2;
                 factor[nt][e2] = a.scale_log2 * __shfl_sync(0xffffffffu, back, (2 * tig + e2) * 4);
-                limit[nt][e2] = rc < sg.rows_total ? min(sg.base + rc / a.group + 1, len) : 0;
             }
         }
         if constexpr (NT > kAttRegisterQ) __syncthreads();
@@ -537,41 +569,53 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             if (here != 0) {
                 constexpr int kG = 2 * kU;                   // groups of 16 tokens
                 const int tok = (g >> 1) + 4 * (g & 1);      // row g of the product is this token of the group, row g + 8 the one 8 further
-                // ---- scores ----
+                // ---- scores (one body for the unit's tiles) ----
                 float x[kG][NT][4];
+#pragma unroll 1
+                for (int i = 0; i < kU; ++i) {
+                    const uint32_t tile = unit + i * T::kBytes;
+                    float y[2][NT][4];
 #pragma unroll
-                for (int u = 0; u < kG; ++u) {
-                    const uint32_t tile = unit + (u / 2) * T::kBytes, row = tile + (16 * (u & 1) + tok) * T::kRow + 4 * kNb * tig;
-                    uint32_t k0[kNb], k1[kNb];
-                    lds_words<kNb>(row, k0);
-                    lds_words<kNb>(row + 8 * T::kRow, k1);
-                    uint32_t s0, s1;
-                    const uint32_t sa = tile + T::kKs + (16 * (u & 1) + tok) * kNb;
-                    if constexpr (kNb == 4) {
-                        s0 = lds_u32(sa), s1 = lds_u32(sa + 8 * kNb);
-                    } else {
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s0) : "r"(sa));
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s1) : "r"(sa + 8 * kNb));
-                    }
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t k0[kNb], k1[kNb], s0, s1;
+                        lds_words<kNb>(tile + (16 * u + tok) * T::kRow + 4 * kNb * tig, k0);
+                        lds_words<kNb>(tile + (16 * u + tok + 8) * T::kRow + 4 * kNb * tig, k1);
+                        const uint32_t sa = tile + T::kKs + (16 * u + tok) * kNb;
+                        if constexpr (kNb == 4) {
+                            s0 = lds_u32(sa), s1 = lds_u32(sa + 8 * kNb);
+                        } else {
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s0) : "r"(sa));
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(s1) : "r"(sa + 8 * kNb));
+                        }
 #pragma unroll
-                    for (int j = 0; j < kNb; ++j) {
-                        uint32_t h0[4], h1[4];
-                        decode4(k0[j], h0);
-                        decode4(k1[j], h1);
-                        const float c0 = scale_factor(s0, j), c1 = scale_factor(s1, j);
+                        for (int j = 0; j < kNb; ++j) {
+                            uint32_t h0[4], h1[4];
+                            decode4(k0[j], h0);
+                            decode4(k1[j], h1);
+                            const float c0 = scale_factor(s0, j), c1 = scale_factor(s1, j);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            uint4 q;
-                            if constexpr (NT > kAttRegisterQ) q = sh_q[(j * NT + nt) * 32 + lane];
-                            else q = qf[nt][j];
-                            float d[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
-                            mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
-                            float(&v)[4] = x[u][nt];
-                            if (j == 0) v[0] = d[0] * c0, v[1] = d[1] * c0, v[2] = d[2] * c1, v[3] = d[3] * c1;
-                            else v[0] += d[0] * c0, v[1] += d[1] * c0, v[2] += d[2] * c1, v[3] += d[3] * c1;
+                            for (int nt = 0; nt < NT; ++nt) {
+                                uint4 q;
+                                if constexpr (NT > kAttRegisterQ) q = sh_q[(j * NT + nt) * 32 + lane];
+                                else q = qf[nt][j];
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
+                                mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
+                                float(&v)[4] = y[u][nt];
+                                if (j == 0) v[0] = d[0] * c0, v[1] = d[1] * c0, v[2] = d[2] * c1, v[3] = d[3] * c1;
+                                else v[0] += d[0] * c0, v[1] += d[1] * c0, v[2] += d[2] * c1, v[3] += d[3] * c1;
+                            }
                         }
                     }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if (kU == 1 || i == 0) x[u][nt][e] = y[u][nt][e];
+                                if (kU == 2) x[kG - 2 + u][nt][e] = y[u][nt][e];
+                            }
                 }
                 // ---- relative to the running maximum; what a row does not see; a new maximum ----
 #pragma unroll
@@ -587,15 +631,16 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 }
                 if (t0 + kUnitTokens > sg.base || here != (1u << kU) - 1) {
 #pragma unroll
-                    for (int u = 0; u < kG; ++u)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                        for (int e = 0; e < 2; ++e) {
+                            const Sight sight = sight_of(s, a, sg, sg.r0 + 8 * nt + 2 * tig + e);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int t = t0 + 16 * u + tok + 8 * (e >> 1);
-                                const bool seen = a.tree == nullptr ? t < limit[nt][e & 1] : row_sees(s, a, sg, sg.r0 + 8 * nt + 2 * tig + (e & 1), t);
-                                if (!seen || ((here >> (u / 2)) & 1u) == 0) x[u][nt][e] = -INFINITY;
-                            }
+                            for (int u = 0; u < kG; ++u)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h)
+                                    if (!sight.sees(t0 + 16 * u + tok + 8 * h) || ((here >> (u / 2)) & 1u) == 0) x[u][nt][2 * h + e] = -INFINITY;
+                        }
                 }
                 bool over = false;
                 float top[NT][2];
@@ -701,19 +746,10 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 // ---- O += P V: which form holds these weights? ----
                 const int range = kHalfRange - max(w.ref - lo, 0);      // binades of weight the scales leave to FP16
                 const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
-                if (__all_sync(0xffffffffu, all_le_half2(pack_half2(small, small), least)) && range >= kHalfRange - kScaleSpread && !nan) {   // (NaN compares false)
-#pragma unroll
-                    for (int i = 0; i < kU; ++i) {
-                        uint32_t p[2][NT][2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(pk[2 * i + u][nt][h]);
-                        add_values<D, NT, 1>(w, unit + i * T::kBytes, g, tig, p, p, 1.f, 1.f);
-                    }
-                } else {
+                const bool plain = __all_sync(0xffffffffu, all_le_half2(pack_half2(small, small), least)) && range >= kHalfRange - kScaleSpread && !nan;   // (NaN compares false)
+                bool four = false, wide = false;
+                const float tiny = small * small, up = __uint_as_float((uint32_t)(127 + max(range, 0)) << 23);
+                if (!plain) {
                     float low = 1.f;             // the smallest weight that is not zero
 #pragma unroll
                     for (int u = 0; u < kG; ++u)
@@ -721,42 +757,35 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) low = fminf(low, x[u][nt][e] == 0.f ? 1.f : x[u][nt][e]);
-                    const float tiny = small * small;
-                    if (nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, low < tiny * tiny)) {
-                        auto sees = [&](int nt, int t) { return row_sees(s, a, sg, sg.r0 + 8 * nt + g, t); };
+                    four = __any_sync(0xffffffffu, low < tiny);
+                    wide = nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, low < tiny * tiny);
+                }
+                if (!wide) {
+                    // plain: the weights as they are.  Else tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in
+                    // small^(i+1) .. small^i
 #pragma unroll 1
-                        for (int part = 0; part < 2; ++part)       // the weights' upper and lower eight bits
+                    for (int pass = four ? 0 : 1; pass < 2; ++pass) {
+                        const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part_ = pass == 0 ? tiny * small : small;
+                        const float from = pass == 1 && four ? tiny : 0.f;
+                        if (four) {
+                            float ff[NT][2];
 #pragma unroll
-                            for (int u = 0; u < kG; ++u) {
-                                uint32_t p[NT][2];
+                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
+                            rescale(w, ff);
+                        }
+#pragma unroll 1
+                        for (int i = 0; i < kU; ++i) {
+                            uint32_t p[2][NT][2], deep[2][NT][2];
+#pragma unroll
+                            for (int u = 0; u < 2; ++u)
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                                     for (int h = 0; h < 2; ++h) {
-                                        float &x0 = x[u][nt][2 * h], &x1 = x[u][nt][2 * h + 1];
-                                        const uint32_t b = pack_bf162(x0, x1);
-                                        x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xFFFF0000u);
-                                        p[nt][h] = transpose8x8(b);
+                                        p[u][nt][h] = kU == 1 || i == 0 ? pk[u][nt][h] : pk[kG - 2 + u][nt][h];
+                                        deep[u][nt][h] = 0;
                                     }
-                                add_values_wide<D, NT>(w, unit + (u / 2) * T::kBytes, u & 1, t0 + 16 * u, g, tig, p, sees);
-                            }
-                    } else {
-                        // tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in small^(i+1) .. small^i
-                        const float up = __uint_as_float((uint32_t)(127 + range) << 23);
-                        const bool four = __any_sync(0xffffffffu, low < tiny);
-#pragma unroll 1
-                        for (int pass = four ? 0 : 1; pass < 2; ++pass) {
-                            const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part = pass == 0 ? tiny * small : small;
-                            const float from = pass == 1 && four ? tiny : 0.f;
-                            if (four) {
-                                float ff[NT][2];
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
-                                rescale(w, ff);
-                            }
-#pragma unroll
-                            for (int i = 0; i < kU; ++i) {
-                                uint32_t p[2][NT][2], deep[2][NT][2];
+                            if (!plain) {
 #pragma unroll
                                 for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -766,17 +795,45 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                                             float lo_[2], hi_[2];
 #pragma unroll
                                             for (int e = 0; e < 2; ++e) {
-                                                const float v = x[2 * i + u][nt][2 * h + e], in_ = v < from || v >= bound ? 0.f : v * gain;
-                                                lo_[e] = v < part ? in_ * up : 0.f;
-                                                hi_[e] = v < part ? 0.f : in_;
+                                                const float v = kU == 1 || i == 0 ? x[u][nt][2 * h + e] : x[kG - 2 + u][nt][2 * h + e];
+                                                const float in_ = v < from || v >= bound ? 0.f : v * gain;
+                                                lo_[e] = v < part_ ? in_ * up : 0.f;
+                                                hi_[e] = v < part_ ? 0.f : in_;
                                             }
-                                            p[u][nt][h] = transpose8x8(pack_half2(hi_[0], hi_[1]));
+                                            p[u][nt][h] = pack_half2(hi_[0], hi_[1]);
                                             deep[u][nt][h] = transpose8x8(pack_half2(lo_[0], lo_[1]));
                                         }
-                                add_values<D, NT, 2>(w, unit + i * T::kBytes, g, tig, p, deep, up, small);
                             }
+#pragma unroll
+                            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(p[u][nt][h]);
+                            add_values<D, NT>(w, unit + i * T::kBytes, g, tig, p, deep, !plain, up, small);
                         }
                     }
+                } else {
+#pragma unroll 1
+                    for (int part_ = 0; part_ < 2; ++part_)       // the weights' upper and lower eight bits
+#pragma unroll 1
+                        for (int i = 0; i < kU; ++i)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                uint32_t p[NT][2];
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h) {
+                                        float x0 = x[u][nt][2 * h], x1 = x[u][nt][2 * h + 1];
+                                        if (kU == 2 && i == 1) x0 = x[kG - 2 + u][nt][2 * h], x1 = x[kG - 2 + u][nt][2 * h + 1];
+                                        uint32_t b = pack_bf162(x0, x1);
+                                        if (part_ == 1) b = pack_bf162(x0 - __uint_as_float(b << 16), x1 - __uint_as_float(b & 0xFFFF0000u));
+                                        p[nt][h] = transpose8x8(b);
+                                    }
+                                add_values_wide<D, NT>(w, unit + i * T::kBytes, u, t0 + 32 * i + 16 * u, g, tig, p,
+                                                       [&](int nt, int t) { return sight_of(s, a, sg, sg.r0 + 8 * nt + g).sees(t); });
+                            }
                 }
             }
             __syncwarp();
@@ -794,34 +851,19 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
                 if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.over[nt][e] == -INFINITY ? -INFINITY : w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
             }
-        const bool whole = steps == n;
-        const int64_t seg_end = seg_start + n;
-        float *slot = a.partials + (2 * (int64_t)blockIdx.x + (step0 == 0)) * kAttSlotFloats<D, NT>;   // 1: starts here, 0: began earlier
-        [[maybe_unused]] const size_t ws_bytes = 2 * (size_t)gridDim.x * kAttSlotFloats<D, NT> * 4;
+        const bool whole = parts == 1;
+        float *const slot = a.partials + (size_t)(slot0 + part) * kAttSlotFloats<D, NT>;
+        [[maybe_unused]] const size_t ws_bytes = (size_t)a.slots * kAttSlotFloats<D, NT> * 4;
 
-        auto store_row = [&](int r, int d, const float4 &v, float m, float l) {   // final result: flattened row r of the sequence, 4 elements, by one warp
-            const int64_t at = ((int64_t)b * s.m + r / a.group) * a.heads + sg.head * a.group + r % a.group;
+        auto store_row = [&](int r, const float4 &v, float m, float l) {   // final result: flattened row r of the sequence, by one warp
+            const int i = token_row(a, r);
+            const int64_t at = ((int64_t)b * s.m + i) * a.heads + sg.head * a.group + r - i * a.group;
             [[maybe_unused]] const size_t o_bytes = (size_t)s.B * s.m * a.heads * D * 2;
-            if (d < D) *reinterpret_cast<uint2 *>(MXQ_AT(a.o + at * D + d, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
-            if (d == 0 && a.lse != nullptr) *MXQ_AT(a.lse + at, 4, a.lse, o_bytes / D * 2) = (m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f);
+            if (4 * lane < D) *reinterpret_cast<uint2 *>(MXQ_AT(a.o + at * D + 4 * lane, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
+            if (lane == 0 && a.lse != nullptr) *MXQ_AT(a.lse + at, 4, a.lse, o_bytes / D * 2) = (m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f);
         };
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            if (8 * nt >= nrows && nt > 0) break;
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float inv = w.l[nt][e] == 0.f ? 0.f : 1.f / w.l[nt][e];
-                float *dst = merge + (warp * 8 + 2 * tig + e) * kMergeRow + 4 * g;
-#pragma unroll
-                for (int j = 0; j < kNb; ++j) {
-                    float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127 - kScaleBias);
-                    *reinterpret_cast<float4 *>(dst + 32 * j) = make_float4(v[0], v[1], v[2], v[3]);
-                }
-            }
-            __syncthreads();
+        // the four warps' parts of rows 8 * nt .. of the tile, in `merge` and sh_ml: one warp per row adds them
+        auto fold = [&](int nt, auto sink) {
             for (int r = warp; r < min(nrows - 8 * nt, 8); r += kAttWarps) {
                 float m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -837,65 +879,114 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     }
                 }
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-                if (whole) {
-                    store_row(sg.r0 + 8 * nt + r, 4 * lane, v, m, l);
-                } else {
-                    if (4 * lane < D) *reinterpret_cast<float4 *>(MXQ_AT(slot + (8 * nt + r) * D + 4 * lane, 16, a.partials, ws_bytes)) = v;
-                    if (lane == 0) *reinterpret_cast<float2 *>(MXQ_AT(slot + kAttRows<NT> * D + 2 * (8 * nt + r), 8, a.partials, ws_bytes)) = make_float2(m, l);
+                sink(8 * nt + r, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv), m, l);
+            }
+        };
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (8 * nt >= nrows) break;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (8 * nt + 2 * tig + e >= nrows) break;
+                const float inv = w.l[nt][e] == 0.f ? 0.f : 1.f / w.l[nt][e];
+                float *dst = merge + (warp * 8 + 2 * tig + e) * kMergeRow + 4 * g;
+#pragma unroll
+                for (int j = 0; j < kNb; ++j) {
+                    float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127 - kScaleBias);
+                    *reinterpret_cast<float4 *>(dst + 32 * j) = make_float4(v[0], v[1], v[2], v[3]);
                 }
             }
+            __syncthreads();
+            fold(nt, [&](int r, const float4 &v, float m, float l) {
+                if (whole) {
+                    store_row(sg.r0 + r, v, m, l);
+                } else {
+                    if (4 * lane < D) *reinterpret_cast<float4 *>(MXQ_AT(slot + r * D + 4 * lane, 16, a.partials, ws_bytes)) = v;
+                    if (lane == 0) *reinterpret_cast<float2 *>(MXQ_AT(slot + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)) = make_float2(m, l);
+                }
+            });
         }
 
-        // ---- join the CTAs of a cut segment: the last to arrive adds the parts in order ----
+        // ---- join the parts of a cut segment: the CTA that finishes the last one adds them, in order ----
         bool finish = whole;
         if (!whole) {
-            // CTA i starts at total * i / grid: step x belongs to the last i whose start is not above it
-            const int64_t i0 = ((seg_start + 1) * grid - 1) / total, i1 = (seg_end * grid - 1) / total;
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                unsigned *ticket = MXQ_AT(a.tickets + i0, 4, a.tickets, kAttMaxCtas * 4);
-                sh_last = atomicAdd(ticket, 1u) == (unsigned)(i1 - i0);
+                unsigned *ticket = MXQ_AT(a.tickets + ((size_t)b * c.heads + head) * a.max_tiles + row_tile, 4, a.tickets, (size_t)s.B * c.heads * a.max_tiles * 4);
+                sh_last = atomicAdd(ticket, 1u) == parts - 1;
                 if (sh_last) *ticket = 0;
             }
             __syncthreads();
             if (sh_last) {
                 finish = true;
                 __threadfence();
-                for (int r = warp; r < nrows; r += kAttWarps) {
-                    auto part = [&](int64_t i) {     // (the first contributor's part starts the segment, or is a share that begins exactly there)
-                        return a.partials + (2 * i + (total * i / grid <= seg_start)) * kAttSlotFloats<D, NT>;
-                    };
-                    float m = -INFINITY, l = 0.f;
-                    for (int64_t i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(part(i) + kAttRows<NT> * D + 2 * r));
+                const float *const p0 = a.partials + (size_t)slot0 * kAttSlotFloats<D, NT>;
+                auto ml_of = [&](uint32_t i, int r) {
+                    return __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
+                };
+                // maximum and sum of every row: a lane per row, a quarter of the parts per warp
+                float m = -INFINITY, l = 0.f;
+                if (lane < nrows) {
+#pragma unroll 4
+                    for (uint32_t i = warp; i < parts; i += kAttWarps) {
+                        const float2 ml = ml_of(i, lane);
+                        const float top = fmaxf(m, ml.x);
+                        l = (l == 0.f ? 0.f : l * exp2_fast(m - top)) + (ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - top));
+                        m = top;
+                    }
+                    sh_ml[warp][lane][0] = m, sh_ml[warp][lane][1] = l;
+                }
+                __syncthreads();
+                m = -INFINITY, l = 0.f;
+                if (lane < nrows) {
 #pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][lane][0]);
+#pragma unroll
+                    for (int i = 0; i < kAttWarps; ++i) l += sh_ml[i][lane][1] == 0.f ? 0.f : sh_ml[i][lane][1] * exp2_fast(sh_ml[i][lane][0] - m);
+                }
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                // the averages: a warp per row, or with one or two rows a share of the parts per warp
+                const int across = nrows == 1 ? 1 : nrows == 2 ? 2 : kAttWarps, share = warp / across, shares = kAttWarps / across;
+                for (int r = warp % across; r < nrows; r += across) {
+                    const float rm = __shfl_sync(0xffffffffu, m, r), rl = __shfl_sync(0xffffffffu, l, r), ri = __shfl_sync(0xffffffffu, inv, r);
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-                    for (int64_t i = i0; i <= i1; ++i) {
-                        const float *p = part(i);
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
-                        const float f = ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - m);
-                        l += f;
+                    for (uint32_t i = share; i < parts; i += shares) {
+                        const float2 ml = ml_of(i, r);
+                        const float f = ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - rm) * ri;
                         if (4 * lane < D) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p + r * D + 4 * lane, 16, a.partials, ws_bytes)));
-                            v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
+                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + r * D + 4 * lane, 16, a.partials, ws_bytes)));
+                            if (ml.y != 0.f) v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
                         }
                     }
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
-                    store_row(sg.r0 + r, 4 * lane, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv), m, l);
+                    if (shares == 1) {
+                        store_row(sg.r0 + r, v, rm, rl);
+                    } else {
+                        if (4 * lane < D) *reinterpret_cast<float4 *>(merge + warp * kMergeRow + 4 * lane) = v;
+                        __syncthreads();
+                        if (share == 0) {
+                            for (int i = 1; i < shares; ++i)
+                                if (4 * lane < D) {
+                                    const float4 x = *reinterpret_cast<const float4 *>(merge + (warp + i * across) * kMergeRow + 4 * lane);
+                                    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+                                }
+                            store_row(sg.r0 + r, v, rm, rl);
+                        }
+                    }
                 }
             }
         }
         // rows the sequence does not have
         if (finish && sg.r0 == 0)
-            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) store_row(r, 4 * lane, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) store_row(r, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+        if (tid == 0) sh_next = next;
         fence_async_proxy();  // (the rings held ordinary stores; bulk copies come next)
         __syncthreads();      // the rings, sh_ml and sh_q are free again
-        first += steps;
-        left -= steps;
-        if (first == b_start + n * tiles * c.heads) b_start = first, ++b;
+        item = sh_next;
     }
 }
 
@@ -918,15 +1009,28 @@ static int att_column_blocks(int M, int group) {
     const int64_t rows = (int64_t)M * group;
     return rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
 }
-template <int D>
-static size_t att_workspace(int nt) {
-    const size_t sms = (size_t)sm_count();
-    auto bytes = [&](size_t per_sm, size_t slot) { return 4096 + 2 * (sms * per_sm < kAttMaxCtas ? sms * per_sm : (size_t)kAttMaxCtas) * slot * 4; };
-    return nt == 1 ? bytes(kAttCtasPerSm<D, 1>, kAttSlotFloats<D, 1>) : nt == 2 ? bytes(kAttCtasPerSm<D, 2>, kAttSlotFloats<D, 2>) : bytes(kAttCtasPerSm<D, 4>, kAttSlotFloats<D, 4>);
+template <int D, int NT>
+static int att_grid() { return sm_count() * kAttCtasPerSm<D, NT>; }
+
+// Workspace: 16 bytes with the counter, a ticket per segment, slots for the parts of cut segments (a cut segment of n units has at
+// most 2 n / item_units of them, and all segments together kAttItemsPerCta * grid * item_units units).
+struct AttLayout {
+    size_t tickets, partials, bytes;
+    uint32_t slots;
+};
+template <int D, int NT>
+static AttLayout att_layout(int B, int heads, int max_tiles) {
+    AttLayout l;
+    l.tickets = 16;
+    l.partials = l.tickets + ((size_t)B * heads * max_tiles * 4 + 255) / 256 * 256;
+    if (l.partials < 4096) l.partials = 4096;
+    l.slots = 2u * kAttItemsPerCta * (uint32_t)att_grid<D, NT>();
+    l.bytes = l.partials + (size_t)l.slots * kAttSlotFloats<D, NT> * 4;
+    return l;
 }
 
 template <int D, int NT>
-static int att_launch(const KvView &c, const KvSeqs &s, const KvQuery &a, cudaStream_t stream) {
+static int att_launch(const KvView &c, const KvSeqs &s, KvQuery a, void *workspace, cudaStream_t stream) {
     constexpr size_t smem = kAttSmem<D, NT>;
     static bool configured[64];
     int dev = 0;
@@ -939,9 +1043,25 @@ static int att_launch(const KvView &c, const KvSeqs &s, const KvQuery &a, cudaSt
         }
         configured[dev] = true;
     }
-    int grid = sm_count() * (kAttCtasPerSm<D, NT>);
-    if (grid > kAttMaxCtas) grid = kAttMaxCtas;
-    return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)grid), kAttThreads, smem, stream, c, s, a);
+    a.max_tiles = (s.m * a.group + kAttRows<NT> - 1) / kAttRows<NT>;
+    const AttLayout l = att_layout<D, NT>(s.B, c.heads, a.max_tiles);
+    a.counter = (unsigned *)workspace;
+    a.tickets = (unsigned *)((char *)workspace + l.tickets);
+    a.partials = (float *)((char *)workspace + l.partials);
+    a.slots = l.slots;
+    return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)att_grid<D, NT>()), kAttThreads, smem, stream, c, s, a);
+}
+
+// the template instance that covers a call: f(head dimension, column blocks) with both as constants
+template <class F>
+static auto att_pick(int head_dim, int M, int group, F f) {
+    using std::integral_constant;
+    const int nt = att_column_blocks(M, group);
+    if (head_dim == 128)
+        return nt == 1 ? f(integral_constant<int, 128>(), integral_constant<int, 1>()) : nt == 2 ? f(integral_constant<int, 128>(), integral_constant<int, 2>())
+                                                                                                : f(integral_constant<int, 128>(), integral_constant<int, 4>());
+    return nt == 1 ? f(integral_constant<int, 64>(), integral_constant<int, 1>()) : nt == 2 ? f(integral_constant<int, 64>(), integral_constant<int, 2>())
+                                                                                           : f(integral_constant<int, 64>(), integral_constant<int, 4>());
 }
 
 }  // namespace mxq
@@ -953,9 +1073,11 @@ size_t mxq_kv_attention_workspace_bytes(int B, int M, int q_heads, int kv_heads,
     if (B < 1 || B > MXQ_KV_MAX_SEQS || M < 1 || kv_heads < 1 || kv_heads > MXQ_KV_MAX_HEADS || q_heads < kv_heads || q_heads % kv_heads ||
         mxq_kv_page_bytes(kv_heads, head_dim, 32) == 0)
         return 0;
-    if ((int64_t)M * (q_heads / kv_heads) > (1 << 24)) return 0;
-    const int nt = mxq::att_column_blocks(M, q_heads / kv_heads);
-    return head_dim == 128 ? mxq::att_workspace<128>(nt) : mxq::att_workspace<64>(nt);
+    const int group = q_heads / kv_heads;
+    if ((int64_t)M * group > 65536 || (int64_t)B * M * q_heads > (1 << 30)) return 0;
+    return mxq::att_pick(head_dim, M, group, [&](auto d, auto nt) {
+        return mxq::att_layout<d(), nt()>(B, kv_heads, (M * group + mxq::kAttRows<nt()> - 1) / mxq::kAttRows<nt()>).bytes;
+    });
 }
 
 int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, int64_t q_stride, int B, int M, int q_heads,
@@ -972,15 +1094,14 @@ int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, i
         return MXQ_ERR_ALIGN;
     if (!workspace || workspace_bytes < need) return MXQ_ERR_WORKSPACE;
     const int group = q_heads / cache->kv_heads;
-    const mxq::KvQuery a = {(const uint16_t *)Q_bf16, q_stride, tree, (uint16_t *)O_bf16, lse, q_heads, group, scale * 1.44269504f,
-                            (float *)((char *)workspace + 4096), (unsigned *)workspace};
+    mxq::KvQuery a = {};
+    a.q = (const uint16_t *)Q_bf16, a.q_stride = q_stride, a.tree = tree, a.o = (uint16_t *)O_bf16, a.lse = lse;
+    a.heads = q_heads, a.group = group, a.scale_log2 = scale * 1.44269504f;
+    a.group_magic = group == 1 ? 0u : (uint32_t)((1ull << 32) / (unsigned)group + 1);
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
     const mxq::KvView c = mxq::kv_view(cache, layer);
-    cudaStream_t st = (cudaStream_t)stream;
-    const int nt = mxq::att_column_blocks(M, group);
-    if (cache->head_dim == 128)
-        return nt == 1 ? mxq::att_launch<128, 1>(c, s, a, st) : nt == 2 ? mxq::att_launch<128, 2>(c, s, a, st) : mxq::att_launch<128, 4>(c, s, a, st);
-    return nt == 1 ? mxq::att_launch<64, 1>(c, s, a, st) : nt == 2 ? mxq::att_launch<64, 2>(c, s, a, st) : mxq::att_launch<64, 4>(c, s, a, st);
+    return mxq::att_pick(cache->head_dim, M, group,
+                         [&](auto d, auto nt) { return mxq::att_launch<d(), nt()>(c, s, a, workspace, (cudaStream_t)stream); });
 }
 
 #pragma GCC visibility pop
