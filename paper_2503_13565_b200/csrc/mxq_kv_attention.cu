@@ -53,7 +53,9 @@ struct KvQuery {
 
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;                  // units in a warp's ring
-constexpr int kAttItemsPerCta = 6;             // items the work is cut into, per CTA
+// The work is cut into items of a share of one CTA's part: a sixth, so that CTAs that meet cheaper tiles take more of them, but not
+// below kAttItemUnits units (an item costs about two units of time by itself) unless a CTA would get less than two items.
+constexpr int kAttItemsPerCta = 6, kAttItemUnits = 32;
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
 constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
@@ -75,6 +77,8 @@ template <int D, int NT>
 constexpr int kAttCtasPerSm = NT == 1 ? (D == 128 ? 3 : 4) : NT == 2 ? (D == 128 ? 2 : 3) : 2;
 template <int D, int NT>
 constexpr size_t kAttSlotFloats = (size_t)kAttRows<NT> * (D + 2);
+template <int D, int NT>
+constexpr uint32_t kAttMaxParts = (uint32_t)((kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes - kAttThreads * 16) / (kAttRows<NT> * 8));   // parts of a segment
 template <int D, int NT>
 constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes + (NT > kAttRegisterQ ? (size_t)(D / 32) * NT * 32 * 16 : 0);
 
@@ -365,7 +369,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     constexpr int kNb = T::kNb;
     extern __shared__ __align__(128) uint8_t att_smem_raw[];
     __shared__ uint64_t sh_scan[kAttWarps];
-    __shared__ int sh_item[7];
+    __shared__ int sh_item[8];
     __shared__ uint32_t sh_next;
     __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
     __shared__ int sh_last;
@@ -376,7 +380,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     uint4 *const sh_q = reinterpret_cast<uint4 *>(att_smem_raw + kAttWarps * kAttStages * kUnitBytes);
     float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][8][D + 4], between segments
     constexpr int kMergeRow = D + 4;
-    static_assert(kAttWarps * 8 * kMergeRow * 4 <= kAttWarps * kAttStages * kUnitBytes, "the merge buffer lies over the rings");
+    static_assert(kAttWarps * (NT > 1 ? 16 : 8) * kMergeRow * 4 <= kAttWarps * kAttStages * kUnitBytes, "the merge buffer lies over the rings");
 
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
     uint32_t issued = 0;      // units the warp has requested before this segment: ring slots and phases run on
@@ -393,9 +397,13 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         n = max(1u, ((uint32_t)len + kUnitTokens - 1) / kUnitTokens);
         tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
+    uint32_t item_units = 0;
+    auto cut_of = [&](uint32_t n) {                // units of an item of a segment of n units: its parts must fit the join's table
+        return max(item_units, (n + kAttWarps * kAttMaxParts<D, NT> - 1) / (kAttWarps * kAttMaxParts<D, NT>) * kAttWarps);
+    };
     const int each = (s.B + kAttThreads - 1) / kAttThreads, b_first = tid * each, b_last = min(s.B, b_first + each);
     int len0 = 0, rows0 = 0;                       // the first of this thread's sequences
-    uint32_t item_units, item_lo, item_hi, part_lo, items;
+    uint32_t item_lo, item_hi, part_lo, items;
     {
         uint64_t units = 0;
         for (int i = b_first; i < b_last; ++i) {
@@ -411,13 +419,13 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         __syncthreads();
         units = 0;
         for (int w = 0; w < kAttWarps; ++w) units += sh_scan[w];
-        const uint64_t want = units / (kAttItemsPerCta * gridDim.x) + 1;
+        const uint64_t want = max(units / (kAttItemsPerCta * gridDim.x), min((uint64_t)kAttItemUnits, units / (2 * gridDim.x))) + 1;
         item_units = (uint32_t)((want + kAttWarps - 1) / kAttWarps) * kAttWarps;
         uint64_t mine = 0;                         // items, and above them the items of segments that are cut
         for (int i = b_first; i < b_last; ++i) {
             uint32_t n, tiles;
             shape_of(i == b_first ? len0 : s.len(i), i == b_first ? rows0 : s.nrows(i), n, tiles);
-            const uint32_t parts = (n + item_units - 1) / item_units, k = parts * tiles * (uint32_t)c.heads;
+            const uint32_t cut = cut_of(n), parts = (n + cut - 1) / cut, k = parts * tiles * (uint32_t)c.heads;
             mine += k | (uint64_t)(parts > 1 ? k : 0) << 32;
         }
         uint64_t upto = mine, total = 0;
@@ -445,21 +453,21 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             if (taken == items - 1) *a.counter = 0;       // one draw per item: this was the last
         }
         if (item_lo <= item && item < item_hi) {
-            uint32_t at = item_lo, part = part_lo, n, tiles, parts;
+            uint32_t at = item_lo, part = part_lo, n, tiles, cut, parts;
             int i = b_first, len = len0, rows = rows0;
             for (;;) {
                 shape_of(len, rows, n, tiles);
-                parts = (n + item_units - 1) / item_units;
+                cut = cut_of(n), parts = (n + cut - 1) / cut;
                 const uint32_t k = parts * tiles * (uint32_t)c.heads;
                 if (at + k > item) break;
                 at += k, part += parts > 1 ? k : 0, ++i;
                 len = s.len(i), rows = s.nrows(i);
             }
-            sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)(item - at), sh_item[4] = (int)part, sh_item[5] = (int)parts, sh_item[6] = (int)tiles;
+            sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)(item - at), sh_item[4] = (int)part, sh_item[5] = (int)parts, sh_item[6] = (int)tiles, sh_item[7] = (int)cut;
         }
         __syncthreads();
         const int b = sh_item[0], len = sh_item[1], rows = sh_item[2];
-        const uint32_t parts = (uint32_t)sh_item[5], tiles = (uint32_t)sh_item[6], seg = (uint32_t)sh_item[3] / parts, part = (uint32_t)sh_item[3] - seg * parts;
+        const uint32_t parts = (uint32_t)sh_item[5], tiles = (uint32_t)sh_item[6], cut = (uint32_t)sh_item[7], seg = (uint32_t)sh_item[3] / parts, part = (uint32_t)sh_item[3] - seg * parts;
         const uint32_t slot0 = (uint32_t)sh_item[4] + seg * parts;      // slot of the segment's first part, if it is cut
         const uint32_t head = tiles == 1 ? seg : seg / tiles, row_tile = tiles == 1 ? 0u : seg - head * tiles;
         Segment sg;
@@ -481,7 +489,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         }
 
         // ---- the warp's units: number k is the segment's unit first_unit + k * kAttWarps ----
-        const int last_unit = (int)min(((uint32_t)len + kUnitTokens - 1) / kUnitTokens, (part + 1) * item_units), first_unit = (int)(part * item_units) + warp;
+        const int last_unit = (int)min(((uint32_t)len + kUnitTokens - 1) / kUnitTokens, (part + 1) * cut), first_unit = (int)(part * cut) + warp;
         const int count = nrows > 0 && first_unit < last_unit ? (last_unit - first_unit + kAttWarps - 1) / kAttWarps : 0;
         const uint8_t *source = nullptr;   // lane i: where tile i of the next 32 tiles of the warp's lies (nullptr: nowhere)
         uint32_t exist = 0, there = 0;     // bit i: that tile exists; the units requested so far, kU bits each, the newest lowest
@@ -855,59 +863,63 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         float *const slot = a.partials + (size_t)(slot0 + part) * kAttSlotFloats<D, NT>;
         [[maybe_unused]] const size_t ws_bytes = (size_t)a.slots * kAttSlotFloats<D, NT> * 4;
 
-        auto store_row = [&](int r, const float4 &v, float m, float l) {   // final result: flattened row r of the sequence, by one warp
+        // final results of flattened row r of the sequence
+        auto out_row = [&](int r) {
             const int i = token_row(a, r);
-            const int64_t at = ((int64_t)b * s.m + i) * a.heads + sg.head * a.group + r - i * a.group;
-            [[maybe_unused]] const size_t o_bytes = (size_t)s.B * s.m * a.heads * D * 2;
-            if (4 * lane < D) *reinterpret_cast<uint2 *>(MXQ_AT(a.o + at * D + 4 * lane, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
-            if (lane == 0 && a.lse != nullptr) *MXQ_AT(a.lse + at, 4, a.lse, o_bytes / D * 2) = (m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f);
+            return ((int64_t)b * s.m + i) * a.heads + sg.head * a.group + r - i * a.group;
         };
-        // the four warps' parts of rows 8 * nt .. of the tile, in `merge` and sh_ml: one warp per row adds them
-        auto fold = [&](int nt, auto sink) {
-            for (int r = warp; r < min(nrows - 8 * nt, 8); r += kAttWarps) {
+        [[maybe_unused]] const size_t o_bytes = (size_t)s.B * s.m * a.heads * D * 2;
+        auto store_part = [&](int r, int d, const float4 &v) {
+            *reinterpret_cast<uint2 *>(MXQ_AT(a.o + out_row(r) * D + d, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
+        };
+        auto store_lse = [&](int r, float m, float l) {
+            if (a.lse != nullptr) *MXQ_AT(a.lse + out_row(r), 4, a.lse, o_bytes / D * 2) = m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f;
+        };
+        constexpr int kAtOnce = NT > 1 ? 2 : 1;      // column blocks whose parts fit the ring together
+#pragma unroll
+        for (int first = 0; first < NT; first += kAtOnce) {
+            if (8 * first >= nrows) break;
+            __syncthreads();
+#pragma unroll
+            for (int nt = first; nt < first + kAtOnce; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (8 * nt + 2 * tig + e >= nrows) break;
+                    const float inv = w.l[nt][e] == 0.f ? 0.f : 1.f / w.l[nt][e];
+                    float *dst = merge + (warp * 8 * kAtOnce + 8 * (nt - first) + 2 * tig + e) * kMergeRow + 4 * g;
+#pragma unroll
+                    for (int j = 0; j < kNb; ++j) {
+                        float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127 - kScaleBias);
+                        *reinterpret_cast<float4 *>(dst + 32 * j) = make_float4(v[0], v[1], v[2], v[3]);
+                    }
+                }
+            __syncthreads();
+            for (int r = 8 * first + warp; r < min(nrows, 8 * (first + kAtOnce)); r += kAttWarps) {      // a warp per row
                 float m = -INFINITY, l = 0.f;
 #pragma unroll
-                for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][8 * nt + r][0]);
+                for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][r][0]);
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < kAttWarps; ++i) {
-                    const float li = sh_ml[i][8 * nt + r][1], f = li == 0.f ? 0.f : li * exp2_fast(sh_ml[i][8 * nt + r][0] - m);
+                    const float li = sh_ml[i][r][1], f = li == 0.f ? 0.f : li * exp2_fast(sh_ml[i][r][0] - m);
                     l += f;
                     if (4 * lane < D && li != 0.f) {
-                        const float4 x = *reinterpret_cast<const float4 *>(merge + (i * 8 + r) * kMergeRow + 4 * lane);
+                        const float4 x = *reinterpret_cast<const float4 *>(merge + (i * 8 * kAtOnce + r - 8 * first) * kMergeRow + 4 * lane);
                         v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
                     }
                 }
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                sink(8 * nt + r, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv), m, l);
-            }
-        };
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            if (8 * nt >= nrows) break;
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (8 * nt + 2 * tig + e >= nrows) break;
-                const float inv = w.l[nt][e] == 0.f ? 0.f : 1.f / w.l[nt][e];
-                float *dst = merge + (warp * 8 + 2 * tig + e) * kMergeRow + 4 * g;
-#pragma unroll
-                for (int j = 0; j < kNb; ++j) {
-                    float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127 - kScaleBias);
-                    *reinterpret_cast<float4 *>(dst + 32 * j) = make_float4(v[0], v[1], v[2], v[3]);
-                }
-            }
-            __syncthreads();
-            fold(nt, [&](int r, const float4 &v, float m, float l) {
+                v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
                 if (whole) {
-                    store_row(sg.r0 + r, v, m, l);
+                    if (4 * lane < D) store_part(sg.r0 + r, 4 * lane, v);
+                    if (lane == 0) store_lse(sg.r0 + r, m, l);
                 } else {
                     if (4 * lane < D) *reinterpret_cast<float4 *>(MXQ_AT(slot + r * D + 4 * lane, 16, a.partials, ws_bytes)) = v;
                     if (lane == 0) *reinterpret_cast<float2 *>(MXQ_AT(slot + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)) = make_float2(m, l);
                 }
-            });
+            }
         }
 
         // ---- join the parts of a cut segment: the CTA that finishes the last one adds them, in order ----
@@ -925,18 +937,20 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 finish = true;
                 __threadfence();
                 const float *const p0 = a.partials + (size_t)slot0 * kAttSlotFloats<D, NT>;
-                auto ml_of = [&](uint32_t i, int r) {
-                    return __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
-                };
-                // maximum and sum of every row: a lane per row, a quarter of the parts per warp
-                float m = -INFINITY, l = 0.f;
+                float2 *const table = reinterpret_cast<float2 *>(att_smem_raw);       // [part][row]: maximum and sum, then the part's share
+                float4 *const sums = reinterpret_cast<float4 *>(att_smem_raw + ((size_t)parts * nrows * 8 + 15) / 16 * 16);
+                const int pairs = (int)parts * nrows;
+                for (int x = tid; x < pairs; x += kAttThreads) {
+                    const int i = x / nrows, r = x - i * nrows;
+                    table[x] = __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
+                }
+                __syncthreads();
+                float m = -INFINITY, l = 0.f;       // of row `lane`
                 if (lane < nrows) {
-#pragma unroll 4
-                    for (uint32_t i = warp; i < parts; i += kAttWarps) {
-                        const float2 ml = ml_of(i, lane);
-                        const float top = fmaxf(m, ml.x);
-                        l = (l == 0.f ? 0.f : l * exp2_fast(m - top)) + (ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - top));
-                        m = top;
+                    for (int i = warp; i < (int)parts; i += kAttWarps) m = fmaxf(m, table[i * nrows + lane].x);
+                    for (int i = warp; i < (int)parts; i += kAttWarps) {
+                        const float2 ml = table[i * nrows + lane];
+                        l += ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - m);
                     }
                     sh_ml[warp][lane][0] = m, sh_ml[warp][lane][1] = l;
                 }
@@ -947,42 +961,52 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][lane][0]);
 #pragma unroll
                     for (int i = 0; i < kAttWarps; ++i) l += sh_ml[i][lane][1] == 0.f ? 0.f : sh_ml[i][lane][1] * exp2_fast(sh_ml[i][lane][0] - m);
+                    if (warp == 0) store_lse(sg.r0 + lane, m, l);
                 }
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                // the averages: a warp per row, or with one or two rows a share of the parts per warp
-                const int across = nrows == 1 ? 1 : nrows == 2 ? 2 : kAttWarps, share = warp / across, shares = kAttWarps / across;
-                for (int r = warp % across; r < nrows; r += across) {
-                    const float rm = __shfl_sync(0xffffffffu, m, r), rl = __shfl_sync(0xffffffffu, l, r), ri = __shfl_sync(0xffffffffu, inv, r);
+                for (int x0 = 32 * warp; x0 < pairs; x0 += kAttThreads) {
+                    const int x = x0 + lane, r = x % nrows;
+                    const float rm = __shfl_sync(0xffffffffu, m, r), ri = __shfl_sync(0xffffffffu, inv, r);
+                    if (x < pairs) table[x].x = table[x].y == 0.f ? 0.f : table[x].y * exp2_fast(table[x].x - rm) * ri;
+                }
+                __syncthreads();
+                // four elements of a row per thread; with few rows several threads share the parts
+                constexpr int kCols = D / 4;
+                const int tasks = nrows * kCols, shares = tasks < kAttThreads ? kAttThreads / tasks : 1;
+                auto add_parts = [&](int task, int from, int stride) {
+                    const int r = task / kCols, d = 4 * (task % kCols);
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (uint32_t i = share; i < parts; i += shares) {
-                        const float2 ml = ml_of(i, r);
-                        const float f = ml.y == 0.f ? 0.f : ml.y * exp2_fast(ml.x - rm) * ri;
-                        if (4 * lane < D) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + r * D + 4 * lane, 16, a.partials, ws_bytes)));
-                            if (ml.y != 0.f) v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
-                        }
+#pragma unroll 8
+                    for (int i = from; i < (int)parts; i += stride) {
+                        const float f = table[i * nrows + r].x;
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + r * D + d, 16, a.partials, ws_bytes)));
+                        v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
                     }
-                    if (shares == 1) {
-                        store_row(sg.r0 + r, v, rm, rl);
-                    } else {
-                        if (4 * lane < D) *reinterpret_cast<float4 *>(merge + warp * kMergeRow + 4 * lane) = v;
-                        __syncthreads();
-                        if (share == 0) {
-                            for (int i = 1; i < shares; ++i)
-                                if (4 * lane < D) {
-                                    const float4 x = *reinterpret_cast<const float4 *>(merge + (warp + i * across) * kMergeRow + 4 * lane);
-                                    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-                                }
-                            store_row(sg.r0 + r, v, rm, rl);
+                    return v;
+                };
+                if (shares == 1) {
+                    for (int task = tid; task < tasks; task += kAttThreads) store_part(sg.r0 + task / kCols, 4 * (task % kCols), add_parts(task, 0, 1));
+                } else {
+                    const int task = tid % tasks, share = tid / tasks;
+                    if (share < shares) sums[tid] = add_parts(task, share, shares);
+                    __syncthreads();
+                    if (share == 0) {
+                        float4 v = sums[task];
+                        for (int i = 1; i < shares; ++i) {
+                            const float4 x = sums[i * tasks + task];
+                            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
                         }
+                        store_part(sg.r0 + task / kCols, 4 * (task % kCols), v);
                     }
                 }
             }
         }
         // rows the sequence does not have
         if (finish && sg.r0 == 0)
-            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) store_row(r, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) {
+                if (4 * lane < D) store_part(r, 4 * lane, make_float4(0.f, 0.f, 0.f, 0.f));
+                if (lane == 0) store_lse(r, -INFINITY, 0.f);
+            }
         if (tid == 0) sh_next = next;
         fence_async_proxy();  // (the rings held ordinary stores; bulk copies come next)
         __syncthreads();      // the rings, sh_ml and sh_q are free again
