@@ -34,6 +34,8 @@ class MxqError(RuntimeError):
 def lib() -> ctypes.CDLL:
     """Load ``libmxq.so`` (built by ``python -m paper_2503_13565_b200.build``)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -129,8 +131,9 @@ def _check(status: int, where: str) -> None:
 
 
 def _stream(stream=None) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is None:   # (the raw handle of the current stream: a stream object would cost as much as a kernel launch)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _dev(t: torch.Tensor, dtype, what: str) -> int:
@@ -611,7 +614,7 @@ class KVCache:
 def _kv_seqs(tables, lens):
     """(B, tables, W, lens) for a call, shapes checked."""
     b, w = tables.shape
-    if tuple(lens.shape) != (b,):
+    if lens.shape != (b,):
         raise ValueError("tables must be [B, W] and lens [B]")
     return b, _dev(tables, torch.int32, "tables"), w, _dev(lens, torch.int32, "lens")
 
@@ -619,7 +622,7 @@ def _kv_seqs(tables, lens):
 def _kv_ints(t, shape, what: str) -> int:
     if t is None:
         return 0
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError("%s must be %s" % (what, list(shape)))
     return _dev(t, torch.int32, what)
 
@@ -627,13 +630,17 @@ def _kv_ints(t, shape, what: str) -> int:
 def _token_rows(t: torch.Tensor, shape, what: str):
     """Pointer and token-row stride (elements) of a BF16 [B, M, heads, D] tensor whose heads lie together: contiguous, or a
     column slice of a fused projection's output."""
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError("%s must be %s" % (what, list(shape)))
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise TypeError("%s must be a CUDA tensor of dtype torch.bfloat16" % what)
     b, m, h, d = shape
+    if t.is_contiguous():
+        return t.data_ptr(), h * d
     sb, sm, sh, sd = t.stride()
     stride = sm if m > 1 else (sb if b > 1 else h * d)
-    if not t.is_cuda or t.dtype != torch.bfloat16 or sd != 1 or (h > 1 and sh != d) or (b > 1 and sb != m * stride):
-        raise TypeError("%s must be a CUDA tensor of dtype torch.bfloat16 with contiguous heads and one stride between token rows" % what)
+    if sd != 1 or (h > 1 and sh != d) or (b > 1 and sb != m * stride):
+        raise TypeError("%s must have contiguous heads and one stride between token rows" % what)
     return t.data_ptr(), stride
 
 
@@ -671,17 +678,19 @@ def mxq_kv_attention(q: torch.Tensor, cache: KVCache, layer: int, tables: torch.
     ``scale`` defaults to D ** -0.5.  Returns O [B, M, q_heads, D] BF16, with ``with_lse`` also lse [B, M, q_heads] FP32.
     ``workspace``: from ``new_workspace(mxq_kv_attention_workspace_bytes(...))``, zero-filled once, one per stream."""
     b, tp, w, lp = _kv_seqs(tables, lens)
-    m, hq, d = q.shape[1], q.shape[2], cache.head_dim
-    qp, qs = _token_rows(q, (b, m, hq, d), "q")
+    _, m, hq, d = q.shape
+    shape = (b, m, hq, cache.head_dim)
+    qp, qs = _token_rows(q, shape, "q")
     if out is None:
-        out = torch.empty((b, m, hq, d), dtype=torch.bfloat16, device=q.device)
-    elif tuple(out.shape) != (b, m, hq, d):
+        out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+    elif out.shape != shape:
         raise ValueError("out must be [B, M, q_heads, D]")
-    if with_lse and lse is None:
-        lse = torch.empty((b, m, hq), dtype=torch.float32, device=q.device)
-    if lse is not None and tuple(lse.shape) != (b, m, hq):
-        raise ValueError("lse must be [B, M, q_heads]")
-    if tree is not None and tuple(tree.shape) != (b, m):
+    if lse is not None:
+        if lse.shape != shape[:3]:
+            raise ValueError("lse must be [B, M, q_heads]")
+    elif with_lse:
+        lse = torch.empty(shape[:3], dtype=torch.float32, device=q.device)
+    if tree is not None and tree.shape != (b, m):
         raise ValueError("tree must be [B, M]")
     if workspace is None:
         workspace = new_workspace(mxq_kv_attention_workspace_bytes(b, m, hq, cache.kv_heads, d), q.device)
