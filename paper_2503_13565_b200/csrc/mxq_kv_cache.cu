@@ -9,18 +9,20 @@
 namespace mxq {
 
 constexpr int kKvThreads = 128;
+// Token rows of a sequence per lane.  One for a decode step (nothing to share, latency counts); several for a prompt, so that a
+// lane's lookups (length, row count, page) are spent once and more loads are in flight.
+constexpr int kPromptRows = 4;
 
 struct RowPlace {
     uint8_t *tile;   // nullptr: no such row
     int slot;        // token in the tile
 };
 
-// where row i of sequence b lives: position len - rows + i
+// where the token at position pos of sequence b lives
 template <int D>
-__device__ __forceinline__ RowPlace row_place(const KvView &c, const KvSeqs &s, int b, int i, int head) {
+__device__ __forceinline__ RowPlace row_place(const KvView &c, const KvSeqs &s, int b, int pos, int head) {
     RowPlace p = {nullptr, 0};
-    const int rows = s.nrows(b), pos = s.len(b) - rows + i;
-    if (i >= rows || pos < 0) return p;
+    if (pos < 0) return p;
     const int page = s.page(b, pos >> c.page_shift);
     if (!kv_page_ok(c, page)) return p;
     const int slot = pos & ((1 << c.page_shift) - 1);
@@ -29,77 +31,99 @@ __device__ __forceinline__ RowPlace row_place(const KvView &c, const KvSeqs &s, 
     return p;
 }
 
+// a lane's part of a call: quarter q of `head`'s rows i .. of sequence b
+struct LaneRows {
+    int b, i, head;
+    uint32_t q;
+};
+template <int ROWS>
+__device__ __forceinline__ LaneRows lane_rows(const KvView &c, const KvSeqs &s, uint32_t idx) {
+    LaneRows l;
+    const uint32_t groups = (uint32_t)(s.m + ROWS - 1) / ROWS, rowhead = idx >> 2, row = rowhead / (uint32_t)c.heads;
+    l.q = idx & 3u, l.head = (int)(rowhead - row * (uint32_t)c.heads);
+    l.b = ROWS == 1 && s.m == 1 ? (int)row : (int)(row / groups);
+    l.i = (int)(row - (uint32_t)l.b * groups) * ROWS;
+    return l;
+}
+
 struct KvRows {   // the BF16 side: [B][M][heads][D], token rows `stride` elements apart
     const uint16_t *k, *v;
     int64_t k_stride, v_stride;
 };
 
-// grid.x covers (sequence, row, head, quarter); grid.y: 0 = K, 1 = V
-template <int D>
+// grid.x covers (sequence, rows, head, quarter); grid.y: 0 = K, 1 = V
+template <int D, int ROWS>
 __global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs s, KvRows in, uint32_t total) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb;
     pdl_trigger();
     const uint32_t idx = blockIdx.x * kKvThreads + threadIdx.x;
-    const uint32_t q = idx & 3u, rowhead = idx >> 2, row = rowhead / (uint32_t)c.heads, head = rowhead - row * (uint32_t)c.heads;
     const bool value = blockIdx.y != 0;
-    const bool live = idx < total;   // (the quads of a warp leave together: total is a multiple of 4)
-    const int b = live ? (int)(row / (uint32_t)s.m) : 0, i = live ? (int)(row - (uint32_t)b * (uint32_t)s.m) : 0;
+    if ((idx & ~31u) >= total) return;   // (warps leave together; total is a multiple of 4)
+    const LaneRows l = lane_rows<ROWS>(c, s, idx < total ? idx : total - 1);
     pdl_wait();
-    RowPlace at = {nullptr, 0};
-    uint4 x[kNb];
-    if (live) {
-        const int64_t stride = value ? in.v_stride : in.k_stride;
-        const uint16_t *base = value ? in.v : in.k;
-        const uint16_t *src = base + (int64_t)row * stride + (int64_t)head * D;
+    const int rows = s.nrows(l.b), live = idx < total ? min(rows - l.i, ROWS) : 0;     // rows of the lane that exist
+    const int64_t stride = value ? in.v_stride : in.k_stride;
+    const uint16_t *base = value ? in.v : in.k;
+    uint4 x[ROWS][kNb];
 #pragma unroll
-        for (int j = 0; j < kNb; ++j)
-            x[j] = ld_dep_u4(MXQ_AT(src + 32 * j + 8 * q, 16, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
-        at = row_place<D>(c, s, b, i, (int)head);
-    } else {
+    for (int i = 0; i < ROWS; ++i) {
+        const uint16_t *src = base + ((int64_t)l.b * s.m + l.i + i) * stride + (int64_t)l.head * D + 8 * l.q;
 #pragma unroll
-        for (int j = 0; j < kNb; ++j) x[j] = make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < kNb; ++j) {
+            x[i][j] = make_uint4(0, 0, 0, 0);
+            if (i < live) x[i][j] = ld_dep_u4(MXQ_AT(src + 32 * j, 16, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
+        }
     }
-    // maxima of blocks 2p and 2p + 1 in the halves of one register
-    uint32_t top[kNb / 2];
+    RowPlace at[ROWS];
+    const int first = s.len(l.b) - rows + l.i;
 #pragma unroll
-    for (int p = 0; p < kNb / 2; ++p) {
-        const uint32_t a = chunk_max2(x[2 * p]), d = chunk_max2(x[2 * p + 1]);
-        top[p] = __vmaxu2(__byte_perm(a, d, 0x5410), __byte_perm(a, d, 0x7632));
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) top[p] = __vmaxu2(top[p], __shfl_xor_sync(0xffffffffu, top[p], o));
+    for (int i = 0; i < ROWS; ++i) {
+        at[i].tile = nullptr;
+        if (i < live) at[i] = row_place<D>(c, s, l.b, first + i, l.head);
     }
-    uint32_t w[kNb], scale = 0;
 #pragma unroll
-    for (int j = 0; j < kNb; ++j) {
-        const uint32_t byte = scale_byte((top[j / 2] >> (16 * (j & 1))) & 0xFFFFu);
-        w[j] = byte == 0xFFu ? 0u : cast_chunk(x[j], __uint_as_float((254u - byte) << 23));
-        scale |= byte << (8 * j);
-    }
-    if (at.tile == nullptr) return;
-    uint32_t out[kNb];
-    if (!value) {
-#pragma unroll
-        for (int j = 0; j < kNb; ++j) out[j] = w[j];
-    } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
+    for (int i = 0; i < ROWS; ++i) {
+        // maxima of blocks 2p and 2p + 1 in the halves of one register
+        uint32_t top[kNb / 2];
 #pragma unroll
         for (int p = 0; p < kNb / 2; ++p) {
-            out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
-            out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
+            const uint32_t a = chunk_max2(x[i][2 * p]), d = chunk_max2(x[i][2 * p + 1]);
+            top[p] = __vmaxu2(__byte_perm(a, d, 0x5410), __byte_perm(a, d, 0x7632));
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) top[p] = __vmaxu2(top[p], __shfl_xor_sync(0xffffffffu, top[p], o));
         }
-    }
-    uint8_t *dst = at.tile + (value ? T::kV : 0) + at.slot * T::kRow + q * 4 * kNb;
-    dst = MXQ_AT(dst, 4 * kNb, c.pool, c.pool_bytes);
-    if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
-    else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
-    if (!value) {
-        if (q == 0) {
-            uint8_t *sc = MXQ_AT(at.tile + T::kKs + at.slot * kNb, kNb, c.pool, c.pool_bytes);
-            if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
-            else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
+        uint32_t w[kNb], scale = 0;
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) {
+            const uint32_t byte = scale_byte((top[j / 2] >> (16 * (j & 1))) & 0xFFFFu);
+            w[j] = byte == 0xFFu ? 0u : cast_chunk(x[i][j], __uint_as_float((254u - byte) << 23));
+            scale |= byte << (8 * j);
         }
-    } else if (q < kNb) {
-        *MXQ_AT(at.tile + T::vs(at.slot, (int)q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * q));
+        if (at[i].tile == nullptr) continue;
+        uint32_t out[kNb];
+        if (!value) {
+#pragma unroll
+            for (int j = 0; j < kNb; ++j) out[j] = w[j];
+        } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
+#pragma unroll
+            for (int p = 0; p < kNb / 2; ++p) {
+                out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
+                out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
+            }
+        }
+        uint8_t *dst = MXQ_AT(at[i].tile + (value ? T::kV : 0) + at[i].slot * T::kRow + l.q * 4 * kNb, 4 * kNb, c.pool, c.pool_bytes);
+        if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+        else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
+        if (!value) {
+            if (l.q == 0) {
+                uint8_t *sc = MXQ_AT(at[i].tile + T::kKs + at[i].slot * kNb, kNb, c.pool, c.pool_bytes);
+                if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
+                else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
+            }
+        } else if (l.q < kNb) {
+            *MXQ_AT(at[i].tile + T::vs(at[i].slot, (int)l.q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * l.q));
+        }
     }
 }
 
@@ -115,49 +139,52 @@ __device__ __forceinline__ uint4 codes_to_bf16(uint32_t w, float s) {
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-template <int D>
+template <int D, int ROWS>
 __global__ void __launch_bounds__(kKvThreads) kv_read_kernel(KvView c, KvSeqs s, uint16_t *K, uint16_t *V, uint32_t total) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb;
     pdl_trigger();
     const uint32_t idx = blockIdx.x * kKvThreads + threadIdx.x;
     if (idx >= total) return;
-    const uint32_t q = idx & 3u, rowhead = idx >> 2, row = rowhead / (uint32_t)c.heads, head = rowhead - row * (uint32_t)c.heads;
     const bool value = blockIdx.y != 0;
-    const int b = (int)(row / (uint32_t)s.m), i = (int)(row - (uint32_t)b * (uint32_t)s.m);
+    const LaneRows l = lane_rows<ROWS>(c, s, idx);
     pdl_wait();
-    const RowPlace at = row_place<D>(c, s, b, i, (int)head);
-    uint4 out[kNb];
-    if (at.tile == nullptr) {
+    const int rows = s.nrows(l.b), first = s.len(l.b) - rows + l.i;
+    uint32_t w[ROWS][kNb], sc[ROWS];
 #pragma unroll
-        for (int j = 0; j < kNb; ++j) out[j] = make_uint4(0, 0, 0, 0);
-    } else {
-        const uint8_t *src = at.tile + (value ? T::kV : 0) + at.slot * T::kRow + q * 4 * kNb;
-        src = MXQ_AT(src, 4 * kNb, c.pool, c.pool_bytes);
-        uint32_t w[kNb], n[kNb];
+    for (int i = 0; i < ROWS; ++i) {
+        RowPlace at = {nullptr, 0};
+        if (l.i + i < rows) at = row_place<D>(c, s, l.b, first + i, l.head);
+        sc[i] = 0;
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) w[i][j] = 0;
+        if (at.tile == nullptr) continue;      // (codes and scales of zero: zero)
+        const uint8_t *src = MXQ_AT(at.tile + (value ? T::kV : 0) + at.slot * T::kRow + l.q * 4 * kNb, 4 * kNb, c.pool, c.pool_bytes);
         if constexpr (kNb == 4) {
             const uint4 r = ld_dep_u4(src);
-            w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;
+            w[i][0] = r.x, w[i][1] = r.y, w[i][2] = r.z, w[i][3] = r.w;
         } else {
-            w[0] = ld_dep_u32(src), w[1] = ld_dep_u32(src + 4);
-        }
-#pragma unroll
-        for (int p = 0; p < kNb / 2; ++p) {
-            n[2 * p] = value ? __byte_perm(w[p], w[kNb / 2 + p], 0x5410) : w[2 * p];
-            n[2 * p + 1] = value ? __byte_perm(w[p], w[kNb / 2 + p], 0x7632) : w[2 * p + 1];
+            w[i][0] = ld_dep_u32(src), w[i][1] = ld_dep_u32(src + 4);
         }
 #pragma unroll
         for (int j = 0; j < kNb; ++j) {
-            const uint8_t *sc = at.tile + (value ? T::vs(at.slot, j) : T::kKs + at.slot * kNb + j);
-            unsigned short sb;
-            asm volatile("ld.global.cg.u8 %0, [%1];" : "=h"(sb) : "l"(MXQ_AT(sc, 1, c.pool, c.pool_bytes)) : "memory");
-            out[j] = codes_to_bf16(n[j], e8m0_to_float(sb));
+            const uint8_t *a = at.tile + (value ? T::vs(at.slot, j) : T::kKs + at.slot * kNb + j);
+            unsigned short byte;
+            asm volatile("ld.global.cg.u8 %0, [%1];" : "=h"(byte) : "l"(MXQ_AT(a, 1, c.pool, c.pool_bytes)) : "memory");
+            sc[i] |= (uint32_t)byte << (8 * j);
         }
     }
     uint16_t *base = value ? V : K;
 #pragma unroll
-    for (int j = 0; j < kNb; ++j)
-        *reinterpret_cast<uint4 *>(MXQ_AT(base + (int64_t)rowhead * D + 32 * j + 8 * q, 16, base, (int64_t)total / 4 * D * 2)) = out[j];
+    for (int i = 0; i < ROWS; ++i) {
+        if (ROWS > 1 && l.i + i >= s.m) break;
+        uint16_t *dst = base + (((int64_t)l.b * s.m + l.i + i) * c.heads + l.head) * D + 8 * l.q;
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) {
+            const uint32_t n = !value ? w[i][j] : (j & 1) ? __byte_perm(w[i][j / 2], w[i][kNb / 2 + j / 2], 0x7632) : __byte_perm(w[i][j / 2], w[i][kNb / 2 + j / 2], 0x5410);
+            *reinterpret_cast<uint4 *>(MXQ_AT(dst + 32 * j, 16, base, (int64_t)s.B * s.m * c.heads * D * 2)) = codes_to_bf16(n, e8m0_to_float((sc[i] >> (8 * j)) & 0xFFu));
+        }
+    }
 }
 
 MXQ_BOUNDS_TU(bounds_take_kv_cache)
@@ -200,6 +227,15 @@ KvView kv_view(const mxq_kv_cache *c, int layer) {
     return v;
 }
 
+// several rows per lane where that still leaves every SM a full set of lanes
+static bool prompt_rows(const mxq_kv_cache *c, int B, int M) {
+    return M >= kPromptRows && (int64_t)B * M * c->kv_heads * 8 >= (int64_t)kPromptRows * 2048 * sm_count();
+}
+static uint32_t lanes_of(const mxq_kv_cache *c, int B, int M, bool prompt) {
+    const int per = prompt ? kPromptRows : 1;
+    return (uint32_t)B * (uint32_t)((M + per - 1) / per) * (uint32_t)c->kv_heads * 4u;
+}
+
 // rows of one call: at most 2^29 (row, head) pairs, so that a lane's index fits 32 bits
 static bool rows_ok(const mxq_kv_cache *c, int B, int M) { return M >= 1 && (int64_t)B * M <= ((int64_t)1 << 29) / c->kv_heads; }
 
@@ -223,11 +259,14 @@ int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int6
     const int64_t width = (int64_t)cache->kv_heads * cache->head_dim;
     if (!mxq::rows_ok(cache, B, M) || k_stride < width || v_stride < width) return MXQ_ERR_SHAPE;
     if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || k_stride % 8 || v_stride % 8 || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
-    const uint32_t total = (uint32_t)B * (uint32_t)M * (uint32_t)cache->kv_heads * 4u;
+    const bool prompt = mxq::prompt_rows(cache, B, M);
+    const uint32_t total = mxq::lanes_of(cache, B, M, prompt);
     const mxq::KvRows in = {(const uint16_t *)K_bf16, (const uint16_t *)V_bf16, k_stride, v_stride};
     const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
-    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_append_kernel<128> : mxq::kv_append_kernel<64>, grid, mxq::kKvThreads, 0,
+    return mxq::kv_launch(cache->head_dim == 128 ? (prompt ? mxq::kv_append_kernel<128, mxq::kPromptRows> : mxq::kv_append_kernel<128, 1>)
+                                                 : (prompt ? mxq::kv_append_kernel<64, mxq::kPromptRows> : mxq::kv_append_kernel<64, 1>),
+                          grid, mxq::kKvThreads, 0,
                           (cudaStream_t)stream, mxq::kv_view(cache, layer), s, in, total);
 }
 
@@ -239,10 +278,13 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
     if (rc != MXQ_OK) return rc;
     if (!mxq::rows_ok(cache, B, M)) return MXQ_ERR_SHAPE;
     if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
-    const uint32_t total = (uint32_t)B * (uint32_t)M * (uint32_t)cache->kv_heads * 4u;
+    const bool prompt = mxq::prompt_rows(cache, B, M);
+    const uint32_t total = mxq::lanes_of(cache, B, M, prompt);
     const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
-    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_read_kernel<128> : mxq::kv_read_kernel<64>, grid, mxq::kKvThreads, 0,
+    return mxq::kv_launch(cache->head_dim == 128 ? (prompt ? mxq::kv_read_kernel<128, mxq::kPromptRows> : mxq::kv_read_kernel<128, 1>)
+                                                 : (prompt ? mxq::kv_read_kernel<64, mxq::kPromptRows> : mxq::kv_read_kernel<64, 1>),
+                          grid, mxq::kKvThreads, 0,
                           (cudaStream_t)stream, mxq::kv_view(cache, layer), s, (uint16_t *)K_bf16, (uint16_t *)V_bf16, total);
 }
 

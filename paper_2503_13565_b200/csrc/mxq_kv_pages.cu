@@ -122,29 +122,40 @@ __device__ __forceinline__ int book_len(const Book &k, int b) {
 }
 __device__ __forceinline__ int pages_for(int64_t n, int shift) { return (int)((n + (1 << shift) - 1) >> shift); }
 
+// x-th of the places that a list of counts with prefix sums `upto` describes: which entry, and which of its places
+struct Owned {
+    int i, k;
+};
+__device__ __forceinline__ Owned owned(const int *upto, int n, int x) {
+    const int i = owner_of(upto, n, x);
+    return {i, x - (i ? upto[i - 1] : 0)};
+}
+
 __global__ void __launch_bounds__(kBookThreads) kv_resize_kernel(Book k, const int32_t *new_lens) {
     extern __shared__ int book_smem[];
-    int *upto = book_smem, *held = book_smem + k.B;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int *upto = book_smem, *held = book_smem + k.B, *drop = book_smem + 2 * k.B;
     const int64_t cap = (int64_t)k.W << k.page_shift;
     pdl_trigger();
     pdl_wait();
-    for (int b = warp; b < k.B; b += kBookWarps) {
-        const int have = pages_for(book_len(k, b), k.page_shift);
-        const int n = (int)ld_dep_u32(MXQ_AT(new_lens + b, 4, new_lens, (size_t)k.B * 4));
+    for (int b = (int)threadIdx.x; b < k.B; b += kBookThreads) {
+        const int n = (int)ld_dep_u32(MXQ_AT(new_lens + b, 4, new_lens, (size_t)k.B * 4)), have = pages_for(book_len(k, b), k.page_shift);
         const int want = n >= 0 && n <= cap ? pages_for(n, k.page_shift) : have;
-        for (int w = want + lane; w < have; w += 32) {
-            const int page = (int)ld_dep_u32(entry_of(k, b, w));
-            if ((unsigned)page < (unsigned)k.num_pages) atomicSub(ref_of(k, page), 1);
-            *entry_of(k, b, w) = -1;
-        }
-        if (lane == 0) upto[b] = max(want - have, 0), held[b] = have;
+        upto[b] = max(want - have, 0), held[b] = have, drop[b] = max(have - want, 0);
     }
     __syncthreads();
-    const int wanted = scan_needs(upto, k.B);
+    const int wanted = scan_needs(upto, k.B), dropped = scan_needs(drop, k.B);
+#pragma unroll 4
+    for (int x = (int)threadIdx.x; x < dropped; x += kBookThreads) {
+        const Owned o = owned(drop, k.B, x);
+        int32_t *e = entry_of(k, o.i, held[o.i] - 1 - o.k);
+        const int page = (int)ld_dep_u32(e);
+        *e = -1;
+        if ((unsigned)page < (unsigned)k.num_pages) atomicSub(ref_of(k, page), 1);
+    }
+    __syncthreads();
     const int found = lowest_free(k.refs, k.num_pages, wanted, [&](int rank, int page) {
-        const int b = owner_of(upto, k.B, rank);
-        *entry_of(k, b, held[b] + rank - (b ? upto[b - 1] : 0)) = page;
+        const Owned o = owned(upto, k.B, rank);
+        *entry_of(k, o.i, held[o.i] + o.k) = page;
         *ref_of(k, page) = 1;
     });
     __syncthreads();
@@ -171,50 +182,47 @@ struct ForkJob {
 __global__ void __launch_bounds__(kBookThreads)
 kv_fork_kernel(Book k, int n, const int32_t *src, const int32_t *dst, ForkJob *jobs) {
     extern __shared__ int book_smem[];
-    int *upto = book_smem, *fresh = book_smem + n;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // per child: pages wanted (summed up), its fresh page or -1 if the pair is refused, whole pages to share (summed up), source, slot, length
+    int *upto = book_smem, *fresh = book_smem + n, *shared = book_smem + 2 * n, *from = book_smem + 3 * n, *to = book_smem + 4 * n, *lens = book_smem + 5 * n;
+    const int mask = (1 << k.page_shift) - 1;
     pdl_trigger();
     pdl_wait();
-    auto pair = [&](int i, int &s, int &d) {
-        s = (int)ld_dep_u32(MXQ_AT(src + i, 4, src, (size_t)n * 4));
-        d = (int)ld_dep_u32(MXQ_AT(dst + i, 4, dst, (size_t)n * 4));
-        return (unsigned)s < (unsigned)k.B && (unsigned)d < (unsigned)k.B && s != d;
-    };
     for (int i = (int)threadIdx.x; i < n; i += kBookThreads) {
-        int s, d;
-        // an occupied slot is refused
-        const bool ok = pair(i, s, d) && book_len(k, d) == 0;
+        const int s = (int)ld_dep_u32(MXQ_AT(src + i, 4, src, (size_t)n * 4)), d = (int)ld_dep_u32(MXQ_AT(dst + i, 4, dst, (size_t)n * 4));
+        const bool in = (unsigned)s < (unsigned)k.B && (unsigned)d < (unsigned)k.B && s != d;
+        const bool ok = in && book_len(k, d) == 0;      // an occupied slot is refused
+        const int len = ok ? book_len(k, s) : 0;
+        from[i] = s, to[i] = d, lens[i] = len;
         fresh[i] = ok ? 0 : -1;
-        upto[i] = ok && (book_len(k, s) & ((1 << k.page_shift) - 1)) != 0;
+        upto[i] = ok && (len & mask) != 0;
     }
     __syncthreads();
     const int wanted = scan_needs(upto, n);
     const int found = lowest_free(k.refs, k.num_pages, wanted, [&](int rank, int page) { fresh[owner_of(upto, n, rank)] = page; });
     __syncthreads();
-    for (int i = warp; i < n; i += kBookWarps) {
+    for (int i = (int)threadIdx.x; i < n; i += kBookThreads) {
+        const bool part = upto[i] != (i ? upto[i - 1] : 0), fits = fresh[i] >= 0 && (!part || upto[i] <= found);
+        const int whole = lens[i] >> k.page_shift;
         ForkJob job = {0, 0, 0, 0};
-        int s, d;
-        const bool part = upto[i] != (i ? upto[i - 1] : 0);
-        const bool fits = pair(i, s, d) && fresh[i] >= 0 && (!part || upto[i] <= found);
-        if (fits) {
-            const int len = book_len(k, s), whole = len >> k.page_shift;
-            for (int w = lane; w < whole; w += 32) {
-                const int page = (int)ld_dep_u32(entry_of(k, s, w));
-                *entry_of(k, d, w) = page;
-                if ((unsigned)page < (unsigned)k.num_pages) atomicAdd(ref_of(k, page), 1);
-            }
-            if (part) {
-                job.src = (int)ld_dep_u32(entry_of(k, s, whole));
-                job.dst = fresh[i];
-                if ((unsigned)job.src < (unsigned)k.num_pages) job.tiles = ((len & ((1 << k.page_shift) - 1)) + kTileTokens - 1) / kTileTokens;
-                if (lane == 0) {
-                    *entry_of(k, d, whole) = job.dst;
-                    *ref_of(k, job.dst) = 1;
-                }
-            }
-            if (lane == 0) *MXQ_AT(k.lens + d, 4, k.lens, (size_t)k.B * 4) = len;
+        if (fits && part) {
+            job.src = (int)ld_dep_u32(entry_of(k, from[i], whole));
+            job.dst = fresh[i];
+            if ((unsigned)job.src < (unsigned)k.num_pages) job.tiles = ((lens[i] & mask) + kTileTokens - 1) / kTileTokens;
+            *entry_of(k, to[i], whole) = job.dst;
+            *ref_of(k, job.dst) = 1;
         }
-        if (lane == 0) *MXQ_AT(jobs + i, sizeof(ForkJob), jobs, (size_t)n * sizeof(ForkJob)) = job;
+        shared[i] = fits ? whole : 0;
+        if (fits) *MXQ_AT(k.lens + to[i], 4, k.lens, (size_t)k.B * 4) = lens[i];
+        *MXQ_AT(jobs + i, sizeof(ForkJob), jobs, (size_t)n * sizeof(ForkJob)) = job;
+    }
+    __syncthreads();
+    const int total = scan_needs(shared, n);
+#pragma unroll 4
+    for (int x = (int)threadIdx.x; x < total; x += kBookThreads) {
+        const Owned o = owned(shared, n, x);
+        const int page = (int)ld_dep_u32(entry_of(k, from[o.i], o.k));
+        *entry_of(k, to[o.i], o.k) = page;
+        if ((unsigned)page < (unsigned)k.num_pages) atomicAdd(ref_of(k, page), 1);
     }
 }
 
@@ -324,6 +332,22 @@ MXQ_BOUNDS_TU(bounds_take_kv_pages)
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 
+// shared memory for the largest call: 24 bytes per sequence
+static int book_smem_ready(const void *kernel) {
+    static const void *ready[64][2];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return MXQ_ERR_CUDA;
+    const void **slot = kernel == (const void *)kv_resize_kernel ? &ready[dev][0] : &ready[dev][1];
+    if (*slot != kernel) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MXQ_KV_MAX_SEQS * 24) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return MXQ_ERR_CUDA;
+        }
+        *slot = kernel;
+    }
+    return MXQ_OK;
+}
+
 static Book book_of(const mxq_kv_cache *c, int B, int32_t *tables, int W, int32_t *lens) {
     Book k;
     k.refs = c->refs, k.tables = tables, k.lens = lens;
@@ -343,7 +367,9 @@ int mxq_kv_resize(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int3
     if (rc == MXQ_OK) rc = mxq::kv_check_seqs(B, W, tables, lens);
     if (rc != MXQ_OK) return rc;
     if (!mxq::aligned_to(new_lens, 4)) return MXQ_ERR_ALIGN;
-    return mxq::kv_launch(mxq::kv_resize_kernel, dim3(1), mxq::kBookThreads, (size_t)B * 8, (cudaStream_t)stream,
+    rc = mxq::book_smem_ready((const void *)mxq::kv_resize_kernel);
+    if (rc != MXQ_OK) return rc;
+    return mxq::kv_launch(mxq::kv_resize_kernel, dim3(1), mxq::kBookThreads, (size_t)B * 12, (cudaStream_t)stream,
                           mxq::book_of(cache, B, tables, W, lens), new_lens);
 }
 
@@ -359,7 +385,9 @@ int mxq_kv_fork(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_
     if (!mxq::aligned_to(src, 4) || !mxq::aligned_to(dst, 4) || !mxq::aligned16(workspace)) return MXQ_ERR_ALIGN;
     if (!workspace || workspace_bytes < mxq_kv_fork_workspace_bytes(n)) return MXQ_ERR_WORKSPACE;
     mxq::ForkJob *jobs = (mxq::ForkJob *)workspace;
-    rc = mxq::kv_launch(mxq::kv_fork_kernel, dim3(1), mxq::kBookThreads, (size_t)n * 8, (cudaStream_t)stream,
+    rc = mxq::book_smem_ready((const void *)mxq::kv_fork_kernel);
+    if (rc != MXQ_OK) return rc;
+    rc = mxq::kv_launch(mxq::kv_fork_kernel, dim3(1), mxq::kBookThreads, (size_t)n * 24, (cudaStream_t)stream,
                         mxq::book_of(cache, B, tables, W, lens), n, src, dst, jobs);
     if (rc != MXQ_OK) return rc;
     const mxq::KvView c = mxq::kv_view(cache, 0);
