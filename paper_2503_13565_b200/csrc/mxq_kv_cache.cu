@@ -9,8 +9,8 @@
 namespace mxq {
 
 constexpr int kKvThreads = 128;
-// Token rows of a sequence per lane.  One for a decode step (nothing to share, latency counts); several for a prompt, so that a
-// lane's lookups (length, row count, page) are spent once and more loads are in flight.
+// Token rows of a sequence per lane of the read: one for a decode step (nothing to share, latency counts); several for a prompt,
+// so that a lane's lookups (length, row count) are spent once and more loads are in flight.
 constexpr int kPromptRows = 4;
 
 struct RowPlace {
@@ -51,8 +51,8 @@ struct KvRows {   // the BF16 side: [B][M][heads][D], token rows `stride` elemen
     int64_t k_stride, v_stride;
 };
 
-// grid.x covers (sequence, rows, head, quarter); grid.y: 0 = K, 1 = V
-template <int D, int ROWS>
+// grid.x covers (sequence, row, head, quarter); grid.y: 0 = K, 1 = V
+template <int D>
 __global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs s, KvRows in, uint32_t total) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb;
@@ -60,70 +60,105 @@ __global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs 
     const uint32_t idx = blockIdx.x * kKvThreads + threadIdx.x;
     const bool value = blockIdx.y != 0;
     if ((idx & ~31u) >= total) return;   // (warps leave together; total is a multiple of 4)
-    const LaneRows l = lane_rows<ROWS>(c, s, idx < total ? idx : total - 1);
+    const LaneRows l = lane_rows<1>(c, s, idx < total ? idx : total - 1);
     pdl_wait();
-    const int rows = s.nrows(l.b), live = idx < total ? min(rows - l.i, ROWS) : 0;     // rows of the lane that exist
+    const int rows = s.nrows(l.b);
+    const bool live = idx < total && l.i < rows;
     const int64_t stride = value ? in.v_stride : in.k_stride;
-    const uint16_t *base = value ? in.v : in.k;
-    uint4 x[ROWS][kNb];
+    const uint16_t *base = value ? in.v : in.k, *src = base + ((int64_t)l.b * s.m + l.i) * stride + (int64_t)l.head * D + 8 * l.q;
+    uint4 x[kNb];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const uint16_t *src = base + ((int64_t)l.b * s.m + l.i + i) * stride + (int64_t)l.head * D + 8 * l.q;
-#pragma unroll
-        for (int j = 0; j < kNb; ++j) {
-            x[i][j] = make_uint4(0, 0, 0, 0);
-            if (i < live) x[i][j] = ld_dep_u4(MXQ_AT(src + 32 * j, 16, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
-        }
+    for (int j = 0; j < kNb; ++j) {
+        x[j] = make_uint4(0, 0, 0, 0);
+        if (live) x[j] = ld_dep_u4(MXQ_AT(src + 32 * j, 16, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
     }
-    RowPlace at[ROWS];
-    const int first = s.len(l.b) - rows + l.i;
+    RowPlace at = {nullptr, 0};
+    if (live) at = row_place<D>(c, s, l.b, s.len(l.b) - rows + l.i, l.head);
+    // maxima of blocks 2p and 2p + 1 in the halves of one register
+    uint32_t top[kNb / 2];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        at[i].tile = nullptr;
-        if (i < live) at[i] = row_place<D>(c, s, l.b, first + i, l.head);
+    for (int p = 0; p < kNb / 2; ++p) {
+        const uint32_t a = chunk_max2(x[2 * p]), d = chunk_max2(x[2 * p + 1]);
+        top[p] = __vmaxu2(__byte_perm(a, d, 0x5410), __byte_perm(a, d, 0x7632));
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) top[p] = __vmaxu2(top[p], __shfl_xor_sync(0xffffffffu, top[p], o));
     }
+    uint32_t w[kNb], scale = 0;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        // maxima of blocks 2p and 2p + 1 in the halves of one register
-        uint32_t top[kNb / 2];
+    for (int j = 0; j < kNb; ++j) {
+        const uint32_t byte = scale_byte((top[j / 2] >> (16 * (j & 1))) & 0xFFFFu);
+        w[j] = byte == 0xFFu ? 0u : cast_chunk(x[j], __uint_as_float((254u - byte) << 23));
+        scale |= byte << (8 * j);
+    }
+    if (at.tile == nullptr) return;
+    uint32_t out[kNb];
+    if (!value) {
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) out[j] = w[j];
+    } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
 #pragma unroll
         for (int p = 0; p < kNb / 2; ++p) {
-            const uint32_t a = chunk_max2(x[i][2 * p]), d = chunk_max2(x[i][2 * p + 1]);
-            top[p] = __vmaxu2(__byte_perm(a, d, 0x5410), __byte_perm(a, d, 0x7632));
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) top[p] = __vmaxu2(top[p], __shfl_xor_sync(0xffffffffu, top[p], o));
+            out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
+            out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
         }
-        uint32_t w[kNb], scale = 0;
-#pragma unroll
-        for (int j = 0; j < kNb; ++j) {
-            const uint32_t byte = scale_byte((top[j / 2] >> (16 * (j & 1))) & 0xFFFFu);
-            w[j] = byte == 0xFFu ? 0u : cast_chunk(x[i][j], __uint_as_float((254u - byte) << 23));
-            scale |= byte << (8 * j);
+    }
+    uint8_t *dst = MXQ_AT(at.tile + (value ? T::kV : 0) + at.slot * T::kRow + l.q * 4 * kNb, 4 * kNb, c.pool, c.pool_bytes);
+    if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+    else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
+    if (!value) {
+        if (l.q == 0) {
+            uint8_t *sc = MXQ_AT(at.tile + T::kKs + at.slot * kNb, kNb, c.pool, c.pool_bytes);
+            if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
+            else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
         }
-        if (at[i].tile == nullptr) continue;
-        uint32_t out[kNb];
-        if (!value) {
+    } else if (l.q < kNb) {
+        *MXQ_AT(at.tile + T::vs(at.slot, (int)l.q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * l.q));
+    }
+}
+
+// The same for prompts, where the arithmetic decides: one lane per MX block (no exchange for the maximum, every scale computed
+// once), four heads of a token row per lane (one lookup of its place).  The words land with 4- and 2-byte stores that the L2
+// gathers.  Launched without overlap, so that the lanes of a row may share its sectors through L1.
+// grid.x covers (sequence, row, group of kHeadsPerLane heads, block); grid.y: 0 = K, 1 = V
+constexpr int kHeadsPerLane = 4;
+template <int D>
+__global__ void __launch_bounds__(kKvThreads) kv_append_prompt_kernel(KvView c, KvSeqs s, KvRows in, uint32_t total) {
+    using T = KvTile<D>;
+    constexpr int kNb = T::kNb;
+    const uint32_t idx = blockIdx.x * kKvThreads + threadIdx.x;
+    const bool value = blockIdx.y != 0;
+    if (idx >= total) return;
+    const uint32_t groups = (uint32_t)(c.heads + kHeadsPerLane - 1) / kHeadsPerLane, j = idx % kNb, u = idx / kNb, row = u / groups;
+    const int head0 = (int)(u - row * groups) * kHeadsPerLane, b = (int)(row / (uint32_t)s.m), i = (int)(row - (uint32_t)b * (uint32_t)s.m);
+    const int rows = s.nrows(b);
+    if (i >= rows) return;
+    const RowPlace at = row_place<D>(c, s, b, s.len(b) - rows + i, head0);
+    if (at.tile == nullptr) return;
+    const int64_t stride = value ? in.v_stride : in.k_stride;
+    const uint16_t *base = value ? in.v : in.k, *src = base + (int64_t)row * stride + (int64_t)head0 * D + 32 * j;
+    const int heads = min(kHeadsPerLane, c.heads - head0);
+#pragma unroll 2
+    for (int h = 0; h < heads; ++h) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(MXQ_AT(src + h * D, 64, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
+        uint4 x[4];
 #pragma unroll
-            for (int j = 0; j < kNb; ++j) out[j] = w[j];
-        } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
+        for (int q = 0; q < 4; ++q) x[q] = __ldg(p + q);
+        const uint32_t top = __vmaxu2(__vmaxu2(chunk_max2(x[0]), chunk_max2(x[1])), __vmaxu2(chunk_max2(x[2]), chunk_max2(x[3])));
+        const uint32_t byte = scale_byte(max(top & 0xFFFFu, top >> 16));
+        const float inv = __uint_as_float((254u - byte) << 23);
+        uint8_t *tile = at.tile + h * T::kBytes;
 #pragma unroll
-            for (int p = 0; p < kNb / 2; ++p) {
-                out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
-                out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t w = byte == 0xFFu ? 0u : cast_chunk(x[q], inv);
+            if (!value) {
+                *reinterpret_cast<uint32_t *>(MXQ_AT(tile + at.slot * T::kRow + q * 4 * kNb + 4 * j, 4, c.pool, c.pool_bytes)) = w;
+            } else {
+                uint8_t *v = tile + T::kV + at.slot * T::kRow + 2 * q * 2 * kNb + 2 * j;
+                *reinterpret_cast<uint16_t *>(MXQ_AT(v, 2, c.pool, c.pool_bytes)) = (uint16_t)w;
+                *reinterpret_cast<uint16_t *>(MXQ_AT(v + 2 * kNb, 2, c.pool, c.pool_bytes)) = (uint16_t)(w >> 16);
             }
         }
-        uint8_t *dst = MXQ_AT(at[i].tile + (value ? T::kV : 0) + at[i].slot * T::kRow + l.q * 4 * kNb, 4 * kNb, c.pool, c.pool_bytes);
-        if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
-        else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
-        if (!value) {
-            if (l.q == 0) {
-                uint8_t *sc = MXQ_AT(at[i].tile + T::kKs + at[i].slot * kNb, kNb, c.pool, c.pool_bytes);
-                if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
-                else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
-            }
-        } else if (l.q < kNb) {
-            *MXQ_AT(at[i].tile + T::vs(at[i].slot, (int)l.q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * l.q));
-        }
+        *MXQ_AT(tile + (value ? T::vs(at.slot, (int)j) : T::kKs + at.slot * kNb + (int)j), 1, c.pool, c.pool_bytes) = (uint8_t)byte;
     }
 }
 
@@ -259,15 +294,20 @@ int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int6
     const int64_t width = (int64_t)cache->kv_heads * cache->head_dim;
     if (!mxq::rows_ok(cache, B, M) || k_stride < width || v_stride < width) return MXQ_ERR_SHAPE;
     if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || k_stride % 8 || v_stride % 8 || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
-    const bool prompt = mxq::prompt_rows(cache, B, M);
-    const uint32_t total = mxq::lanes_of(cache, B, M, prompt);
     const mxq::KvRows in = {(const uint16_t *)K_bf16, (const uint16_t *)V_bf16, k_stride, v_stride};
-    const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
-    return mxq::kv_launch(cache->head_dim == 128 ? (prompt ? mxq::kv_append_kernel<128, mxq::kPromptRows> : mxq::kv_append_kernel<128, 1>)
-                                                 : (prompt ? mxq::kv_append_kernel<64, mxq::kPromptRows> : mxq::kv_append_kernel<64, 1>),
-                          grid, mxq::kKvThreads, 0,
-                          (cudaStream_t)stream, mxq::kv_view(cache, layer), s, in, total);
+    const mxq::KvView c = mxq::kv_view(cache, layer);
+    if (mxq::prompt_rows(cache, B, M)) {
+        const uint32_t groups = (uint32_t)(cache->kv_heads + mxq::kHeadsPerLane - 1) / mxq::kHeadsPerLane;
+        const uint32_t total = (uint32_t)B * (uint32_t)M * groups * (uint32_t)(cache->head_dim / 32);
+        const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
+        if (cache->head_dim == 128) mxq::kv_append_prompt_kernel<128><<<grid, mxq::kKvThreads, 0, (cudaStream_t)stream>>>(c, s, in, total);
+        else mxq::kv_append_prompt_kernel<64><<<grid, mxq::kKvThreads, 0, (cudaStream_t)stream>>>(c, s, in, total);
+        return mxq::launch_status();
+    }
+    const uint32_t total = mxq::lanes_of(cache, B, M, false);
+    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_append_kernel<128> : mxq::kv_append_kernel<64>,
+                          dim3((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2), mxq::kKvThreads, 0, (cudaStream_t)stream, c, s, in, total);
 }
 
 int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16, int B, int M, const int32_t *tables, int W,
