@@ -117,8 +117,7 @@ __global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs 
 }
 
 // The same for prompts, where the arithmetic decides: one lane per MX block (no exchange for the maximum, every scale computed
-// once), four heads of a token row per lane (one lookup of its place).  The words land with 4- and 2-byte stores that the L2
-// gathers.  Launched without overlap, so that the lanes of a row may share its sectors through L1.
+// once), four heads of a token row per lane (one lookup of its place); the words change lanes before they are stored.  Launched without overlap, so that the lanes of a row may share its sectors through L1.
 // grid.x covers (sequence, row, group of kHeadsPerLane heads, block); grid.y: 0 = K, 1 = V
 constexpr int kHeadsPerLane = 4;
 template <int D>
@@ -132,32 +131,56 @@ __global__ void __launch_bounds__(kKvThreads) kv_append_prompt_kernel(KvView c, 
     const int head0 = (int)(u - row * groups) * kHeadsPerLane, b = (int)(row / (uint32_t)s.m), i = (int)(row - (uint32_t)b * (uint32_t)s.m);
     const int rows = s.nrows(b);
     if (i >= rows) return;
-    const RowPlace at = row_place<D>(c, s, b, s.len(b) - rows + i, head0);
-    if (at.tile == nullptr) return;
     const int64_t stride = value ? in.v_stride : in.k_stride;
     const uint16_t *base = value ? in.v : in.k, *src = base + (int64_t)row * stride + (int64_t)head0 * D + 32 * j;
     const int heads = min(kHeadsPerLane, c.heads - head0);
-#pragma unroll 2
-    for (int h = 0; h < heads; ++h) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(MXQ_AT(src + h * D, 64, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
-        uint4 x[4];
+    const uint32_t lanes = ((1u << kNb) - 1) << (threadIdx.x & 31 & ~(kNb - 1));      // the row's lanes: they leave together
+    uint4 x[kHeadsPerLane][4];          // all on their way while the row's place is looked up
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] = __ldg(p + q);
-        const uint32_t top = __vmaxu2(__vmaxu2(chunk_max2(x[0]), chunk_max2(x[1])), __vmaxu2(chunk_max2(x[2]), chunk_max2(x[3])));
+    for (int h = 0; h < kHeadsPerLane; ++h) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(MXQ_AT(src + (h < heads ? h : 0) * D, 64, base, (((int64_t)s.B * s.m - 1) * stride + (int64_t)c.heads * D) * 2));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[h][q] = __ldg(p + q);
+    }
+    const RowPlace at = row_place<D>(c, s, b, s.len(b) - rows + i, head0);
+    if (at.tile == nullptr) return;
+#pragma unroll
+    for (int h = 0; h < kHeadsPerLane; ++h) {
+        if (h >= heads) break;
+        const uint32_t top = __vmaxu2(__vmaxu2(chunk_max2(x[h][0]), chunk_max2(x[h][1])), __vmaxu2(chunk_max2(x[h][2]), chunk_max2(x[h][3])));
         const uint32_t byte = scale_byte(max(top & 0xFFFFu, top >> 16));
         const float inv = __uint_as_float((254u - byte) << 23);
-        uint8_t *tile = at.tile + h * T::kBytes;
+        uint32_t w[4];       // words 0..3 of block j; then what this lane stores: 16 bytes of the row, from every block
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t w = byte == 0xFFu ? 0u : cast_chunk(x[q], inv);
-            if (!value) {
-                *reinterpret_cast<uint32_t *>(MXQ_AT(tile + at.slot * T::kRow + q * 4 * kNb + 4 * j, 4, c.pool, c.pool_bytes)) = w;
+        for (int q = 0; q < 4; ++q) w[q] = byte == 0xFFu ? 0u : cast_chunk(x[h][q], inv);
+        if constexpr (kNb == 4) {          // transposed over the quad: lane c gets word c of every block
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                const bool upper = (j & o) != 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (q & o) continue;
+                    const uint32_t got = __shfl_xor_sync(lanes, upper ? w[q] : w[q + o], o);
+                    if (upper) w[q] = got;
+                    else w[q + o] = got;
+                }
+            }
+        } else {                           // over two lanes: lane c gets words 2c and 2c + 1 of both blocks
+            const bool upper = j != 0;
+            const uint32_t got0 = __shfl_xor_sync(lanes, upper ? w[0] : w[2], 1), got1 = __shfl_xor_sync(lanes, upper ? w[1] : w[3], 1);
+            const uint32_t a0 = upper ? got0 : w[0], b0 = upper ? w[2] : got0, a1 = upper ? got1 : w[1], b1 = upper ? w[3] : got1;
+            w[0] = a0, w[1] = b0, w[2] = a1, w[3] = b1;
+        }
+        if (value) {                       // V: the halfwords of a chunk's words, low ones first
+            const uint32_t v0 = w[0], v1 = w[1], v2 = w[2], v3 = w[3];
+            if constexpr (kNb == 4) {
+                w[0] = __byte_perm(v0, v1, 0x5410), w[1] = __byte_perm(v2, v3, 0x5410), w[2] = __byte_perm(v0, v1, 0x7632), w[3] = __byte_perm(v2, v3, 0x7632);
             } else {
-                uint8_t *v = tile + T::kV + at.slot * T::kRow + 2 * q * 2 * kNb + 2 * j;
-                *reinterpret_cast<uint16_t *>(MXQ_AT(v, 2, c.pool, c.pool_bytes)) = (uint16_t)w;
-                *reinterpret_cast<uint16_t *>(MXQ_AT(v + 2 * kNb, 2, c.pool, c.pool_bytes)) = (uint16_t)(w >> 16);
+                w[0] = __byte_perm(v0, v1, 0x5410), w[1] = __byte_perm(v0, v1, 0x7632), w[2] = __byte_perm(v2, v3, 0x5410), w[3] = __byte_perm(v2, v3, 0x7632);
             }
         }
+        uint8_t *tile = at.tile + h * T::kBytes;
+        *reinterpret_cast<uint4 *>(MXQ_AT(tile + (value ? T::kV : 0) + at.slot * T::kRow + 16 * j, 16, c.pool, c.pool_bytes)) = make_uint4(w[0], w[1], w[2], w[3]);
         *MXQ_AT(tile + (value ? T::vs(at.slot, (int)j) : T::kKs + at.slot * kNb + (int)j), 1, c.pool, c.pool_bytes) = (uint8_t)byte;
     }
 }

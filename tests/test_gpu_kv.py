@@ -105,6 +105,30 @@ def test_append_writes_the_cast_and_nothing_else(lens, m, rows, d, h, page, laye
                     assert (got_b[r[b]:] == 0).all()
 
 
+@pytest.mark.parametrize("d,h,lens,rows", [(128, 32, [4900, 60], [4800, 37]), (64, 33, [4700], None)])
+def test_append_of_a_prompt(d, h, lens, rows):
+    """Large enough for the prompt kernel; heads that do not fill its groups; rows that are not there; slices of a fused tensor."""
+    s = Setup(5, lens, d, h, 64, layers=2)
+    m = 4800 if rows else 4700
+    fused = torch.from_numpy(s.rng.standard_normal((len(lens), m, (2 * h + 1) * d)).astype(np.float32)).to(torch.bfloat16)
+    fused[0, 7, 5] = float("inf")
+    fused[0, 8] = 0
+    g = fused.cuda()
+    k, v = (x[..., d:(h + 1) * d].unflatten(-1, (h, d)) for x in (fused, g)), (x[..., (h + 1) * d:].unflatten(-1, (h, d)) for x in (fused, g))
+    (k, gk), (v, gv) = tuple(k), tuple(v)
+    r = rows or [m]
+    mxq.mxq_kv_append(s.cache, 1, gk, gv, s.t_tables, s.t_lens, rows=None if rows is None else i32(rows))
+    kv_plain.append(s.host, 1, bits_of(k.contiguous()), bits_of(v.contiguous()), s.tables, s.lens, r)
+    s.check_pool()
+    rk, rv = mxq.mxq_kv_read(s.cache, 1, s.t_tables, s.t_lens, m, rows=None if rows is None else i32(rows))
+    for b in range(len(lens)):
+        for head in (0, 1, h // 2, h - 1):
+            for which, got in ((0, rk), (1, rv)):
+                want, _ = s.host.values(which, 1, s.tables[b], lens[b], head)
+                x = got[b, :, head].float().cpu().numpy().astype(np.float64)
+                assert np.array_equal(x[:r[b]], want[lens[b] - r[b]:], equal_nan=True) and (x[r[b]:] == 0).all()
+
+
 def test_append_of_special_values():
     s = Setup(2, [64], 128, 2, 64)
     k, v = s.random_rows(64)
