@@ -53,9 +53,11 @@ struct KvQuery {
 
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;                  // units in a warp's ring
-// The work is cut into items of a share of one CTA's part: a sixth, so that CTAs that meet cheaper tiles take more of them, but not
-// below kAttItemUnits units (an item costs about two units of time by itself) unless a CTA would get less than two items.
-constexpr int kAttItemsPerCta = 6, kAttItemUnits = 32;
+// The work is cut into items that CTAs draw in turn.  An item costs about two units of time by itself, and the last ones leave CTAs idle for up to
+// an item's time; tiles differ in cost.  So with kTwoSizes units or more per CTA, three quarters of every segment go into items of four tenths
+// of a CTA's share, drawn first, the rest into items of a tenth; below that all items are of half a CTA's share, at most kItemUnits units.
+constexpr uint32_t kTwoSizes = 128, kItemUnits = 32, kSmallUnits = 16, kBigSmalls = 4;
+
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
 constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
@@ -71,16 +73,15 @@ constexpr int kAttRows = 8 * NT;
 template <int NT>
 constexpr int kAttTiles = NT == 1 ? 2 : 1;     // tiles a warp takes at a time (a unit): with few rows the checks and the ring's upkeep
                                                // cost as much as a product, and two tiles share them
-constexpr int kAttRegisterQ = 2;               // up to this NT the query fragments stay in registers
 
 template <int D, int NT>
-constexpr int kAttCtasPerSm = NT == 1 ? (D == 128 ? 3 : 4) : NT == 2 ? (D == 128 ? 2 : 3) : 2;
+constexpr int kAttCtasPerSm = NT == 1 ? (D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
 template <int D, int NT>
 constexpr size_t kAttSlotFloats = (size_t)kAttRows<NT> * (D + 2);
 template <int D, int NT>
 constexpr uint32_t kAttMaxParts = (uint32_t)((kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes - kAttThreads * 16) / (kAttRows<NT> * 8));   // parts of a segment
 template <int D, int NT>
-constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes + (NT > kAttRegisterQ ? (size_t)(D / 32) * NT * 32 * 16 : 0);
+constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes;
 
 // ---- fragments ------------------------------------------------------------------------------------------------------------
 
@@ -368,8 +369,8 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     using T = KvTile<D>;
     constexpr int kNb = T::kNb;
     extern __shared__ __align__(128) uint8_t att_smem_raw[];
-    __shared__ uint64_t sh_scan[kAttWarps];
-    __shared__ int sh_item[8];
+    __shared__ uint64_t sh_scan[kAttWarps][2];
+    __shared__ int sh_item[10];
     __shared__ uint32_t sh_next;
     __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
     __shared__ int sh_last;
@@ -377,10 +378,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, tig = lane & 3;
     constexpr int kU = kAttTiles<NT>, kUnitTokens = kU * kTileTokens, kUnitBytes = kU * T::kBytes;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * kUnitBytes;
-    uint4 *const sh_q = reinterpret_cast<uint4 *>(att_smem_raw + kAttWarps * kAttStages * kUnitBytes);
-    float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][8][D + 4], between segments
+    float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][row][D + 4], between items
     constexpr int kMergeRow = D + 4;
-    static_assert(kAttWarps * (NT > 1 ? 16 : 8) * kMergeRow * 4 <= kAttWarps * kAttStages * kUnitBytes, "the merge buffer lies over the rings");
+    static_assert(kAttWarps * kAttRows<NT> * kMergeRow * 4 <= kAttWarps * kAttStages * kUnitBytes, "the merge buffer lies over the rings");
 
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
     uint32_t issued = 0;      // units the warp has requested before this segment: ring slots and phases run on
@@ -392,18 +392,25 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     pdl_wait();
     asm volatile("fence.proxy.async;" ::: "memory");      // tiles may have been written by the kernel before, with ordinary stores
 
-    // ---- the items: every segment (sequence, kv head, row tile) is cut into parts of at most `item_units` units ----
+    // ---- the items: parts of segments (sequence, kv head, row tile) ----
     auto shape_of = [&](int len, int rows, uint32_t &n, uint32_t &tiles) {      // units of a segment, segments per kv head
         n = max(1u, ((uint32_t)len + kUnitTokens - 1) / kUnitTokens);
         tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
-    uint32_t item_units = 0;
-    auto cut_of = [&](uint32_t n) {                // units of an item of a segment of n units: its parts must fit the join's table
-        return max(item_units, (n + kAttWarps * kAttMaxParts<D, NT> - 1) / (kAttWarps * kAttMaxParts<D, NT>) * kAttWarps);
+    uint32_t small = 0, big = 0;                   // units of an item; 0: no big ones
+    struct Cut {
+        uint32_t small, bigs, parts;               // units of its small items, number of its big ones, of all its items
+    };
+    auto cut_of = [&](uint32_t n) {                // of a segment of n units (its parts must fit the join's table)
+        Cut k;
+        k.small = max(small, (n + kAttWarps * kAttMaxParts<D, NT> - 1) / (kAttWarps * kAttMaxParts<D, NT>) * kAttWarps);
+        k.bigs = big == 0 ? 0u : (n - n / 4) / big;
+        k.parts = k.bigs + max(1u, (n - k.bigs * big + k.small - 1) / k.small);
+        return k;
     };
     const int each = (s.B + kAttThreads - 1) / kAttThreads, b_first = tid * each, b_last = min(s.B, b_first + each);
     int len0 = 0, rows0 = 0;                       // the first of this thread's sequences
-    uint32_t item_lo, item_hi, part_lo, items;
+    uint32_t big_lo, big_hi, small_lo, small_hi, slot_lo, bigs, items;      // this thread's items and slots; all big items, all items
     {
         uint64_t units = 0;
         for (int i = b_first; i < b_last; ++i) {
@@ -415,33 +422,45 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
-        if (lane == 0) sh_scan[warp] = units;
+        if (lane == 0) sh_scan[warp][0] = units;
         __syncthreads();
         units = 0;
-        for (int w = 0; w < kAttWarps; ++w) units += sh_scan[w];
-        const uint64_t want = max(units / (kAttItemsPerCta * gridDim.x), min((uint64_t)kAttItemUnits, units / (2 * gridDim.x))) + 1;
-        item_units = (uint32_t)((want + kAttWarps - 1) / kAttWarps) * kAttWarps;
-        uint64_t mine = 0;                         // items, and above them the items of segments that are cut
+        for (int w = 0; w < kAttWarps; ++w) units += sh_scan[w][0];
+        const uint32_t share = (uint32_t)min(units / gridDim.x, (uint64_t)1 << 30);      // of a CTA
+        if (share >= kTwoSizes) {
+            small = (max(kSmallUnits, share / 10) + kAttWarps - 1) / kAttWarps * kAttWarps;
+            big = kBigSmalls * small;
+        } else {
+            small = min(kItemUnits, share / 2 + kAttWarps) / kAttWarps * kAttWarps;
+        }
+        uint64_t mine[2] = {0, 0};                 // big items and small ones; slots (items of segments that are cut)
         for (int i = b_first; i < b_last; ++i) {
             uint32_t n, tiles;
             shape_of(i == b_first ? len0 : s.len(i), i == b_first ? rows0 : s.nrows(i), n, tiles);
-            const uint32_t cut = cut_of(n), parts = (n + cut - 1) / cut, k = parts * tiles * (uint32_t)c.heads;
-            mine += k | (uint64_t)(parts > 1 ? k : 0) << 32;
+            const Cut k = cut_of(n);
+            const uint32_t segs = tiles * (uint32_t)c.heads;
+            mine[0] += (uint64_t)k.bigs * segs | (uint64_t)(k.parts - k.bigs) * segs << 32;
+            mine[1] += k.parts > 1 ? (uint64_t)k.parts * segs : 0;
         }
-        uint64_t upto = mine, total = 0;
+        uint64_t upto[2] = {mine[0], mine[1]}, total = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t up = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += up;
-        }
+        for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint64_t before = __shfl_up_sync(0xffffffffu, upto[e], o);
+                if (lane >= o) upto[e] += before;
+            }
         __syncthreads();
-        if (lane == 31) sh_scan[warp] = upto;
+        if (lane == 31) sh_scan[warp][0] = upto[0], sh_scan[warp][1] = upto[1];
         __syncthreads();
         for (int w = 0; w < kAttWarps; ++w) {
-            if (w < warp) upto += sh_scan[w];
-            total += sh_scan[w];
+            if (w < warp) upto[0] += sh_scan[w][0], upto[1] += sh_scan[w][1];
+            total += sh_scan[w][0];
         }
-        item_hi = (uint32_t)upto, item_lo = (uint32_t)(upto - mine), part_lo = (uint32_t)((upto - mine) >> 32), items = (uint32_t)total;
+        bigs = (uint32_t)total, items = bigs + (uint32_t)(total >> 32);
+        big_hi = (uint32_t)upto[0], big_lo = big_hi - (uint32_t)mine[0];
+        small_hi = bigs + (uint32_t)(upto[0] >> 32), small_lo = small_hi - (uint32_t)(mine[0] >> 32);
+        slot_lo = (uint32_t)(upto[1] - mine[1]);
     }
 
     // Items are taken in turn as CTAs become free; which CTA computes an item does not matter to its result.
@@ -452,23 +471,29 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             next = gridDim.x + taken;
             if (taken == items - 1) *a.counter = 0;       // one draw per item: this was the last
         }
-        if (item_lo <= item && item < item_hi) {
-            uint32_t at = item_lo, part = part_lo, n, tiles, cut, parts;
+        const bool is_big = item < bigs;
+        if (is_big ? big_lo <= item && item < big_hi : small_lo <= item && item < small_hi) {
+            uint32_t at = is_big ? big_lo : small_lo, slot = slot_lo, n, tiles;
+            Cut k;
             int i = b_first, len = len0, rows = rows0;
             for (;;) {
                 shape_of(len, rows, n, tiles);
-                cut = cut_of(n), parts = (n + cut - 1) / cut;
-                const uint32_t k = parts * tiles * (uint32_t)c.heads;
-                if (at + k > item) break;
-                at += k, part += parts > 1 ? k : 0, ++i;
+                k = cut_of(n);
+                const uint32_t segs = tiles * (uint32_t)c.heads, count = (is_big ? k.bigs : k.parts - k.bigs) * segs;
+                if (at + count > item) break;
+                at += count, slot += k.parts > 1 ? k.parts * segs : 0, ++i;
                 len = s.len(i), rows = s.nrows(i);
             }
-            sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)(item - at), sh_item[4] = (int)part, sh_item[5] = (int)parts, sh_item[6] = (int)tiles, sh_item[7] = (int)cut;
+            // the segment, the item's place among its parts, its units
+            const uint32_t of = is_big ? k.bigs : k.parts - k.bigs, seg = (item - at) / of, p = item - at - seg * of;
+            sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)seg, sh_item[4] = (int)tiles, sh_item[5] = (int)k.parts;
+            sh_item[6] = (int)(is_big ? p : k.bigs + p), sh_item[7] = (int)(slot + seg * k.parts);
+            sh_item[8] = (int)(is_big ? p * big : k.bigs * big + p * k.small), sh_item[9] = (int)(is_big ? big : k.small);
         }
         __syncthreads();
         const int b = sh_item[0], len = sh_item[1], rows = sh_item[2];
-        const uint32_t parts = (uint32_t)sh_item[5], tiles = (uint32_t)sh_item[6], cut = (uint32_t)sh_item[7], seg = (uint32_t)sh_item[3] / parts, part = (uint32_t)sh_item[3] - seg * parts;
-        const uint32_t slot0 = (uint32_t)sh_item[4] + seg * parts;      // slot of the segment's first part, if it is cut
+        const uint32_t seg = (uint32_t)sh_item[3], tiles = (uint32_t)sh_item[4], parts = (uint32_t)sh_item[5], part = (uint32_t)sh_item[6];
+        const uint32_t slot0 = (uint32_t)sh_item[7], unit0 = (uint32_t)sh_item[8], units = (uint32_t)sh_item[9];      // slot of the segment's first part, if it is cut
         const uint32_t head = tiles == 1 ? seg : seg / tiles, row_tile = tiles == 1 ? 0u : seg - head * tiles;
         Segment sg;
         sg.b = b, sg.head = (int)head, sg.r0 = (int)row_tile * kAttRows<NT>;
@@ -489,7 +514,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         }
 
         // ---- the warp's units: number k is the segment's unit first_unit + k * kAttWarps ----
-        const int last_unit = (int)min(((uint32_t)len + kUnitTokens - 1) / kUnitTokens, (part + 1) * cut), first_unit = (int)(part * cut) + warp;
+        const int last_unit = (int)min(((uint32_t)len + kUnitTokens - 1) / kUnitTokens, unit0 + units), first_unit = (int)unit0 + warp;
         const int count = nrows > 0 && first_unit < last_unit ? (last_unit - first_unit + kAttWarps - 1) / kAttWarps : 0;
         const uint8_t *source = nullptr;   // lane i: where tile i of the next 32 tiles of the warp's lies (nullptr: nowhere)
         uint32_t exist = 0, there = 0;     // bit i: that tile exists; the units requested so far, kU bits each, the newest lowest
@@ -518,7 +543,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         for (int k = 0; k < kAttStages; ++k) issue(k);
 
         // ---- query fragments: elements 32 j + 8 tig .. + 7 of row g, normalised by a power of two ----
-        uint4 qf[NT > kAttRegisterQ ? 1 : NT][kNb];
+        uint4 qf[NT][kNb];
         float factor[NT][2];               // score -> log2 domain, for the lane's two columns
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -539,19 +564,13 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 uint32_t out[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) out[i] = pack_half2(__uint_as_float(in[i] << 16) * mul, __uint_as_float(in[i] & 0xFFFF0000u) * mul);
-                const uint4 f = make_uint4(out[0], out[1], out[2], out[3]);
-                if constexpr (NT > kAttRegisterQ) {
-                    if (warp == 0) sh_q[(j * NT + nt) * 32 + lane] = f;
-                } else {
-                    qf[nt][j] = f;
-                }
+                qf[nt][j] = make_uint4(out[0], out[1], out[2], out[3]);
             }
 #pragma unroll
             for (int e2 = 0; e2 < 2; ++e2) {
                 factor[nt][e2] = a.scale_log2 * __shfl_sync(0xffffffffu, back, (2 * tig + e2) * 4);
             }
         }
-        if constexpr (NT > kAttRegisterQ) __syncthreads();
 
         WarpState<D, NT> w;
         w.ref = w.ref_max = 0;
@@ -603,9 +622,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                             const float c0 = scale_factor(s0, j), c1 = scale_factor(s1, j);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                uint4 q;
-                                if constexpr (NT > kAttRegisterQ) q = sh_q[(j * NT + nt) * 32 + lane];
-                                else q = qf[nt][j];
+                                const uint4 &q = qf[nt][j];
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
                                 mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
                                 mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
@@ -875,18 +892,15 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         auto store_lse = [&](int r, float m, float l) {
             if (a.lse != nullptr) *MXQ_AT(a.lse + out_row(r), 4, a.lse, o_bytes / D * 2) = m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f;
         };
-        constexpr int kAtOnce = NT > 1 ? 2 : 1;      // column blocks whose parts fit the ring together
-#pragma unroll
-        for (int first = 0; first < NT; first += kAtOnce) {
-            if (8 * first >= nrows) break;
+        {
             __syncthreads();
 #pragma unroll
-            for (int nt = first; nt < first + kAtOnce; ++nt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     if (8 * nt + 2 * tig + e >= nrows) break;
                     const float inv = w.l[nt][e] == 0.f ? 0.f : 1.f / w.l[nt][e];
-                    float *dst = merge + (warp * 8 * kAtOnce + 8 * (nt - first) + 2 * tig + e) * kMergeRow + 4 * g;
+                    float *dst = merge + (warp * kAttRows<NT> + 8 * nt + 2 * tig + e) * kMergeRow + 4 * g;
 #pragma unroll
                     for (int j = 0; j < kNb; ++j) {
                         float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
@@ -896,7 +910,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     }
                 }
             __syncthreads();
-            for (int r = 8 * first + warp; r < min(nrows, 8 * (first + kAtOnce)); r += kAttWarps) {      // a warp per row
+            for (int r = warp; r < nrows; r += kAttWarps) {      // a warp per row
                 float m = -INFINITY, l = 0.f;
 #pragma unroll
                 for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][r][0]);
@@ -906,7 +920,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     const float li = sh_ml[i][r][1], f = li == 0.f ? 0.f : li * exp2_fast(sh_ml[i][r][0] - m);
                     l += f;
                     if (4 * lane < D && li != 0.f) {
-                        const float4 x = *reinterpret_cast<const float4 *>(merge + (i * 8 * kAtOnce + r - 8 * first) * kMergeRow + 4 * lane);
+                        const float4 x = *reinterpret_cast<const float4 *>(merge + (i * kAttRows<NT> + r) * kMergeRow + 4 * lane);
                         v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
                     }
                 }
@@ -1009,7 +1023,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             }
         if (tid == 0) sh_next = next;
         fence_async_proxy();  // (the rings held ordinary stores; bulk copies come next)
-        __syncthreads();      // the rings, sh_ml and sh_q are free again
+        __syncthreads();      // the rings and sh_ml are free again
         item = sh_next;
     }
 }
@@ -1027,17 +1041,15 @@ int kv_take_status(uint32_t *out) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
 
-// Column blocks per tile: as many as the rows of one kv head fill, so that K and V are decoded once for all of them; 32 rows
-// are what a lane's registers hold.
-static int att_column_blocks(int M, int group) {
-    const int64_t rows = (int64_t)M * group;
-    return rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-}
+// Column blocks per row tile: two from nine rows on.  (Four would decode K and V half as often, but their accumulators leave only
+// two warps per scheduler: 8 x 8 rows over 4-fold grouped heads, 16384 tokens: 251 us with up to four blocks, 180 with two, 206 with one.)
+static int att_column_blocks(int M, int group) { return (int64_t)M * group <= 8 ? 1 : 2; }
+
 template <int D, int NT>
 static int att_grid() { return sm_count() * kAttCtasPerSm<D, NT>; }
 
-// Workspace: 16 bytes with the counter, a ticket per segment, slots for the parts of cut segments (a cut segment of n units has at
-// most 2 n / item_units of them, and all segments together kAttItemsPerCta * grid * item_units units).
+// Workspace: 16 bytes with the counter, a ticket per segment, slots for the parts of cut segments.  No part but a segment's last is smaller
+// than a small item, so a cut segment of n units has at most 2 n / small of them, and a small item is at least a tenth of a CTA's share.
 struct AttLayout {
     size_t tickets, partials, bytes;
     uint32_t slots;
@@ -1048,7 +1060,7 @@ static AttLayout att_layout(int B, int heads, int max_tiles) {
     l.tickets = 16;
     l.partials = l.tickets + ((size_t)B * heads * max_tiles * 4 + 255) / 256 * 256;
     if (l.partials < 4096) l.partials = 4096;
-    l.slots = 2u * kAttItemsPerCta * (uint32_t)att_grid<D, NT>();
+    l.slots = 24u * (uint32_t)att_grid<D, NT>();
     l.bytes = l.partials + (size_t)l.slots * kAttSlotFloats<D, NT> * 4;
     return l;
 }
@@ -1080,12 +1092,10 @@ static int att_launch(const KvView &c, const KvSeqs &s, KvQuery a, void *workspa
 template <class F>
 static auto att_pick(int head_dim, int M, int group, F f) {
     using std::integral_constant;
-    const int nt = att_column_blocks(M, group);
+    const bool one = att_column_blocks(M, group) == 1;
     if (head_dim == 128)
-        return nt == 1 ? f(integral_constant<int, 128>(), integral_constant<int, 1>()) : nt == 2 ? f(integral_constant<int, 128>(), integral_constant<int, 2>())
-                                                                                                : f(integral_constant<int, 128>(), integral_constant<int, 4>());
-    return nt == 1 ? f(integral_constant<int, 64>(), integral_constant<int, 1>()) : nt == 2 ? f(integral_constant<int, 64>(), integral_constant<int, 2>())
-                                                                                           : f(integral_constant<int, 64>(), integral_constant<int, 4>());
+        return one ? f(integral_constant<int, 128>(), integral_constant<int, 1>()) : f(integral_constant<int, 128>(), integral_constant<int, 2>());
+    return one ? f(integral_constant<int, 64>(), integral_constant<int, 1>()) : f(integral_constant<int, 64>(), integral_constant<int, 2>());
 }
 
 }  // namespace mxq
