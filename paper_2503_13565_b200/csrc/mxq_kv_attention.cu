@@ -56,7 +56,7 @@ constexpr int kAttStages = 2;                  // units in a warp's ring
 // The work is cut into items that CTAs draw in turn.  An item costs about two units of time by itself, and the last ones leave CTAs idle for up to
 // an item's time; tiles differ in cost.  So with kTwoSizes units or more per CTA, three quarters of every segment go into items of four tenths
 // of a CTA's share, drawn first, the rest into items of a tenth; below that all items are of half a CTA's share, at most kItemUnits units.
-constexpr uint32_t kTwoSizes = 128, kItemUnits = 32, kSmallUnits = 16, kBigSmalls = 4;
+constexpr uint32_t kTwoSizes = 48, kItemUnits = 32, kSmallUnits = 12, kBigSmalls = 4;
 
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
@@ -207,6 +207,19 @@ struct Segment {
 // A warp's state of a segment.  Column c of column block nt is flattened row r0 + 8 * nt + c; a lane (g = lane / 4, tig = lane % 4) holds
 // columns 2 * tig and 2 * tig + 1.
 __device__ unsigned int g_kv_status = 0;   // sticky: bit 0 a requested tile never arrived
+
+struct Cut {
+    uint32_t small, bigs, parts;  // of a segment: units of its small items, number of its big ones, of all its items
+};
+struct Owner {                    // the items that a thread's sequences own, and the first of these sequences
+    uint32_t big_lo, big_count, small_lo, small_count, slot_lo, tiles;
+    Cut cut;
+    int len, rows;
+};
+struct Part {                     // a segment whose part has been delivered: its rows, how many parts it has, the first one's slot
+    int b, head, r0, nrows;
+    uint32_t parts, slot0;
+};
 
 template <int D, int NT>
 struct WarpState {
@@ -371,6 +384,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     extern __shared__ __align__(128) uint8_t att_smem_raw[];
     __shared__ uint64_t sh_scan[kAttWarps][2];
     __shared__ int sh_item[10];
+    __shared__ Owner sh_owner[kAttThreads];
     __shared__ uint32_t sh_next;
     __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
     __shared__ int sh_last;
@@ -398,9 +412,6 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
     uint32_t small = 0, big = 0;                   // units of an item; 0: no big ones
-    struct Cut {
-        uint32_t small, bigs, parts;               // units of its small items, number of its big ones, of all its items
-    };
     auto cut_of = [&](uint32_t n) {                // of a segment of n units (its parts must fit the join's table)
         Cut k;
         k.small = max(small, (n + kAttWarps * kAttMaxParts<D, NT> - 1) / (kAttWarps * kAttMaxParts<D, NT>) * kAttWarps);
@@ -409,9 +420,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         return k;
     };
     const int each = (s.B + kAttThreads - 1) / kAttThreads, b_first = tid * each, b_last = min(s.B, b_first + each);
-    int len0 = 0, rows0 = 0;                       // the first of this thread's sequences
-    uint32_t big_lo, big_hi, small_lo, small_hi, slot_lo, bigs, items;      // this thread's items and slots; all big items, all items
+    uint32_t bigs, items;                          // all big items, all items
     {
+        int len0 = 0, rows0 = 0;                   // the first of this thread's sequences
         uint64_t units = 0;
         for (int i = b_first; i < b_last; ++i) {
             const int len = s.len(i), rows = s.nrows(i);
@@ -458,39 +469,63 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             total += sh_scan[w][0];
         }
         bigs = (uint32_t)total, items = bigs + (uint32_t)(total >> 32);
-        big_hi = (uint32_t)upto[0], big_lo = big_hi - (uint32_t)mine[0];
-        small_hi = bigs + (uint32_t)(upto[0] >> 32), small_lo = small_hi - (uint32_t)(mine[0] >> 32);
-        slot_lo = (uint32_t)(upto[1] - mine[1]);
+        uint32_t n, tiles;
+        shape_of(len0, rows0, n, tiles);
+        Owner &o = sh_owner[tid];
+        o.cut = cut_of(n), o.tiles = tiles, o.len = len0, o.rows = rows0;
+        o.big_lo = (uint32_t)(upto[0] - mine[0]), o.big_count = (uint32_t)mine[0];
+        o.small_lo = bigs + (uint32_t)((upto[0] - mine[0]) >> 32), o.small_count = (uint32_t)(mine[0] >> 32);
+        o.slot_lo = (uint32_t)(upto[1] - mine[1]);
     }
 
-    // Items are taken in turn as CTAs become free; which CTA computes an item does not matter to its result.
-    for (uint32_t item = blockIdx.x; item < items;) {
-        uint32_t next = items;
-        if (tid == 0 && items > gridDim.x) {
-            const uint32_t taken = atomicAdd(MXQ_AT(a.counter, 4, a.counter, 4), 1u);
-            next = gridDim.x + taken;
-            if (taken == items - 1) *a.counter = 0;       // one draw per item: this was the last
-        }
+    // Items are taken in turn as CTAs become free; which CTA computes an item does not matter to its result.  Whether a delivered part
+    // was its segment's last is asked one item later, when the answer has arrived.
+    Part pending = {};
+    pending.parts = 0;
+    unsigned before = 0;                           // thread 0: parts of the pending segment delivered before this CTA's
+    for (uint32_t item = blockIdx.x;;) {
+        const bool have = item < items, drawn = have && items > gridDim.x;
+        if (!have && pending.parts == 0) break;
+        unsigned taken = 0;
+        if (drawn && tid == 0) taken = atomicAdd(MXQ_AT(a.counter, 4, a.counter, 4), 1u);
         const bool is_big = item < bigs;
-        if (is_big ? big_lo <= item && item < big_hi : small_lo <= item && item < small_hi) {
-            uint32_t at = is_big ? big_lo : small_lo, slot = slot_lo, n, tiles;
-            Cut k;
-            int i = b_first, len = len0, rows = rows0;
+        const Owner &mine = sh_owner[tid];
+        const uint32_t lo = is_big ? mine.big_lo : mine.small_lo;
+        if (have && item - lo < (is_big ? mine.big_count : mine.small_count)) {
+            uint32_t at = lo, slot = mine.slot_lo, tiles = mine.tiles;
+            Cut k = mine.cut;
+            int i = b_first, len = mine.len, rows = mine.rows;
             for (;;) {
-                shape_of(len, rows, n, tiles);
-                k = cut_of(n);
                 const uint32_t segs = tiles * (uint32_t)c.heads, count = (is_big ? k.bigs : k.parts - k.bigs) * segs;
-                if (at + count > item) break;
+                if (item - at < count) break;
                 at += count, slot += k.parts > 1 ? k.parts * segs : 0, ++i;
                 len = s.len(i), rows = s.nrows(i);
+                uint32_t n;
+                shape_of(len, rows, n, tiles);
+                k = cut_of(n);
             }
             // the segment, the item's place among its parts, its units
-            const uint32_t of = is_big ? k.bigs : k.parts - k.bigs, seg = (item - at) / of, p = item - at - seg * of;
+            const uint32_t of = is_big ? k.bigs : k.parts - k.bigs, seg = of == 1 ? item - at : (item - at) / of, p = item - at - seg * of;
             sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)seg, sh_item[4] = (int)tiles, sh_item[5] = (int)k.parts;
             sh_item[6] = (int)(is_big ? p : k.bigs + p), sh_item[7] = (int)(slot + seg * k.parts);
             sh_item[8] = (int)(is_big ? p * big : k.bigs * big + p * k.small), sh_item[9] = (int)(is_big ? big : k.small);
         }
         __syncthreads();
+        bool whole = true;
+        Part mine_now = {};
+        [[maybe_unused]] const size_t ws_bytes = (size_t)a.slots * kAttSlotFloats<D, NT> * 4, o_bytes = (size_t)s.B * s.m * a.heads * D * 2;
+        // final results of flattened row r of a sequence
+        auto out_row = [&](int b, int head, int r) {
+            const int i = token_row(a, r);
+            return ((int64_t)b * s.m + i) * a.heads + head * a.group + r - i * a.group;
+        };
+        auto store_part = [&](int64_t row, int d, const float4 &v) {
+            *reinterpret_cast<uint2 *>(MXQ_AT(a.o + row * D + d, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
+        };
+        auto store_lse = [&](int64_t row, float m, float l) {
+            if (a.lse != nullptr) *MXQ_AT(a.lse + row, 4, a.lse, o_bytes / D * 2) = m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f;
+        };
+        if (have) {
         const int b = sh_item[0], len = sh_item[1], rows = sh_item[2];
         const uint32_t seg = (uint32_t)sh_item[3], tiles = (uint32_t)sh_item[4], parts = (uint32_t)sh_item[5], part = (uint32_t)sh_item[6];
         const uint32_t slot0 = (uint32_t)sh_item[7], unit0 = (uint32_t)sh_item[8], units = (uint32_t)sh_item[9];      // slot of the segment's first part, if it is cut
@@ -876,22 +911,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
                 if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.over[nt][e] == -INFINITY ? -INFINITY : w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
             }
-        const bool whole = parts == 1;
+        whole = parts == 1;
+        mine_now = {b, sg.head, sg.r0, nrows, parts, slot0};
         float *const slot = a.partials + (size_t)(slot0 + part) * kAttSlotFloats<D, NT>;
-        [[maybe_unused]] const size_t ws_bytes = (size_t)a.slots * kAttSlotFloats<D, NT> * 4;
-
-        // final results of flattened row r of the sequence
-        auto out_row = [&](int r) {
-            const int i = token_row(a, r);
-            return ((int64_t)b * s.m + i) * a.heads + sg.head * a.group + r - i * a.group;
-        };
-        [[maybe_unused]] const size_t o_bytes = (size_t)s.B * s.m * a.heads * D * 2;
-        auto store_part = [&](int r, int d, const float4 &v) {
-            *reinterpret_cast<uint2 *>(MXQ_AT(a.o + out_row(r) * D + d, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
-        };
-        auto store_lse = [&](int r, float m, float l) {
-            if (a.lse != nullptr) *MXQ_AT(a.lse + out_row(r), 4, a.lse, o_bytes / D * 2) = m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f;
-        };
         {
             __syncthreads();
 #pragma unroll
@@ -927,8 +949,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
                 if (whole) {
-                    if (4 * lane < D) store_part(sg.r0 + r, 4 * lane, v);
-                    if (lane == 0) store_lse(sg.r0 + r, m, l);
+                    const int64_t row = out_row(b, sg.head, sg.r0 + r);
+                    if (4 * lane < D) store_part(row, 4 * lane, v);
+                    if (lane == 0) store_lse(row, m, l);
                 } else {
                     if (4 * lane < D) *reinterpret_cast<float4 *>(MXQ_AT(slot + r * D + 4 * lane, 16, a.partials, ws_bytes)) = v;
                     if (lane == 0) *reinterpret_cast<float2 *>(MXQ_AT(slot + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)) = make_float2(m, l);
@@ -936,20 +959,31 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             }
         }
 
-        // ---- join the parts of a cut segment: the CTA that finishes the last one adds them, in order ----
-        bool finish = whole;
-        if (!whole) {
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                unsigned *ticket = MXQ_AT(a.tickets + ((size_t)b * c.heads + head) * a.max_tiles + row_tile, 4, a.tickets, (size_t)s.B * c.heads * a.max_tiles * 4);
-                sh_last = atomicAdd(ticket, 1u) == parts - 1;
-                if (sh_last) *ticket = 0;
+        // rows the sequence does not have
+        if (part == 0 && sg.r0 == 0)
+            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) {
+                const int64_t row = out_row(b, sg.head, r);
+                if (4 * lane < D) store_part(row, 4 * lane, make_float4(0.f, 0.f, 0.f, 0.f));
+                if (lane == 0) store_lse(row, -INFINITY, 0.f);
             }
-            __syncthreads();
+        }   // (have)
+
+        // ---- join the parts of the segment delivered to before: the CTA that brought the last one adds them, in order ----
+        auto ticket_of = [&](const Part &p) {
+            return MXQ_AT(a.tickets + ((size_t)p.b * c.heads + p.head) * a.max_tiles + p.r0 / kAttRows<NT>, 4, a.tickets, (size_t)s.B * c.heads * a.max_tiles * 4);
+        };
+        if (pending.parts != 0 || !whole) {
+            if (tid == 0) {
+                sh_last = pending.parts != 0 && before == pending.parts - 1;
+                if (sh_last) {
+                    *ticket_of(pending) = 0;
+                    __threadfence();
+                }
+            }
+            __syncthreads();          // (and every thread's part of this item's result is stored before the ticket below)
             if (sh_last) {
-                finish = true;
-                __threadfence();
+                const int nrows = pending.nrows;
+                const uint32_t parts = pending.parts, slot0 = pending.slot0;
                 const float *const p0 = a.partials + (size_t)slot0 * kAttSlotFloats<D, NT>;
                 float2 *const table = reinterpret_cast<float2 *>(att_smem_raw);       // [part][row]: maximum and sum, then the part's share
                 float4 *const sums = reinterpret_cast<float4 *>(att_smem_raw + ((size_t)parts * nrows * 8 + 15) / 16 * 16);
@@ -975,7 +1009,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][lane][0]);
 #pragma unroll
                     for (int i = 0; i < kAttWarps; ++i) l += sh_ml[i][lane][1] == 0.f ? 0.f : sh_ml[i][lane][1] * exp2_fast(sh_ml[i][lane][0] - m);
-                    if (warp == 0) store_lse(sg.r0 + lane, m, l);
+                    if (warp == 0) store_lse(out_row(pending.b, pending.head, pending.r0 + lane), m, l);
                 }
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 for (int x0 = 32 * warp; x0 < pairs; x0 += kAttThreads) {
@@ -999,7 +1033,8 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     return v;
                 };
                 if (shares == 1) {
-                    for (int task = tid; task < tasks; task += kAttThreads) store_part(sg.r0 + task / kCols, 4 * (task % kCols), add_parts(task, 0, 1));
+                    for (int task = tid; task < tasks; task += kAttThreads)
+                        store_part(out_row(pending.b, pending.head, pending.r0 + task / kCols), 4 * (task % kCols), add_parts(task, 0, 1));
                 } else {
                     const int task = tid % tasks, share = tid / tasks;
                     if (share < shares) sums[tid] = add_parts(task, share, shares);
@@ -1010,18 +1045,23 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                             const float4 x = sums[i * tasks + task];
                             v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
                         }
-                        store_part(sg.r0 + task / kCols, 4 * (task % kCols), v);
+                        store_part(out_row(pending.b, pending.head, pending.r0 + task / kCols), 4 * (task % kCols), v);
                     }
                 }
             }
         }
-        // rows the sequence does not have
-        if (finish && sg.r0 == 0)
-            for (int r = sg.rows_total + warp; r < s.m * a.group; r += kAttWarps) {
-                if (4 * lane < D) store_part(r, 4 * lane, make_float4(0.f, 0.f, 0.f, 0.f));
-                if (lane == 0) store_lse(r, -INFINITY, 0.f);
+        pending.parts = 0;
+        if (!whole) {
+            pending = mine_now;
+            if (tid == 0) {
+                __threadfence();
+                before = atomicAdd(ticket_of(pending), 1u);
             }
-        if (tid == 0) sh_next = next;
+        }
+        if (tid == 0) {
+            sh_next = drawn ? gridDim.x + taken : items;
+            if (drawn && taken == items - 1) *a.counter = 0;       // one draw per item: this was the last
+        }
         fence_async_proxy();  // (the rings held ordinary stores; bulk copies come next)
         __syncthreads();      // the rings and sh_ml are free again
         item = sh_next;
