@@ -52,11 +52,11 @@ struct KvQuery {
 };
 
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
-constexpr int kAttStages = 2;                  // units in a warp's ring
+constexpr int kAttStages = 2;                  // tiles in a warp's ring
 // The work is cut into items that CTAs draw in turn.  An item costs about two units of time by itself, and the last ones leave CTAs idle for up to
 // an item's time; tiles differ in cost.  So with kTwoSizes units or more per CTA, three quarters of every segment go into items of four tenths
-// of a CTA's share, drawn first, the rest into items of a tenth; below that all items are of half a CTA's share, at most kItemUnits units.
-constexpr uint32_t kTwoSizes = 48, kItemUnits = 32, kSmallUnits = 12, kBigSmalls = 4;
+// of a CTA's share, drawn first, the rest into items of a tenth; below that all items are of half a CTA's share, at most kItemTiles units.
+constexpr uint32_t kTwoSizes = 96, kItemTiles = 48, kSmallTiles = 24, kBigSmalls = 4, kOneRound = 8;
 
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
@@ -70,18 +70,14 @@ constexpr int kScaleDrop = 12;                 // how far ref may fall below its
 // rows of the flattened (token row, head of the group) index per tile of NT column blocks
 template <int NT>
 constexpr int kAttRows = 8 * NT;
-template <int NT>
-constexpr int kAttTiles = NT == 1 ? 2 : 1;     // tiles a warp takes at a time (a unit): with few rows the checks and the ring's upkeep
-                                               // cost as much as a product, and two tiles share them
-
 template <int D, int NT>
 constexpr int kAttCtasPerSm = NT == 1 ? (D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
 template <int D, int NT>
 constexpr size_t kAttSlotFloats = (size_t)kAttRows<NT> * (D + 2);
 template <int D, int NT>
-constexpr uint32_t kAttMaxParts = (uint32_t)((kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes - kAttThreads * 16) / (kAttRows<NT> * 8));   // parts of a segment
+constexpr uint32_t kAttMaxParts = (uint32_t)((kAttWarps * kAttStages * KvTile<D>::kBytes - kAttThreads * 16) / (kAttRows<NT> * 8));   // parts of a segment
 template <int D, int NT>
-constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * kAttTiles<NT> * KvTile<D>::kBytes;
+constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * KvTile<D>::kBytes;
 
 // ---- fragments ------------------------------------------------------------------------------------------------------------
 
@@ -271,11 +267,10 @@ __device__ __forceinline__ void rescale(WarpState<D, NT> &w, const float (&f)[NT
 }
 
 // O += P . V for a whole tile, in FP16.  p[u][n][h]: packed weights of row g of column block n, tokens 16 u + tig + 8 h (low half) and
-// + 4 (high half).  With `two`, deep[..] are the weights too small for p, scaled up by `up`; `down` = 1 / up.  (One body for both: the
-// kernel's loop has to stay in the instruction cache.)
-template <int D, int NT>
+// + 4 (high half).  kTiers == 2: deep[..] are the weights too small for p, scaled up by `up`; `down` = 1 / up.
+template <int D, int NT, int kTiers>
 __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, int g, int tig, const uint32_t (&p)[2][NT][2],
-                                           const uint32_t (&deep)[2][NT][2], bool two, float up, float down) {
+                                           const uint32_t (&deep)[2][NT][2], float up, float down) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb, kW = kNb / 2;   // words of V codes per lane and token
     uint32_t sw[2][kNb];                        // scales: [group][h, block pair] words of (A.j, B.j, A.j+1, B.j+1)
@@ -316,16 +311,15 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
                     mma16816<false>(w.o[2 * j + 1][n], e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
                 }
             };
-            if (two) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (kTiers == 2) {
                     scale4(w.o[2 * j][n], up, up), scale4(w.o[2 * j + 1][n], up, up);
                     product(n, deep);
                     scale4(w.o[2 * j][n], down, down), scale4(w.o[2 * j + 1][n], down, down);
                 }
+                product(n, p);
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) product(n, p);
         }
     }
 }
@@ -390,16 +384,15 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     __shared__ int sh_last;
     __shared__ __align__(8) uint64_t sh_bars[kAttWarps][kAttStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, tig = lane & 3;
-    constexpr int kU = kAttTiles<NT>, kUnitTokens = kU * kTileTokens, kUnitBytes = kU * T::kBytes;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * kUnitBytes;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * T::kBytes;
     float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][row][D + 4], between items
     constexpr int kMergeRow = D + 4;
-    static_assert(kAttWarps * kAttRows<NT> * kMergeRow * 4 <= kAttWarps * kAttStages * kUnitBytes, "the merge buffer lies over the rings");
+    static_assert(kAttWarps * kAttRows<NT> * kMergeRow * 4 <= kAttWarps * kAttStages * T::kBytes, "the merge buffer lies over the rings");
 
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
     uint32_t issued = 0;      // units the warp has requested before this segment: ring slots and phases run on
     if (lane == 0) {
-        for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, kU);
+        for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_trigger();
@@ -408,7 +401,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
 
     // ---- the items: parts of segments (sequence, kv head, row tile) ----
     auto shape_of = [&](int len, int rows, uint32_t &n, uint32_t &tiles) {      // units of a segment, segments per kv head
-        n = max(1u, ((uint32_t)len + kUnitTokens - 1) / kUnitTokens);
+        n = max(1u, ((uint32_t)len + kTileTokens - 1) / kTileTokens);
         tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
     uint32_t small = 0, big = 0;                   // units of an item; 0: no big ones
@@ -439,10 +432,10 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         for (int w = 0; w < kAttWarps; ++w) units += sh_scan[w][0];
         const uint32_t share = (uint32_t)min(units / gridDim.x, (uint64_t)1 << 30);      // of a CTA
         if (share >= kTwoSizes) {
-            small = (max(kSmallUnits, share / 10) + kAttWarps - 1) / kAttWarps * kAttWarps;
+            small = (max(kSmallTiles, share / 10) + kAttWarps - 1) / kAttWarps * kAttWarps;
             big = kBigSmalls * small;
         } else {
-            small = min(kItemUnits, share / 2 + kAttWarps) / kAttWarps * kAttWarps;
+            small = share < kOneRound ? kOneRound : min(kItemTiles, share / 2 + kAttWarps) / kAttWarps * kAttWarps;
         }
         uint64_t mine[2] = {0, 0};                 // big items and small ones; slots (items of segments that are cut)
         for (int i = b_first; i < b_last; ++i) {
@@ -528,7 +521,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         if (have) {
         const int b = sh_item[0], len = sh_item[1], rows = sh_item[2];
         const uint32_t seg = (uint32_t)sh_item[3], tiles = (uint32_t)sh_item[4], parts = (uint32_t)sh_item[5], part = (uint32_t)sh_item[6];
-        const uint32_t slot0 = (uint32_t)sh_item[7], unit0 = (uint32_t)sh_item[8], units = (uint32_t)sh_item[9];      // slot of the segment's first part, if it is cut
+        const uint32_t slot0 = (uint32_t)sh_item[7], tile0 = (uint32_t)sh_item[8], ntiles = (uint32_t)sh_item[9];      // slot of the segment's first part, if it is cut
         const uint32_t head = tiles == 1 ? seg : seg / tiles, row_tile = tiles == 1 ? 0u : seg - head * tiles;
         Segment sg;
         sg.b = b, sg.head = (int)head, sg.r0 = (int)row_tile * kAttRows<NT>;
@@ -548,30 +541,29 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             }
         }
 
-        // ---- the warp's units: number k is the segment's unit first_unit + k * kAttWarps ----
-        const int last_unit = (int)min(((uint32_t)len + kUnitTokens - 1) / kUnitTokens, unit0 + units), first_unit = (int)unit0 + warp;
-        const int count = nrows > 0 && first_unit < last_unit ? (last_unit - first_unit + kAttWarps - 1) / kAttWarps : 0;
-        const uint8_t *source = nullptr;   // lane i: where tile i of the next 32 tiles of the warp's lies (nullptr: nowhere)
-        uint32_t exist = 0, there = 0;     // bit i: that tile exists; the units requested so far, kU bits each, the newest lowest
+        // ---- the warp's tiles: number k is the segment's tile first_tile + k * kAttWarps ----
+        const int last_tile = (int)min(((uint32_t)len + kTileTokens - 1) / kTileTokens, tile0 + ntiles), first_tile = (int)tile0 + warp;
+        const int count = nrows > 0 && first_tile < last_tile ? (last_tile - first_tile + kAttWarps - 1) / kAttWarps : 0;
+        const uint8_t *source = nullptr;   // lane i: where tile i of the warp's next 32 lies (nullptr: nowhere)
+        uint32_t exist = 0, there = 0;     // bit i: that tile exists; the tiles requested so far, the newest lowest
         auto issue = [&](int k) {
-            there <<= kU;
+            there <<= 1;
             if (k >= count) return;
-            const int at = (k * kU) & 31;
+            const int at = k & 31;
             if (at == 0) {
-                const int t = ((first_unit + (k + lane / kU) * kAttWarps) * kU + lane % kU) * kTileTokens;
+                const int t = (first_tile + (k + lane) * kAttWarps) * kTileTokens;
                 source = nullptr;
-                if (k + lane / kU < count && t < len) {
+                if (k + lane < count) {
                     const int page = s.page(b, t >> c.page_shift);
                     if (kv_page_ok(c, page)) source = kv_tile<D>(c, page, t & ((1 << c.page_shift) - 1), sg.head);
                 }
                 exist = __ballot_sync(0xffffffffu, source != nullptr);
             }
-            there |= (exist >> at) & ((1u << kU) - 1);
-            if ((unsigned)(lane - at) < (unsigned)kU) {      // the lane that knows a tile requests it; one that is not there completes at once
+            there |= (exist >> at) & 1u;
+            if (lane == at) {              // the lane that knows a tile requests it; one that is not there completes at once
                 const uint32_t slot = (issued + (uint32_t)k) % kAttStages, bar = bars + 8 * slot;
                 mbar_expect_tx(bar, source != nullptr ? T::kBytes : 0);
-                if (source != nullptr)
-                    bulk_load(ring + slot * kUnitBytes + (uint32_t)(lane - at) * T::kBytes, MXQ_AT(source, T::kBytes, c.pool, c.pool_bytes), T::kBytes, bar);
+                if (source != nullptr) bulk_load(ring + slot * T::kBytes, MXQ_AT(source, T::kBytes, c.pool, c.pool_bytes), T::kBytes, bar);
             }
         };
 #pragma unroll
@@ -621,22 +613,17 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
 
         bool arrived = true;
         for (int k = 0; k < count; ++k) {
-            const uint32_t at = issued + (uint32_t)k, slot = at % kAttStages, unit = ring + slot * kUnitBytes;
-            const int t0 = (first_unit + k * kAttWarps) * kUnitTokens;
+            const uint32_t at = issued + (uint32_t)k, slot = at % kAttStages, tile = ring + slot * T::kBytes;
+            const int t0 = (first_tile + k * kAttWarps) * kTileTokens;
             if (!mbar_wait(bars + 8 * slot, (at / kAttStages) & 1u)) {      // (never in normal operation; the segment's rows become NaN)
                 if (lane == 0) atomicOr(&g_kv_status, 1u);
                 arrived = false;
             }
-            const uint32_t here = (there >> (kU * (kAttStages - 1))) & ((1u << kU) - 1);
-            if (here != 0) {
-                constexpr int kG = 2 * kU;                   // groups of 16 tokens
+            if ((there >> (kAttStages - 1)) & 1u) {
                 const int tok = (g >> 1) + 4 * (g & 1);      // row g of the product is this token of the group, row g + 8 the one 8 further
-                // ---- scores (one body for the unit's tiles) ----
-                float x[kG][NT][4];
-#pragma unroll 1
-                for (int i = 0; i < kU; ++i) {
-                    const uint32_t tile = unit + i * T::kBytes;
-                    float y[2][NT][4];
+                // ---- scores ----
+                float x[2][NT][4];       // of the tile's two groups of 16 tokens
+                {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         uint32_t k0[kNb], k1[kNb], s0, s1;
@@ -661,45 +648,36 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
                                 mma16816<false>(d, h0[0], h1[0], h0[1], h1[1], q.x, q.y);
                                 mma16816<false>(d, h0[2], h1[2], h0[3], h1[3], q.z, q.w);
-                                float(&v)[4] = y[u][nt];
+                                float(&v)[4] = x[u][nt];
                                 if (j == 0) v[0] = d[0] * c0, v[1] = d[1] * c0, v[2] = d[2] * c1, v[3] = d[3] * c1;
                                 else v[0] += d[0] * c0, v[1] += d[1] * c0, v[2] += d[2] * c1, v[3] += d[3] * c1;
                             }
                         }
                     }
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if (kU == 1 || i == 0) x[u][nt][e] = y[u][nt][e];
-                                if (kU == 2) x[kG - 2 + u][nt][e] = y[u][nt][e];
-                            }
                 }
                 // ---- relative to the running maximum; what a row does not see; a new maximum ----
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint64_t f = pair2(factor[nt][0], factor[nt][1]), m = pair2(-w.m[nt][0], -w.m[nt][1]);
 #pragma unroll
-                    for (int u = 0; u < kG; ++u)
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             float(&v)[4] = x[u][nt];
                             split2(fma2(pair2(v[2 * h], v[2 * h + 1]), f, m), v[2 * h], v[2 * h + 1]);
                         }
                 }
-                if (t0 + kUnitTokens > sg.base || here != (1u << kU) - 1) {
+                if (t0 + kTileTokens > sg.base) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const Sight sight = sight_of(s, a, sg, sg.r0 + 8 * nt + 2 * tig + e);
 #pragma unroll
-                            for (int u = 0; u < kG; ++u)
+                            for (int u = 0; u < 2; ++u)
 #pragma unroll
                                 for (int h = 0; h < 2; ++h)
-                                    if (!sight.sees(t0 + 16 * u + tok + 8 * h) || ((here >> (u / 2)) & 1u) == 0) x[u][nt][2 * h + e] = -INFINITY;
+                                    if (!sight.sees(t0 + 16 * u + tok + 8 * h)) x[u][nt][2 * h + e] = -INFINITY;
                         }
                 }
                 bool over = false;
@@ -709,8 +687,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         float v = fmaxf(x[0][nt][e], x[0][nt][2 + e]);
-#pragma unroll
-                        for (int u = 1; u < kG; ++u) v = fmaxf(v, fmaxf(x[u][nt][e], x[u][nt][2 + e]));
+                        v = fmaxf(v, fmaxf(x[1][nt][e], x[1][nt][2 + e]));
                         top[nt][e] = v;
                         over |= v > w.over[nt][e];
                     }
@@ -731,17 +708,17 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                             w.m[nt][e] += up;
                             w.l[nt][e] *= f[nt][e];
 #pragma unroll
-                            for (int u = 0; u < kG; ++u) x[u][nt][e] -= up, x[u][nt][2 + e] -= up;
+                            for (int u = 0; u < 2; ++u) x[u][nt][e] -= up, x[u][nt][2 + e] -= up;
                         }
                     rescale(w, f);
                 }
                 // ---- weights ----
-                uint32_t pk[kG][NT][2], least = 0x7C007C00u;
+                uint32_t pk[2][NT][2], least = 0x7C007C00u;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     uint64_t sum = pair2(w.l[nt][0], w.l[nt][1]);
 #pragma unroll
-                    for (int u = 0; u < kG; ++u)
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             float &p0 = x[u][nt][2 * h], &p1 = x[u][nt][2 * h + 1];
@@ -753,22 +730,17 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     split2(sum, w.l[nt][0], w.l[nt][1]);
                 }
                 // ---- V scales: largest and smallest ----
-                const bool tail = t0 + kUnitTokens > len || here != (1u << kU) - 1;
-                const uint32_t sv_at = unit + T::kVs + 4 * lane;
-                uint32_t sv[kU], in[kU], hi2 = 0, lo2 = 0x00FF00FFu;     // a word of a tile's scales per lane, and the bytes of tokens that are there
-#pragma unroll
-                for (int i = 0; i < kU; ++i) {
-                    sv[i] = 0, in[i] = 0xFFFFFFFFu;
-                    if (8 * kNb < 32 && lane >= 8 * kNb) in[i] = 0;
-                    else sv[i] = lds_u32(sv_at + i * T::kBytes);
-                    if (tail && in[i] != 0) {
-                        const int t = t0 + 32 * i + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
-                        in[i] = ((here >> i) & 1u) == 0 ? 0u : (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
-                    }
-                    const uint32_t up = sv[i] & in[i], dn = sv[i] | ~in[i];
-                    hi2 = __vmaxu2(hi2, __vmaxu2(__byte_perm(up, 0, 0x4240), __byte_perm(up, 0, 0x4341)));
-                    lo2 = __vminu2(lo2, __vminu2(__byte_perm(dn, 0, 0x4240), __byte_perm(dn, 0, 0x4341)));
+                const bool tail = t0 + kTileTokens > len;
+                const uint32_t sv_at = tile + T::kVs + 4 * lane;
+                uint32_t sv = 0, in = 0xFFFFFFFFu;           // a word of them per lane, and the bytes of tokens that are there
+                if (8 * kNb < 32 && lane >= 8 * kNb) in = 0;
+                else sv = lds_u32(sv_at);
+                if (tail && in != 0) {
+                    const int t = t0 + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
+                    in = (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
                 }
+                uint32_t hi2 = __vmaxu2(__byte_perm(sv & in, 0, 0x4240), __byte_perm(sv & in, 0, 0x4341));
+                uint32_t lo2 = __vminu2(__byte_perm(sv | ~in, 0, 0x4240), __byte_perm(sv | ~in, 0, 0x4341));
                 hi2 = __vmaxu2(hi2, __byte_perm(hi2, 0, 0x1032)), lo2 = __vminu2(lo2, __byte_perm(lo2, 0, 0x1032));
                 int hi = (int)(__reduce_max_sync(0xffffffffu, hi2) & 0xFFFFu);
                 const int lo = (int)(__reduce_min_sync(0xffffffffu, lo2) & 0xFFFFu);
@@ -778,8 +750,8 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     if (nan) {       // the largest that is a number
                         hi = 0;
 #pragma unroll
-                        for (int i = 0; i < 4 * kU; ++i) {
-                            const int v = (int)(((sv[i / 4] & in[i / 4]) >> (8 * (i & 3))) & 0xFFu);
+                        for (int i = 0; i < 4; ++i) {
+                            const int v = (int)(((sv & in) >> (8 * i)) & 0xFFu);
                             if (v != 255) hi = max(hi, v);
                         }
                         hi = (int)__reduce_max_sync(0xffffffffu, (uint32_t)hi);
@@ -796,10 +768,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                         w.ref = ref;
                     }
                     if (tail) {      // tokens that are not there carry no weight: any scale that fits will do
-#pragma unroll
-                        for (int i = 0; i < kU; ++i)
-                            if (lane < 8 * kNb)
-                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at + i * T::kBytes), "r"((sv[i] & in[i]) | ((uint32_t)w.ref * 0x01010101u & ~in[i])) : "memory");
+                        if (lane < 8 * kNb) asm volatile("st.shared.u32 [%0], %1;" ::"r"(sv_at), "r"((sv & in) | ((uint32_t)w.ref * 0x01010101u & ~in)) : "memory");
                         __syncwarp();
                     }
                 }
@@ -807,22 +776,29 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 const int range = kHalfRange - max(w.ref - lo, 0);      // binades of weight the scales leave to FP16
                 const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
                 const bool plain = __all_sync(0xffffffffu, all_le_half2(pack_half2(small, small), least)) && range >= kHalfRange - kScaleSpread && !nan;   // (NaN compares false)
-                bool four = false, wide = false;
-                const float tiny = small * small, up = __uint_as_float((uint32_t)(127 + max(range, 0)) << 23);
+                float low = 1.f;             // the smallest weight that is not zero
+                const float tiny = small * small;
                 if (!plain) {
-                    float low = 1.f;             // the smallest weight that is not zero
 #pragma unroll
-                    for (int u = 0; u < kG; ++u)
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) low = fminf(low, x[u][nt][e] == 0.f ? 1.f : x[u][nt][e]);
-                    four = __any_sync(0xffffffffu, low < tiny);
-                    wide = nan || range < kHalfRange - kScaleSpread || __any_sync(0xffffffffu, low < tiny * tiny);
                 }
-                if (!wide) {
-                    // plain: the weights as they are.  Else tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in
-                    // small^(i+1) .. small^i
+                if (plain) {
+                    uint32_t p[2][NT][2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(pk[u][nt][h]);
+                    add_values<D, NT, 1>(w, tile, g, tig, p, p, 1.f, 1.f);
+                } else if (!nan && range >= kHalfRange - kScaleSpread && !__any_sync(0xffffffffu, low < tiny * tiny)) {
+                    // tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in small^(i+1) .. small^i
+                    const float up = __uint_as_float((uint32_t)(127 + range) << 23);
+                    const bool four = __any_sync(0xffffffffu, low < tiny);
 #pragma unroll 1
                     for (int pass = four ? 0 : 1; pass < 2; ++pass) {
                         const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part_ = pass == 0 ? tiny * small : small;
@@ -833,67 +809,42 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                             for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
                             rescale(w, ff);
                         }
-#pragma unroll 1
-                        for (int i = 0; i < kU; ++i) {
-                            uint32_t p[2][NT][2], deep[2][NT][2];
+                        uint32_t p[2][NT][2], deep[2][NT][2];
 #pragma unroll
-                            for (int u = 0; u < 2; ++u)
+                        for (int u = 0; u < 2; ++u)
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
+                            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                    for (int h = 0; h < 2; ++h) {
-                                        p[u][nt][h] = kU == 1 || i == 0 ? pk[u][nt][h] : pk[kG - 2 + u][nt][h];
-                                        deep[u][nt][h] = 0;
+                                for (int h = 0; h < 2; ++h) {
+                                    float lo_[2], hi_[2];
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        const float v = x[u][nt][2 * h + e], in_ = v < from || v >= bound ? 0.f : v * gain;
+                                        lo_[e] = v < part_ ? in_ * up : 0.f;
+                                        hi_[e] = v < part_ ? 0.f : in_;
                                     }
-                            if (!plain) {
-#pragma unroll
-                                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                        for (int h = 0; h < 2; ++h) {
-                                            float lo_[2], hi_[2];
-#pragma unroll
-                                            for (int e = 0; e < 2; ++e) {
-                                                const float v = kU == 1 || i == 0 ? x[u][nt][2 * h + e] : x[kG - 2 + u][nt][2 * h + e];
-                                                const float in_ = v < from || v >= bound ? 0.f : v * gain;
-                                                lo_[e] = v < part_ ? in_ * up : 0.f;
-                                                hi_[e] = v < part_ ? 0.f : in_;
-                                            }
-                                            p[u][nt][h] = pack_half2(hi_[0], hi_[1]);
-                                            deep[u][nt][h] = transpose8x8(pack_half2(lo_[0], lo_[1]));
-                                        }
-                            }
-#pragma unroll
-                            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                    for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(p[u][nt][h]);
-                            add_values<D, NT>(w, unit + i * T::kBytes, g, tig, p, deep, !plain, up, small);
-                        }
+                                    p[u][nt][h] = transpose8x8(pack_half2(hi_[0], hi_[1]));
+                                    deep[u][nt][h] = transpose8x8(pack_half2(lo_[0], lo_[1]));
+                                }
+                        add_values<D, NT, 2>(w, tile, g, tig, p, deep, up, small);
                     }
                 } else {
 #pragma unroll 1
                     for (int part_ = 0; part_ < 2; ++part_)       // the weights' upper and lower eight bits
-#pragma unroll 1
-                        for (int i = 0; i < kU; ++i)
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                uint32_t p[NT][2];
+                        for (int u = 0; u < 2; ++u) {
+                            uint32_t p[NT][2];
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
+                            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                    for (int h = 0; h < 2; ++h) {
-                                        float x0 = x[u][nt][2 * h], x1 = x[u][nt][2 * h + 1];
-                                        if (kU == 2 && i == 1) x0 = x[kG - 2 + u][nt][2 * h], x1 = x[kG - 2 + u][nt][2 * h + 1];
-                                        uint32_t b = pack_bf162(x0, x1);
-                                        if (part_ == 1) b = pack_bf162(x0 - __uint_as_float(b << 16), x1 - __uint_as_float(b & 0xFFFF0000u));
-                                        p[nt][h] = transpose8x8(b);
-                                    }
-                                add_values_wide<D, NT>(w, unit + i * T::kBytes, u, t0 + 32 * i + 16 * u, g, tig, p,
-                                                       [&](int nt, int t) { return sight_of(s, a, sg, sg.r0 + 8 * nt + g).sees(t); });
-                            }
+                                for (int h = 0; h < 2; ++h) {
+                                    const float x0 = x[u][nt][2 * h], x1 = x[u][nt][2 * h + 1];
+                                    uint32_t b = pack_bf162(x0, x1);
+                                    if (part_ == 1) b = pack_bf162(x0 - __uint_as_float(b << 16), x1 - __uint_as_float(b & 0xFFFF0000u));
+                                    p[nt][h] = transpose8x8(b);
+                                }
+                            add_values_wide<D, NT>(w, tile, u, t0 + 16 * u, g, tig, p, [&](int nt, int t) { return sight_of(s, a, sg, sg.r0 + 8 * nt + g).sees(t); });
+                        }
                 }
             }
             __syncwarp();
