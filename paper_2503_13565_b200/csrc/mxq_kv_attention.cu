@@ -146,7 +146,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // factor is then 1 + 2^-23 of the power of two, the same for every score); byte 0 becomes 2^-149: blocks scaled by 2^-127 count as zero.
 template <int J>
 __device__ __forceinline__ float scale_factor(uint32_t w) {
-    return __uint_as_float(((J == 3 ? w >> 1 : w * (1u << (23 - 8 * (J & 3)))) & 0x7F800000u) | 1u);
+    if constexpr (J == 3) return __uint_as_float(__byte_perm(w, 0, 0x4344) * 128u | 1u);      // (shifts to the left only: they are multiplications on the other pipe)
+    else return __uint_as_float((w * (1u << (23 - 8 * (J & 3))) & 0x7F800000u) | 1u);
 }
 __device__ __forceinline__ float scale_factor(uint32_t w, int j) {   // (j a constant after unrolling)
     return j == 0 ? scale_factor<0>(w) : j == 1 ? scale_factor<1>(w) : j == 2 ? scale_factor<2>(w) : scale_factor<3>(w);
@@ -273,52 +274,44 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
                                            const uint32_t (&deep)[2][NT][2], float up, float down) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb, kW = kNb / 2;   // words of V codes per lane and token
-    uint32_t sw[2][kNb];                        // scales: [group][h, block pair] words of (A.j, B.j, A.j+1, B.j+1)
-    uint32_t v[2][4][kW];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        lds_words<kNb>(tile + T::kVs + 16 * kNb * u + 4 * kNb * tig, sw[u]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) lds_words<kW>(tile + T::kV + (16 * u + tig + 4 * k) * T::kRow + 2 * kNb * g, v[u][k]);
-    }
     // exponent field of 2^(scale - ref + kScaleBias): never below 1 here, so both halves fit one 32-bit multiply-add
     const uint32_t bias = (uint32_t)(15 + kScaleBias - w.ref) * (0x10001u << 10);
 #pragma unroll
-    for (int x = 0; x < kW; ++x) {
-        uint32_t e[2][2][4], o[2][2][4];        // pairs (token A, token B) of even and odd elements
+    for (int u = 0; u < 2; ++u) {
+        uint32_t sw[kNb], v[4][kW];             // scales: [h, block pair] words of (A.j, B.j, A.j+1, B.j+1); codes
+        lds_words<kNb>(tile + T::kVs + 16 * kNb * u + 4 * kNb * tig, sw);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int k = 0; k < 4; ++k) lds_words<kW>(tile + T::kV + (16 * u + tig + 4 * k) * T::kRow + 2 * kNb * g, v[k]);
+#pragma unroll
+        for (int x = 0; x < kW; ++x) {
+            uint32_t e[2][4], o[2][4];          // pairs (token A, token B) of even and odd elements
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t A = v[u][2 * h][x], B = v[u][2 * h + 1][x];
-                decode4((A & 0x0F0F0F0Fu) | ((B * 16u) & 0xF0F0F0F0u), e[u][h]);
-                decode4(((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u), o[u][h]);
+                const uint32_t A = v[2 * h][x], B = v[2 * h + 1][x];
+                decode4((A & 0x0F0F0F0Fu) | ((B * 16u) & 0xF0F0F0F0u), e[h]);
+                decode4(((A >> 4) & 0x0F0F0F0Fu) | (B & 0xF0F0F0F0u), o[h]);
             }
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int j = 2 * x + y;
-            uint32_t sc[2][2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int y = 0; y < 2; ++y) {
+                const int j = 2 * x + y;
+                uint32_t sc[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)     // (the two tokens' scales as 16-bit numbers)
-                    sc[u][h] = __byte_perm(sw[u][h * kW + x], 0, y ? 0x4342 : 0x4140) * 1024u + bias;
-            auto product = [&](int n, const uint32_t(&q)[2][NT][2]) {
+                    sc[h] = __byte_perm(sw[h * kW + x], 0, y ? 0x4342 : 0x4140) * 1024u + bias;
+                auto product = [&](int n, const uint32_t(&q)[2][NT][2]) {
+                    const uint32_t b0 = mul_half2(q[u][n][0], sc[0]), b1 = mul_half2(q[u][n][1], sc[1]);
+                    mma16816<false>(w.o[2 * j][n], e[0][2 * y], o[0][2 * y], e[1][2 * y], o[1][2 * y], b0, b1);
+                    mma16816<false>(w.o[2 * j + 1][n], e[0][2 * y + 1], o[0][2 * y + 1], e[1][2 * y + 1], o[1][2 * y + 1], b0, b1);
+                };
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t b0 = mul_half2(q[u][n][0], sc[u][0]), b1 = mul_half2(q[u][n][1], sc[u][1]);
-                    mma16816<false>(w.o[2 * j][n], e[u][0][2 * y], o[u][0][2 * y], e[u][1][2 * y], o[u][1][2 * y], b0, b1);
-                    mma16816<false>(w.o[2 * j + 1][n], e[u][0][2 * y + 1], o[u][0][2 * y + 1], e[u][1][2 * y + 1], o[u][1][2 * y + 1], b0, b1);
+                for (int n = 0; n < NT; ++n) {
+                    if constexpr (kTiers == 2) {
+                        scale4(w.o[2 * j][n], up, up), scale4(w.o[2 * j + 1][n], up, up);
+                        product(n, deep);
+                        scale4(w.o[2 * j][n], down, down), scale4(w.o[2 * j + 1][n], down, down);
+                    }
+                    product(n, p);
                 }
-            };
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if constexpr (kTiers == 2) {
-                    scale4(w.o[2 * j][n], up, up), scale4(w.o[2 * j + 1][n], up, up);
-                    product(n, deep);
-                    scale4(w.o[2 * j][n], down, down), scale4(w.o[2 * j + 1][n], down, down);
-                }
-                product(n, p);
             }
         }
     }
@@ -733,14 +726,16 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 const bool tail = t0 + kTileTokens > len;
                 const uint32_t sv_at = tile + T::kVs + 4 * lane;
                 uint32_t sv = 0, in = 0xFFFFFFFFu;           // a word of them per lane, and the bytes of tokens that are there
-                if (8 * kNb < 32 && lane >= 8 * kNb) in = 0;
-                else sv = lds_u32(sv_at);
-                if (tail && in != 0) {
+                if (8 * kNb == 32 || lane < 8 * kNb) sv = lds_u32(sv_at);
+                else in = 0;
+                uint32_t up_ = sv, dn_ = 8 * kNb == 32 ? sv : sv | ~in;
+                if (tail) {
                     const int t = t0 + 16 * (4 * lane / (16 * kNb)) + (4 * lane / (4 * kNb)) % 4 + 8 * ((4 * lane / (2 * kNb)) % 2);
-                    in = (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
+                    in &= (t < len ? 0x00FF00FFu : 0u) | (t + 4 < len ? 0xFF00FF00u : 0u);
+                    up_ = sv & in, dn_ = sv | ~in;
                 }
-                uint32_t hi2 = __vmaxu2(__byte_perm(sv & in, 0, 0x4240), __byte_perm(sv & in, 0, 0x4341));
-                uint32_t lo2 = __vminu2(__byte_perm(sv | ~in, 0, 0x4240), __byte_perm(sv | ~in, 0, 0x4341));
+                uint32_t hi2 = __vmaxu2(__byte_perm(up_, 0, 0x4240), __byte_perm(up_, 0, 0x4341));
+                uint32_t lo2 = __vminu2(__byte_perm(dn_, 0, 0x4240), __byte_perm(dn_, 0, 0x4341));
                 hi2 = __vmaxu2(hi2, __byte_perm(hi2, 0, 0x1032)), lo2 = __vminu2(lo2, __byte_perm(lo2, 0, 0x1032));
                 int hi = (int)(__reduce_max_sync(0xffffffffu, hi2) & 0xFFFFu);
                 const int lo = (int)(__reduce_min_sync(0xffffffffu, lo2) & 0xFFFFu);
