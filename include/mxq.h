@@ -409,8 +409,9 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
  * A row that sees no token gives O = 0 and lse = -inf; tokens a row does not see do not touch it, whatever they hold.
  * Scores, maxima, sums and the accumulators are FP32; each weight is rounded to 11 bits before it meets V, so that
  * |O - exact| <= 2^-10 * sum_t w_t |v^_t| / sum_t w_t + BF16's rounding.  Bit-reproducible run to run for given lengths.
- *   workspace  device memory, >= mxq_kv_attention_workspace_bytes, 16-byte aligned; zero its first 4096 bytes once before
- *              the first use, every call leaves them zero again; one per stream. */
+ *   workspace  device memory, >= mxq_kv_attention_workspace_bytes, 16-byte aligned; zero all of it once before the first
+ *              use: it holds counters that every call leaves zero again, so calls of any shape it is large enough for may
+ *              share it.  One per stream.  After a non-zero mxq_linear_device_status zero it again. */
 size_t mxq_kv_attention_workspace_bytes(int B, int M, int q_heads, int kv_heads, int head_dim);
 int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, int64_t q_stride, int B, int M, int q_heads,
                      const int32_t *tables, int W, const int32_t *lens, const int32_t *rows, const uint64_t *tree, float scale,

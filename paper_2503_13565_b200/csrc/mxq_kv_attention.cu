@@ -43,9 +43,8 @@ struct KvQuery {
     float *lse;              // [B][M][heads] or nullptr
     int32_t heads, group;    // query heads, query heads per kv head
     uint32_t group_magic;    // floor(2^32 / group) + 1 (0: group = 1): r / group = umulhi(r, group_magic) for r * group < 2^32
-    int32_t max_tiles;       // row tiles of a sequence with all its rows
     float scale_log2;        // scale * log2(e)
-    unsigned *counter;       // workspace: next item, one ticket per segment (both zero between calls), slots of partial results
+    unsigned *counter;       // workspace: next item; parts delivered, per cut segment (both zero between calls); slots of partial results
     unsigned *tickets;
     float *partials;
     uint32_t slots;
@@ -915,9 +914,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         }   // (have)
 
         // ---- join the parts of the segment delivered to before: the CTA that brought the last one adds them, in order ----
-        auto ticket_of = [&](const Part &p) {
-            return MXQ_AT(a.tickets + ((size_t)p.b * c.heads + p.head) * a.max_tiles + p.r0 / kAttRows<NT>, 4, a.tickets, (size_t)s.B * c.heads * a.max_tiles * 4);
-        };
+        auto ticket_of = [&](const Part &p) { return MXQ_AT(a.tickets + p.slot0, 4, a.tickets, (size_t)a.slots * 4); };
         if (pending.parts != 0 || !whole) {
             if (tid == 0) {
                 sh_last = pending.parts != 0 && before == pending.parts - 1;
@@ -1034,21 +1031,17 @@ static int att_column_blocks(int M, int group) { return (int64_t)M * group <= 8 
 template <int D, int NT>
 static int att_grid() { return sm_count() * kAttCtasPerSm<D, NT>; }
 
-// Workspace: 16 bytes with the counter, a ticket per segment, slots for the parts of cut segments.  No part but a segment's last is smaller
-// than a small item, so a cut segment of n units has at most 2 n / small of them, and a small item is at least a tenth of a CTA's share.
-struct AttLayout {
-    size_t tickets, partials, bytes;
-    uint32_t slots;
-};
+// Workspace: the counter, a ticket per cut segment (under its first part's slot), slots for the parts.  No part but a segment's last is
+// smaller than a small item, so a cut segment of n tiles has at most 2 n / small of them; a small item is at least a tenth of a CTA's share
+// (rounded down, at least 24), which bounds all parts by 22 per CTA.  Counter and tickets lie in the same place for every shape, so that
+// calls of different shapes may share a workspace: they find them zero.
+constexpr uint32_t kAttSlotsPerCta = 24;
+constexpr int kAttMostCtasPerSm = 4;
+static size_t att_partials_offset() { return 16 + (((size_t)kAttSlotsPerCta * kAttMostCtasPerSm * sm_count() * 4 + 255) / 256 * 256); }
 template <int D, int NT>
-static AttLayout att_layout(int B, int heads, int max_tiles) {
-    AttLayout l;
-    l.tickets = 16;
-    l.partials = l.tickets + ((size_t)B * heads * max_tiles * 4 + 255) / 256 * 256;
-    if (l.partials < 4096) l.partials = 4096;
-    l.slots = 24u * (uint32_t)att_grid<D, NT>();
-    l.bytes = l.partials + (size_t)l.slots * kAttSlotFloats<D, NT> * 4;
-    return l;
+static size_t att_workspace() {
+    static_assert(kAttCtasPerSm<D, NT> <= kAttMostCtasPerSm, "");
+    return att_partials_offset() + (size_t)kAttSlotsPerCta * att_grid<D, NT>() * kAttSlotFloats<D, NT> * 4;
 }
 
 template <int D, int NT>
@@ -1065,12 +1058,10 @@ static int att_launch(const KvView &c, const KvSeqs &s, KvQuery a, void *workspa
         }
         configured[dev] = true;
     }
-    a.max_tiles = (s.m * a.group + kAttRows<NT> - 1) / kAttRows<NT>;
-    const AttLayout l = att_layout<D, NT>(s.B, c.heads, a.max_tiles);
     a.counter = (unsigned *)workspace;
-    a.tickets = (unsigned *)((char *)workspace + l.tickets);
-    a.partials = (float *)((char *)workspace + l.partials);
-    a.slots = l.slots;
+    a.tickets = (unsigned *)((char *)workspace + 16);
+    a.partials = (float *)((char *)workspace + att_partials_offset());
+    a.slots = kAttSlotsPerCta * (uint32_t)att_grid<D, NT>();
     return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)att_grid<D, NT>()), kAttThreads, smem, stream, c, s, a);
 }
 
@@ -1095,9 +1086,7 @@ size_t mxq_kv_attention_workspace_bytes(int B, int M, int q_heads, int kv_heads,
         return 0;
     const int group = q_heads / kv_heads;
     if ((int64_t)M * group > 65536 || (int64_t)B * M * q_heads > (1 << 30)) return 0;
-    return mxq::att_pick(head_dim, M, group, [&](auto d, auto nt) {
-        return mxq::att_layout<d(), nt()>(B, kv_heads, (M * group + mxq::kAttRows<nt()> - 1) / mxq::kAttRows<nt()>).bytes;
-    });
+    return mxq::att_pick(head_dim, M, group, [](auto d, auto nt) { return mxq::att_workspace<d(), nt()>(); });
 }
 
 int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, int64_t q_stride, int B, int M, int q_heads,

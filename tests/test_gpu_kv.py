@@ -382,6 +382,24 @@ def test_attention_long_and_many():
     check_attention(s, 0, queries(s, 1, 2, 2.0))
 
 
+def test_attention_calls_of_all_shapes_share_a_workspace():
+    """Small and large batches, both head dimensions, few and many rows, cut and whole segments, in turn on one workspace."""
+    shapes = [(64, 1, 2, 2, [40]), (128, 5, 8, 2, [700, 90]), (64, 1, 4, 1, [2000] * 3), (128, 1, 1, 1, [5000]), (64, 16, 8, 1, [300] * 40),
+              (128, 1, 8, 8, [64] * 100)]
+    cases = []
+    for i, (d, m, hq, h, lens) in enumerate(shapes):
+        s = Setup(80 + i, lens, d, h, 64)
+        s.fill_cache(0)
+        cases.append((s, queries(s, m, hq).cuda()))
+    ws = mxq.new_workspace(max(mxq.mxq_kv_attention_workspace_bytes(len(lens), m, hq, h, d) for d, m, hq, h, lens in shapes))
+    run = lambda s, q, w: mxq.mxq_kv_attention(q, s.cache, 0, s.t_tables, s.t_lens, workspace=w)
+    alone = [run(s, q, None) for s, q in cases]
+    for order in (range(6), reversed(range(6)), (3, 0, 5, 1, 4, 2, 3, 3)):
+        for i in order:
+            assert torch.equal(run(*cases[i], ws), alone[i]), shapes[i]
+    assert mxq.mxq_linear_device_status() == 0
+
+
 def test_attention_lengths_beyond_the_table_count_as_its_end():
     s = Setup(24, [64, 64], 64, 1, 32)
     s.fill_cache(0)
