@@ -3,29 +3,42 @@
 // The mathematics.  A step reads every K and V row of the cache once (D + D / 16 bytes per token and kv head) for a handful
 // of query rows, so the cache's bytes bound it as long as decoding 4-bit codes and the two products keep up with them.
 //   - One pass with a running maximum m and sum l per row (base 2: the softmax scale times log2 e multiplies the score).
-//     The maximum only moves when a score exceeds it by 2^8, so that the warp-wide reduction and the rescaling of the
-//     accumulators happen a few times per sequence, not per tile; weights up to 2^8 are accounted for in the ranges below.
+//     The maximum only moves when a score exceeds it by 2^4 (kMaxSlack), so that the warp-wide reduction and the rescaling of
+//     the accumulators happen a few times per sequence, not per tile; weights up to 2^4 are accounted for in the ranges below.
 //   - Both products run on m16n8k16 with the TOKENS (K) or the head dimension (V) as the 16 rows and eight query rows as the
 //     8 columns: a decode step with few rows wastes no half of a 16-row tile.  Codes become FP16 with the conversion
 //     instruction, exactly, without their scales.
 //   - K: S^T[16 tokens][8 rows] += K[16][16 d] . Q^T.  A block of 32 d is two instructions; their sum is scaled per token in
-//     FP32 (the product of codes and q is exact, q being normalised per row by a power of two into FP16, which holds BF16's
-//     8 bits over 2^28 of range below the row's largest element).
+//     FP32 (the product of codes and q is exact, q being normalised per row by a power of two to a largest element of 2^14 in
+//     FP16, which holds BF16's 8 bits over 2^28 of range below it).  So a score stays finite while K is below 2^103.
 //   - V: O^T[16 d][8 rows] += V^T[16 d][16 tokens] . P^T.  V's scale varies along the contracted tokens and per block of
 //     32 d, so it goes into P: one multiplication of the packed weights per block, shared by the block's two instructions.
 //     FP16 holds P * scale at 11 bits over 2^24 (kHalfRange) between the largest weight times the largest scale met so far (`ref`, an
 //     exponent common to the warp's accumulators) and the smallest.  Weights below that are still right to 11 bits: a tile that has any
-//     adds them in a second product over accumulators scaled up by the width of the first (two tiers).  A tile with weights
-//     or scales spread even wider, or a NaN scale, takes the step in BF16, whose range holds any, with the weights as a sum of two
-//     BF16 numbers.
+//     adds them in a second product over accumulators scaled up by the width of the first (two tiers; four for weights smaller
+//     yet).  A tile with weights or scales spread even wider, or a NaN scale, takes the step in BF16, whose range holds any, with
+//     the weights as a sum of two BF16 numbers.  (All wide: 0.61 ms on the long case below; tiers: 0.28.)
 //   - S^T leaves the tensor core with a lane holding one token and two rows; the second product wants one row and two
 //     tokens: one 8x8 transposition (movmatrix) per packed register.
 //
-// The split.  Lengths live on the device, so the grid is fixed (as many CTAs as fit) and every CTA takes an equal share
-// of the steps of all (sequence, kv head, row tile) segments, a step being 128 tokens, 32 for each of its four warps.  A warp
-// keeps its own m, l, O and a ring of tiles filled by 16-byte asynchronous copies (no warp waits for another until the segment ends).
-// A segment cut over several CTAs is joined by the last of them to arrive (a ticket; nobody waits), in order of the CTAs:
-// the result does not depend on scheduling.
+// The split.  Lengths live on the device, so the grid is fixed: as many CTAs as fit.  The work, all (sequence, kv head, row tile)
+// segments, is cut along the tokens into items, which CTAs draw from a counter as they become free: tiles cost between one
+// product and four, and equal shares left the GPU waiting for the unluckiest CTA (batched decode 58 us, items 39).  Within an item each
+// of the four warps takes every fourth 32-token tile and keeps its own m, l, O and a ring of two tiles, each filled by ONE bulk copy
+// that completes on an mbarrier; no warp waits for another until the item ends.  (Waits are bounded: a tile that never arrives sets a
+// status bit and makes its rows NaN.)  The results of a segment's items go to the workspace, in slots in the order of the tokens; the
+// CTA that delivered the last of them adds them up in that order.  Nobody waits for it, and it learns that it was the last one item
+// later, when the ticket's answer has long arrived.  So which CTA did what does not show in the result.
+//
+// What bounds it.  Not the bytes: 2 x 131071 tokens of 32 heads (1.14 GB) take 244 us with even weights, 4.7 TB/s = 71 % of the copy rate,
+// 276 us (63 %) with peaked ones, whose tiles need the tiers; bringing the tiles in without computing takes 177 us.  A warp spends
+// some 600 instructions on a tile, half of them on the integer pipe (half rate: unpacking nibbles into the order of the products, scale
+// bytes), which is 55 % busy; the rest is latency of one warp's chain of products, shuffles and exponentials with only
+// 12 warps per SM to hide it (the accumulators and both operands of 32 x 128 tiles: 168 registers).  More warps or more work per
+// warp spill, and spills lose more than they give: the L1 is what the rings leave.  32 decode rows over 100 to 4000 tokens (77.5 MB):
+// 39 us, 20 of them without computing; one row over 2047 tokens: 13 us, 9 without computing: launch, the division of the work, one
+// item of two tiles per warp, the join; tree verification, 8 x 16 rows, head dimension 64: 38 us, 23 without computing.  Requesting the next
+// item's tiles before this one's result is put together gained nothing (the SM's other CTAs fill the gap) and cost registers.
 #include <math.h>
 
 #include <type_traits>
@@ -52,9 +65,12 @@ struct KvQuery {
 
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;                  // tiles in a warp's ring
-// The work is cut into items that CTAs draw in turn.  An item costs about two units of time by itself, and the last ones leave CTAs idle for up to
-// an item's time; tiles differ in cost.  So with kTwoSizes units or more per CTA, three quarters of every segment go into items of four tenths
-// of a CTA's share, drawn first, the rest into items of a tenth; below that all items are of half a CTA's share, at most kItemTiles units.
+// The sizes of items.  An item costs about two tiles' time by itself, and the last ones leave CTAs idle for up to an item's time.  With
+// kTwoSizes tiles or more per CTA, three quarters of every segment go into items of four tenths of a CTA's share, drawn first, the rest into
+// items of a tenth (2 x 131071 tokens, 591 tiles per CTA, even weights: 244 us; all items of half a share, at most kItemTiles tiles: 271; 32 x
+// 16384 tokens of 8 heads: 142 and 150); below that all items are of half a CTA's share, at most kItemTiles tiles (32 sequences of 100 to 4000
+// tokens, 40 tiles per CTA: 39 us, two sizes 68; tree verification, 23 per CTA: 40 us, two sizes 47).
+// With less than kOneRound tiles per CTA items have that many, two per warp, the ring's depth: fewer would leave part of it empty.
 constexpr uint32_t kTwoSizes = 96, kItemTiles = 48, kSmallTiles = 24, kBigSmalls = 4, kOneRound = 8;
 
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
@@ -121,11 +137,6 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t mul_bf162(uint32_t a, uint32_t b) {
     uint32_t o;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
-    return o;
-}
-__device__ __forceinline__ uint32_t max_half2(uint32_t a, uint32_t b) {   // (NaN wins)
-    uint32_t o;
-    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
     return o;
 }
 __device__ __forceinline__ uint32_t min_half2(uint32_t a, uint32_t b) {
@@ -205,7 +216,7 @@ struct Segment {
 __device__ unsigned int g_kv_status = 0;   // sticky: bit 0 a requested tile never arrived
 
 struct Cut {
-    uint32_t small, bigs, parts;  // of a segment: units of its small items, number of its big ones, of all its items
+    uint32_t small, bigs, parts;  // of a segment: tiles of its small items, number of its big ones, of all its items
 };
 struct Owner {                    // the items that a thread's sequences own, and the first of these sequences
     uint32_t big_lo, big_count, small_lo, small_count, slot_lo, tiles;
@@ -382,7 +393,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     static_assert(kAttWarps * kAttRows<NT> * kMergeRow * 4 <= kAttWarps * kAttStages * T::kBytes, "the merge buffer lies over the rings");
 
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
-    uint32_t issued = 0;      // units the warp has requested before this segment: ring slots and phases run on
+    uint32_t issued = 0;      // tiles the warp has requested before this segment: ring slots and phases run on
     if (lane == 0) {
         for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -392,12 +403,12 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     asm volatile("fence.proxy.async;" ::: "memory");      // tiles may have been written by the kernel before, with ordinary stores
 
     // ---- the items: parts of segments (sequence, kv head, row tile) ----
-    auto shape_of = [&](int len, int rows, uint32_t &n, uint32_t &tiles) {      // units of a segment, segments per kv head
-        n = max(1u, ((uint32_t)len + kTileTokens - 1) / kTileTokens);
+    auto shape_of = [&](int len, int rows, uint32_t &n, uint32_t &tiles) {      // tiles of a segment, segments per kv head
+        n = rows == 0 ? 1u : max(1u, ((uint32_t)len + kTileTokens - 1) / kTileTokens);      // (no rows: nothing to read, nothing to join)
         tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
-    uint32_t small = 0, big = 0;                   // units of an item; 0: no big ones
-    auto cut_of = [&](uint32_t n) {                // of a segment of n units (its parts must fit the join's table)
+    uint32_t small = 0, big = 0;                   // tiles of an item; 0: no big ones
+    auto cut_of = [&](uint32_t n) {                // of a segment of n tiles (its parts must fit the join's table)
         Cut k;
         k.small = max(small, (n + kAttWarps * kAttMaxParts<D, NT> - 1) / (kAttWarps * kAttMaxParts<D, NT>) * kAttWarps);
         k.bigs = big == 0 ? 0u : (n - n / 4) / big;
@@ -408,21 +419,21 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     uint32_t bigs, items;                          // all big items, all items
     {
         int len0 = 0, rows0 = 0;                   // the first of this thread's sequences
-        uint64_t units = 0;
+        uint64_t work = 0;
         for (int i = b_first; i < b_last; ++i) {
             const int len = s.len(i), rows = s.nrows(i);
             if (i == b_first) len0 = len, rows0 = rows;
             uint32_t n, tiles;
             shape_of(len, rows, n, tiles);
-            units += (uint64_t)n * (tiles * (uint32_t)c.heads);
+            work += (uint64_t)n * (tiles * (uint32_t)c.heads);
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
-        if (lane == 0) sh_scan[warp][0] = units;
+        for (int o = 16; o > 0; o >>= 1) work += __shfl_xor_sync(0xffffffffu, work, o);
+        if (lane == 0) sh_scan[warp][0] = work;
         __syncthreads();
-        units = 0;
-        for (int w = 0; w < kAttWarps; ++w) units += sh_scan[w][0];
-        const uint32_t share = (uint32_t)min(units / gridDim.x, (uint64_t)1 << 30);      // of a CTA
+        work = 0;
+        for (int w = 0; w < kAttWarps; ++w) work += sh_scan[w][0];
+        const uint32_t share = (uint32_t)min(work / gridDim.x, (uint64_t)1 << 30);      // of a CTA
         if (share >= kTwoSizes) {
             small = (max(kSmallTiles, share / 10) + kAttWarps - 1) / kAttWarps * kAttWarps;
             big = kBigSmalls * small;
@@ -489,7 +500,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 shape_of(len, rows, n, tiles);
                 k = cut_of(n);
             }
-            // the segment, the item's place among its parts, its units
+            // the segment, the item's place among its parts, its tiles
             const uint32_t of = is_big ? k.bigs : k.parts - k.bigs, seg = of == 1 ? item - at : (item - at) / of, p = item - at - seg * of;
             sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)seg, sh_item[4] = (int)tiles, sh_item[5] = (int)k.parts;
             sh_item[6] = (int)(is_big ? p : k.bigs + p), sh_item[7] = (int)(slot + seg * k.parts);
@@ -919,8 +930,8 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             if (tid == 0) {
                 sh_last = pending.parts != 0 && before == pending.parts - 1;
                 if (sh_last) {
-                    *ticket_of(pending) = 0;
                     __threadfence();
+                    *ticket_of(pending) = 0;
                 }
             }
             __syncthreads();          // (and every thread's part of this item's result is stored before the ticket below)
@@ -967,7 +978,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 auto add_parts = [&](int task, int from, int stride) {
                     const int r = task / kCols, d = 4 * (task % kCols);
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
+#pragma unroll 4       // (8: tree verification 40 us, 4: 38)
                     for (int i = from; i < (int)parts; i += stride) {
                         const float f = table[i * nrows + r].x;
                         const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + r * D + d, 16, a.partials, ws_bytes)));

@@ -1,9 +1,14 @@
 // mxq_kv_append / mxq_kv_read: the direct cast of new K and V rows into the pages of a 4-bit cache, and its inverse.
 //
-// Both are streams: 2 bytes of BF16 against 0.53 bytes of codes and scales per element, in opposite directions.  Four
+// Both are streams: 2 bytes of BF16 against 0.53 bytes of codes and scales per element, in opposite directions; a decode
+// step's few rows are a launch's latency.  In the append of a few rows and in the read four
 // lanes share a row: lane c takes elements 8c..8c+7 of every MX block (16-byte accesses, 64 consecutive bytes per quad),
 // the quad agrees on the blocks' maxima with two exchanges (two blocks per register), and the permutation of the layout
 // (mxq_kv.cuh) makes the lane's codes of the row ONE store: K wants word c of every block side by side, V its halfwords.
+// Measured in a replayed graph, head dimension 128: 48 rows of 8 heads 1.8 us (append) and 1.8 us (read), the launch's own
+// time; 5718 rows of 32 heads (94 MB of BF16, 25 MB of cache) 27.6 us for the append, 4.3 TB/s.  The prompt's append issues about
+// as many integer instructions per byte as the direct cast of weights, plus the exchange of words and the scattered scale bytes.  The
+// read of a batch padded to 16380 rows (its zeros are written too: 268 MB) takes 49 us, 6.0 TB/s = 92 % of the copy rate.
 #include "mxq_kv.cuh"
 
 namespace mxq {
@@ -117,7 +122,9 @@ __global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs 
 }
 
 // The same for prompts, where the arithmetic decides: one lane per MX block (no exchange for the maximum, every scale computed
-// once), four heads of a token row per lane (one lookup of its place); the words change lanes before they are stored.  Launched without overlap, so that the lanes of a row may share its sectors through L1.
+// once), four heads of a token row per lane (one lookup of its place); the words change lanes before they are stored.  Launched without
+// overlap, so that the lanes of a row may share its sectors through L1.  (The prompt above: 50 us with the quads, 38 with this split and
+// 4-byte stores, 28 with the exchange and 16-byte stores.  A few rows take the quads: four times the lanes, an eighth of the chain.)
 // grid.x covers (sequence, row, group of kHeadsPerLane heads, block); grid.y: 0 = K, 1 = V
 constexpr int kHeadsPerLane = 4;
 template <int D>

@@ -257,6 +257,14 @@ def test_attention_ragged_rows_and_empty_sequences(d):
     check_attention(s, 0, queries(s, 6, 6), rows=[6, 0, 4, 6, 1])
 
 
+@pytest.mark.parametrize("rows", [[0], [0, 2], [3, 0, 0, 1]])
+def test_attention_long_sequences_without_rows(rows):
+    lens = [9000, 5000, 7777, 100][:len(rows)]
+    s = Setup(29, lens, 64, 2, 64)
+    s.fill_cache(0)
+    check_attention(s, 0, queries(s, max(max(rows), 1), 8), rows=rows)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("m", [1, 5, 16, 48, 64])
 def test_attention_token_trees(m, d):
