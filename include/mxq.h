@@ -409,7 +409,8 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
  * A row that sees no token gives O = 0 and lse = -inf; tokens a row does not see do not touch it, whatever they hold.
  * Scores, maxima, sums and the accumulators are FP32; each weight is rounded to 11 bits before it meets V, so that
  * |O - exact| <= 2^-10 * sum_t w_t |v^_t| / sum_t w_t + BF16's rounding (while |k^| < 2^103: scores are sums in FP32 of q
- * normalised to 2^14; K blocks of scale 2^-127 count as zero).  Bit-reproducible run to run for given lengths.
+ * normalised to 2^14; K blocks of scale 2^-127, and V blocks whose scale is
+ * 2^136 and more below the largest of the sequence's, count as zero).  Bit-reproducible run to run for given lengths.
  *   workspace  device memory, >= mxq_kv_attention_workspace_bytes, 16-byte aligned; zero all of it once before the first
  *              use: it holds counters that every call leaves zero again, so calls of any shape it is large enough for may
  *              share it.  One per stream.  After a non-zero mxq_linear_device_status zero it again. */

@@ -13,7 +13,7 @@
 //     FP16, which holds BF16's 8 bits over 2^28 of range below it).  So a score stays finite while K is below 2^103.
 //   - V: O^T[16 d][8 rows] += V^T[16 d][16 tokens] . P^T.  V's scale varies along the contracted tokens and per block of
 //     32 d, so it goes into P: one multiplication of the packed weights per block, shared by the block's two instructions.
-//     FP16 holds P * scale at 11 bits over 2^24 (kHalfRange) between the largest weight times the largest scale met so far (`ref`, an
+//     FP16 holds P * scale at 11 bits over 2^24 between the largest weight times the largest scale met so far (`ref`, an
 //     exponent common to the warp's accumulators) and the smallest.  Weights below that are still right to 11 bits: a tile that has any
 //     adds them in a second product over accumulators scaled up by the width of the first (two tiers; four for weights smaller
 //     yet).  A tile with weights or scales spread even wider, or a NaN scale, takes the step in BF16, whose range holds any, with
@@ -73,10 +73,10 @@ constexpr int kAttStages = 2;                  // tiles in a warp's ring
 // With less than kOneRound tiles per CTA items have that many, two per warp, the ring's depth: fewer would leave part of it empty.
 constexpr uint32_t kTwoSizes = 96, kItemTiles = 48, kSmallTiles = 24, kBigSmalls = 4, kOneRound = 8;
 
+constexpr int kWeightBias = 10;                // weights carry a factor 2^10 from the exponential on: in FP16 they keep 11 bits down to 2^-14
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
-constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`
-constexpr int kScaleBias = 10;                 // P' = P * 2^(scale - ref + kScaleBias) <= 2^(4 + 1 + 10) fits FP16, and is
-constexpr int kHalfRange = kScaleBias + 14;    // a normal number while P * 2^(scale - ref) >= 2^-24
+constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`: P * 2^(scale - ref) <= 2^(10 + 4 + 1) fits FP16,
+constexpr int kHalfRange = 14;                 // and is a normal number while it is at least 2^-14
 constexpr int kScaleSpread = 14;               // scales this far below ref still take the FP16 step
 constexpr int kScaleLag = 3;                   // how far (log2) a tile's largest scale may lie below ref
 constexpr int kScaleDrop = 12;                 // how far ref may fall below its highest: accumulators are below 2^18 per token, and
@@ -232,7 +232,7 @@ template <int D, int NT>
 struct WarpState {
     float o[D / 16][NT][4];   // rows of block j: d = 32 j + 4 g + {0, 1} in o[2j], + {2, 3} in o[2j + 1]; [d][column]: 00 01 10 11
     float m[NT][2], l[NT][2];     // maximum and sum; m = 0 while over = -inf
-    float over[NT][2];            // how far a score may exceed m: kMaxSlack, or -inf before the first token the row sees
+    float over[NT][2];            // how far a biased score may exceed m: kWeightBias + kMaxSlack, or -inf before the first token the row sees
     int ref, ref_max;
 };
 
@@ -284,8 +284,8 @@ __device__ __forceinline__ void add_values(WarpState<D, NT> &w, uint32_t tile, i
                                            const uint32_t (&deep)[2][NT][2], float up, float down) {
     using T = KvTile<D>;
     constexpr int kNb = T::kNb, kW = kNb / 2;   // words of V codes per lane and token
-    // exponent field of 2^(scale - ref + kScaleBias): never below 1 here, so both halves fit one 32-bit multiply-add
-    const uint32_t bias = (uint32_t)(15 + kScaleBias - w.ref) * (0x10001u << 10);
+    // exponent field of 2^(scale - ref): never below 1 here, so both halves fit one 32-bit multiply-add
+    const uint32_t bias = (uint32_t)(15 - w.ref) * (0x10001u << 10);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         uint32_t sw[kNb], v[4][kW];             // scales: [h, block pair] words of (A.j, B.j, A.j+1, B.j+1); codes
@@ -335,7 +335,7 @@ __device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t ti
     uint32_t sw[kNb];
     lds_words<kNb>(tile + T::kVs + 16 * kNb * u + 4 * kNb * tig, sw);
     const uint32_t row = tile + T::kV + (16 * u + tig) * T::kRow + 2 * kNb * g;
-    const uint32_t bias = ((uint32_t)(127 + kScaleBias - w.ref) & 0xFFFFu) * 0x10001u;
+    const uint32_t bias = ((uint32_t)(127 + kWeightBias - w.ref) & 0xFFFFu) * 0x10001u;
     auto widen = [](uint32_t h) {
         const float2 f = __half22float2(*reinterpret_cast<__half2 *>(&h));
         return pack_bf162(f.x, f.y);
@@ -661,7 +661,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 // ---- relative to the running maximum; what a row does not see; a new maximum ----
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const uint64_t f = pair2(factor[nt][0], factor[nt][1]), m = pair2(-w.m[nt][0], -w.m[nt][1]);
+                    const uint64_t f = pair2(factor[nt][0], factor[nt][1]), m = pair2(kWeightBias - w.m[nt][0], kWeightBias - w.m[nt][1]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -704,10 +704,10 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
 #pragma unroll
                             for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
                             const bool none = w.over[nt][e] == -INFINITY;      // no token seen before: m is 0 for want of a better
-                            float up = none ? v : fmaxf(v, 0.f);               // how far the maximum rises
+                            float up = none ? v - kWeightBias : fmaxf(v - kWeightBias, 0.f);      // how far the maximum rises
                             f[nt][e] = none ? 1.f : exp2_fast(-up);
                             if (v == -INFINITY) up = 0.f;
-                            else w.over[nt][e] = kMaxSlack;
+                            else w.over[nt][e] = kWeightBias + kMaxSlack;
                             w.m[nt][e] += up;
                             w.l[nt][e] *= f[nt][e];
 #pragma unroll
@@ -782,7 +782,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 const float small = __uint_as_float((uint32_t)(127 - max(range, 0)) << 23);
                 const bool plain = __all_sync(0xffffffffu, all_le_half2(pack_half2(small, small), least)) && range >= kHalfRange - kScaleSpread && !nan;   // (NaN compares false)
                 float low = 1.f;             // the smallest weight that is not zero
-                const float tiny = small * small;
+                // tiers below `small`: each as wide as what FP16 holds, 2^width
+                const int width = range + kWeightBias;
+                const float step = __uint_as_float((uint32_t)(127 - max(width, 0)) << 23), tiny = small * step;
                 if (!plain) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
@@ -800,18 +802,18 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
 #pragma unroll
                             for (int h = 0; h < 2; ++h) p[u][nt][h] = transpose8x8(pk[u][nt][h]);
                     add_values<D, NT, 1>(w, tile, g, tig, p, p, 1.f, 1.f);
-                } else if (!nan && range >= kHalfRange - kScaleSpread && !__any_sync(0xffffffffu, low < tiny * tiny)) {
-                    // tiers 3 and 2 if there are such weights, then 1 and 0: tier i holds weights in small^(i+1) .. small^i
-                    const float up = __uint_as_float((uint32_t)(127 + range) << 23);
+                } else if (!nan && range >= kHalfRange - kScaleSpread && !__any_sync(0xffffffffu, low < tiny * step * step)) {
+                    // tiers 3 and 2 if there are such weights, then 1 and 0: tier i > 0 holds weights in small * step^i .. small * step^(i - 1)
+                    const float up = __uint_as_float((uint32_t)(127 + width) << 23);
                     const bool four = __any_sync(0xffffffffu, low < tiny);
 #pragma unroll 1
                     for (int pass = four ? 0 : 1; pass < 2; ++pass) {
-                        const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part_ = pass == 0 ? tiny * small : small;
+                        const float gain = pass == 0 ? up * up : 1.f, bound = pass == 0 ? tiny : INFINITY, part_ = pass == 0 ? tiny * step : small;
                         const float from = pass == 1 && four ? tiny : 0.f;
                         if (four) {
                             float ff[NT][2];
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : tiny;
+                            for (int nt = 0; nt < NT; ++nt) ff[nt][0] = ff[nt][1] = pass == 0 ? up * up : step * step;
                             rescale(w, ff);
                         }
                         uint32_t p[2][NT][2], deep[2][NT][2];
@@ -831,9 +833,10 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                                     p[u][nt][h] = transpose8x8(pack_half2(hi_[0], hi_[1]));
                                     deep[u][nt][h] = transpose8x8(pack_half2(lo_[0], lo_[1]));
                                 }
-                        add_values<D, NT, 2>(w, tile, g, tig, p, deep, up, small);
+                        add_values<D, NT, 2>(w, tile, g, tig, p, deep, up, step);
                     }
                 } else {
+                    constexpr float kUnbias = 1.f / (1 << kWeightBias);          // (the factor goes to the scales, which may lie 126 and more below ref)
 #pragma unroll 1
                     for (int part_ = 0; part_ < 2; ++part_)       // the weights' upper and lower eight bits
 #pragma unroll
@@ -843,7 +846,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                                 for (int h = 0; h < 2; ++h) {
-                                    const float x0 = x[u][nt][2 * h], x1 = x[u][nt][2 * h + 1];
+                                    const float x0 = x[u][nt][2 * h] * kUnbias, x1 = x[u][nt][2 * h + 1] * kUnbias;
                                     uint32_t b = pack_bf162(x0, x1);
                                     if (part_ == 1) b = pack_bf162(x0 - __uint_as_float(b << 16), x1 - __uint_as_float(b & 0xFFFF0000u));
                                     p[nt][h] = transpose8x8(b);
@@ -865,7 +868,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 if (!arrived) w.l[nt][e] = NAN;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
-                if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.over[nt][e] == -INFINITY ? -INFINITY : w.m[nt][e], sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
+                if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.over[nt][e] == -INFINITY ? -INFINITY : w.m[nt][e] - kWeightBias, sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
             }
         whole = parts == 1;
         mine_now = {b, sg.head, sg.r0, nrows, parts, slot0};
@@ -883,7 +886,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     for (int j = 0; j < kNb; ++j) {
                         float v[4] = {w.o[2 * j][nt][e], w.o[2 * j][nt][2 + e], w.o[2 * j + 1][nt][e], w.o[2 * j + 1][nt][2 + e]};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127 - kScaleBias);
+                        for (int i = 0; i < 4; ++i) v[i] = scale_by_power(v[i] * inv, w.ref - 127);
                         *reinterpret_cast<float4 *>(dst + 32 * j) = make_float4(v[0], v[1], v[2], v[3]);
                     }
                 }

@@ -335,6 +335,28 @@ def test_attention_values_of_very_different_size(shift, d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [0.5, 1.0, 7 / 6, 4 / 3, 1.5, 2.0, 4.0])
+def test_attention_small_weights_where_the_large_ones_meet_zeros(scale, d):
+    """One token takes nearly all the weight, but holds zeros in half of the elements: there the result is the others', whose
+    weights are e^-6 .. e^-48 of the largest, and must be right to its own size."""
+    s = Setup(30, [96, 700], d, 2, 32)
+
+    def big(b, k, v):
+        k[:] = 0
+        k[..., 0] = -12.0
+        k[0, 3] = 0
+        v[..., 31::32] = 6.0             # every block has the same scale
+        v[0, 3] = 4.0
+        v[0, 3].view(2, d // 32, 32)[:, :, :16] = 0
+        return k, v
+
+    s.fill_cache(0, big=big)
+    q = torch.zeros(2, 1, 4, d)
+    q[..., 0] = 1.0
+    check_attention(s, 0, q.to(torch.bfloat16), scale=scale)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("bad", [0xFF, 0xFE, 0xF0])
 def test_what_a_row_does_not_see_does_not_touch_it(bad, d):
     """The pool outside the sequences, the tokens behind a sequence's end on its last page, and the drafted tokens a row
