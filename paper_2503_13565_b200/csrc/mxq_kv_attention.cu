@@ -17,7 +17,7 @@
 //     exponent common to the warp's accumulators) and the smallest.  Weights below that are still right to 11 bits: a tile that has any
 //     adds them in a second product over accumulators scaled up by the width of the first (two tiers; four for weights smaller
 //     yet).  A tile with weights or scales spread even wider, or a NaN scale, takes the step in BF16, whose range holds any, with
-//     the weights as a sum of two BF16 numbers.  (All wide: 0.61 ms on the long case below; tiers: 0.28.)
+//     the weights as a sum of two BF16 numbers.  (The tiers took the long case below, peaked weights, from 0.61 to 0.39 ms.)
 //   - S^T leaves the tensor core with a lane holding one token and two rows; the second product wants one row and two
 //     tokens: one 8x8 transposition (movmatrix) per packed register.
 //
@@ -30,14 +30,14 @@
 // CTA that delivered the last of them adds them up in that order.  Nobody waits for it, and it learns that it was the last one item
 // later, when the ticket's answer has long arrived.  So which CTA did what does not show in the result.
 //
-// What bounds it.  Not the bytes: 2 x 131071 tokens of 32 heads (1.14 GB) take 244 us with even weights, 4.7 TB/s = 71 % of the copy rate,
-// 276 us (63 %) with peaked ones, whose tiles need the tiers; bringing the tiles in without computing takes 177 us.  A warp spends
+// What bounds it.  Not the bytes: 2 x 131071 tokens of 32 heads (1.14 GB) take 248 us with even weights, 4.6 TB/s = 70 % of the copy rate,
+// 267 us (65 %) with peaked ones, whose tiles need the tiers; bringing the tiles in without computing takes 177 us.  A warp spends
 // some 600 instructions on a tile, half of them on the integer pipe (half rate: unpacking nibbles into the order of the products, scale
-// bytes), which is 55 % busy; the rest is latency of one warp's chain of products, shuffles and exponentials with only
+// bytes), which is 52 % busy; the rest is latency of one warp's chain of products, shuffles and exponentials with only
 // 12 warps per SM to hide it (the accumulators and both operands of 32 x 128 tiles: 168 registers).  More warps or more work per
 // warp spill, and spills lose more than they give: the L1 is what the rings leave.  32 decode rows over 100 to 4000 tokens (77.5 MB):
 // 39 us, 20 of them without computing; one row over 2047 tokens: 13 us, 9 without computing: launch, the division of the work, one
-// item of two tiles per warp, the join; tree verification, 8 x 16 rows, head dimension 64: 38 us, 23 without computing.  Requesting the next
+// item of two tiles per warp, the join; tree verification, 8 x 16 rows, head dimension 64: 36 us, 23 without computing.  Requesting the next
 // item's tiles before this one's result is put together gained nothing (the SM's other CTAs fill the gap) and cost registers.
 #include <math.h>
 
@@ -66,9 +66,12 @@ struct KvQuery {
 constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;                  // tiles in a warp's ring
 // The sizes of items.  An item costs about two tiles' time by itself, and the last ones leave CTAs idle for up to an item's time.  With
-// kTwoSizes tiles or more per CTA, three quarters of every segment go into items of four tenths of a CTA's share, drawn first, the rest into
-// items of a tenth (2 x 131071 tokens, 591 tiles per CTA, even weights: 244 us; all items of half a share, at most kItemTiles tiles: 271; 32 x
-// 16384 tokens of 8 heads: 142 and 150); below that all items are of half a CTA's share, at most kItemTiles tiles (32 sequences of 100 to 4000
+// kTwoSizes tiles or more per CTA, three quarters of every segment go into big items, drawn first, the rest into small ones of a tenth of a
+// CTA's share, at least kSmallTiles (2 x 131071 tokens, 591 tiles per CTA, even weights: 244 us; all items of half a share, at most kItemTiles tiles:
+// 271; 32 x 16384 tokens of 8 heads: 142 and 150).  A big one is three tenths of a share with one column block (peaked weights, 2 x 131071 tokens: 267 us,
+// four small ones 280; 4 x 16384 tokens of 32 heads, where four small ones are two thirds of a share: 86 and 107), but kBigSmalls small
+// ones with two, whose results are twice as long to put together (even weights, 8 x 16384 tokens of 8 heads, 16 rows: 74 us, three tenths 89).
+// Below kTwoSizes all items are of half a CTA's share, at most kItemTiles tiles (32 sequences of 100 to 4000
 // tokens, 40 tiles per CTA: 39 us, two sizes 68; tree verification, 23 per CTA: 40 us, two sizes 47).
 // With less than kOneRound tiles per CTA items have that many, two per warp, the ring's depth: fewer would leave part of it empty.
 constexpr uint32_t kTwoSizes = 96, kItemTiles = 48, kSmallTiles = 24, kBigSmalls = 4, kOneRound = 8;
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         const uint32_t share = (uint32_t)min(work / gridDim.x, (uint64_t)1 << 30);      // of a CTA
         if (share >= kTwoSizes) {
             small = (max(kSmallTiles, share / 10) + kAttWarps - 1) / kAttWarps * kAttWarps;
-            big = kBigSmalls * small;
+            big = NT == 1 ? max(small, share * 3u / 10u / kAttWarps * kAttWarps) : kBigSmalls * small;
         } else {
             small = share < kOneRound ? kOneRound : min(kItemTiles, share / 2 + kAttWarps) / kAttWarps * kAttWarps;
         }
@@ -976,16 +979,25 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 }
                 __syncthreads();
                 // four elements of a row per thread; with few rows several threads share the parts
-                constexpr int kCols = D / 4;
+                constexpr int kCols = D / 4, kAhead = 8;       // loads in flight per thread (one request of 100000 tokens: 64 us, a loop unrolled by four 72)
                 const int tasks = nrows * kCols, shares = tasks < kAttThreads ? kAttThreads / tasks : 1;
                 auto add_parts = [&](int task, int from, int stride) {
                     const int r = task / kCols, d = 4 * (task % kCols);
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4       // (8: tree verification 40 us, 4: 38)
-                    for (int i = from; i < (int)parts; i += stride) {
-                        const float f = table[i * nrows + r].x;
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + r * D + d, 16, a.partials, ws_bytes)));
-                        v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
+                    for (int i0 = from; i0 < (int)parts; i0 += kAhead * stride) {
+                        float4 x[kAhead];
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) {
+                            const int i = i0 + u * stride;
+                            x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (i < (int)parts) x[u] = __ldcg(reinterpret_cast<const float4 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + r * D + d, 16, a.partials, ws_bytes)));
+                        }
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) {
+                            const int i = i0 + u * stride;
+                            const float f = i < (int)parts ? table[i * nrows + r].x : 0.f;
+                            v.x += f * x[u].x, v.y += f * x[u].y, v.z += f * x[u].z, v.w += f * x[u].w;
+                        }
                     }
                     return v;
                 };
