@@ -44,6 +44,7 @@
 #include <type_traits>
 
 #include "mxq_kv.cuh"
+#include "mxq_kv_division.h"
 #include "mxq_tcgen05.cuh"
 
 namespace mxq {
@@ -63,19 +64,6 @@ struct KvQuery {
     uint32_t slots;
 };
 
-constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
-constexpr int kAttStages = 2;                  // tiles in a warp's ring
-// The sizes of items.  An item costs about two tiles' time by itself, and the last ones leave CTAs idle for up to an item's time.  With
-// kTwoSizes tiles or more per CTA, three quarters of every segment go into big items, drawn first, the rest into small ones of a tenth of a
-// CTA's share, at least kSmallTiles (2 x 131071 tokens, 591 tiles per CTA, even weights: 244 us; all items of half a share, at most kItemTiles tiles:
-// 271; 32 x 16384 tokens of 8 heads: 142 and 150).  A big one is three tenths of a share with one column block (peaked weights, 2 x 131071 tokens: 267 us,
-// four small ones 280; 4 x 16384 tokens of 32 heads, where four small ones are two thirds of a share: 86 and 107), but kBigSmalls small
-// ones with two, whose results are twice as long to put together (even weights, 8 x 16384 tokens of 8 heads, 16 rows: 74 us, three tenths 89).
-// Below kTwoSizes all items are of half a CTA's share, at most kItemTiles tiles (32 sequences of 100 to 4000
-// tokens, 40 tiles per CTA: 39 us, two sizes 68; tree verification, 23 per CTA: 40 us, two sizes 47).
-// With less than kOneRound tiles per CTA items have that many, two per warp, the ring's depth: fewer would leave part of it empty.
-constexpr uint32_t kTwoSizes = 96, kItemTiles = 48, kSmallTiles = 24, kBigSmalls = 4, kOneRound = 8;
-
 constexpr int kWeightBias = 10;                // weights carry a factor 2^10 from the exponential on: in FP16 they keep 11 bits down to 2^-14
 constexpr float kMaxSlack = 4.f;               // how far (log2) a score may exceed the running maximum
 constexpr int kScaleHeadroom = 1;              // how far (log2) a V scale may exceed `ref`: P * 2^(scale - ref) <= 2^(10 + 4 + 1) fits FP16,
@@ -85,17 +73,16 @@ constexpr int kScaleLag = 3;                   // how far (log2) a tile's larges
 constexpr int kScaleDrop = 12;                 // how far ref may fall below its highest: accumulators are below 2^18 per token, and
                                                // the deepest of the tiers below scales them by up to 2^72
 
-// rows of the flattened (token row, head of the group) index per tile of NT column blocks
 template <int NT>
-constexpr int kAttRows = 8 * NT;
+constexpr int kAttRows = att_rows(NT);
 template <int D, int NT>
-constexpr int kAttCtasPerSm = NT == 1 ? (D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
+constexpr int kAttCtasPerSm = att_ctas_per_sm(D, NT);
 template <int D, int NT>
 constexpr size_t kAttSlotFloats = (size_t)kAttRows<NT> * (D + 2);
 template <int D, int NT>
-constexpr uint32_t kAttMaxParts = (uint32_t)((kAttWarps * kAttStages * KvTile<D>::kBytes - kAttThreads * 16) / (kAttRows<NT> * 8));   // parts of a segment
+constexpr uint32_t kAttMaxParts = att_max_parts(D, NT);   // parts of a segment
 template <int D, int NT>
-constexpr size_t kAttSmem = (size_t)kAttWarps * kAttStages * KvTile<D>::kBytes;
+constexpr size_t kAttSmem = (size_t)att_smem(D);
 
 // ---- fragments ------------------------------------------------------------------------------------------------------------
 
@@ -218,12 +205,9 @@ struct Segment {
 // columns 2 * tig and 2 * tig + 1.
 __device__ unsigned int g_kv_status = 0;   // sticky: bit 0 a requested tile never arrived
 
-struct Cut {
-    uint32_t small, bigs, parts;  // of a segment: tiles of its small items, number of its big ones, of all its items
-};
 struct Owner {                    // the items that a thread's sequences own, and the first of these sequences
     uint32_t big_lo, big_count, small_lo, small_count, slot_lo, tiles;
-    Cut cut;
+    AttCut cut;
     int len, rows;
 };
 struct Part {                     // a segment whose part has been delivered: its rows, how many parts it has, the first one's slot
@@ -393,6 +377,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * T::kBytes;
     float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][row][D + 4], between items
     constexpr int kMergeRow = D + 4;
+    static_assert(T::kBytes * kAttWarps * kAttStages == att_smem(D), "the rings are the shared memory the join's table has");
     static_assert(kAttWarps * kAttRows<NT> * kMergeRow * 4 <= kAttWarps * kAttStages * T::kBytes, "the merge buffer lies over the rings");
 
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
@@ -410,14 +395,13 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         n = rows == 0 ? 1u : max(1u, ((uint32_t)len + kTileTokens - 1) / kTileTokens);      // (no rows: nothing to read, nothing to join)
         tiles = max(1u, (uint32_t)(rows * a.group + kAttRows<NT> - 1) / kAttRows<NT>);
     };
-    uint32_t small = 0, big = 0;                   // tiles of an item; 0: no big ones
-    auto cut_of = [&](uint32_t n) {                // of a segment of n tiles (its parts must fit the join's table)
-        Cut k;
-        k.small = max(small, (n + kAttWarps * kAttMaxParts<D, NT> - 1) / (kAttWarps * kAttMaxParts<D, NT>) * kAttWarps);
-        k.bigs = big == 0 ? 0u : (n - n / 4) / big;
-        k.parts = k.bigs + max(1u, (n - k.bigs * big + k.small - 1) / k.small);
-        return k;
-    };
+    // Two column blocks' accumulators at head dimension 128 leave no register for the sizes: there they stay in shared
+    // memory (8 x 8 rows over 16384 tokens: 170 us, in registers 184); elsewhere reading them costs more (tree verification: 37.1 us, in registers 36.6).
+    constexpr bool kSizesShared = D == 128 && NT == 2;
+    __shared__ AttSizes sh_sizes;
+    AttSizes sizes_own = {0, 0};
+    const AttSizes &sizes = kSizesShared ? sh_sizes : sizes_own;
+    auto cut_of = [&](uint32_t n) { return att_cut(sizes, n, kAttMaxParts<D, NT>); };
     const int each = (s.B + kAttThreads - 1) / kAttThreads, b_first = tid * each, b_last = min(s.B, b_first + each);
     uint32_t bigs, items;                          // all big items, all items
     {
@@ -437,17 +421,14 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         work = 0;
         for (int w = 0; w < kAttWarps; ++w) work += sh_scan[w][0];
         const uint32_t share = (uint32_t)min(work / gridDim.x, (uint64_t)1 << 30);      // of a CTA
-        if (share >= kTwoSizes) {
-            small = (max(kSmallTiles, share / 10) + kAttWarps - 1) / kAttWarps * kAttWarps;
-            big = NT == 1 ? max(small, share * 3u / 10u / kAttWarps * kAttWarps) : kBigSmalls * small;
-        } else {
-            small = share < kOneRound ? kOneRound : min(kItemTiles, share / 2 + kAttWarps) / kAttWarps * kAttWarps;
-        }
+        if constexpr (!kSizesShared) sizes_own = att_sizes(share, NT);
+        else if (tid == 0) sh_sizes = att_sizes(share, NT);
+        __syncthreads();                           // (and sh_scan is free again)
         uint64_t mine[2] = {0, 0};                 // big items and small ones; slots (items of segments that are cut)
         for (int i = b_first; i < b_last; ++i) {
             uint32_t n, tiles;
             shape_of(i == b_first ? len0 : s.len(i), i == b_first ? rows0 : s.nrows(i), n, tiles);
-            const Cut k = cut_of(n);
+            const AttCut k = cut_of(n);
             const uint32_t segs = tiles * (uint32_t)c.heads;
             mine[0] += (uint64_t)k.bigs * segs | (uint64_t)(k.parts - k.bigs) * segs << 32;
             mine[1] += k.parts > 1 ? (uint64_t)k.parts * segs : 0;
@@ -460,7 +441,6 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 const uint64_t before = __shfl_up_sync(0xffffffffu, upto[e], o);
                 if (lane >= o) upto[e] += before;
             }
-        __syncthreads();
         if (lane == 31) sh_scan[warp][0] = upto[0], sh_scan[warp][1] = upto[1];
         __syncthreads();
         for (int w = 0; w < kAttWarps; ++w) {
@@ -492,7 +472,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         const uint32_t lo = is_big ? mine.big_lo : mine.small_lo;
         if (have && item - lo < (is_big ? mine.big_count : mine.small_count)) {
             uint32_t at = lo, slot = mine.slot_lo, tiles = mine.tiles;
-            Cut k = mine.cut;
+            AttCut k = mine.cut;
             int i = b_first, len = mine.len, rows = mine.rows;
             for (;;) {
                 const uint32_t segs = tiles * (uint32_t)c.heads, count = (is_big ? k.bigs : k.parts - k.bigs) * segs;
@@ -507,7 +487,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             const uint32_t of = is_big ? k.bigs : k.parts - k.bigs, seg = of == 1 ? item - at : (item - at) / of, p = item - at - seg * of;
             sh_item[0] = i, sh_item[1] = len, sh_item[2] = rows, sh_item[3] = (int)seg, sh_item[4] = (int)tiles, sh_item[5] = (int)k.parts;
             sh_item[6] = (int)(is_big ? p : k.bigs + p), sh_item[7] = (int)(slot + seg * k.parts);
-            sh_item[8] = (int)(is_big ? p * big : k.bigs * big + p * k.small), sh_item[9] = (int)(is_big ? big : k.small);
+            sh_item[8] = (int)(is_big ? p * k.big : k.bigs * k.big + p * k.small), sh_item[9] = (int)(is_big ? k.big : k.small);
         }
         __syncthreads();
         bool whole = true;
@@ -1057,11 +1037,8 @@ static int att_column_blocks(int M, int group) { return (int64_t)M * group <= 8 
 template <int D, int NT>
 static int att_grid() { return sm_count() * kAttCtasPerSm<D, NT>; }
 
-// Workspace: the counter, a ticket per cut segment (under its first part's slot), slots for the parts.  No part but a segment's last is
-// smaller than a small item, so a cut segment of n tiles has at most 2 n / small of them; a small item is at least a tenth of a CTA's share
-// (rounded down, at least 24), which bounds all parts by 22 per CTA.  Counter and tickets lie in the same place for every shape, so that
-// calls of different shapes may share a workspace: they find them zero.
-constexpr uint32_t kAttSlotsPerCta = 24;
+// Workspace: the counter, a ticket per cut segment (under its first part's slot), slots for the parts.  Counter and tickets lie in the
+// same place for every shape, so that calls of different shapes may share a workspace: they find them zero.
 constexpr int kAttMostCtasPerSm = 4;
 static size_t att_partials_offset() { return 16 + (((size_t)kAttSlotsPerCta * kAttMostCtasPerSm * sm_count() * 4 + 255) / 256 * 256); }
 template <int D, int NT>
