@@ -7,6 +7,7 @@ library is missing, or a call returns a non-zero status, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import threading
@@ -134,6 +135,15 @@ def _stream(stream=None) -> int:
     if stream is None:   # (the raw handle of the current stream: a stream object would cost as much as a kernel launch)
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
+
+
+def _on(stream):
+    """Context for what the binding allocates for a call on ``stream``: its fill runs there, before the kernel, and the allocator gives
+    its memory to nobody else while the kernel runs.  (An output made so belongs to that stream, like the kernel that fills it.)"""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
+
+
+_CURRENT = contextlib.nullcontext()
 
 
 def _dev(t: torch.Tensor, dtype, what: str) -> int:
@@ -660,8 +670,9 @@ def mxq_kv_read(cache: KVCache, layer: int, tables: torch.Tensor, lens: torch.Te
     """What one layer of the cache holds for the last ``m`` (or rows[b]) tokens of every sequence: K, V [B, m, kv_heads, D]
     BF16, exactly; zero where there is no such token."""
     b, tp, w, lp = _kv_seqs(tables, lens)
-    k = torch.empty((b, m, cache.kv_heads, cache.head_dim), dtype=torch.bfloat16, device=tables.device)
-    v = torch.empty_like(k)
+    with _on(stream):
+        k = torch.empty((b, m, cache.kv_heads, cache.head_dim), dtype=torch.bfloat16, device=tables.device)
+        v = torch.empty_like(k)
     _check(lib().mxq_kv_read(cache.ptr, layer, k.data_ptr(), v.data_ptr(), b, m, tp, w, lp, _kv_ints(rows, (b,), "rows"), _stream(stream)), "mxq_kv_read")
     return k, v
 
@@ -676,24 +687,25 @@ def mxq_kv_attention(q: torch.Tensor, cache: KVCache, layer: int, tables: torch.
     """Attention of the rows q [B, M, q_heads, D] BF16 over one layer of the cache, whose last rows[b] tokens they are (see
     mxq.h).  ``tree`` int64 [B, M] (bits as uint64): which of the rows each row sees, itself included; None: causal.
     ``scale`` defaults to D ** -0.5.  Returns O [B, M, q_heads, D] BF16, with ``with_lse`` also lse [B, M, q_heads] FP32.
-    ``workspace``: from ``new_workspace(mxq_kv_attention_workspace_bytes(...))``, zero-filled once, one per stream."""
+    ``workspace``: from ``new_workspace(mxq_kv_attention_workspace_bytes(...))``, zero-filled once, one per stream.  What is not
+    given is allocated on the stream the call runs on (so in every call on the cache)."""
     b, tp, w, lp = _kv_seqs(tables, lens)
     _, m, hq, d = q.shape
     shape = (b, m, hq, cache.head_dim)
     qp, qs = _token_rows(q, shape, "q")
-    if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
-    elif out.shape != shape:
+    if out is not None and out.shape != shape:
         raise ValueError("out must be [B, M, q_heads, D]")
-    if lse is not None:
-        if lse.shape != shape[:3]:
-            raise ValueError("lse must be [B, M, q_heads]")
-    elif with_lse:
-        lse = torch.empty(shape[:3], dtype=torch.float32, device=q.device)
+    if lse is not None and lse.shape != shape[:3]:
+        raise ValueError("lse must be [B, M, q_heads]")
     if tree is not None and tree.shape != (b, m):
         raise ValueError("tree must be [B, M]")
-    if workspace is None:
-        workspace = new_workspace(mxq_kv_attention_workspace_bytes(b, m, hq, cache.kv_heads, d), q.device)
+    with _on(stream):
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        if lse is None and with_lse:
+            lse = torch.empty(shape[:3], dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = new_workspace(mxq_kv_attention_workspace_bytes(b, m, hq, cache.kv_heads, d), q.device)
     _check(lib().mxq_kv_attention(cache.ptr, layer, qp, qs, b, m, hq, tp, w, lp, _kv_ints(rows, (b,), "rows"),
                                   0 if tree is None else _dev(tree, torch.int64, "tree"), d ** -0.5 if scale is None else scale,
                                   _dev(out, torch.bfloat16, "out"), 0 if lse is None else _dev(lse, torch.float32, "lse"),
@@ -719,7 +731,8 @@ def mxq_kv_fork(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, src: t
     b, tp, w, lp = _kv_seqs(tables, lens)
     n = int(src.shape[0])
     if workspace is None:
-        workspace = new_workspace(mxq_kv_fork_workspace_bytes(n), tables.device)
+        with _on(stream):
+            workspace = new_workspace(mxq_kv_fork_workspace_bytes(n), tables.device)
     _check(lib().mxq_kv_fork(cache.ptr, b, tp, w, lp, n, _kv_ints(src, (n,), "src"), _kv_ints(dst, (n,), "dst"),
                              _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_kv_fork")
 
@@ -731,7 +744,8 @@ def mxq_kv_compact(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, row
     b, tp, w, lp = _kv_seqs(tables, lens)
     m = int(keep.shape[1])
     if lens_out is None:
-        lens_out = torch.empty(b, dtype=torch.int32, device=tables.device)
+        with _on(stream):
+            lens_out = torch.empty(b, dtype=torch.int32, device=tables.device)
     _check(lib().mxq_kv_compact(cache.ptr, b, m, tp, w, lp, _kv_ints(rows, (b,), "rows"), _kv_ints(keep, (b, m), "keep"),
                                 _kv_ints(kept, (b,), "kept"), _kv_ints(lens_out, (b,), "lens_out"), _stream(stream)), "mxq_kv_compact")
     return lens_out

@@ -242,7 +242,7 @@ kv_fork_copy_kernel(const ForkJob *jobs, int n, KvView c, int64_t layer_bytes, i
     pdl_wait();
     const uint4 j = ld_dep_u4(MXQ_AT(jobs + blockIdx.x, 16, jobs, (size_t)n * 16));
     const int tile = (int)blockIdx.z / pieces, piece = (int)blockIdx.z - tile * pieces;
-    if (tile >= (int)j.z) return;
+    if (tile >= (int)j.z || !kv_page_ok(c, (int)j.x) || !kv_page_ok(c, (int)j.y)) return;
     uint8_t *layer = c.base + (int64_t)blockIdx.y * layer_bytes;
     const int64_t off = tile * row_bytes, first = (int64_t)piece * kCopyPiece;
     const uint8_t *from = layer + (int64_t)(int)j.x * c.page_bytes + off;
