@@ -232,13 +232,15 @@ def mxq_accept_workspace_bytes(b: int, r: int, v: int) -> int:
 _default_ws = {}
 
 
-def _default_workspace(nbytes: int, device) -> torch.Tensor:
-    """A cached, zero-initialised workspace per device for callers that pass none."""
+def _default_workspace(nbytes: int, device, stream=None) -> torch.Tensor:
+    """A cached, zero-initialised workspace for callers that pass none: one per device, and one per stream for calls on a stream= of
+    their own (calls on two streams may overlap, and the zero fill must come before the call)."""
     key = (torch.device(device).type, torch.device(device).index if torch.device(device).index is not None
-           else torch.cuda.current_device())
+           else torch.cuda.current_device(), None if stream is None else stream.cuda_stream)
     ws = _default_ws.get(key)
     if ws is None or ws.numel() < nbytes:
-        ws = new_workspace(nbytes, device)
+        with _on(stream):
+            ws = new_workspace(nbytes, device)
         _default_ws[key] = ws
     return ws
 
@@ -252,10 +254,11 @@ def mxq_quantize(w: torch.Tensor, codes: torch.Tensor = None, scales: torch.Tens
                  nonfinite_blocks: torch.Tensor = None, stream=None):
     """BF16 W[N,K] -> (codes u8 [N,K/2], scales u8 [N,K/32])."""
     n, k = w.shape
-    if codes is None:
-        codes = torch.empty((n, k // 2), dtype=torch.uint8, device=w.device)
-    if scales is None:
-        scales = torch.empty((n, k // 32), dtype=torch.uint8, device=w.device)
+    with _on(stream):
+        if codes is None:
+            codes = torch.empty((n, k // 2), dtype=torch.uint8, device=w.device)
+        if scales is None:
+            scales = torch.empty((n, k // 32), dtype=torch.uint8, device=w.device)
     cnt = 0 if nonfinite_blocks is None else _dev(nonfinite_blocks, torch.int32, "nonfinite_blocks")
     _check(lib().mxq_quantize(_dev(w, torch.bfloat16, "W"), n, k, _dev(codes, torch.uint8, "codes"),
                               _dev(scales, torch.uint8, "scales"), cnt, _stream(stream)), "mxq_quantize")
@@ -265,7 +268,8 @@ def mxq_quantize(w: torch.Tensor, codes: torch.Tensor = None, scales: torch.Tens
 def mxq_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor = None, stream=None) -> torch.Tensor:
     n, k = codes.shape[0], codes.shape[1] * 2
     if out is None:
-        out = torch.empty((n, k), dtype=torch.bfloat16, device=codes.device)
+        with _on(stream):
+            out = torch.empty((n, k), dtype=torch.bfloat16, device=codes.device)
     _check(lib().mxq_dequantize(_dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), n, k,
                                 _dev(out, torch.bfloat16, "out"), _stream(stream)), "mxq_dequantize")
     return out
@@ -279,10 +283,11 @@ def mxq_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, out: 
     if codes.shape[1] * 2 != k or tuple(scales.shape) != (n, k // 32):
         raise ValueError("shape mismatch between X, codes and scales")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=x.device)
+        with _on(stream):
+            out = torch.empty((m, n), dtype=out_dtype, device=x.device)
     if workspace is None:
         need = mxq_linear_workspace_bytes(m, n, k)
-        workspace = _default_workspace(need, x.device) if need else None
+        workspace = _default_workspace(need, x.device, stream) if need else None
     ws_ptr, ws_bytes = (0, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace"), workspace.numel())
     _check(lib().mxq_linear(_dev(x, torch.bfloat16, "X"), m, _dev(codes, torch.uint8, "codes"),
                             _dev(scales, torch.uint8, "scales"), n, k, _dev(out, out.dtype, "Y"), _dt(out.dtype),
@@ -303,7 +308,7 @@ def mxq_linear_host(x_host: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
         raise ValueError("staging buffers too small")
     if workspace is None:
         need = mxq_linear_workspace_bytes(m, n, k)
-        workspace = _default_workspace(need, codes.device) if need else None
+        workspace = _default_workspace(need, codes.device, stream) if need else None
     ws_ptr, ws_bytes = (0, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace"), workspace.numel())
     _check(lib().mxq_linear_host(x_host.data_ptr(), m, _dev(codes, torch.uint8, "codes"),
                                  _dev(scales, torch.uint8, "scales"), n, k, y_host.data_ptr(), _dt(y_host.dtype),
@@ -313,16 +318,14 @@ def mxq_linear_host(x_host: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
 
 def mxq_greedy_accept(logits: torch.Tensor, draft: torch.Tensor, workspace: torch.Tensor = None, stream=None, out=None):
     """logits [B,R,V] (fp32 or bf16), draft [B,T] int32 -> (accept_len [B], next_token [B]) int32.  ``out``: optional
-    pair of int32 [B] tensors to write into (pass them when the call runs on another stream than the current one)."""
+    pair of int32 [B] tensors to write into (made here, they belong to the stream the call runs on)."""
     b, r, v = logits.shape
     t = draft.shape[1]
-    if workspace is None:
-        workspace = new_workspace(mxq_accept_workspace_bytes(b, r, v), logits.device)
-    if out is None:
-        g = torch.empty(b, dtype=torch.int32, device=logits.device)
-        nxt = torch.empty(b, dtype=torch.int32, device=logits.device)
-    else:
-        g, nxt = out
+    with _on(stream):
+        if workspace is None:
+            workspace = new_workspace(mxq_accept_workspace_bytes(b, r, v), logits.device)
+        g, nxt = out if out is not None else (torch.empty(b, dtype=torch.int32, device=logits.device) for _ in range(2))
+    if out is not None:
         if tuple(g.shape) != (b,) or tuple(nxt.shape) != (b,):
             raise ValueError("out must be two int32 tensors of shape [B]")
     _check(lib().mxq_greedy_accept(_dev(logits, logits.dtype, "logits"), _dt(logits.dtype), b, r, v,
@@ -355,8 +358,9 @@ def mxq_greedy_accept_static(logits: torch.Tensor, draft: torch.Tensor, accept_l
 def mxq_greedy_accept_tokens(draft: torch.Tensor, verifier: torch.Tensor, stream=None):
     b, t = draft.shape
     r = verifier.shape[1]
-    g = torch.empty(b, dtype=torch.int32, device=draft.device)
-    nxt = torch.empty(b, dtype=torch.int32, device=draft.device)
+    with _on(stream):
+        g = torch.empty(b, dtype=torch.int32, device=draft.device)
+        nxt = torch.empty(b, dtype=torch.int32, device=draft.device)
     _check(lib().mxq_greedy_accept_tokens(_dev(draft, torch.int32, "draft"), _dev(verifier, torch.int32, "verifier"),
                                           b, t, r, g.data_ptr(), nxt.data_ptr(), _stream(stream)),
            "mxq_greedy_accept_tokens")
@@ -376,11 +380,12 @@ def mxq_lm_head_accept(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     r, k = x.shape
     v = codes.shape[0]
     t = 0 if draft is None else int(draft.numel())
-    if workspace is None:
-        workspace = new_workspace(mxq_lm_head_accept_workspace_bytes(r, v, k), x.device)
-    verifier = torch.empty(r, dtype=torch.int32, device=x.device)
-    g = torch.empty(1, dtype=torch.int32, device=x.device)
-    nxt = torch.empty(1, dtype=torch.int32, device=x.device)
+    with _on(stream):
+        if workspace is None:
+            workspace = new_workspace(mxq_lm_head_accept_workspace_bytes(r, v, k), x.device)
+        verifier = torch.empty(r, dtype=torch.int32, device=x.device)
+        g = torch.empty(1, dtype=torch.int32, device=x.device)
+        nxt = torch.empty(1, dtype=torch.int32, device=x.device)
     _check(lib().mxq_lm_head_accept(_dev(x, torch.bfloat16, "x"), r, _dev(codes, torch.uint8, "codes"),
                                     _dev(scales, torch.uint8, "scales"), v, k,
                                     0 if draft is None else _dev(draft, torch.int32, "draft"), t,
@@ -395,7 +400,8 @@ def mxq_linear_bf16(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor = None, 
     m, k = x.shape
     n = w.shape[0]
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=x.device)
+        with _on(stream):
+            out = torch.empty((m, n), dtype=out_dtype, device=x.device)
     _check(lib().mxq_linear_bf16(_dev(x, torch.bfloat16, "x"), m, _dev(w, torch.bfloat16, "w"), n, k,
                                  _dev(out, out.dtype, "out"), _dt(out.dtype), _stream(stream)), "mxq_linear_bf16")
     return out
@@ -412,10 +418,11 @@ def mxq_linear_residual(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
     ``mxq_linear_fused_workspace_bytes(M, N, K)`` bytes (allocated here if None: pass one in a hot loop)."""
     m, k = x.shape
     n = codes.shape[0]
-    if out is None:
-        out = torch.empty((m, n), dtype=residual.dtype, device=x.device)
-    if workspace is None:
-        workspace = torch.empty(max(16, mxq_linear_fused_workspace_bytes(m, n, k)), dtype=torch.uint8, device=x.device)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((m, n), dtype=residual.dtype, device=x.device)
+        if workspace is None:
+            workspace = torch.empty(max(16, mxq_linear_fused_workspace_bytes(m, n, k)), dtype=torch.uint8, device=x.device)
     _check(lib().mxq_linear_residual(_dev(x, torch.bfloat16, "x"), m, _dev(codes, torch.uint8, "codes"),
                                      _dev(scales, torch.uint8, "scales"), n, k, _dev(residual, out.dtype, "residual"),
                                      _dev(out, out.dtype, "out"), _dt(out.dtype),
@@ -430,10 +437,11 @@ def mxq_linear_swiglu(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor
     matrix whose row 2i is gate row i and row 2i+1 up row i (``interleave_gate_up``)."""
     m, k = x.shape
     n = codes.shape[0]
-    if out is None:
-        out = torch.empty((m, n // 2), dtype=out_dtype, device=x.device)
-    if workspace is None:
-        workspace = torch.empty(max(16, mxq_linear_fused_workspace_bytes(m, n, k)), dtype=torch.uint8, device=x.device)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((m, n // 2), dtype=out_dtype, device=x.device)
+        if workspace is None:
+            workspace = torch.empty(max(16, mxq_linear_fused_workspace_bytes(m, n, k)), dtype=torch.uint8, device=x.device)
     _check(lib().mxq_linear_swiglu(_dev(x, torch.bfloat16, "x"), m, _dev(codes, torch.uint8, "codes"),
                                    _dev(scales, torch.uint8, "scales"), n, k, _dev(out, out.dtype, "out"), _dt(out.dtype),
                                    _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)),
@@ -533,7 +541,8 @@ def mxq_linear_batch(layers, workspace: torch.Tensor = None, stream=None) -> Lin
     (zero-filled once; reusable by calls in one stream)."""
     batch = layers if isinstance(layers, LinearBatch) else LinearBatch(layers)
     if workspace is None:
-        workspace = new_workspace(batch.workspace_bytes(), batch.device)
+        with _on(stream):
+            workspace = new_workspace(batch.workspace_bytes(), batch.device)
     batch.run(workspace, stream)
     return batch
 

@@ -80,3 +80,31 @@ def test_fork_and_compact(sequences):
     assert torch.equal(got, want) and torch.equal(tables, t2) and torch.equal(lens, l2) and torch.equal(cache.refs, twin.refs)
     assert np.array_equal(cache.pages.cpu().numpy(), twin.pages.cpu().numpy())
     del blocks
+
+
+def test_layers_on_two_streams_at_once():
+    """Split layers (whose workspace holds counters) on two streams side by side, nothing passed but the operands."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = [mxq.mxq_quantize(torch.randn(1024, 4096, generator=g, device="cuda").bfloat16()) for _ in range(2)]
+    x = [torch.randn(m, 4096, generator=g, device="cuda").bfloat16() for m in (1, 8)]
+    want = [[mxq.mxq_linear(a, *b) for a in x] for b in w]
+    wc = mxq.mxq_quantize(x[1])
+    draft = torch.zeros(7, dtype=torch.int32, device="cuda")
+    wv = mxq.mxq_lm_head_accept(x[1], *w[0], draft)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    dirty(mxq.mxq_linear_workspace_bytes(8, 1024, 4096))
+    dirty(mxq.mxq_lm_head_accept_workspace_bytes(8, 1024, 4096))
+    torch.cuda.synchronize()
+    torch.cuda._sleep(BUSY)
+    got = [[] for _ in sides]
+    for _ in range(20):
+        for i, s in enumerate(sides):
+            got[i].append([mxq.mxq_linear(a, *w[i], stream=s) for a in x])
+    codes = mxq.mxq_quantize(x[1], stream=sides[0])
+    tokens = mxq.mxq_lm_head_accept(x[1], *w[0], draft, stream=sides[1])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for ys in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(ys, want[i]))
+    assert all(torch.equal(a, b) for a, b in zip(codes + tokens, wc + wv))
+    assert mxq.mxq_linear_device_status() == 0

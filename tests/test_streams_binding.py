@@ -89,3 +89,36 @@ def test_cache_calls_allocate_on_the_stream_they_run_on(call, record):
     record.made.clear()
     call(None)
     assert record.launches == [77, None] and record.made and set(record.made) == {None}
+
+
+W, X = (torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(8, 2, dtype=torch.uint8)), torch.ones(3, 64, dtype=torch.bfloat16)
+Y, BIG, LOGITS, DRAFT, TOKENS = torch.ones(3, 8), torch.ones(1000), torch.ones(2, 4, 100), torch.ones(2, 3), torch.ones(2, 4)
+LAYERS = {
+    "quantize": lambda s: mxq.mxq_quantize(X, stream=s),
+    "dequantize": lambda s: mxq.mxq_dequantize(*W, stream=s),
+    "linear": lambda s: mxq.mxq_linear(X, *W, stream=s),
+    "linear_host": lambda s: mxq.mxq_linear_host(X, *W, Y, BIG, BIG, stream=s),
+    "linear_bf16": lambda s: mxq.mxq_linear_bf16(X, torch.ones(8, 64), stream=s),
+    "linear_residual": lambda s: mxq.mxq_linear_residual(X, *W, Y, stream=s),
+    "linear_swiglu": lambda s: mxq.mxq_linear_swiglu(X, *W, stream=s),
+    "linear_batch": lambda s: mxq.mxq_linear_batch([dict(x=X, codes=W[0], scales=W[1], out=Y)], stream=s),
+    "greedy_accept": lambda s: mxq.mxq_greedy_accept(LOGITS, DRAFT, stream=s),
+    "greedy_accept_tokens": lambda s: mxq.mxq_greedy_accept_tokens(DRAFT, TOKENS, stream=s),
+    "lm_head_accept": lambda s: mxq.mxq_lm_head_accept(X, *W, stream=s),
+}
+
+
+@pytest.mark.parametrize("name", LAYERS)
+def test_layer_calls_allocate_on_the_stream_they_run_on(name, record, monkeypatch):
+    monkeypatch.setattr(binding, "_any_mem", lambda t, dtype, what: t.data_ptr())
+    LAYERS[name](STREAM)
+    assert record.launches == [77] and record.made and set(record.made) == {77}
+    record.made.clear()
+    LAYERS[name](None)
+    assert record.launches == [77, None] and record.made and set(record.made) == {None}
+
+
+def test_workspaces_kept_for_callers_that_pass_none_are_one_per_stream(record):
+    for s in (None, STREAM, types.SimpleNamespace(cuda_stream=78), None, STREAM):
+        LAYERS["linear"](s)
+    assert sorted(str(k[2]) for k in binding._default_ws) == ["77", "78", "None"]
