@@ -406,7 +406,8 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
  * (M <= 64), all tokens before the rows and those rows j whose bit j is set in tree[b][i].
  *   Q_bf16  [B][M][q_heads][head_dim] BF16, token rows q_stride elements apart (as in mxq_kv_append)
  *   O_bf16  [B][M][q_heads][head_dim] BF16;  lse  float [B][M][q_heads], ln of the sum of w_t, or NULL
- * A row that sees no token gives O = 0 and lse = -inf; tokens a row does not see do not touch it, whatever they hold.
+ * A row that sees no token, or only scores of -inf, gives O = 0 and lse = -inf; a row that sees a score of NaN or +inf gives
+ * NaN in both; tokens a row does not see do not touch it, whatever they hold.
  * Scores, maxima, sums and the accumulators are FP32; each weight is rounded to 11 bits before it meets V, so that
  * |O - exact| <= 2^-10 * sum_t w_t |v^_t| / sum_t w_t + BF16's rounding (while |k^| < 2^103: scores are sums in FP32 of q
  * normalised to 2^14; K blocks of scale 2^-127, and V blocks whose scale is

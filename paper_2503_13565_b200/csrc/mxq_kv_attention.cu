@@ -502,7 +502,8 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             *reinterpret_cast<uint2 *>(MXQ_AT(a.o + row * D + d, 8, a.o, o_bytes)) = make_uint2(pack_bf162(v.x, v.y), pack_bf162(v.z, v.w));
         };
         auto store_lse = [&](int64_t row, float m, float l) {
-            if (a.lse != nullptr) *MXQ_AT(a.lse + row, 4, a.lse, o_bytes / D * 2) = m == -INFINITY ? m : (m + log2f(l)) * 0.693147181f;
+            // (no weight at all: -inf; scores that are all NaN leave m at -inf too, but their sum is NaN)
+            if (a.lse != nullptr) *MXQ_AT(a.lse + row, 4, a.lse, o_bytes / D * 2) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147181f;
         };
         if (have) {
         const int b = sh_item[0], len = sh_item[1], rows = sh_item[2];
@@ -567,8 +568,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             top = max(top & 0xFFFFu, top >> 16);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // exponent field e of the largest element -> 2^14 (rows with an Inf or NaN as they are: their scores are NaN or infinite)
-            const int e = (int)(top >> 7), up = e == 255 ? 127 : min(268 - e, 254);
+            // exponent field e of the largest element -> 2^14 (beside an Inf or NaN finite elements are scaled as beside the largest number:
+            // they stay finite, and the scores are what the Inf or NaN makes them)
+            const int e = min((int)(top >> 7), 254), up = min(268 - e, 254);
             const float mul = __uint_as_float((uint32_t)up << 23);
             const float back = up == 254 ? __uint_as_float(0x00400000u) : __uint_as_float((uint32_t)(254 - up) << 23);
 #pragma unroll
