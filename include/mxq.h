@@ -157,7 +157,7 @@ int mxq_linear_plan_info(int kernel, int M, int64_t N, int64_t K, int32_t *info)
  * MXQ_KERNEL_UMMA, bits 8-11 the same for MXQ_KERNEL_FP4, bits 16-20 for mxq_linear_bf16; bits 24-27 for
  * mxq_linear_batch: data of a stage never arrived, a ring slot was never released, an accumulator never completed,
  * the rewritten token rows never became ready; bit 28 for MXQ_KERNEL_MMA: the wait for a reduction slot; bit 29 for
- * mxq_kv_attention: a tile of the cache never arrived, its rows are NaN).  0 in normal
+ * mxq_kv_attention: a tile of the cache never arrived).  0 in normal
  * operation; a non-zero word means the affected output tiles were written as NaN.  Synchronises with
  * the device (a blocking copy), so call it outside the hot loop. */
 int mxq_linear_device_status(uint32_t *status_host);
@@ -461,9 +461,13 @@ int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *table
  * mxq_debug_bounds_selftest: checked build only (otherwise MXQ_ERR_SHAPE): one kernel stores 4 bytes at offset 100
  *   through the checked address of a 64-byte buffer that lies inside a larger array of the library's own (so that not
  *   even an unchecked store could leave it) and 4 bytes at offset 60; returns MXQ_OK if the array shows the second
- *   store and nothing else.  The refused store is then in mxq_debug_bounds_report. */
+ *   store and nothing else.  The refused store is then in mxq_debug_bounds_report.
+ * mxq_debug_kv_lost_tile: checked build only (otherwise MXQ_ERR_SHAPE), a test hook for the bounded waits of mxq_kv_attention: its
+ *   NEXT call (one-shot) waits for tile `tile` (32 tokens) of sequence 0, kv head 0 without requesting it.  The call still completes
+ *   within a few seconds, mxq_linear_device_status reports bit 29, and what the CTAs concerned had still to deliver is NaN.  -1 cancels. */
 int mxq_debug_bounds_report(uint64_t *report);
 int mxq_debug_bounds_selftest(void *stream);
+int mxq_debug_kv_lost_tile(int tile);
 
 #ifdef __cplusplus
 }

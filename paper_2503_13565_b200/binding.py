@@ -120,6 +120,8 @@ def lib() -> ctypes.CDLL:
             L.mxq_kv_fork.argtypes = [vp, i32, vp, i32, vp, i32, vp, vp, vp, sz, vp]
             L.mxq_kv_compact.restype = i32
             L.mxq_kv_compact.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
+            L.mxq_debug_kv_lost_tile.restype = i32
+            L.mxq_debug_kv_lost_tile.argtypes = [i32]
             L.mxq_debug_batch_fault.restype = i32
             L.mxq_debug_batch_fault.argtypes = [i32, ctypes.c_uint]
             _lib = L
@@ -780,3 +782,8 @@ def mxq_debug_bounds_selftest(stream=None) -> None:
 def mxq_debug_batch_fault(unit: int, wait_us: int) -> None:
     """Test hook: the next mxq_linear_batch call leaves out one weight copy and bounds its waits (see mxq.h)."""
     _check(lib().mxq_debug_batch_fault(int(unit), int(wait_us)), "mxq_debug_batch_fault")
+
+
+def mxq_debug_kv_lost_tile(tile: int) -> None:
+    """Test hook, checked build only: the next mxq_kv_attention call waits for a tile that nobody requested (see mxq.h)."""
+    _check(lib().mxq_debug_kv_lost_tile(int(tile)), "mxq_debug_kv_lost_tile")

@@ -25,9 +25,9 @@
 // segments, is cut along the tokens into items, which CTAs draw from a counter as they become free: tiles cost between one
 // product and four, and equal shares left the GPU waiting for the unluckiest CTA (batched decode 58 us, items 39).  Within an item each
 // of the four warps takes every fourth 32-token tile and keeps its own m, l, O and a ring of two tiles, each filled by ONE bulk copy
-// that completes on an mbarrier; no warp waits for another until the item ends.  (Waits are bounded: a tile that never arrives sets a
-// status bit and makes its rows NaN.)  The results of a segment's items go to the workspace, in slots in the order of the tokens; the
-// CTA that delivered the last of them adds them up in that order.  Nobody waits for it, and it learns that it was the last one item
+// that completes on an mbarrier; no warp waits for another until the item ends.  (Waits are bounded: where a tile never arrives a
+// status bit is set, the CTA requests nothing more, and what it had still to deliver is NaN.)  The results of a segment's items go to the
+// workspace, in slots in the order of the tokens; the CTA that delivered the last of them adds them up in that order.  Nobody waits for it, and it learns that it was the last one item
 // later, when the ticket's answer has long arrived.  So which CTA did what does not show in the result.
 //
 // What bounds it.  Not the bytes: 2 x 131071 tokens of 32 heads (1.14 GB) take 248 us with even weights, 4.6 TB/s = 70 % of the copy rate,
@@ -41,6 +41,7 @@
 // item's tiles before this one's result is put together gained nothing (the SM's other CTAs fill the gap) and cost registers.
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "mxq_kv.cuh"
@@ -62,6 +63,9 @@ struct KvQuery {
     unsigned *tickets;
     float *partials;
     uint32_t slots;
+#ifdef MXQ_DEBUG_BOUNDS
+    int32_t lost_tile;       // test hook: this tile of sequence 0, kv head 0 is waited for but never requested
+#endif
 };
 
 constexpr int kWeightBias = 10;                // weights carry a factor 2^10 from the exponential on: in FP16 they keep 11 bits down to 2^-14
@@ -361,6 +365,41 @@ __device__ __forceinline__ void add_values_wide(WarpState<D, NT> &w, uint32_t ti
     }
 }
 
+// A wait for tile number `at` of a warp, up to about a second.  It returns the same to all lanes of the warp: those that come to
+// the long wait agree through a word behind the warp's barriers (tile number and outcome; the first one's stands), and where a lane has
+// left the short one, the tile has arrived for good and no other can run out of time.  (A vote after every wait instead: tree
+// verification 36.4 -> 37.8 us.)
+__device__ __noinline__ bool tile_wait_long(uint32_t bar, uint32_t at) {
+    const uint64_t t0 = global_ns();
+    const uint32_t parity = (at / kAttStages) & 1u, verdict = bar + 8 * (kAttStages - at % kAttStages);
+    bool here = false;
+    while (!here && global_ns() - t0 <= 1000000000ull)
+        for (int i = 0; i < 256 && !here; ++i) here = mbar_try_wait(bar, parity);
+    const uint32_t mine = 2u * at + (here ? 3u : 2u);
+    uint32_t seen = lds_u32(verdict);
+    while (seen >> 1 != at + 1u) {
+        uint32_t was;
+        asm volatile("atom.shared.cas.b32 %0, [%1], %2, %3;" : "=r"(was) : "r"(verdict), "r"(seen), "r"(mine) : "memory");
+        seen = was == seen ? mine : was;
+    }
+    return (seen & 1u) != 0 && (here || mbar_wait(bar, parity));
+}
+__device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t at) {
+    const uint32_t parity = (at / kAttStages) & 1u;
+    for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return tile_wait_long(bar, at);
+}
+// What follows where tile `at` did not arrive (never in normal operation): the CTA requests nothing more, and what it has still to deliver
+// becomes NaN.  What the warp has requested, up to tile `requested`, gets one more wait each first, as the rings' memory is used
+// for other things.
+__device__ __noinline__ void tile_lost(uint32_t bars, uint32_t at, uint32_t requested, int *lost) {
+    *lost = 1;
+    if ((threadIdx.x & 31) == 0) atomicOr(&g_kv_status, 1u);
+    for (uint32_t i = at; i < requested; ++i) (void)mbar_wait(bars + 8 * (i % kAttStages), (i / kAttStages) & 1u);
+    __syncwarp();
+}
+
 template <int D, int NT>
 __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attention_kernel(KvView c, KvSeqs s, KvQuery a) {
     using T = KvTile<D>;
@@ -371,8 +410,8 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     __shared__ Owner sh_owner[kAttThreads];
     __shared__ uint32_t sh_next;
     __shared__ float sh_ml[kAttWarps][kAttRows<NT>][2];
-    __shared__ int sh_last;
-    __shared__ __align__(8) uint64_t sh_bars[kAttWarps][kAttStages];
+    __shared__ int sh_last, sh_lost;       // (sh_lost: a tile never arrived)
+    __shared__ __align__(8) uint64_t sh_bars[kAttWarps][kAttStages + 1];      // (the last: see tile_wait_long)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, tig = lane & 3;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem_raw) + warp * kAttStages * T::kBytes;
     float *const merge = reinterpret_cast<float *>(att_smem_raw);   // [warp][row][D + 4], between items
@@ -383,9 +422,11 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(sh_bars[warp]);
     uint32_t issued = 0;      // tiles the warp has requested before this segment: ring slots and phases run on
     if (lane == 0) {
+        sh_bars[warp][kAttStages] = 0;
         for (int i = 0; i < kAttStages; ++i) mbar_init(bars + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid == 0) sh_lost = 0;
     pdl_trigger();
     pdl_wait();
     asm volatile("fence.proxy.async;" ::: "memory");      // tiles may have been written by the kernel before, with ordinary stores
@@ -530,7 +571,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
 
         // ---- the warp's tiles: number k is the segment's tile first_tile + k * kAttWarps ----
         const int last_tile = (int)min(((uint32_t)len + kTileTokens - 1) / kTileTokens, tile0 + ntiles), first_tile = (int)tile0 + warp;
-        const int count = nrows > 0 && first_tile < last_tile ? (last_tile - first_tile + kAttWarps - 1) / kAttWarps : 0;
+        const int count = nrows > 0 && sh_lost == 0 && first_tile < last_tile ? (last_tile - first_tile + kAttWarps - 1) / kAttWarps : 0;
         const uint8_t *source = nullptr;   // lane i: where tile i of the warp's next 32 lies (nullptr: nowhere)
         uint32_t exist = 0, there = 0;     // bit i: that tile exists; the tiles requested so far, the newest lowest
         auto issue = [&](int k) {
@@ -550,6 +591,9 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
             if (lane == at) {              // the lane that knows a tile requests it; one that is not there completes at once
                 const uint32_t slot = (issued + (uint32_t)k) % kAttStages, bar = bars + 8 * slot;
                 mbar_expect_tx(bar, source != nullptr ? T::kBytes : 0);
+#ifdef MXQ_DEBUG_BOUNDS
+                if (first_tile + k * kAttWarps == a.lost_tile && sg.b == 0 && sg.head == 0) return;
+#endif
                 if (source != nullptr) bulk_load(ring + slot * T::kBytes, MXQ_AT(source, T::kBytes, c.pool, c.pool_bytes), T::kBytes, bar);
             }
         };
@@ -599,14 +643,11 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 for (int e = 0; e < 4; ++e) w.o[i][nt][e] = 0.f;
         }
 
-        bool arrived = true;
-        for (int k = 0; k < count; ++k) {
+        int k = 0;
+        for (; k < count; ++k) {
             const uint32_t at = issued + (uint32_t)k, slot = at % kAttStages, tile = ring + slot * T::kBytes;
             const int t0 = (first_tile + k * kAttWarps) * kTileTokens;
-            if (!mbar_wait(bars + 8 * slot, (at / kAttStages) & 1u)) {      // (never in normal operation; the segment's rows become NaN)
-                if (lane == 0) atomicOr(&g_kv_status, 1u);
-                arrived = false;
-            }
+            if (!tile_wait(bars + 8 * slot, at)) break;
             if ((there >> (kAttStages - 1)) & 1u) {
                 const int tok = (g >> 1) + 4 * (g & 1);      // row g of the product is this token of the group, row g + 8 the one 8 further
                 // ---- scores ----
@@ -845,12 +886,14 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
         }
 
         // ---- join the warps: each as (maximum, sum, average), eight rows at a time over the drained rings ----
+        __syncwarp();
+        if (k < count) tile_lost(bars, issued + (uint32_t)k, issued + (uint32_t)min(count, k + kAttStages), &sh_lost);
         issued += (uint32_t)count;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                if (!arrived) w.l[nt][e] = NAN;
+                if (sh_lost != 0) w.l[nt][e] = NAN;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) w.l[nt][e] += __shfl_xor_sync(0xffffffffu, w.l[nt][e], o);
                 if (g == 0) sh_ml[warp][8 * nt + 2 * tig + e][0] = w.over[nt][e] == -INFINITY ? -INFINITY : w.m[nt][e] - kWeightBias, sh_ml[warp][8 * nt + 2 * tig + e][1] = w.l[nt][e];
@@ -951,13 +994,14 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                     for (int i = 0; i < kAttWarps; ++i) m = fmaxf(m, sh_ml[i][lane][0]);
 #pragma unroll
                     for (int i = 0; i < kAttWarps; ++i) l += sh_ml[i][lane][1] == 0.f ? 0.f : sh_ml[i][lane][1] * exp2_fast(sh_ml[i][lane][0] - m);
+                    if (sh_lost != 0) l = NAN;        // (a copy that comes late may have changed the table)
                     if (warp == 0) store_lse(out_row(pending.b, pending.head, pending.r0 + lane), m, l);
                 }
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 for (int x0 = 32 * warp; x0 < pairs; x0 += kAttThreads) {
                     const int x = x0 + lane, r = x % nrows;
                     const float rm = __shfl_sync(0xffffffffu, m, r), ri = __shfl_sync(0xffffffffu, inv, r);
-                    if (x < pairs) table[x].x = table[x].y == 0.f ? 0.f : table[x].y * exp2_fast(table[x].x - rm) * ri;
+                    if (x < pairs) table[x].x = table[x].y == 0.f ? 0.f * ri : table[x].y * exp2_fast(table[x].x - rm) * ri;
                 }
                 __syncthreads();
                 // four elements of a row per thread; with few rows several threads share the parts
@@ -1049,6 +1093,9 @@ static size_t att_workspace() {
     return att_partials_offset() + (size_t)kAttSlotsPerCta * att_grid<D, NT>() * kAttSlotFloats<D, NT> * 4;
 }
 
+// test hook (mxq_debug_kv_lost_tile): consumed by the next launch
+[[maybe_unused]] static std::atomic<int> g_lost_tile{-1};
+
 template <int D, int NT>
 static int att_launch(const KvView &c, const KvSeqs &s, KvQuery a, void *workspace, cudaStream_t stream) {
     constexpr size_t smem = kAttSmem<D, NT>;
@@ -1067,6 +1114,9 @@ static int att_launch(const KvView &c, const KvSeqs &s, KvQuery a, void *workspa
     a.tickets = (unsigned *)((char *)workspace + 16);
     a.partials = (float *)((char *)workspace + att_partials_offset());
     a.slots = kAttSlotsPerCta * (uint32_t)att_grid<D, NT>();
+#ifdef MXQ_DEBUG_BOUNDS
+    a.lost_tile = g_lost_tile.exchange(-1, std::memory_order_relaxed);
+#endif
     return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)att_grid<D, NT>()), kAttThreads, smem, stream, c, s, a);
 }
 
@@ -1116,6 +1166,16 @@ int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, i
     const mxq::KvView c = mxq::kv_view(cache, layer);
     return mxq::att_pick(cache->head_dim, M, group,
                          [&](auto d, auto nt) { return mxq::att_launch<d(), nt()>(c, s, a, workspace, (cudaStream_t)stream); });
+}
+
+int mxq_debug_kv_lost_tile(int tile) {
+#ifdef MXQ_DEBUG_BOUNDS
+    mxq::g_lost_tile.store(tile, std::memory_order_relaxed);
+    return MXQ_OK;
+#else
+    (void)tile;
+    return MXQ_ERR_SHAPE;
+#endif
 }
 
 #pragma GCC visibility pop
