@@ -391,7 +391,7 @@ size_t mxq_kv_page_bytes(int kv_heads, int head_dim, int page_tokens);
 /* Casts the M new K and V rows of every sequence into their places in one layer.  K_bf16, V_bf16 [B][M][kv_heads][head_dim]
  * BF16, token rows k_stride / v_stride elements apart (>= kv_heads * head_dim, a multiple of 8: a column slice of a fused
  * projection's output will do).  Same cast as mxq_quantize (a block with an Inf or NaN becomes scale 0xFF, codes 0).  The
- * pages written must not be shared (mxq_kv_fork copies the one that would be).  B * M * kv_heads <= 2^29. */
+ * pages written must not be shared; those of rows that mxq_kv_resize has just made room for never are.  B * M * kv_heads <= 2^29. */
 int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int64_t k_stride, const void *V_bf16, int64_t v_stride,
                   int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows, void *stream);
 
@@ -423,9 +423,11 @@ int mxq_kv_attention(const mxq_kv_cache *cache, int layer, const void *Q_bf16, i
 /* Gives and takes pages so that sequence b holds new_lens[b] tokens, and sets lens[b] to it: growth before the append,
  * rollback after the verification, 0 to free the sequence.  Pages behind the new end lose this sequence's reference
  * (entry -1); then the pages wanted are taken in order of (sequence, place) from the free pages in order of their index, the
- * ones just released among them.  From the first sequence on whose pages do not fit any more, no sequence gets pages: one
- * that wants some keeps its old length and pages (lens[b] != new_lens[b] tells).  The same for a new length outside
- * 0..W*page_tokens. */
+ * ones just released among them.  A sequence whose new end lies inside a page that others hold too (a rollback behind a fork) wants one
+ * page: it takes the place of the shared one, and the tokens that stay are copied into it in every layer, so that what is
+ * appended next touches no other sequence.  From the first sequence on whose pages do not fit any more, no sequence gets pages: one
+ * that wants to grow keeps its old length and pages, one that shares the page of its new end goes back to the end of that page
+ * (lens[b] != new_lens[b] tells).  A new length outside 0..W*page_tokens changes nothing. */
 int mxq_kv_resize(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_t *lens, const int32_t *new_lens, void *stream);
 
 /* Makes slots dst[0..n) copies of the sequences in slots src[0..n) (int32, device; slots of tables / lens): whole pages are

@@ -135,16 +135,51 @@ __device__ __forceinline__ Owned owned(const int *upto, int n, int x) {
     return {i, x - (i ? upto[i - 1] : 0)};
 }
 
-__global__ void __launch_bounds__(kBookThreads) kv_resize_kernel(Book k, const int32_t *new_lens) {
+// 16-byte pieces of a page's filled tiles, in every layer, by the whole block: a warp per layer, four loads in flight per lane
+__device__ __forceinline__ void copy_page(const KvView &c, int layers, int64_t layer_bytes, int from_page, int to_page, int64_t bytes) {
+    constexpr int kU = 4;
+    const int lane = threadIdx.x & 31;
+    for (int layer = (int)threadIdx.x >> 5; layer < layers; layer += kBookWarps) {
+        const uint8_t *from = c.base + layer * layer_bytes + (int64_t)from_page * c.page_bytes;
+        uint8_t *to = c.base + layer * layer_bytes + (int64_t)to_page * c.page_bytes;
+        for (int64_t at0 = lane * 16; at0 < bytes; at0 += kU * 32 * 16) {
+            uint4 v[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                if (at0 + u * 512 < bytes) v[u] = ld_dep_u4(MXQ_AT(from + at0 + u * 512, 16, c.pool, c.pool_bytes));
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                if (at0 + u * 512 < bytes) *reinterpret_cast<uint4 *>(MXQ_AT(to + at0 + u * 512, 16, c.pool, c.pool_bytes)) = v[u];
+        }
+    }
+}
+
+// A sequence that is cut inside a page which others hold too (a rollback behind a fork) would append into their tokens: it gets
+// a page of its own with the tokens that stay.  The copy is this CTA's work as well (49 us for a page of 64 tokens in 32 layers of 8 heads
+// of 128): it happens once per branch at most, and a launch of its own would cost every resize.  To find such a page a rollback reads
+// the entry and the count of the page it ends in, two dependent loads (0.5 to 1 us).
+__global__ void __launch_bounds__(kBookThreads) kv_resize_kernel(Book k, const int32_t *new_lens, KvView c, int layers, int64_t layer_bytes) {
     extern __shared__ int book_smem[];
-    int *upto = book_smem, *held = book_smem + k.B, *drop = book_smem + 2 * k.B;
+    // per sequence: pages wanted and pages dropped (both summed up), pages held, the shared page that it ends in or -1
+    int *upto = book_smem, *held = book_smem + k.B, *drop = book_smem + 2 * k.B, *split = book_smem + 3 * k.B;
+    __shared__ int any_split;
     const int64_t cap = (int64_t)k.W << k.page_shift;
+    const int mask = (1 << k.page_shift) - 1;
+    if (threadIdx.x == 0) any_split = 0;
+    __syncthreads();
     pdl_trigger();
     pdl_wait();
     for (int b = (int)threadIdx.x; b < k.B; b += kBookThreads) {
-        const int n = (int)ld_dep_u32(MXQ_AT(new_lens + b, 4, new_lens, (size_t)k.B * 4)), have = pages_for(book_len(k, b), k.page_shift);
-        const int want = n >= 0 && n <= cap ? pages_for(n, k.page_shift) : have;
-        upto[b] = max(want - have, 0), held[b] = have, drop[b] = max(have - want, 0);
+        const int n = (int)ld_dep_u32(MXQ_AT(new_lens + b, 4, new_lens, (size_t)k.B * 4)), len = book_len(k, b), have = pages_for(len, k.page_shift);
+        const bool valid = n >= 0 && n <= cap;
+        const int want = valid ? pages_for(n, k.page_shift) : have;
+        int page = -1;
+        if (valid && n < len && (n & mask) != 0) {
+            page = (int)ld_dep_u32(entry_of(k, b, n >> k.page_shift));
+            if ((unsigned)page >= (unsigned)k.num_pages || (int)ld_dep_u32(ref_of(k, page)) <= 1) page = -1;
+            else any_split = 1;
+        }
+        upto[b] = page >= 0 ? 1 : max(want - have, 0), held[b] = have, drop[b] = max(have - want, 0), split[b] = page;
     }
     __syncthreads();
     const int wanted = scan_needs(upto, k.B), dropped = scan_needs(drop, k.B);
@@ -157,9 +192,10 @@ __global__ void __launch_bounds__(kBookThreads) kv_resize_kernel(Book k, const i
         if ((unsigned)page < (unsigned)k.num_pages) atomicSub(ref_of(k, page), 1);
     }
     __syncthreads();
+    auto last_place = [&](int b) { return held[b] - (drop[b] - (b ? drop[b - 1] : 0)) - 1; };      // of the pages that stay
     const int found = lowest_free(k.refs, k.num_pages, wanted, [&](int rank, int page) {
         const Owned o = owned(upto, k.B, rank);
-        *entry_of(k, o.i, held[o.i] + o.k) = page;
+        *entry_of(k, o.i, split[o.i] >= 0 ? last_place(o.i) : held[o.i] + o.k) = page;
         *ref_of(k, page) = 1;
     });
     __syncthreads();
@@ -173,8 +209,18 @@ __global__ void __launch_bounds__(kBookThreads) kv_resize_kernel(Book k, const i
     }
     for (int b = (int)threadIdx.x; b < k.B; b += kBookThreads) {
         const int n = (int)ld_dep_u32(MXQ_AT(new_lens + b, 4, new_lens, (size_t)k.B * 4));
-        const bool none = upto[b] == (b ? upto[b - 1] : 0);
-        if (n >= 0 && n <= cap && (none || upto[b] <= found)) *MXQ_AT(k.lens + b, 4, k.lens, (size_t)k.B * 4) = n;
+        const bool none = upto[b] == (b ? upto[b - 1] : 0), fits = none || upto[b] <= found;
+        int32_t *len = MXQ_AT(k.lens + b, 4, k.lens, (size_t)k.B * 4);
+        if (n >= 0 && n <= cap && fits) *len = n;
+        else if (split[b] >= 0) *len = min(book_len(k, b), (last_place(b) + 1) << k.page_shift);      // as far back as it goes without a page
+    }
+    if (any_split == 0) return;
+    for (int b = 0; b < k.B; ++b) {
+        if (split[b] < 0 || upto[b] > found) continue;
+        const int n = (int)ld_dep_u32(MXQ_AT(new_lens + b, 4, new_lens, (size_t)k.B * 4));
+        const int tiles = ((n & mask) + kTileTokens - 1) / kTileTokens;
+        copy_page(c, layers, layer_bytes, split[b], (int)ld_dep_u32(entry_of(k, b, last_place(b))), c.page_bytes * tiles >> (k.page_shift - 5));
+        if (threadIdx.x == 0) atomicSub(ref_of(k, split[b]), 1);
     }
 }
 
@@ -376,8 +422,9 @@ int mxq_kv_resize(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int3
     if (!mxq::aligned_to(new_lens, 4)) return MXQ_ERR_ALIGN;
     rc = mxq::book_smem_ready((const void *)mxq::kv_resize_kernel);
     if (rc != MXQ_OK) return rc;
-    return mxq::kv_launch(mxq::kv_resize_kernel, dim3(1), mxq::kBookThreads, (size_t)B * 12, (cudaStream_t)stream,
-                          mxq::book_of(cache, B, tables, W, lens), new_lens);
+    const mxq::KvView c = mxq::kv_view(cache, 0);
+    return mxq::kv_launch(mxq::kv_resize_kernel, dim3(1), mxq::kBookThreads, (size_t)B * 16, (cudaStream_t)stream,
+                          mxq::book_of(cache, B, tables, W, lens), new_lens, c, cache->layers, c.page_bytes * cache->num_pages);
 }
 
 size_t mxq_kv_fork_workspace_bytes(int n) { return n < 1 || n > MXQ_KV_MAX_SEQS ? 0 : (size_t)n * sizeof(mxq::ForkJob); }
