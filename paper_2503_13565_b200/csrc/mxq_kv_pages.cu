@@ -9,6 +9,8 @@
 // together 7 us (16 sequences, 1024 pages) and 22 us (256 sequences that grow by up to 64 pages each, 65536 pages), where the search of the counts, a
 // chain of loads and barriers per 16384 pages, and the entries' scattered loads and stores bound it; one CTA hides them because every list is
 // dealt out flat, entry by entry, to 1024 threads.
+#include <algorithm>
+
 #include "mxq_kv.cuh"
 
 namespace mxq {
@@ -280,29 +282,30 @@ kv_fork_kernel(Book k, int n, const int32_t *src, const int32_t *dst, ForkJob *j
 // tiles of all heads, which lie together), four 16-byte loads in flight per thread.  Bound by the copy rate from some tens of
 // children on: 64 children of 16 parents, 32 layers of 8 heads (205 MB read and written), fork and the freeing of the children
 // together 33.5 us, the copy alone at the roof 31.3; 4 children of one: 12 us for two launches of bookkeeping and 17.8 MB.
-constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll * 16;
+constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll * 16, kMaxGridY = 65535;
 
 __global__ void __launch_bounds__(kCopyThreads)
-kv_fork_copy_kernel(const ForkJob *jobs, int n, KvView c, int64_t layer_bytes, int64_t row_bytes, int pieces) {
+kv_fork_copy_kernel(const ForkJob *jobs, int n, KvView c, int layers, int64_t layer_bytes, int64_t row_bytes, int pieces) {
     pdl_trigger();
     pdl_wait();
     const uint4 j = ld_dep_u4(MXQ_AT(jobs + blockIdx.x, 16, jobs, (size_t)n * 16));
     const int tile = (int)blockIdx.z / pieces, piece = (int)blockIdx.z - tile * pieces;
     if (tile >= (int)j.z || !kv_page_ok(c, (int)j.x) || !kv_page_ok(c, (int)j.y)) return;
-    uint8_t *layer = c.base + (int64_t)blockIdx.y * layer_bytes;
     const int64_t off = tile * row_bytes, first = (int64_t)piece * kCopyPiece;
-    const uint8_t *from = layer + (int64_t)(int)j.x * c.page_bytes + off;
-    uint8_t *to = layer + (int64_t)(int)j.y * c.page_bytes + off;
-    uint4 v[kCopyUnroll];
+    for (int layer = (int)blockIdx.y; layer < layers; layer += (int)gridDim.y) {      // (a grid has at most kMaxGridY of them)
+        const uint8_t *from = c.base + layer * layer_bytes + (int64_t)(int)j.x * c.page_bytes + off;
+        uint8_t *to = c.base + layer * layer_bytes + (int64_t)(int)j.y * c.page_bytes + off;
+        uint4 v[kCopyUnroll];
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
-        const int64_t at = first + (u * kCopyThreads + (int)threadIdx.x) * 16;
-        if (at < row_bytes) v[u] = ld_dep_u4(MXQ_AT(from + at, 16, c.pool, c.pool_bytes));
-    }
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            const int64_t at = first + (u * kCopyThreads + (int)threadIdx.x) * 16;
+            if (at < row_bytes) v[u] = ld_dep_u4(MXQ_AT(from + at, 16, c.pool, c.pool_bytes));
+        }
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
-        const int64_t at = first + (u * kCopyThreads + (int)threadIdx.x) * 16;
-        if (at < row_bytes) *reinterpret_cast<uint4 *>(MXQ_AT(to + at, 16, c.pool, c.pool_bytes)) = v[u];
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            const int64_t at = first + (u * kCopyThreads + (int)threadIdx.x) * 16;
+            if (at < row_bytes) *reinterpret_cast<uint4 *>(MXQ_AT(to + at, 16, c.pool, c.pool_bytes)) = v[u];
+        }
     }
 }
 
@@ -448,8 +451,8 @@ int mxq_kv_fork(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_
     const int tiles = cache->page_tokens / mxq::kTileTokens;
     const int64_t row_bytes = c.page_bytes / tiles;
     const int pieces = (int)((row_bytes + mxq::kCopyPiece - 1) / mxq::kCopyPiece);
-    return mxq::kv_launch(mxq::kv_fork_copy_kernel, dim3((unsigned)n, (unsigned)cache->layers, (unsigned)(tiles * pieces)), mxq::kCopyThreads,
-                          0, (cudaStream_t)stream, (const mxq::ForkJob *)jobs, n, c, c.page_bytes * cache->num_pages, row_bytes, pieces);
+    return mxq::kv_launch(mxq::kv_fork_copy_kernel, dim3((unsigned)n, (unsigned)std::min(cache->layers, mxq::kMaxGridY), (unsigned)(tiles * pieces)), mxq::kCopyThreads,
+                          0, (cudaStream_t)stream, (const mxq::ForkJob *)jobs, n, c, cache->layers, c.page_bytes * cache->num_pages, row_bytes, pieces);
 }
 
 int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows,
