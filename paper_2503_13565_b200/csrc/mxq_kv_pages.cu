@@ -258,10 +258,12 @@ kv_fork_kernel(Book k, int n, const int32_t *src, const int32_t *dst, ForkJob *j
         ForkJob job = {0, 0, 0, 0};
         if (fits && part) {
             job.src = (int)ld_dep_u32(entry_of(k, from[i], whole));
-            job.dst = fresh[i];
-            if ((unsigned)job.src < (unsigned)k.num_pages) job.tiles = ((lens[i] & mask) + kTileTokens - 1) / kTileTokens;
+            job.dst = -1;      // (where the parent's tokens are on no page, so are the child's, and the page stays free)
+            if ((unsigned)job.src < (unsigned)k.num_pages) {
+                job.dst = fresh[i], job.tiles = ((lens[i] & mask) + kTileTokens - 1) / kTileTokens;
+                *ref_of(k, job.dst) = 1;
+            }
             *entry_of(k, to[i], whole) = job.dst;
-            *ref_of(k, job.dst) = 1;
         }
         shared[i] = fits ? whole : 0;
         if (fits) *MXQ_AT(k.lens + to[i], 4, k.lens, (size_t)k.B * 4) = lens[i];
