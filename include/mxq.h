@@ -373,8 +373,8 @@ int mxq_debug_batch_fault(int unit, unsigned wait_us);
  *   rows   int32 [B] or NULL: how many of the call's M token rows sequence b has (NULL: all M); row i of sequence b is the
  *          token at position lens[b] - rows[b] + i.  Rows beyond rows[b] are ignored as input and zero as output
  * 1 <= B <= MXQ_KV_MAX_SEQS, W >= 1, B * W <= 2^30, head_dim 64 or 128, page_tokens 32, 64, 128 or 256 (MXQ_ERR_SHAPE
- * otherwise).  `cache` is a HOST struct read during the call; int32 and float arrays need their own alignment only,
- * everything else 16 bytes. */
+ * otherwise).  `cache` is a HOST struct read during the call; refs and everything that is not an int32 or float array must be
+ * 16-byte aligned, the other arrays need their own alignment only. */
 #define MXQ_KV_MAX_SEQS 4096
 #define MXQ_KV_MAX_HEADS 256
 #define MXQ_KV_MAX_PAGES (1 << 24)
@@ -408,10 +408,13 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
  *   O_bf16  [B][M][q_heads][head_dim] BF16;  lse  float [B][M][q_heads], ln of the sum of w_t, or NULL
  * A row that sees no token, or only scores of -inf, gives O = 0 and lse = -inf; a row that sees a score of NaN or +inf gives
  * NaN in both; tokens a row does not see do not touch it, whatever they hold.
- * Scores, maxima, sums and the accumulators are FP32; each weight is rounded to 11 bits before it meets V, so that
- * |O - exact| <= 2^-10 * sum_t w_t |v^_t| / sum_t w_t + BF16's rounding (while |k^| < 2^103: scores are sums in FP32 of q
- * normalised to 2^14; K blocks of scale 2^-127, and V blocks whose scale is
- * 2^136 and more below the largest of the sequence's, count as zero).  Bit-reproducible run to run for given lengths.
+ * Scores, maxima, sums and the accumulators are FP32; each weight is rounded to 11 bits before it meets V.  With S the largest
+ * sum_d |scale * q_d * k^_d| of a token that the row sees,
+ *     |O - exact| <= (2^-10 + (2 * head_dim + 8) * 2^-24 * S) * sum_t w_t |v^_t| / sum_t w_t + BF16's rounding,
+ *     |lse - exact| <= (head_dim + 4) * 2^-24 * S + 2^-21 * |lse| + 2^-19 + 2^-24 for each addition of a chain (a few hundred),
+ * while |k^| < 2^103 (scores are sums of q normalised to 2^14).  Held in fewer bits than they come with: elements of q 2^28 and more
+ * below the largest of their row (FP16 after the normalisation); K blocks of scale 2^-127, and V blocks whose scale is 2^136 and more below
+ * the largest of the sequence's, which count as zero.  Bit-reproducible run to run for given lengths.
  *   workspace  device memory, >= mxq_kv_attention_workspace_bytes, 16-byte aligned; zero all of it once before the first
  *              use: it holds counters that every call leaves zero again, so calls of any shape it is large enough for may
  *              share it.  One per stream.  After a non-zero mxq_linear_device_status zero it again. */
@@ -441,7 +444,7 @@ int mxq_kv_fork(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_
 
 /* Cuts the last rows[b] tokens of every sequence (a verified token tree) down to its accepted path: the token of row
  * keep[b][j] moves to the place of row j, j < kept[b], in all layers and heads.  keep int32 [B][M], ascending in each row,
- * 0 <= keep < rows[b]; kept int32 [B]; 1 <= M <= 64.  lens_out[b] (an array of its own) = lens[b] - rows[b] + kept[b]; lens stays, so that
+ * 0 <= keep < rows[b]; kept int32 [B]; 1 <= M <= 64; rows[b] <= lens[b] (an empty slot, of which nothing is kept, stays empty).  lens_out[b] (an array of its own) = lens[b] - rows[b] + kept[b]; lens stays, so that
  * mxq_kv_resize(lens, lens_out) then gives back the pages behind it.  The pages of the rows must not be shared. */
 int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows,
                    const int32_t *keep, const int32_t *kept, int32_t *lens_out, void *stream);
