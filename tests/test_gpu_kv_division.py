@@ -126,6 +126,13 @@ def test_few_long_segments(d, h, hq, m, lens):
     run(lens, [m] * len(lens), h, hq, d, 256, 400 + d)
 
 
+@pytest.mark.skipif(CHECKED, reason="the sizes before it take every branch of the checked build")
+@pytest.mark.parametrize("d,h,hq,rows,lens", [(128, 2, 8, [700, 33, 0], [700, 900, 50]), (64, 4, 4, [300, 1, 300], [300, 5000, 4001])])
+def test_prompt_rows(d, h, hq, rows, lens):
+    """A prompt that is the whole sequence, and chunks of one behind what is there already: many row tiles per segment."""
+    run(lens, rows, h, hq, d, 64, 500 + d, missing=[(len(lens) - 1, 0)])
+
+
 @pytest.mark.skipif(CHECKED, reason="already inside the checked run")
 def test_nothing_outside_its_buffers_at_these_sizes():
     env = dict(os.environ, MXQ_LIBRARY="checked")
