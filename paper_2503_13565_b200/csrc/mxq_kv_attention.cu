@@ -30,15 +30,18 @@
 // workspace, in slots in the order of the tokens; the CTA that delivered the last of them adds them up in that order.  Nobody waits for it, and it learns that it was the last one item
 // later, when the ticket's answer has long arrived.  So which CTA did what does not show in the result.
 //
-// What bounds it.  Not the bytes: 2 x 131071 tokens of 32 heads (1.14 GB) take 248 us with even weights, 4.6 TB/s = 70 % of the copy rate,
-// 267 us (65 %) with peaked ones, whose tiles need the tiers; bringing the tiles in without computing takes 177 us.  A warp spends
-// some 600 instructions on a tile, half of them on the integer pipe (half rate: unpacking nibbles into the order of the products, scale
-// bytes), which is 52 % busy; the rest is latency of one warp's chain of products, shuffles and exponentials with only
-// 12 warps per SM to hide it (the accumulators and both operands of 32 x 128 tiles: 168 registers).  More warps or more work per
-// warp spill, and spills lose more than they give: the L1 is what the rings leave.  32 decode rows over 100 to 4000 tokens (77.5 MB):
-// 39 us, 20 of them without computing; one row over 2047 tokens: 13 us, 9 without computing: launch, the division of the work, one
-// item of two tiles per warp, the join; tree verification, 8 x 16 rows, head dimension 64: 36 us, 23 without computing.  Requesting the next
-// item's tiles before this one's result is put together gained nothing (the SM's other CTAs fill the gap) and cost registers.
+// What bounds it.  Not the bytes: 2 x 131071 tokens of 32 heads (1.14 GB) take 249 us with even weights, 4.6 TB/s = 70 % of the copy rate,
+// 268 us (65 %) with peaked ones, whose tiles need the tiers; bringing the tiles in without computing takes 177 us.  No unit is saturated:
+// a warp spends some 660 instructions on a tile, the integer pipe (half rate: unpacking nibbles into the order of the products, scale
+// bytes) is 51 % busy, and a scheduler issues in every second cycle; the rest is the latency of one warp's chain of products, shuffles and
+// exponentials, and of the barriers at an item's end, with only 12 warps per SM to hide it (the accumulators and both operands of
+// 32 x 128 tiles: 165 registers).  More warps or more work per warp spill, and spills lose more than they give: the L1 is what the rings
+// leave.  32 decode rows over 279 to 8047 tokens (77 MB): 39 us, 20 of them without computing; one row over 2047 tokens: 13 us, 9 without
+// computing: launch, the division of the work, one item of two tiles per warp, the join; tree verification, 8 x 16 rows, head dimension
+// 64: 36.5 us, 23 without computing.  Requesting the next item's tiles before this one's result is put together gained nothing (the
+// SM's other CTAs fill the gap) and cost registers.
+// A prompt's rows are taken, 16 flattened rows per pass over K and V, tiles behind the last token that a row sees included: 2048 rows of
+// 32 heads over themselves 812 us, 256 rows behind 8192 tokens 322 us (42 and 108 TFLOP/s).
 #include <math.h>
 
 #include <atomic>

@@ -6,8 +6,10 @@
 // the quad agrees on the blocks' maxima with two exchanges (two blocks per register), and the permutation of the layout
 // (mxq_kv.cuh) makes the lane's codes of the row ONE store: K wants word c of every block side by side, V its halfwords.
 // Measured in a replayed graph, head dimension 128: 48 rows of 8 heads 1.8 us (append) and 1.8 us (read), the launch's own
-// time; 5718 rows of 32 heads (94 MB of BF16, 25 MB of cache) 27.6 us for the append, 4.3 TB/s.  The prompt's append issues about
-// as many integer instructions per byte as the direct cast of weights, plus the exchange of words and the scattered scale bytes.  The
+// time; 5718 rows of 32 heads (94 MB of BF16, 25 MB of cache) 27.5 us for the append, 4.3 TB/s = 66 % of the copy rate (the direct cast of
+// weights, the same arithmetic: 92 %).  No unit is saturated there (integer pipe 41 %, L1 58 %): its 96 registers leave 17 warps per SM, which
+// wait for their loads; what it has beside the cast are the exchange of words, scale bytes stored one by one, and a grid over padded
+// rows (two thirds of them leave at once in this batch).  The
 // read of a batch padded to 16380 rows (its zeros are written too: 268 MB) takes 49 us, 6.0 TB/s = 92 % of the copy rate.
 #include "mxq_kv.cuh"
 

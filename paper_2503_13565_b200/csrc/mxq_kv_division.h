@@ -18,12 +18,13 @@ constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;                  // tiles in a warp's ring
 // The sizes of items.  An item costs about two tiles' time by itself, and the last ones leave CTAs idle for up to an item's time.  With
 // kTwoSizes tiles or more per CTA, three quarters of every segment go into big items, drawn first, the rest into small ones of a tenth of a
-// CTA's share, at least kSmallTiles (2 x 131071 tokens, 591 tiles per CTA, even weights: 244 us; all items of half a share, at most kItemTiles tiles:
-// 271; 32 x 16384 tokens of 8 heads: 142 and 150).  A big one is three tenths of a share with one column block (peaked weights, 2 x 131071 tokens: 267 us,
-// four small ones 280; 4 x 16384 tokens of 32 heads, where four small ones are two thirds of a share: 86 and 107), but kBigSmalls small
-// ones with two, whose results are twice as long to put together (even weights, 8 x 16384 tokens of 8 heads, 16 rows: 74 us, three tenths 89).
-// Below kTwoSizes all items are of half a CTA's share, at most kItemTiles tiles (32 sequences of 100 to 4000
-// tokens, 40 tiles per CTA: 39 us, two sizes 68; tree verification, 23 per CTA: 40 us, two sizes 47).
+// CTA's share, at least kSmallTiles (2 x 131071 tokens of 32 heads, 591 tiles per CTA, even weights: 249 us; all items of half a share, at
+// most kItemTiles tiles: 269; 32 x 16384 tokens of 8 heads: 152 and 157).  A big one is three tenths of a share with one column block
+// (4 x 16384 tokens of 32 heads: 87 us; kBigSmalls small ones, two thirds of a share there, 104; 2 x 131071 tokens, peaked weights: 269 and
+// 276, even ones 249 and 247), but kBigSmalls small ones with two, whose results are twice as long to put together (even weights,
+// 8 x 16384 tokens of 8 heads, 16 rows: 70 us, three tenths 86).
+// Below kTwoSizes all items are of half a CTA's share, at most kItemTiles tiles (tree verification, 23 tiles per CTA: 36.5 us, two sizes 43.4;
+// it goes the other way for one column block: 32 sequences of 279 to 8047 tokens, 40 per CTA, 39.0 us, two sizes 36.8).
 // With less than kOneRound tiles per CTA items have that many, two per warp, the ring's depth: fewer would leave part of it empty.
 constexpr uint32_t kTwoSizes = 96, kItemTiles = 48, kSmallTiles = 24, kBigSmalls = 4, kOneRound = 8;
 

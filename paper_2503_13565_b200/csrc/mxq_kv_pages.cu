@@ -5,10 +5,11 @@
 // bookkeeping of a call, so that its steps (drop references, prefix sum of what is wanted, hand out free pages) are
 // separated by block barriers instead of launches, and so that the result does not depend on scheduling: the r-th page
 // wanted, counted over sequences in order, is the r-th free page of the pool, counted by index.
-// Measured in replayed graphs: a resize that changes nothing 2.0 us (16 sequences) to 2.4 us (256); growth and the shrinking back
-// together 7 us (16 sequences, 1024 pages) and 22 us (256 sequences that grow by up to 64 pages each, 65536 pages), where the search of the counts, a
-// chain of loads and barriers per 16384 pages, and the entries' scattered loads and stores bound it; one CTA hides them because every list is
-// dealt out flat, entry by entry, to 1024 threads.
+// Measured in replayed graphs: a resize that changes nothing 2.6 us (16 to 256 sequences); growth and the shrinking back
+// together 7.8 us (16 sequences, 1024 pages) and 24 us (256 sequences that grow by up to 64 pages each, 65536 pages), where the search of the counts, a
+// chain of loads and barriers per 16384 pages, and the entries' scattered loads and stores bound it; every list is dealt out flat, entry by
+// entry, to 1024 threads.  One CTA is a choice (no launch and no flag between the steps), not a limit: the large pool's counts could be
+// searched by several.
 #include <algorithm>
 
 #include "mxq_kv.cuh"
@@ -283,7 +284,7 @@ kv_fork_kernel(Book k, int n, const int32_t *src, const int32_t *dst, ForkJob *j
 // Copies the filled part of the last pages: grid = (child, layer, piece), a piece being 16 KB of one 32-token tile row (the
 // tiles of all heads, which lie together), four 16-byte loads in flight per thread.  Bound by the copy rate from some tens of
 // children on: 64 children of 16 parents, 32 layers of 8 heads (205 MB read and written), fork and the freeing of the children
-// together 33.5 us, the copy alone at the roof 31.3; 4 children of one: 12 us for two launches of bookkeeping and 17.8 MB.
+// together 34 us, the copy alone at the roof 31.3; 4 children of one: 12.5 us for two launches of bookkeeping and 17.8 MB.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll * 16, kMaxGridY = 65535;
 
 __global__ void __launch_bounds__(kCopyThreads)
@@ -313,8 +314,9 @@ kv_fork_copy_kernel(const ForkJob *jobs, int n, KvView c, int layers, int64_t la
 
 // Moves kept tokens down within the last `rows` positions of a sequence: one warp per (sequence, layer, head).  keep is
 // ascending, so token j's source lies at or behind its destination and a batch of pieces may be stored once all of the
-// batch is loaded: later sources lie behind every destination written so far.  Latency (one or a few rounds of dependent loads, page
-// entry then data): 32 layers x 8 heads of one 16-row tree 3.2 us, 64 trees of up to 48 rows in 16 layers x 8 heads 7.5 us.
+// batch is loaded: later sources lie behind every destination written so far.  Latency (a chain of dependent loads: lengths and
+// counts, keep, page entries, data; a batch is one round of it): 32 layers x 8 heads of one 16-row tree 3.2 us, 64 trees of 48 rows in
+// 16 layers x 8 heads, 2 to 6 rows kept, 7.5 us, one round in 8192 warps (0.4 of the issue slots, loads are what is waited for).
 constexpr int kCompactThreads = 128, kCompactBatch = 4;
 
 template <int D>
