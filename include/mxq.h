@@ -369,7 +369,7 @@ int mxq_debug_batch_fault(int unit, unsigned wait_us);
  *   tables int32 [B][W]: page of tokens w*page_tokens .. of sequence b; -1 = none.  Tokens on an entry that is no page of
  *          the pool are left out by every call
  *   lens   int32 [B]: tokens of the sequence, those of this call's rows included (values outside 0..W*page_tokens count
- *          as the nearest end)
+ *          as the nearest end; at most 2^31 - 256 tokens)
  *   rows   int32 [B] or NULL: how many of the call's M token rows sequence b has (NULL: all M); row i of sequence b is the
  *          token at position lens[b] - rows[b] + i.  Rows beyond rows[b] are ignored as input and zero as output
  * 1 <= B <= MXQ_KV_MAX_SEQS, W >= 1, B * W <= 2^30, head_dim 64 or 128, page_tokens 32, 64, 128 or 256 (MXQ_ERR_SHAPE

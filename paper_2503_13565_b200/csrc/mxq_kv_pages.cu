@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kBookThreads) kv_resize_kernel(Book k, const i
         const bool none = upto[b] == (b ? upto[b - 1] : 0), fits = none || upto[b] <= found;
         int32_t *len = MXQ_AT(k.lens + b, 4, k.lens, (size_t)k.B * 4);
         if (n >= 0 && n <= cap && fits) *len = n;
-        else if (split[b] >= 0) *len = min(book_len(k, b), (last_place(b) + 1) << k.page_shift);      // as far back as it goes without a page
+        else if (split[b] >= 0) *len = (int)min((int64_t)book_len(k, b), (int64_t)(last_place(b) + 1) << k.page_shift);      // as far back as it goes without a page
     }
     if (any_split == 0) return;
     for (int b = 0; b < k.B; ++b) {

@@ -184,3 +184,15 @@ def test_rollback_with_no_page_at_all():
     s.resize([32, 5, 0])
     assert s.lens.tolist() == [32, 5, 0]
     s.check_tokens()
+
+
+def test_rollback_at_the_largest_lengths():
+    """The end of a shared page that lies at 2^31 tokens, and no free page: the length stays what it was."""
+    cache = mxq.KVCache.new(1, 1, 1, 64, 256)
+    cache.refs.fill_(2)
+    width, n = 1 << 23, (1 << 31) - 100
+    tables = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    tables[0, width - 1] = 0
+    lens = i32([n])
+    mxq.mxq_kv_resize(cache, tables, lens, i32([n - 50]))
+    assert lens.tolist() == [n] and cache.refs.tolist() == [2] and int(tables[0, -1]) == 0
