@@ -973,12 +973,12 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                 const int nrows = pending.nrows;
                 const uint32_t parts = pending.parts, slot0 = pending.slot0;
                 const float *const p0 = a.partials + (size_t)slot0 * kAttSlotFloats<D, NT>;
-                float2 *const table = reinterpret_cast<float2 *>(att_smem_raw);       // [part][row]: maximum and sum, then the part's share
+                float2 *const table = reinterpret_cast<float2 *>(att_smem_raw);       // [part][row]: maximum and sum, then the part's share (its bounds are in mxq_kv_division.h)
                 float4 *const sums = reinterpret_cast<float4 *>(att_smem_raw + ((size_t)parts * nrows * 8 + 15) / 16 * 16);
                 const int pairs = (int)parts * nrows;
                 for (int x = tid; x < pairs; x += kAttThreads) {
                     const int i = x / nrows, r = x - i * nrows;
-                    table[x] = __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
+                    *MXQ_AT(table + x, 8, att_smem_raw, (kAttSmem<D, NT>)) = __ldcg(reinterpret_cast<const float2 *>(MXQ_AT(p0 + i * (kAttSlotFloats<D, NT>) + kAttRows<NT> * D + 2 * r, 8, a.partials, ws_bytes)));
                 }
                 __syncthreads();
                 float m = -INFINITY, l = 0.f;       // of row `lane`
@@ -1035,7 +1035,7 @@ __global__ void __launch_bounds__(kAttThreads, (kAttCtasPerSm<D, NT>)) kv_attent
                         store_part(out_row(pending.b, pending.head, pending.r0 + task / kCols), 4 * (task % kCols), add_parts(task, 0, 1));
                 } else {
                     const int task = tid % tasks, share = tid / tasks;
-                    if (share < shares) sums[tid] = add_parts(task, share, shares);
+                    if (share < shares) *MXQ_AT(sums + tid, 16, att_smem_raw, (kAttSmem<D, NT>)) = add_parts(task, share, shares);
                     __syncthreads();
                     if (share == 0) {
                         float4 v = sums[task];

@@ -115,12 +115,11 @@ def test_more_than_32_tiles_per_warp(d, h, hq, lens):
     run(lens, [1] * 3, h, hq, d, 256, 300 + d, missing=[(0, w) for w in far])
 
 
-@pytest.mark.skipif(CHECKED, reason="the sizes before it take every branch of the checked build")
 @pytest.mark.parametrize("d,h,hq,m,lens", [
     (64, 1, 8, 1, [1900001]), (64, 1, 7, 1, [260700] * 7), (64, 1, 16, 1, [456001] * 3), (64, 2, 32, 1, [455007] * 2),
     (128, 1, 8, 1, [700001] * 2), (128, 1, 16, 1, [1000001]), (128, 1, 1, 16, [1000001])])
 def test_few_long_segments(d, h, hq, m, lens):
-    """A segment of hundreds of CTAs' shares: as many parts as the join's table holds."""
+    """A segment of hundreds of CTAs' shares: as many parts as the join's table holds (the checked build tests the table's stores too)."""
     nt, share = share_of(lens, [m] * len(lens), h, hq // h, d)
     assert share >= 96 and max(lens) // 32 > 80 * share, share
     run(lens, [m] * len(lens), h, hq, d, 256, 400 + d)
