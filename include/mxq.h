@@ -449,9 +449,124 @@ int mxq_kv_fork(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_
 int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows,
                    const int32_t *keep, const int32_t *kept, int32_t *lens_out, void *stream);
 
+/* ---- what a decoder step needs between its linear layers and its cache --------------------------------------------------------- */
+
+/* Root-mean-square norm with the residual's addition:  h = x + residual,  y = h / sqrt(mean(h^2) + eps) * w,  row by row, all in FP32
+ * (the norm is that of the unrounded h; rows whose squares sum to more than FLT_MAX give 0, rows with a NaN NaN).
+ *   X [M][K], rows x_stride elements apart (>= K, rows 16-byte aligned), MXQ_F32 or MXQ_BF16 (x_dtype)
+ *   residual [M][K] in r_dtype, or NULL;  residual_out [M][K] in r_dtype receives h, or NULL (may be residual itself)
+ *   weight [K] in w_dtype
+ *   Y_bf16 [M][K] BF16, or NULL;  codes uint8 [M][K] with scales uint8 [M][K/32], or both NULL; one of the two forms at least.
+ *          Y may be X or residual where type and stride are its own.
+ * The MXFP8 pair: blocks of 32 along K, one E8M0 scale byte each (as in the MXFP4 pair: 2^(b-127), 0xFF = NaN), E4M3 elements in their
+ * natural order: the scale is 2^(floor(log2 max|y|) - 8), never below 2^-127; elements divided by it are rounded to nearest even,
+ * magnitudes above 448 clamp to 448.  A block with an Inf or NaN gets scale 0xFF and codes 0.
+ * 1 <= M < 2^31, K a multiple of 32 up to MXQ_MAX_NORM_K, eps finite and >= 0.  Bit-reproducible run to run.  `weight` is read before
+ * earlier calls of the library in the stream have ended (so are the adapters and ids below): it must not be their output. */
+#define MXQ_MAX_NORM_K 32768
+int mxq_rmsnorm(const void *X, int x_dtype, int64_t x_stride, const void *residual, int r_dtype, void *residual_out, const void *weight,
+                int w_dtype, float eps, int64_t M, int64_t K, void *Y_bf16, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* The values of an MXFP8 pair [N][K]: FP32 exactly (scale bytes up to 246, the largest that the cast gives), BF16 rounded to nearest
+ * even (exact from 2^-133 on). */
+int mxq_dequantize_mxfp8(const uint8_t *codes, const uint8_t *scales, int64_t N, int64_t K, void *out, int out_dtype, void *stream);
+
+/* Rotary positions on the way into the 4-bit cache: mxq_kv_append with the keys rotated before their cast, and the queries of the same rows
+ * rotated beside them.  A pair (a, b) of a head's elements at position p turns into (x_a c - x_b s, x_b c + x_a s), c and s from row p of
+ * the table; FP32, every product and sum rounded once; queries are then rounded to BF16, keys cast from FP32.
+ *   rope   HOST struct, read during the call: table float [positions][rotary_dim], cosines of pair 0.., then sines; rotary_dim a multiple
+ *          of 16 up to head_dim: the elements d < rotary_dim take part, the others pass; style MXQ_ROPE_HALVES: pairs
+ *          (d, d + rotary_dim / 2); MXQ_ROPE_PAIRS: pairs (2d, 2d + 1)
+ *   Q_bf16 [B][M][q_heads][head_dim], token rows q_stride apart -> Q_out, token rows q_out_stride apart (may be Q_bf16 itself with its stride);
+ *          both NULL: keys and values only (q_heads and the strides are then ignored)
+ *   positions  int32 [B][M]: the position of every row (a token tree's rows: by their depth); NULL: its place in the sequence,
+ *          lens[b] - rows[b] + i.  A position outside the table turns what it rotates into NaN (keys: blocks of scale 0xFF)
+ * Everything else as in mxq_kv_append; B * M * (q_heads + 2 * kv_heads) <= 2^29.  Rows that are not there (i >= rows[b], or before the
+ * sequence's first token) give queries of zero; rows whose token has no page are rotated, but not stored.
+ * mxq_rope_table fills a table: angle p * inv_freq[i] in 64 bits, amplitude * cosine and sine rounded to FP32.  inv_freq double
+ * [rotary_dim / 2] (device); positions 1 .. 2^31, rotary_dim a multiple of 16 up to 128. */
+enum mxq_rope_style { MXQ_ROPE_HALVES = 0, MXQ_ROPE_PAIRS = 1 };
+typedef struct mxq_rope {
+    const float *table;
+    int64_t positions;
+    int32_t rotary_dim, style;
+} mxq_rope;
+int mxq_rope_table(const double *inv_freq, int64_t positions, int rotary_dim, float amplitude, float *table, void *stream);
+int mxq_kv_append_rope(const mxq_kv_cache *cache, int layer, const void *Q_bf16, int64_t q_stride, int q_heads, void *Q_out, int64_t q_out_stride,
+                       const void *K_bf16, int64_t k_stride, const void *V_bf16, int64_t v_stride, int B, int M, const int32_t *tables, int W,
+                       const int32_t *lens, const int32_t *rows, const mxq_rope *rope, const int32_t *positions, void *stream);
+
+/* Rules on logits: penalties for tokens that were there before, biases, a grammar's mask.  For the logit x of token v in row r of sequence b,
+ * in FP32, every operation rounded once:
+ *     x = x > 0 ? x / repetition : x * repetition      if v was prompted, or generated (count > 0)
+ *     x = x - frequency * count - presence             if v was generated, count times
+ *     x = x + bias                                     if v has an entry in the sequence's list (of several the last one counts)
+ *     x = -inf                                         if bit v of the row's mask is 0, whatever x is
+ * Where no rule applies x stays as it is.  In row r the proposals before it, draft[b][0..r), count as generated once each.
+ *   penalties  float [B][3]: repetition (1: none), presence, frequency (0: none); NULL: no penalties, counts are not read
+ *   counts     uint32 [B][V]: bits 0-30 how often the token was generated, bit 31 the prompt has it; NULL: nothing was before
+ *   bias_tokens int32 [B][bias_count], bias_values float [B][bias_count]; a token outside 0..V-1 is no entry; bias_count up to MXQ_MAX_BIASES
+ *   allowed    uint32 [B][R][(V + 31) / 32]: bit v % 32 of word v / 32; NULL: everything is allowed
+ * The struct is a HOST struct read during the call; the arrays need their own alignment only, logits and out 16 bytes.
+ *   logits [B][R][V] MXQ_F32 or MXQ_BF16;  draft [B][T] int32, T <= MXQ_MAX_T;  R == T or T + 1 (T == 0, R == 1: no proposals, draft NULL)
+ * mxq_logits_adjust writes the adjusted logits in the same type (BF16 rounded to nearest even) to out (may be logits itself).
+ * mxq_greedy_accept_rules verifies the proposals against the argmax of the adjusted logits (in FP32), which it does not write: verifier
+ * int32 [B][R] the argmax of every row, accept_len and next_token [B] as mxq_greedy_accept (ties to the lowest index, NaN and -inf never
+ * chosen; a row with nothing above -inf yields 0).
+ *   workspace  device memory, >= mxq_greedy_accept_rules_workspace_bytes, 16-byte aligned; zero all of it once before the first use; every
+ *              call leaves it zero again, so calls of any shape it is large enough for may share it.  One per stream.
+ * mxq_token_counts adds the tokens [B][L] (the first n[b] of each row; n NULL: all) to counts: as generated (prompt == 0) or marked as
+ * prompted (prompt != 0); with next_token [B] also that one token per sequence.  Tokens outside 0..V-1 are left out.  After a verification:
+ * tokens = draft, n = accept_len, next_token.  counts is the caller's: zero a sequence's row when it starts. */
+#define MXQ_MAX_BIASES 1024
+typedef struct mxq_logit_rules {
+    const uint32_t *counts;
+    const float *penalties;
+    const int32_t *bias_tokens;
+    const float *bias_values;
+    const uint32_t *allowed;
+    int32_t bias_count;
+    int32_t reserved;     /* 0 */
+} mxq_logit_rules;
+int mxq_logits_adjust(const void *logits, int dtype, int64_t B, int R, int64_t V, const int32_t *draft, int T, const mxq_logit_rules *rules,
+                      void *out, void *stream);
+size_t mxq_greedy_accept_rules_workspace_bytes(int64_t B, int R, int64_t V);
+int mxq_greedy_accept_rules(const void *logits, int dtype, int64_t B, int R, int64_t V, const int32_t *draft, int T, const mxq_logit_rules *rules,
+                            int32_t *verifier, int32_t *accept_len, int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream);
+int mxq_token_counts(uint32_t *counts, int64_t B, int64_t V, const int32_t *tokens, int64_t L, const int32_t *n, const int32_t *next_token,
+                     int prompt, void *stream);
+
+/* Low-rank adapters of many requests at once, beside a shared projection:
+ *     Y[m] = base[m] + s_a B_a (A_a x[m]),   a = ids[m];   Y[m] = base[m] where ids[m] is no adapter (outside 0..count-1).
+ *   adapters  HOST struct: A_bf16 [count][rank][K], B_bf16 [count][N][rank] BF16, scale float [count] or NULL (1); rank a multiple of 8 up to
+ *             128 (pad with zeros), count up to MXQ_LORA_MAX_ADAPTERS
+ *   X_bf16 [M][K] BF16;  ids int32 [M] (device), in any order (rows of one adapter next to one another are fastest)
+ *   base [M][N] in Y's type (may be Y itself: added in place, rows without an adapter are then not touched), or NULL: zero
+ *   Y [M][N] MXQ_F32, or MXQ_BF16 rounded to nearest even
+ *   workspace  device memory, >= the *_workspace_bytes, 16-byte aligned, no initialisation needed; one per stream
+ * K a multiple of 32, any N, 1 <= M <= MXQ_LORA_MAX_M (mxq_lora) or MXQ_MAX_M.  Sums are FP32; A x meets B with all its bits for an FP32 Y, with 16
+ * bits of mantissa for a BF16 Y:
+ *     |Y - exact| <= ((K / 16 + 96) * 2^-22 [+ 2^-17, BF16]) * |s_a| sum_r |B_nr| sum_k |A_rk x_k| + 2^-23 |Y| + BF16's rounding.
+ * An adapter's own Inf or NaN stay in the rows that have it.  Bit-reproducible run to run.
+ * mxq_linear_lora is mxq_linear with the adapters added: base = X . w^T, kept in FP32 until the sum is rounded; arguments as there. */
+#define MXQ_LORA_MAX_M (1 << 20)
+#define MXQ_LORA_MAX_ADAPTERS 65536
+typedef struct mxq_lora_adapters {
+    const void *A_bf16;
+    const void *B_bf16;
+    const float *scale;
+    int32_t rank, count;
+} mxq_lora_adapters;
+size_t mxq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int rank, int adapters);
+int mxq_lora(const void *X_bf16, int64_t M, const mxq_lora_adapters *adapters, const int32_t *ids, int64_t N, int64_t K, const void *base,
+             void *Y, int y_dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t mxq_linear_lora_workspace_bytes(int M, int64_t N, int64_t K, int rank, int adapters);
+int mxq_linear_lora(const void *X_bf16, int M, const uint8_t *codes, const uint8_t *scales, int64_t N, int64_t K, const mxq_lora_adapters *adapters,
+                    const int32_t *ids, void *Y, int y_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
 /* The bounds-checked build (the library compiled with -DMXQ_DEBUG_BOUNDS; python -m paper_2503_13565_b200.build
  * --checked writes it to libmxq_checked.so): in the linear kernels (mxq_linear with every kernel choice, the layer
- * epilogues, mxq_lm_head_accept, mxq_linear_batch, mxq_linear_bf16) and those of the key/value cache every plain load and store of global memory whose
+ * epilogues, mxq_lm_head_accept, mxq_linear_batch, mxq_linear_bf16), those of the key/value cache, the norm, the logit rules and the adapters every plain load and store of global memory whose
  * address is formed from an index -- X, codes, scales, Y, residual, workspace images, partial sums, correction lists,
  * tickets -- is tested against its buffer first.  An access outside it is counted, the first one recorded, and the
  * access itself redirected to a scratch area: a wrong index shows as a report, never as a fault.  (TMA copies are
@@ -460,7 +575,7 @@ int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *table
  * mxq_debug_bounds_report: report[0] = 1 if this library is the checked build (else 0 and the rest stays 0);
  *   report[1] = accesses refused since the last call; of the first one: report[2] = source file (0 mxq_linear.cu, 1
  *   mxq_linear_umma.cu, 2 mxq_linear_fp4.cu, 3 mxq_linear_mma.cu, 4 mxq_linear_batch.cu, 5 mxq_linear_bf16.cu, 6 mxq_kv_cache.cu,
- *   7 mxq_kv_pages.cu, 8 mxq_kv_attention.cu),
+ *   7 mxq_kv_pages.cu, 8 mxq_kv_attention.cu, 9 mxq_norm.cu, 10 mxq_kv_rope.cu, 11 mxq_logits.cu, 12 mxq_lora.cu),
  *   report[3] = source line, report[4] = byte offset from the buffer's base (modulo 2^64), report[5] = the buffer's size.
  *   Reading clears the record.  Synchronises with the device.
  * mxq_debug_bounds_selftest: checked build only (otherwise MXQ_ERR_SHAPE): one kernel stores 4 bytes at offset 100

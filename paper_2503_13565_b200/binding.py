@@ -124,6 +124,30 @@ def lib() -> ctypes.CDLL:
             L.mxq_debug_kv_lost_tile.argtypes = [i32]
             L.mxq_debug_batch_fault.restype = i32
             L.mxq_debug_batch_fault.argtypes = [i32, ctypes.c_uint]
+            L.mxq_rmsnorm.restype = i32
+            L.mxq_rmsnorm.argtypes = [vp, i32, i64, vp, i32, vp, vp, i32, ctypes.c_float, i64, i64, vp, vp, vp, vp]
+            L.mxq_dequantize_mxfp8.restype = i32
+            L.mxq_dequantize_mxfp8.argtypes = [vp, vp, i64, i64, vp, i32, vp]
+            L.mxq_rope_table.restype = i32
+            L.mxq_rope_table.argtypes = [vp, i64, i32, ctypes.c_float, vp, vp]
+            L.mxq_kv_append_rope.restype = i32
+            L.mxq_kv_append_rope.argtypes = [vp, i32, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp]
+            L.mxq_logits_adjust.restype = i32
+            L.mxq_logits_adjust.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp]
+            L.mxq_greedy_accept_rules_workspace_bytes.restype = sz
+            L.mxq_greedy_accept_rules_workspace_bytes.argtypes = [i64, i32, i64]
+            L.mxq_greedy_accept_rules.restype = i32
+            L.mxq_greedy_accept_rules.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+            L.mxq_token_counts.restype = i32
+            L.mxq_token_counts.argtypes = [vp, i64, i64, vp, i64, vp, vp, i32, vp]
+            L.mxq_lora_workspace_bytes.restype = sz
+            L.mxq_lora_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+            L.mxq_lora.restype = i32
+            L.mxq_lora.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, i32, vp, sz, vp]
+            L.mxq_linear_lora_workspace_bytes.restype = sz
+            L.mxq_linear_lora_workspace_bytes.argtypes = [i32, i64, i64, i32, i32]
+            L.mxq_linear_lora.restype = i32
+            L.mxq_linear_lora.argtypes = [vp, i32, vp, vp, i64, i64, vp, vp, vp, i32, vp, sz, vp]
             _lib = L
     return _lib
 
@@ -762,12 +786,281 @@ def mxq_kv_compact(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, row
     return lens_out
 
 
+# ---- what a decoder step needs between its linear layers and its cache --------------------
+
+
+def _rows_of(t: torch.Tensor, what: str):
+    """Pointer and row stride (elements) of a CUDA tensor [M, K] whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise TypeError("%s must be a CUDA tensor [M, K] with contiguous rows" % what)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _same(t, shape, what: str):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s" % (what, list(shape)))
+    return t
+
+
+def mxq_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: torch.Tensor = None, residual_out: torch.Tensor = None,
+                bf16: bool = True, mxfp8: bool = False, out: torch.Tensor = None, codes: torch.Tensor = None, scales: torch.Tensor = None,
+                stream=None):
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight for rows x [M, K] (FP32 or BF16, a column slice will do).  ``residual_out``
+    receives h (``residual`` itself: the stream is updated in place).  Returns y BF16 and / or its MXFP8 pair: y with ``bf16``,
+    (codes u8 [M, K], scales u8 [M, K/32]) with ``mxfp8``, (y, codes, scales) with both."""
+    xp, stride = _rows_of(x, "x")
+    m, k = x.shape
+    _same(weight, (k,), "weight")
+    if residual is not None:
+        _same(residual, (m, k), "residual")
+    if residual_out is not None:
+        if residual is None or residual_out.dtype != residual.dtype:
+            raise TypeError("residual_out needs a residual of its dtype")
+        _same(residual_out, (m, k), "residual_out")
+    bf16, mxfp8 = bf16 or out is not None, mxfp8 or codes is not None or scales is not None
+    if not bf16 and not mxfp8:
+        raise ValueError("nothing to return: bf16 or mxfp8")
+    with _on(stream):
+        if bf16 and out is None:
+            out = torch.empty((m, k), dtype=torch.bfloat16, device=x.device)
+        if mxfp8 and codes is None:
+            codes = torch.empty((m, k), dtype=torch.uint8, device=x.device)
+        if mxfp8 and scales is None:
+            scales = torch.empty((m, k // 32), dtype=torch.uint8, device=x.device)
+    if bf16:
+        _same(out, (m, k), "out")
+    if mxfp8:
+        _same(codes, (m, k), "codes"), _same(scales, (m, k // 32), "scales")
+    _check(lib().mxq_rmsnorm(xp, _dt(x.dtype), stride, 0 if residual is None else _dev(residual, residual.dtype, "residual"),
+                             0 if residual is None else _dt(residual.dtype), 0 if residual_out is None else _dev(residual_out, residual.dtype, "residual_out"),
+                             _dev(weight, weight.dtype, "weight"), _dt(weight.dtype), eps, m, k, _dev(out, torch.bfloat16, "out") if bf16 else 0,
+                             _dev(codes, torch.uint8, "codes") if mxfp8 else 0, _dev(scales, torch.uint8, "scales") if mxfp8 else 0, _stream(stream)),
+           "mxq_rmsnorm")
+    return (out, codes, scales) if bf16 and mxfp8 else out if bf16 else (codes, scales)
+
+
+def mxq_dequantize_mxfp8(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor = None, out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """The values [N, K] that an MXFP8 pair stands for."""
+    n, k = codes.shape
+    _same(scales, (n, k // 32), "scales")
+    if out is None:
+        with _on(stream):
+            out = torch.empty((n, k), dtype=out_dtype, device=codes.device)
+    _same(out, (n, k), "out")
+    _check(lib().mxq_dequantize_mxfp8(_dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), n, k, _dev(out, out.dtype, "out"),
+                                      _dt(out.dtype), _stream(stream)), "mxq_dequantize_mxfp8")
+    return out
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32), ("style", ctypes.c_int32)]
+
+
+ROPE_STYLES = {"halves": 0, "pairs": 1}
+
+
+class Rope:
+    """Angles of the rotary positions, marshalled once: ``table`` FP32 [positions, rotary_dim], cosines then sines of the rotary_dim / 2
+    pairs (``mxq_rope_table`` makes one); ``style`` "halves": pairs (d, d + rotary_dim / 2), "pairs": (2d, 2d + 1)."""
+
+    def __init__(self, table: torch.Tensor, style: str = "halves"):
+        if table.dim() != 2 or style not in ROPE_STYLES:
+            raise ValueError("table must be [positions, rotary_dim], style one of %s" % sorted(ROPE_STYLES))
+        self.table, self.style = table, style
+        self._struct = _RopeStruct(_dev(table, torch.float32, "table"), table.shape[0], table.shape[1], ROPE_STYLES[style])
+        self.ptr = ctypes.addressof(self._struct)
+
+
+def mxq_rope_table(inv_freq: torch.Tensor, positions: int, amplitude: float = 1.0, out: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Table FP32 [positions, rotary_dim] for ``Rope``: angle p * inv_freq[i], inv_freq FP64 [rotary_dim / 2]."""
+    rotary = 2 * inv_freq.shape[0]
+    if out is None:
+        with _on(stream):
+            out = torch.empty((positions, rotary), dtype=torch.float32, device=inv_freq.device)
+    _same(out, (positions, rotary), "out")
+    _check(lib().mxq_rope_table(_dev(inv_freq, torch.float64, "inv_freq"), positions, rotary, amplitude, _dev(out, torch.float32, "out"), _stream(stream)),
+           "mxq_rope_table")
+    return out
+
+
+def mxq_kv_append_rope(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor,
+                       rope: Rope, rows: torch.Tensor = None, positions: torch.Tensor = None, q_out: torch.Tensor = None, stream=None):
+    """mxq_kv_append with rotary positions: the keys of the new rows are rotated on their way into one layer of the cache, and the
+    queries q [B, M, q_heads, D] of the same rows are returned rotated (``q_out``; may be ``q`` itself; q None: keys and values only).
+    ``positions`` int32 [B, M], or None: the rows' places in their sequences."""
+    b, tp, w, lp = _kv_seqs(tables, lens)
+    m = k.shape[1]
+    shape = (b, m, cache.kv_heads, cache.head_dim)
+    kp, ks = _token_rows(k, shape, "k")
+    vp, vs = _token_rows(v, shape, "v")
+    qp = qs = hq = op = os_ = 0
+    if q is not None:
+        hq = q.shape[2]
+        shape = (b, m, hq, cache.head_dim)
+        qp, qs = _token_rows(q, shape, "q")
+        if q_out is None:
+            with _on(stream):
+                q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        op, os_ = _token_rows(q_out, shape, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _check(lib().mxq_kv_append_rope(cache.ptr, layer, qp, qs, hq, op, os_, kp, ks, vp, vs, b, m, tp, w, lp, _kv_ints(rows, (b,), "rows"), rope.ptr,
+                                    _kv_ints(positions, (b, m), "positions"), _stream(stream)), "mxq_kv_append_rope")
+    return q_out
+
+
+class _LogitRulesStruct(ctypes.Structure):
+    _fields_ = [("counts", ctypes.c_void_p), ("penalties", ctypes.c_void_p), ("bias_tokens", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("allowed", ctypes.c_void_p), ("bias_count", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class LogitRules:
+    """The rules of a batch (see mxq_logit_rules in mxq.h), marshalled once; the tensors stay the caller's and may be written between
+    calls.  ``counts`` int32 [B, V] (bit 31: prompted), ``penalties`` FP32 [B, 3] (repetition, presence, frequency), ``bias_tokens`` int32 and
+    ``bias_values`` FP32 [B, J], ``allowed`` int32 [B, R, (V + 31) // 32]; each may be None."""
+
+    def __init__(self, counts=None, penalties=None, bias_tokens=None, bias_values=None, allowed=None):
+        if (bias_tokens is None) != (bias_values is None) or (bias_tokens is not None and bias_tokens.shape != bias_values.shape):
+            raise ValueError("bias_tokens and bias_values must both be [B, J]")
+        self.counts, self.penalties, self.bias_tokens, self.bias_values, self.allowed = counts, penalties, bias_tokens, bias_values, allowed
+        p = [0 if t is None else _dev(t, d, n) for t, d, n in ((counts, torch.int32, "counts"), (penalties, torch.float32, "penalties"),
+                                                               (bias_tokens, torch.int32, "bias_tokens"), (bias_values, torch.float32, "bias_values"),
+                                                               (allowed, torch.int32, "allowed"))]
+        self._struct = _LogitRulesStruct(*p, 0 if bias_tokens is None else bias_tokens.shape[1], 0)
+        self.ptr = ctypes.addressof(self._struct)
+
+    def fit(self, b: int, r: int, v: int) -> int:
+        """The struct's address for a call on logits [b, r, v]."""
+        for t, shape, what in ((self.counts, (b, v), "counts"), (self.penalties, (b, 3), "penalties"), (self.allowed, (b, r, (v + 31) // 32), "allowed")):
+            if t is not None and t.shape != shape:
+                raise ValueError("%s must be %s" % (what, list(shape)))
+        if self.bias_tokens is not None and (self.bias_tokens.dim() != 2 or self.bias_tokens.shape[0] != b):
+            raise ValueError("bias_tokens must be [B, J]")
+        return self.ptr
+
+
+def _draft(draft, b: int):
+    if draft is None:
+        return 0, 0
+    if draft.dim() != 2 or draft.shape[0] != b:
+        raise ValueError("draft must be [B, T]")
+    return _dev(draft, torch.int32, "draft"), draft.shape[1]
+
+
+def mxq_logits_adjust(logits: torch.Tensor, rules: LogitRules, draft: torch.Tensor = None, out: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Logits [B, R, V] after the rules, in their own dtype (``out`` may be ``logits``); row r counts draft[:, :r] as generated."""
+    b, r, v = logits.shape
+    dp, t = _draft(draft, b)
+    if out is None:
+        with _on(stream):
+            out = torch.empty_like(logits)
+    _same(out, (b, r, v), "out")
+    _check(lib().mxq_logits_adjust(_dev(logits, logits.dtype, "logits"), _dt(logits.dtype), b, r, v, dp, t, rules.fit(b, r, v),
+                                   _dev(out, logits.dtype, "out"), _stream(stream)), "mxq_logits_adjust")
+    return out
+
+
+def mxq_greedy_accept_rules_workspace_bytes(b: int, r: int, v: int) -> int:
+    return int(lib().mxq_greedy_accept_rules_workspace_bytes(b, r, v))
+
+
+def mxq_greedy_accept_rules(logits: torch.Tensor, draft: torch.Tensor, rules: LogitRules, workspace: torch.Tensor = None, stream=None, out=None):
+    """mxq_greedy_accept on the logits [B, R, V] after the rules, which are not written -> (verifier [B, R], accept_len [B], next_token [B])
+    int32.  ``draft`` [B, T] int32, or None with R = 1: next_token is the argmax.  ``out``: optional triple of tensors to write into."""
+    b, r, v = logits.shape
+    dp, t = _draft(draft, b)
+    with _on(stream):
+        if workspace is None:
+            workspace = new_workspace(mxq_greedy_accept_rules_workspace_bytes(b, r, v), logits.device)
+        if out is None:
+            out = (torch.empty((b, r), dtype=torch.int32, device=logits.device), torch.empty(b, dtype=torch.int32, device=logits.device),
+                   torch.empty(b, dtype=torch.int32, device=logits.device))
+    ver, n, nxt = out
+    _same(ver, (b, r), "verifier"), _same(n, (b,), "accept_len"), _same(nxt, (b,), "next_token")
+    _check(lib().mxq_greedy_accept_rules(_dev(logits, logits.dtype, "logits"), _dt(logits.dtype), b, r, v, dp, t, rules.fit(b, r, v),
+                                         _dev(ver, torch.int32, "verifier"), _dev(n, torch.int32, "accept_len"), _dev(nxt, torch.int32, "next_token"),
+                                         _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_greedy_accept_rules")
+    return ver, n, nxt
+
+
+def mxq_token_counts(counts: torch.Tensor, tokens: torch.Tensor, n: torch.Tensor = None, next_token: torch.Tensor = None, prompt: bool = False,
+                     stream=None) -> None:
+    """Add the first n[b] (None: all) of tokens [B, L] int32, and next_token [B] if given, to counts int32 [B, V]: as generated, or with
+    ``prompt`` marked as prompted.  After a verification: tokens = draft, n = accept_len, next_token."""
+    b, v = counts.shape
+    if tokens.dim() != 2 or tokens.shape[0] != b:
+        raise ValueError("tokens must be [B, L]")
+    _check(lib().mxq_token_counts(_dev(counts, torch.int32, "counts"), b, v, _dev(tokens, torch.int32, "tokens"), tokens.shape[1],
+                                  _kv_ints(n, (b,), "n"), _kv_ints(next_token, (b,), "next_token"), 1 if prompt else 0, _stream(stream)), "mxq_token_counts")
+
+
+class _LoraStruct(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rank", ctypes.c_int32), ("count", ctypes.c_int32)]
+
+
+def _adapters(a, b, scale, ids, m, k):
+    """(struct, ids pointer, N) of adapters a [L, r, K], b [L, N, r] for rows [m, k]."""
+    if a.dim() != 3 or b.dim() != 3 or a.shape[2] != k or b.shape[0] != a.shape[0] or b.shape[2] != a.shape[1]:
+        raise ValueError("a must be [L, r, K] and b [L, N, r]")
+    if scale is not None:
+        _same(scale, (a.shape[0],), "scale")
+    return (_LoraStruct(_dev(a, torch.bfloat16, "a"), _dev(b, torch.bfloat16, "b"), 0 if scale is None else _dev(scale, torch.float32, "scale"),
+                        a.shape[1], a.shape[0]), _kv_ints(ids, (m,), "ids"), b.shape[1])
+
+
+def mxq_lora_workspace_bytes(m: int, n: int, k: int, rank: int, adapters: int) -> int:
+    return int(lib().mxq_lora_workspace_bytes(m, n, k, rank, adapters))
+
+
+def mxq_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, scale: torch.Tensor = None, base: torch.Tensor = None,
+             out: torch.Tensor = None, out_dtype=torch.float32, workspace: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Y[m] = base[m] + scale[i] * b[i] (a[i] x[m]), i = ids[m] (no adapter: base[m]); x [M, K] BF16, a [L, r, K], b [L, N, r] BF16, ids int32 [M].
+    ``base`` has Y's dtype and may be ``out`` itself (added in place); None: zero."""
+    m, k = x.shape
+    ad, ip, n = _adapters(a, b, scale, ids, m, k)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((m, n), dtype=out_dtype if base is None else base.dtype, device=x.device)
+        if workspace is None:
+            workspace = torch.empty(max(16, mxq_lora_workspace_bytes(m, n, k, ad.rank, ad.count)), dtype=torch.uint8, device=x.device)
+    _same(out, (m, n), "out")
+    if base is not None:
+        _same(base, (m, n), "base")
+    _check(lib().mxq_lora(_dev(x, torch.bfloat16, "x"), m, ctypes.addressof(ad), ip, n, k, 0 if base is None else _dev(base, out.dtype, "base"),
+                          _dev(out, out.dtype, "out"), _dt(out.dtype), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_lora")
+    return out
+
+
+def mxq_linear_lora_workspace_bytes(m: int, n: int, k: int, rank: int, adapters: int) -> int:
+    return int(lib().mxq_linear_lora_workspace_bytes(m, n, k, rank, adapters))
+
+
+def mxq_linear_lora(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor,
+                    scale: torch.Tensor = None, out: torch.Tensor = None, out_dtype=torch.float32, workspace: torch.Tensor = None,
+                    stream=None) -> torch.Tensor:
+    """mxq_linear with the adapters of its rows added (see ``mxq_lora``): X . w^T + scale[i] * b[i] (a[i] x[m])."""
+    m, k = x.shape
+    ad, ip, n = _adapters(a, b, scale, ids, m, k)
+    if tuple(codes.shape) != (n, k // 2) or tuple(scales.shape) != (n, k // 32):
+        raise ValueError("shape mismatch between X, codes, scales and b")
+    with _on(stream):
+        if out is None:
+            out = torch.empty((m, n), dtype=out_dtype, device=x.device)
+        if workspace is None:
+            workspace = torch.empty(max(16, mxq_linear_lora_workspace_bytes(m, n, k, ad.rank, ad.count)), dtype=torch.uint8, device=x.device)
+    _same(out, (m, n), "out")
+    _check(lib().mxq_linear_lora(_dev(x, torch.bfloat16, "x"), m, _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), n, k,
+                                 ctypes.addressof(ad), ip, _dev(out, out.dtype, "out"), _dt(out.dtype), _dev(workspace, torch.uint8, "workspace"),
+                                 workspace.numel(), _stream(stream)), "mxq_linear_lora")
+    return out
+
+
 def mxq_debug_bounds_report() -> dict:
     """What the bounds-checked build has refused since the last call (see mxq.h); ``checked`` is False for the ordinary build."""
     r = (ctypes.c_uint64 * 6)()
     _check(lib().mxq_debug_bounds_report(ctypes.cast(r, ctypes.c_void_p)), "mxq_debug_bounds_report")
     files = ("mxq_linear.cu", "mxq_linear_umma.cu", "mxq_linear_fp4.cu", "mxq_linear_mma.cu", "mxq_linear_batch.cu", "mxq_linear_bf16.cu",
-             "mxq_kv_cache.cu", "mxq_kv_pages.cu", "mxq_kv_attention.cu")
+             "mxq_kv_cache.cu", "mxq_kv_pages.cu", "mxq_kv_attention.cu", "mxq_norm.cu", "mxq_kv_rope.cu", "mxq_logits.cu", "mxq_lora.cu")
     out = {"checked": bool(r[0]), "refused": int(r[1])}
     if r[1]:
         out.update(file=files[int(r[2])], line=int(r[3]), offset=int(r[4]), extent=int(r[5]))

@@ -91,5 +91,29 @@ int bounds_take_linear_bf16(unsigned long long *out);   // mxq_linear_bf16.cu
 int bounds_take_kv_cache(unsigned long long *out);      // mxq_kv_cache.cu
 int bounds_take_kv_pages(unsigned long long *out);      // mxq_kv_pages.cu
 int bounds_take_kv_attention(unsigned long long *out);  // mxq_kv_attention.cu
+int bounds_take_norm(unsigned long long *out);          // mxq_norm.cu
+int bounds_take_kv_rope(unsigned long long *out);       // mxq_kv_rope.cu
+int bounds_take_logits(unsigned long long *out);        // mxq_logits.cu
+int bounds_take_lora(unsigned long long *out);          // mxq_lora.cu
+
+// launch with the programmatic-dependent-launch attribute (the kernel waits before it touches memory)
+template <class... P, class... A>
+int launch_pdl(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MXQ_ERR_CUDA;
+    }
+    return MXQ_OK;
+}
 
 }  // namespace mxq

@@ -68,35 +68,65 @@ __device__ __forceinline__ uint8_t *kv_tile(const KvView &c, int page, int slot,
 }
 __device__ __forceinline__ bool kv_page_ok(const KvView &c, int page) { return (unsigned)page < (unsigned)c.num_pages; }
 
+struct RowPlace {
+    uint8_t *tile;   // nullptr: no such row
+    int slot;        // token in the tile
+};
+
+// where the token at position pos of sequence b lives
+template <int D>
+__device__ __forceinline__ RowPlace row_place(const KvView &c, const KvSeqs &s, int b, int pos, int head) {
+    RowPlace p = {nullptr, 0};
+    if (pos < 0) return p;
+    const int page = s.page(b, pos >> c.page_shift);
+    if (!kv_page_ok(c, page)) return p;
+    const int slot = pos & ((1 << c.page_shift) - 1);
+    p.tile = kv_tile<D>(c, page, slot, head);
+    p.slot = slot & (kTileTokens - 1);
+    return p;
+}
+
+// stores lane q's quarter of a row, q = 0..3: its words w[j] of every block (natural bytes 16j + 4q ..), and its share of the scale bytes
+// (`scale`: block j's in byte j)
+template <int D>
+__device__ __forceinline__ void store_quarter(const KvView &c, const RowPlace &at, bool value, uint32_t q, const uint32_t (&w)[D / 32], uint32_t scale) {
+    using T = KvTile<D>;
+    constexpr int kNb = T::kNb;
+    uint32_t out[kNb];
+    if (!value) {
+#pragma unroll
+        for (int j = 0; j < kNb; ++j) out[j] = w[j];
+    } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
+#pragma unroll
+        for (int p = 0; p < kNb / 2; ++p) {
+            out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
+            out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
+        }
+    }
+    uint8_t *dst = MXQ_AT(at.tile + (value ? T::kV : 0) + at.slot * T::kRow + q * 4 * kNb, 4 * kNb, c.pool, c.pool_bytes);
+    if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+    else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
+    if (!value) {
+        if (q == 0) {
+            uint8_t *sc = MXQ_AT(at.tile + T::kKs + at.slot * kNb, kNb, c.pool, c.pool_bytes);
+            if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
+            else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
+        }
+    } else if (q < kNb) {
+        *MXQ_AT(at.tile + T::vs(at.slot, (int)q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * q));
+    }
+}
+
 // ---- host side --------------------------------------------------------------------------------------------------------
 int kv_check_cache(const mxq_kv_cache *cache, int layer);   // MXQ_OK or the error
 int kv_check_seqs(int B, int W, const int32_t *tables, const int32_t *lens);
 KvView kv_view(const mxq_kv_cache *cache, int layer);
+bool kv_rows_ok(int heads, int B, int M);   // a call of B x M rows of `heads` heads fits 32-bit lane indices
 inline KvSeqs kv_seqs(const mxq_kv_cache *cache, int B, int M, const int32_t *tables, int W, const int32_t *lens, const int32_t *rows) {
     KvSeqs s;
     s.tables = tables, s.lens = lens, s.rows = rows, s.B = B, s.W = W, s.m = M, s.page_tokens = cache->page_tokens;
     return s;
 }
 inline bool aligned_to(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-// launch with the programmatic-dependent-launch attribute (the kernel waits before it touches memory)
-template <class... P, class... A>
-int kv_launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, A... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pdl_enabled() ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return MXQ_ERR_CUDA;
-    }
-    return MXQ_OK;
-}
 
 }  // namespace mxq

@@ -1120,7 +1120,7 @@ static int att_launch(const KvView &c, const KvSeqs &s, KvQuery a, void *workspa
 #ifdef MXQ_DEBUG_BOUNDS
     a.lost_tile = g_lost_tile.exchange(-1, std::memory_order_relaxed);
 #endif
-    return kv_launch(kv_attention_kernel<D, NT>, dim3((unsigned)att_grid<D, NT>()), kAttThreads, smem, stream, c, s, a);
+    return launch_pdl(kv_attention_kernel<D, NT>, dim3((unsigned)att_grid<D, NT>()), kAttThreads, smem, stream, c, s, a);
 }
 
 // the template instance that covers a call: f(head dimension, column blocks) with both as constants

@@ -20,24 +20,6 @@ constexpr int kKvThreads = 128;
 // so that a lane's lookups (length, row count) are spent once and more loads are in flight.
 constexpr int kPromptRows = 4;
 
-struct RowPlace {
-    uint8_t *tile;   // nullptr: no such row
-    int slot;        // token in the tile
-};
-
-// where the token at position pos of sequence b lives
-template <int D>
-__device__ __forceinline__ RowPlace row_place(const KvView &c, const KvSeqs &s, int b, int pos, int head) {
-    RowPlace p = {nullptr, 0};
-    if (pos < 0) return p;
-    const int page = s.page(b, pos >> c.page_shift);
-    if (!kv_page_ok(c, page)) return p;
-    const int slot = pos & ((1 << c.page_shift) - 1);
-    p.tile = kv_tile<D>(c, page, slot, head);
-    p.slot = slot & (kTileTokens - 1);
-    return p;
-}
-
 // a lane's part of a call: quarter q of `head`'s rows i .. of sequence b
 struct LaneRows {
     int b, i, head;
@@ -98,29 +80,7 @@ __global__ void __launch_bounds__(kKvThreads) kv_append_kernel(KvView c, KvSeqs 
         scale |= byte << (8 * j);
     }
     if (at.tile == nullptr) return;
-    uint32_t out[kNb];
-    if (!value) {
-#pragma unroll
-        for (int j = 0; j < kNb; ++j) out[j] = w[j];
-    } else {   // chunk 2q: the low halves of every block's word, chunk 2q + 1: the high halves
-#pragma unroll
-        for (int p = 0; p < kNb / 2; ++p) {
-            out[p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x5410);
-            out[kNb / 2 + p] = __byte_perm(w[2 * p], w[2 * p + 1], 0x7632);
-        }
-    }
-    uint8_t *dst = MXQ_AT(at.tile + (value ? T::kV : 0) + at.slot * T::kRow + l.q * 4 * kNb, 4 * kNb, c.pool, c.pool_bytes);
-    if constexpr (kNb == 4) *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
-    else *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
-    if (!value) {
-        if (l.q == 0) {
-            uint8_t *sc = MXQ_AT(at.tile + T::kKs + at.slot * kNb, kNb, c.pool, c.pool_bytes);
-            if constexpr (kNb == 4) *reinterpret_cast<uint32_t *>(sc) = scale;
-            else *reinterpret_cast<uint16_t *>(sc) = (uint16_t)scale;
-        }
-    } else if (l.q < kNb) {
-        *MXQ_AT(at.tile + T::vs(at.slot, (int)l.q), 1, c.pool, c.pool_bytes) = (uint8_t)(scale >> (8 * l.q));
-    }
+    store_quarter<D>(c, at, value, l.q, w, scale);
 }
 
 // The same for prompts, where the arithmetic decides: one lane per MX block (no exchange for the maximum, every scale computed
@@ -304,7 +264,7 @@ static uint32_t lanes_of(const mxq_kv_cache *c, int B, int M, bool prompt) {
 }
 
 // rows of one call: at most 2^29 (row, head) pairs, so that a lane's index fits 32 bits
-static bool rows_ok(const mxq_kv_cache *c, int B, int M) { return M >= 1 && (int64_t)B * M <= ((int64_t)1 << 29) / c->kv_heads; }
+bool kv_rows_ok(int heads, int B, int M) { return M >= 1 && (int64_t)B * M <= ((int64_t)1 << 29) / heads; }
 
 }  // namespace mxq
 
@@ -324,7 +284,7 @@ int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int6
     if (rc == MXQ_OK) rc = mxq::kv_check_seqs(B, W, tables, lens);
     if (rc != MXQ_OK) return rc;
     const int64_t width = (int64_t)cache->kv_heads * cache->head_dim;
-    if (!mxq::rows_ok(cache, B, M) || k_stride < width || v_stride < width) return MXQ_ERR_SHAPE;
+    if (!mxq::kv_rows_ok(cache->kv_heads, B, M) || k_stride < width || v_stride < width) return MXQ_ERR_SHAPE;
     if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || k_stride % 8 || v_stride % 8 || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
     const mxq::KvRows in = {(const uint16_t *)K_bf16, (const uint16_t *)V_bf16, k_stride, v_stride};
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
@@ -338,7 +298,7 @@ int mxq_kv_append(const mxq_kv_cache *cache, int layer, const void *K_bf16, int6
         return mxq::launch_status();
     }
     const uint32_t total = mxq::lanes_of(cache, B, M, false);
-    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_append_kernel<128> : mxq::kv_append_kernel<64>,
+    return mxq::launch_pdl(cache->head_dim == 128 ? mxq::kv_append_kernel<128> : mxq::kv_append_kernel<64>,
                           dim3((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2), mxq::kKvThreads, 0, (cudaStream_t)stream, c, s, in, total);
 }
 
@@ -348,13 +308,13 @@ int mxq_kv_read(const mxq_kv_cache *cache, int layer, void *K_bf16, void *V_bf16
     int rc = mxq::kv_check_cache(cache, layer);
     if (rc == MXQ_OK) rc = mxq::kv_check_seqs(B, W, tables, lens);
     if (rc != MXQ_OK) return rc;
-    if (!mxq::rows_ok(cache, B, M)) return MXQ_ERR_SHAPE;
+    if (!mxq::kv_rows_ok(cache->kv_heads, B, M)) return MXQ_ERR_SHAPE;
     if (!mxq::aligned16(K_bf16) || !mxq::aligned16(V_bf16) || !mxq::aligned_to(rows, 4)) return MXQ_ERR_ALIGN;
     const bool prompt = mxq::prompt_rows(cache, B, M);
     const uint32_t total = mxq::lanes_of(cache, B, M, prompt);
     const dim3 grid((total + mxq::kKvThreads - 1) / mxq::kKvThreads, 2);
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
-    return mxq::kv_launch(cache->head_dim == 128 ? (prompt ? mxq::kv_read_kernel<128, mxq::kPromptRows> : mxq::kv_read_kernel<128, 1>)
+    return mxq::launch_pdl(cache->head_dim == 128 ? (prompt ? mxq::kv_read_kernel<128, mxq::kPromptRows> : mxq::kv_read_kernel<128, 1>)
                                                  : (prompt ? mxq::kv_read_kernel<64, mxq::kPromptRows> : mxq::kv_read_kernel<64, 1>),
                           grid, mxq::kKvThreads, 0,
                           (cudaStream_t)stream, mxq::kv_view(cache, layer), s, (uint16_t *)K_bf16, (uint16_t *)V_bf16, total);

@@ -430,7 +430,7 @@ int mxq_kv_resize(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int3
     rc = mxq::book_smem_ready((const void *)mxq::kv_resize_kernel);
     if (rc != MXQ_OK) return rc;
     const mxq::KvView c = mxq::kv_view(cache, 0);
-    return mxq::kv_launch(mxq::kv_resize_kernel, dim3(1), mxq::kBookThreads, (size_t)B * 16, (cudaStream_t)stream,
+    return mxq::launch_pdl(mxq::kv_resize_kernel, dim3(1), mxq::kBookThreads, (size_t)B * 16, (cudaStream_t)stream,
                           mxq::book_of(cache, B, tables, W, lens), new_lens, c, cache->layers, c.page_bytes * cache->num_pages);
 }
 
@@ -448,14 +448,14 @@ int mxq_kv_fork(const mxq_kv_cache *cache, int B, int32_t *tables, int W, int32_
     mxq::ForkJob *jobs = (mxq::ForkJob *)workspace;
     rc = mxq::book_smem_ready((const void *)mxq::kv_fork_kernel);
     if (rc != MXQ_OK) return rc;
-    rc = mxq::kv_launch(mxq::kv_fork_kernel, dim3(1), mxq::kBookThreads, (size_t)n * 24, (cudaStream_t)stream,
+    rc = mxq::launch_pdl(mxq::kv_fork_kernel, dim3(1), mxq::kBookThreads, (size_t)n * 24, (cudaStream_t)stream,
                         mxq::book_of(cache, B, tables, W, lens), n, src, dst, jobs);
     if (rc != MXQ_OK) return rc;
     const mxq::KvView c = mxq::kv_view(cache, 0);
     const int tiles = cache->page_tokens / mxq::kTileTokens;
     const int64_t row_bytes = c.page_bytes / tiles;
     const int pieces = (int)((row_bytes + mxq::kCopyPiece - 1) / mxq::kCopyPiece);
-    return mxq::kv_launch(mxq::kv_fork_copy_kernel, dim3((unsigned)n, (unsigned)std::min(cache->layers, mxq::kMaxGridY), (unsigned)(tiles * pieces)), mxq::kCopyThreads,
+    return mxq::launch_pdl(mxq::kv_fork_copy_kernel, dim3((unsigned)n, (unsigned)std::min(cache->layers, mxq::kMaxGridY), (unsigned)(tiles * pieces)), mxq::kCopyThreads,
                           0, (cudaStream_t)stream, (const mxq::ForkJob *)jobs, n, c, cache->layers, c.page_bytes * cache->num_pages, row_bytes, pieces);
 }
 
@@ -472,7 +472,7 @@ int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *table
     if (grid > 0x7FFFFFFF) return MXQ_ERR_SHAPE;
     const mxq::KvView c = mxq::kv_view(cache, 0);
     const mxq::KvSeqs s = mxq::kv_seqs(cache, B, M, tables, W, lens, rows);
-    return mxq::kv_launch(cache->head_dim == 128 ? mxq::kv_compact_kernel<128> : mxq::kv_compact_kernel<64>, dim3((unsigned)grid),
+    return mxq::launch_pdl(cache->head_dim == 128 ? mxq::kv_compact_kernel<128> : mxq::kv_compact_kernel<64>, dim3((unsigned)grid),
                           mxq::kCompactThreads, 0, (cudaStream_t)stream, c, s, cache->layers, c.page_bytes * cache->num_pages, keep, kept, lens_out);
 }
 

@@ -859,10 +859,12 @@ int mxq_debug_bounds_report(uint64_t *report) {
 #ifdef MXQ_DEBUG_BOUNDS
     report[0] = 1;
 #endif
-    int (*const take[9])(unsigned long long *) = {mxq::bounds_take_linear,     mxq::bounds_take_linear_umma,  mxq::bounds_take_linear_fp4,
+    int (*const take[13])(unsigned long long *) = {mxq::bounds_take_linear,     mxq::bounds_take_linear_umma,  mxq::bounds_take_linear_fp4,
                                                  mxq::bounds_take_linear_mma, mxq::bounds_take_linear_batch, mxq::bounds_take_linear_bf16,
-                                                 mxq::bounds_take_kv_cache,   mxq::bounds_take_kv_pages,     mxq::bounds_take_kv_attention};
-    for (int u = 0; u < 9; ++u) {
+                                                 mxq::bounds_take_kv_cache,   mxq::bounds_take_kv_pages,     mxq::bounds_take_kv_attention,
+                                                 mxq::bounds_take_norm,       mxq::bounds_take_kv_rope,      mxq::bounds_take_logits,
+                                                 mxq::bounds_take_lora};
+    for (int u = 0; u < 13; ++u) {
         unsigned long long r[4] = {0, 0, 0, 0};
         const int rc = take[u](r);
         if (rc != MXQ_OK) return rc;
