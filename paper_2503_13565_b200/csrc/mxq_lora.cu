@@ -28,12 +28,15 @@ struct LoraCall {
     const uint8_t *base;     // [M][N] or nullptr (zero)
     uint8_t *y;              // [M][N]
     float *t;                // [splits][M][r]
+    uint4 *frag;             // many rows: T as BF16 parts in the order of the product's first operand
     int64_t N, K;
     int32_t M, r, L;
     int32_t slots;           // CTAs of a window; slot s takes its adapters s, s + slots, ...
     int32_t splits, split_k; // shrink: CTAs along K, and how much of K each takes (a multiple of 32)
     int32_t base_f32, y_f32;
     int32_t parts;           // BF16 parts of T
+    int32_t stages;          // shrink: steps of a warp's ring
+    int32_t tiles;           // many rows: tiles of 16 rows per CTA of the expansion
 };
 
 struct Window {
@@ -82,77 +85,119 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 }
 
 // ---- T = A x --------------------------------------------------------------------------------------------------------------------
-// grid (windows, slots, splits).  MT tiles of 16 rows per window; a warp takes tile warp % MT and every (8 / MT)th step of 32 k.  RT: most tiles of 8
-// ranks.  A step's element order: lane t of a quad holds k = 8t .. 8t+7 of the 32, of rows and of ranks alike.
-template <int MT, int RT>
+// grid (windows, slots, splits).  A window has WM * MW tiles of 16 rows; a warp takes MW of them and every (8 / WM)th step of 32 k.  RT: most
+// tiles of 8 ranks.  A step's element order: lane t of a quad holds k = 8t .. 8t+7 of the 32, of rows and of ranks alike.
+// Every lane copies its own 16-byte pieces of the next steps into a ring in shared memory (cp.async) and reads back what it copied: the ring
+// holds `stages` steps per warp, no registers are spent on loads in flight, and no warp waits for another one.
+__device__ __forceinline__ void copy16(void *smem, const void *global, bool there) {      // zeros where there is nothing
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy16_shared(void *smem, const void *global) {           // through L1: other warps of the CTA read it too
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
+}
+constexpr int kMostStages = 4;
+__device__ __forceinline__ void wait_oldest(int stages) {        // of `stages` groups
+    if (stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+template <int MW, int WM, int RT>
 __global__ void __launch_bounds__(kShrinkThreads) lora_shrink_kernel(LoraCall c) {
-    constexpr int kSub = kShrinkWarps / MT;
-    extern __shared__ float part[];     // [kSub - 1][MT * 16][r]
+    constexpr int kSub = kShrinkWarps / WM, kRows = 16 * MW * WM;
+    extern __shared__ uint4 ring[];     // [warps][stages][ranks / 8 + 2 * MW][32 lanes]; then the warps' parts of T, [kSub - 1][kRows][r] floats
     __shared__ Window win;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int tile = warp % MT, sub = warp / MT, row0 = blockIdx.x * MT * 16;
-    const int64_t k0 = (int64_t)blockIdx.z * c.split_k, k1 = min(c.K, k0 + c.split_k);
-    const int ranks = c.r / 8;
-    load_window(win, c, row0, MT * 16);
+    const int sub = warp / WM, row0 = blockIdx.x * kRows, m0 = warp % WM * 16 * MW + g;     // this lane's rows: m0 + 8 * j, j < 2 * MW
+    const int64_t k0 = (int64_t)blockIdx.z * c.split_k + 32 * sub, k1 = min(c.K, (int64_t)(blockIdx.z + 1) * c.split_k);
+    const int ranks = c.r / 8, pieces = ranks + 2 * MW, steps = k0 < k1 ? (int)((k1 - k0 + 32 * kSub - 1) / (32 * kSub)) : 0;
+    uint4 *mine = ring + warp * c.stages * pieces * 32 + lane;
+    const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2, t_bytes = (size_t)c.splits * c.M * c.r * 4;
+    load_window(win, c, row0, kRows);
     __syncthreads();
     bool waited = false;
     for (int at = blockIdx.y; at < win.count; at += c.slots) {
         const int adapter = win.list[at];
-        const uint16_t *wa = c.a + (int64_t)adapter * c.r * c.K;
-        const int m0 = tile * 16 + g, m1 = m0 + 8;
-        const bool own0 = win.owner[m0] == adapter, own1 = win.owner[m1] == adapter;
-        const bool any = __any_sync(0xffffffffu, own0 || own1);
-        const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2;
-        float acc[RT][4];
+        const uint16_t *wa = c.a + ((int64_t)adapter * c.r + g) * c.K + k0 + 8 * t, *xa = c.x + (int64_t)(row0 + m0) * c.K + k0 + 8 * t;
+        bool own[2 * MW], any = false;
 #pragma unroll
-        for (int n = 0; n < RT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
-        if (any) {
-            for (int64_t k = k0 + 32 * sub; k < k1; k += 32 * kSub) {
-                uint4 w[RT];
+        for (int j = 0; j < 2 * MW; ++j) own[j] = win.owner[m0 + 8 * j] == adapter, any |= own[j];
+        const int todo = __any_sync(0xffffffffu, any) ? steps : 0;
+        auto copy_a = [&](int step, int slot) {
+            uint4 *to = mine + slot * pieces * 32;
+            for (int n = 0; n < ranks; ++n) copy16_shared(to + n * 32, MXQ_AT(wa + (int64_t)8 * n * c.K + (int64_t)step * 32 * kSub, 16, c.a, a_bytes));
+        };
+        auto copy_x = [&](int step, int slot) {
+            uint4 *to = mine + (slot * pieces + ranks) * 32;
 #pragma unroll
-                for (int n = 0; n < RT; ++n)
-                    if (n < ranks) w[n] = __ldg(reinterpret_cast<const uint4 *>(MXQ_AT(wa + (int64_t)(8 * n + g) * c.K + k + 8 * t, 16, c.a, a_bytes)));
-                if (!waited) {           // (the adapters' first step is on its way before the previous kernel has ended)
-                    pdl_wait();
-                    waited = true;
-                }
-                uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
-                if (own0) x0 = ld_dep_u4(MXQ_AT(c.x + (int64_t)(row0 + m0) * c.K + k + 8 * t, 16, c.x, x_bytes));
-                if (own1) x1 = ld_dep_u4(MXQ_AT(c.x + (int64_t)(row0 + m1) * c.K + k + 8 * t, 16, c.x, x_bytes));
-#pragma unroll
-                for (int n = 0; n < RT; ++n) {
-                    if (n >= ranks) break;
-                    mma_bf16(acc[n], x0.x, x1.x, x0.y, x1.y, w[n].x, w[n].y);
-                    mma_bf16(acc[n], x0.z, x1.z, x0.w, x1.w, w[n].z, w[n].w);
-                }
-            }
-        }
+            for (int j = 0; j < 2 * MW; ++j)     // (a row that is not there is not read: its address is the array's own)
+                copy16(to + j * 32, own[j] ? MXQ_AT(xa + (int64_t)8 * j * c.K + (int64_t)step * 32 * kSub, 16, c.x, x_bytes) : c.x, own[j]);
+        };
+        // (the adapters' first steps are on their way before the previous kernel has ended)
+        for (int u = 0; u < c.stages && u < todo; ++u) copy_a(u, u);
         if (!waited) pdl_wait(), waited = true;
-        // the warps' parts of K, added in order
-        if (sub > 0 && any) {
+        for (int u = 0; u < c.stages; ++u) {
+            if (u < todo) copy_x(u, u);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        float acc[MW][RT][4];
+#pragma unroll
+        for (int w = 0; w < MW; ++w)
+#pragma unroll
+            for (int n = 0; n < RT; ++n) acc[w][n][0] = acc[w][n][1] = acc[w][n][2] = acc[w][n][3] = 0.f;
+        for (int step = 0, slot = 0; step < todo; ++step) {
+            wait_oldest(c.stages);
+            const uint4 *from = mine + slot * pieces * 32;
+            uint4 x[2 * MW];
+#pragma unroll
+            for (int j = 0; j < 2 * MW; ++j) x[j] = from[(ranks + j) * 32];
 #pragma unroll
             for (int n = 0; n < RT; ++n) {
                 if (n >= ranks) break;
-                float *p = part + ((int64_t)(sub - 1) * MT * 16 + m0) * c.r + 8 * n + 2 * t;
-                p[0] = acc[n][0], p[1] = acc[n][1];
-                p[8 * c.r] = acc[n][2], p[8 * c.r + 1] = acc[n][3];
+                const uint4 v = from[n * 32];
+#pragma unroll
+                for (int w = 0; w < MW; ++w) {
+                    mma_bf16(acc[w][n], x[2 * w].x, x[2 * w + 1].x, x[2 * w].y, x[2 * w + 1].y, v.x, v.y);
+                    mma_bf16(acc[w][n], x[2 * w].z, x[2 * w + 1].z, x[2 * w].w, x[2 * w + 1].w, v.z, v.w);
+                }
+            }
+            if (step + c.stages < todo) copy_a(step + c.stages, slot), copy_x(step + c.stages, slot);     // (this lane has read the slot)
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++slot == c.stages) slot = 0;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        // the warps' parts of K, added in order; the ring is free for them now
+        __syncthreads();
+        float *part = reinterpret_cast<float *>(ring);
+#pragma unroll
+        for (int w = 0; w < MW; ++w) {
+            if (sub == 0) break;
+#pragma unroll
+            for (int n = 0; n < RT; ++n) {
+                if (n >= ranks) break;
+                float *p = part + ((sub - 1) * kRows + m0 + 16 * w) * c.r + 8 * n + 2 * t;
+                *reinterpret_cast<float2 *>(p) = make_float2(acc[w][n][0], acc[w][n][1]);
+                *reinterpret_cast<float2 *>(p + 8 * c.r) = make_float2(acc[w][n][2], acc[w][n][3]);
             }
         }
         __syncthreads();
-        if (sub == 0 && any) {
-            const size_t t_bytes = (size_t)c.splits * c.M * c.r * 4;
+        if (sub == 0 && __any_sync(0xffffffffu, any)) {
 #pragma unroll
-            for (int n = 0; n < RT; ++n) {
-                if (n >= ranks) break;
-                for (int u = 0; u < kSub - 1; ++u) {
-                    const float *p = part + ((int64_t)u * MT * 16 + m0) * c.r + 8 * n + 2 * t;
-                    acc[n][0] += p[0], acc[n][1] += p[1], acc[n][2] += p[8 * c.r], acc[n][3] += p[8 * c.r + 1];
+            for (int w = 0; w < MW; ++w)
+#pragma unroll
+                for (int n = 0; n < RT; ++n) {
+                    if (n >= ranks) break;
+                    for (int u = 0; u < kSub - 1; ++u) {
+                        const float *p = part + (u * kRows + m0 + 16 * w) * c.r + 8 * n + 2 * t;
+                        const float2 p0 = *reinterpret_cast<const float2 *>(p), p1 = *reinterpret_cast<const float2 *>(p + 8 * c.r);
+                        acc[w][n][0] += p0.x, acc[w][n][1] += p0.y, acc[w][n][2] += p1.x, acc[w][n][3] += p1.y;
+                    }
+                    float *out = c.t + ((int64_t)blockIdx.z * c.M + row0 + m0 + 16 * w) * c.r + 8 * n + 2 * t;
+                    if (own[2 * w]) *reinterpret_cast<float2 *>(MXQ_AT(out, 8, c.t, t_bytes)) = make_float2(acc[w][n][0], acc[w][n][1]);
+                    if (own[2 * w + 1]) *reinterpret_cast<float2 *>(MXQ_AT(out + 8 * (int64_t)c.r, 8, c.t, t_bytes)) = make_float2(acc[w][n][2], acc[w][n][3]);
                 }
-                float *out = c.t + ((int64_t)blockIdx.z * c.M + row0 + m0) * c.r + 8 * n + 2 * t;
-                if (own0) *reinterpret_cast<float2 *>(MXQ_AT(out, 8, c.t, t_bytes)) = make_float2(acc[n][0], acc[n][1]);
-                if (own1) *reinterpret_cast<float2 *>(MXQ_AT(out + 8 * (int64_t)c.r, 8, c.t, t_bytes)) = make_float2(acc[n][2], acc[n][3]);
-            }
         }
         __syncthreads();
     }
@@ -206,114 +251,229 @@ __device__ __forceinline__ uint2 load_b(const LoraCall &c, int adapter, int64_t 
     return __ldg(reinterpret_cast<const uint2 *>(MXQ_AT(c.b + ((int64_t)adapter * c.N + col) * c.r + 16 * s + 4 * t, 8, c.b, (size_t)c.L * c.N * c.r * 2)));
 }
 
-template <int MT, int KT, int WARPS>
+__device__ __forceinline__ void put_parts(uint4 *tile_step, int row, int quarter, float (&v)[4], int parts) {
+    // ranks 4 q + 2 e + {0, 1} of the step, row `row` of the tile: register 2 e + (row >> 3) of lane 4 (row & 7) + q
+    uint32_t *dst = reinterpret_cast<uint32_t *>(tile_step + 4 * (row & 7) + quarter) + (row >> 3);
+    for (int u = 0; u < parts; ++u) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const __nv_bfloat162 part = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+            dst[u * 128 + 2 * e] = *reinterpret_cast<const uint32_t *>(&part);
+            const float2 f = __bfloat1622float2(part);       // (an infinite part leaves nothing)
+            v[2 * e] = isfinite(f.x) ? v[2 * e] - f.x : 0.f, v[2 * e + 1] = isfinite(f.y) ? v[2 * e + 1] - f.y : 0.f;
+        }
+    }
+}
+// the four ranks' sum over the splits, times the adapter's scale
+__device__ __forceinline__ void sum_splits(float (&v)[4], const LoraCall &c, int m, int rank, int adapter) {
+    const size_t t_bytes = (size_t)c.splits * c.M * c.r * 4;
+    const float *p = c.t + (int64_t)m * c.r + rank;
+    for (int u0 = 0; u0 < c.splits; u0 += 8) {
+        uint4 q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (u0 + u < c.splits) q[u] = ld_dep_u4(MXQ_AT(p + (int64_t)(u0 + u) * c.M * c.r, 16, c.t, t_bytes));
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (u0 + u < c.splits)
+                v[0] += __uint_as_float(q[u].x), v[1] += __uint_as_float(q[u].y), v[2] += __uint_as_float(q[u].z), v[3] += __uint_as_float(q[u].w);
+    }
+    const float s = c.scale ? __ldg(MXQ_AT(c.scale + adapter, 4, c.scale, (size_t)c.L * 4)) : 1.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= s;
+}
+// A lane's eight columns of a row of base as they come from memory (whole vectors only).
+struct Columns {
+    uint4 lo, hi;
+};
+__device__ __forceinline__ Columns load_ahead(const uint8_t *base, bool f32, int64_t at, int64_t n) {
+    const uint8_t *p = MXQ_AT(base + at * (f32 ? 4 : 2), f32 ? 32 : 16, base, n * (f32 ? 4 : 2));
+    Columns c;
+    c.lo = ld_dep_u4(p);
+    c.hi = f32 ? ld_dep_u4(p + 16) : make_uint4(0, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ void unpack_columns(float (&f)[8], const Columns &c, bool f32) {
+    if (!f32) {
+        unpack_bf16(f, c.lo);
+        return;
+    }
+    const uint32_t w[8] = {c.lo.x, c.lo.y, c.lo.z, c.lo.w, c.hi.x, c.hi.y, c.hi.z, c.hi.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
+}
+
+// few rows: a CTA has one adapter of the window (there are as many slots as a window can have adapters)
+template <int KT, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
-    extern __shared__ uint4 frag[];      // [MT][steps][parts][32 lanes]: T as the product's first operand
+    extern __shared__ uint4 frag[];      // [steps][parts][32 lanes]: T as the product's first operand
     __shared__ Window win;
-    constexpr bool kAhead = MT == 1 && KT <= 4;   // B waits in registers for T
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.z * MT * 16;
-    const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32;
-    const int steps = (c.r + 15) / 16;
-    load_window(win, c, row0, MT * 16);
+    const int row0 = blockIdx.z * 16, steps = (c.r + 15) / 16;
+    const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32, col = col0 + 8 * t, n = (int64_t)c.M * c.N;
+    load_window(win, c, row0, 16);
     __syncthreads();
-    uint2 w[kAhead ? KT : 1][4];
-    if constexpr (kAhead) {
-        if ((int)blockIdx.y < win.count) {
-            const int adapter = win.list[blockIdx.y];
+    const int adapter = (int)blockIdx.y < win.count ? win.list[blockIdx.y] : -2;
+    uint2 w[KT][4];                      // this warp's columns of B wait here for T
+    if (adapter >= 0) {
 #pragma unroll
-            for (int s = 0; s < KT; ++s)
+        for (int s = 0; s < KT; ++s)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (s < steps) w[s][i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
-        }
+            for (int i = 0; i < 4; ++i)
+                if (s < steps) w[s][i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
+    }
+    // the rows that this CTA stores: its adapter's; the first slot also copies those without one, unless they are there already
+    const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
+    bool own[2], mine[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        own[h] = win.owner[8 * h + g] == adapter;
+        mine[h] = there > 0 && (own[h] || (blockIdx.y == 0 && c.base != c.y && win.owner[8 * h + g] < 0 && row0 + 8 * h + g < c.M));
     }
     pdl_wait();
-    if ((int)blockIdx.y >= win.count && blockIdx.y != 0) return;
-
-    // T of the window's rows: sum over the splits, times the adapter's scale, in two BF16 parts, in the order of the fragments
-    const size_t t_bytes = (size_t)c.splits * c.M * c.r * 4;
-    for (int n = threadIdx.x; n < MT * 16 * steps * 8; n += 32 * WARPS) {
-        const int pair = n % (steps * 8), m = n / (steps * 8);           // ranks 2 * pair, 2 * pair + 1 of row m
-        float v[2] = {0.f, 0.f};
-        const int adapter = win.owner[m];
-        if (adapter >= 0 && 2 * pair < c.r) {
-            const float *p = c.t + (int64_t)(row0 + m) * c.r + 2 * pair;
-            for (int u = 0; u < c.splits; ++u) {
-                const float *q = MXQ_AT(p + (int64_t)u * c.M * c.r, 8, c.t, t_bytes);
-                v[0] += ld_dep_f32(q), v[1] += ld_dep_f32(q + 1);
-            }
-            const float s = c.scale ? __ldg(MXQ_AT(c.scale + adapter, 4, c.scale, (size_t)c.L * 4)) : 1.f;
-            v[0] *= s, v[1] *= s;
+    const bool vec = c.N % 8 == 0;
+    Columns ahead[2];                    // base, on its way while T is made ready
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (c.base && vec && mine[h]) ahead[h] = load_ahead(c.base, c.base_f32, (int64_t)(row0 + 8 * h + g) * c.N + col, n);
+    if (adapter >= 0) {
+        for (int i = threadIdx.x; i < 16 * steps * 4; i += 32 * WARPS) {
+            const int quarter = i % (steps * 4), m = i / (steps * 4);       // ranks 4 * quarter .. + 3 of row m
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (win.owner[m] == adapter && 4 * quarter < c.r) sum_splits(v, c, row0 + m, 4 * quarter, adapter);
+            put_parts(frag + quarter / 4 * c.parts * 32, m, quarter % 4, v, c.parts);
         }
-        // rank 16 s + 4 t + 2 e + {0, 1} of row 16 mt + g + 8 h: register 2 e + h of lane 4 g + t
-        const int s = pair / 8, tt = pair % 8 / 2, e = pair & 1, mt = m / 16, row = m % 16;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(frag + (mt * steps + s) * c.parts * 32 + 4 * (row & 7) + tt) + 2 * e + (row >> 3);
-        for (int u = 0; u < c.parts; ++u) {
-            const __nv_bfloat162 part = __floats2bfloat162_rn(v[0], v[1]);
-            dst[u * 128] = *reinterpret_cast<const uint32_t *>(&part);
-            const float2 f = __bfloat1622float2(part);
-            v[0] = isfinite(f.x) ? v[0] - f.x : 0.f, v[1] = isfinite(f.y) ? v[1] - f.y : 0.f;    // (an infinite part leaves nothing)
+        __syncthreads();
+    }
+    float acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+    if (adapter >= 0) {
+#pragma unroll
+        for (int s = 0; s < KT; ++s) {
+            if (s >= steps) break;
+            for (int p = 0; p < c.parts; ++p) {
+                const uint4 q = frag[(s * c.parts + p) * 32 + lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_bf16(acc[i], q.x, q.y, q.z, q.w, w[s][i].x, w[s][i].y);
+            }
         }
     }
+    // (rows of other adapters went through the product as zeros; nothing of it is stored)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (!mine[h]) continue;
+        const int64_t at = (int64_t)(row0 + 8 * h + g) * c.N + col;
+        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (c.base && vec) unpack_columns(f, ahead[h], c.base_f32);
+        else if (c.base) load_columns(f, c.base, c.base_f32, at, there, vec, n);
+        if (own[h]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[2 * i] += acc[i][2 * h], f[2 * i + 1] += acc[i][2 * h + 1];
+        }
+        store_columns(f, c.y, c.y_f32, at, there, vec, n);
+    }
+}
+
+// ---- many rows ------------------------------------------------------------------------------------------------------------------------
+// T's partial sums -> its fragments, [tiles of 16 rows][steps][parts][32 lanes]: once, not for every block of columns.  A thread per row and four ranks.
+__global__ void __launch_bounds__(256) lora_fragments_kernel(LoraCall c) {
+    pdl_trigger();
+    const int quarters = (c.r + 15) / 16 * 4, tiles = (c.M + 15) / 16;
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int m = (int)(n / quarters), quarter = (int)(n - (int64_t)m * quarters);
+    pdl_wait();
+    if (m >= tiles * 16) return;
+    const int adapter = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (adapter >= 0 && adapter < c.L && 4 * quarter < c.r) sum_splits(v, c, m, 4 * quarter, adapter);
+    put_parts(MXQ_AT(c.frag + ((int64_t)(m / 16) * (quarters / 4) + quarter / 4) * c.parts * 32, c.parts * 512, c.frag, (size_t)tiles * (quarters / 4) * c.parts * 512),
+              m % 16, quarter % 4, v, c.parts);
+}
+
+// grid (blocks of 256 columns, blocks of c.tiles tiles of rows); a warp takes 32 columns, whose B stays in registers while the adapter does, and
+// goes through the tiles; base and ids of the next tile are on their way meanwhile.
+template <int KT>
+__global__ void __launch_bounds__(256) lora_expand_many_kernel(LoraCall c) {
+    extern __shared__ uint4 frag[];      // the rows' fragments of T
+    pdl_trigger();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t col0 = ((int64_t)blockIdx.x * 8 + warp) * 32, col = col0 + 8 * t, n = (int64_t)c.M * c.N;
+    const int steps = (c.r + 15) / 16, all = (c.M + 15) / 16, tile0 = blockIdx.y * c.tiles, tiles = min(c.tiles, all - tile0);
+    const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
+    const bool vec = c.N % 8 == 0, early = c.base && !c.base_f32 && vec && there > 0, copies = c.base != c.y;
+    auto owner = [&](int tile, int h) {
+        const int m = (tile0 + tile) * 16 + 8 * h + g;
+        const int a = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
+        return a >= 0 && a < c.L ? a : -1;
+    };
+    auto base_of = [&](int tile, int h) {        // BF16 in whole vectors; anything else is loaded where it is needed
+        const int m = (tile0 + tile) * 16 + 8 * h + g;
+        return early && m < c.M ? ld_dep_u4(MXQ_AT(c.base + ((int64_t)m * c.N + col) * 2, 16, c.base, n * 2)) : make_uint4(0, 0, 0, 0);
+    };
+    uint2 w[KT][4];
+    auto load = [&](int adapter) {
+#pragma unroll
+        for (int s = 0; s < KT; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s < steps) w[s][i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
+    };
+    int own[2] = {owner(0, 0), owner(0, 1)};
+    int current = (int)__reduce_max_sync(0xffffffffu, max(own[0], own[1]));
+    if (current >= 0) load(current);
+    pdl_wait();
+    const int pieces = steps * c.parts * 32;
+    const size_t bytes = (size_t)all * pieces * 16;
+    for (int i = threadIdx.x; i < tiles * pieces; i += 256)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(frag + i)), "l"(MXQ_AT(c.frag + (int64_t)tile0 * pieces + i, 16, c.frag, bytes)) : "memory");
+    uint4 base[2] = {base_of(0, 0), base_of(0, 1)};
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     if (col0 >= c.N) return;
-
-    const int64_t col = col0 + 8 * t, n = (int64_t)c.M * c.N;
-    const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
-    const bool vec = c.N % 8 == 0;
-    // rows without an adapter are copied (by the first slot, unless they are there already)
-    if (blockIdx.y == 0 && c.base != c.y) {
-        for (int m = g; m < MT * 16; m += 8) {
-            if (win.owner[m] >= 0 || row0 + m >= c.M || there == 0) continue;
-            const int64_t at = (int64_t)(row0 + m) * c.N + col;
-            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (c.base) load_columns(f, c.base, c.base_f32, at, there, vec, n);
-            store_columns(f, c.y, c.y_f32, at, there, vec, n);
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int m0 = (tile0 + tile) * 16 + g;
+        const int now[2] = {own[0], own[1]};
+        float f[2][8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            unpack_bf16(f[h], base[h]);
+            if (c.base && !early && there > 0 && m0 + 8 * h < c.M) load_columns(f[h], c.base, c.base_f32, (int64_t)(m0 + 8 * h) * c.N + col, there, vec, n);
         }
-    }
-    for (int at = blockIdx.y; at < win.count; at += c.slots) {
-        const int adapter = win.list[at];
-        float acc[MT][4][4];
+        if (tile + 1 < tiles) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+            for (int h = 0; h < 2; ++h) own[h] = owner(tile + 1, h), base[h] = base_of(tile + 1, h);
+        }
+        int left[2] = {now[0], now[1]};
+        while (true) {                       // the tile's adapters, one after the other
+            const int adapter = (int)__reduce_max_sync(0xffffffffu, max(left[0], left[1]));
+            if (adapter < 0) break;
+            if (adapter != current) load(adapter), current = adapter;
+            float acc[4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[mt][i][0] = acc[mt][i][1] = acc[mt][i][2] = acc[mt][i][3] = 0.f;
-#pragma unroll(kAhead ? KT : 1)
-        for (int s = 0; s < (kAhead ? KT : steps); ++s) {
-            if (s >= steps) break;
-            uint2 b[4];
+            for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (kAhead && at == (int)blockIdx.y) b[i] = w[kAhead ? s : 0][i];
-                else b[i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
-            }
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const bool own0 = win.owner[16 * mt + g] == adapter, own1 = win.owner[16 * mt + g + 8] == adapter;
-                if (!__any_sync(0xffffffffu, own0 || own1)) continue;
+            for (int s = 0; s < KT; ++s) {
+                if (s >= steps) break;
                 for (int p = 0; p < c.parts; ++p) {
-                    const uint4 f = frag[((mt * steps + s) * c.parts + p) * 32 + lane];
+                    const uint4 q = frag[((tile * steps + s) * c.parts + p) * 32 + lane];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mma_bf16(acc[mt][i], f.x, f.y, f.z, f.w, b[i].x, b[i].y);
+                    for (int i = 0; i < 4; ++i) mma_bf16(acc[i], q.x, q.y, q.z, q.w, w[s][i].x, w[s][i].y);
                 }
             }
-        }
-        // (rows of other adapters went through the product too; what they got is dropped here)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+            // (rows of other adapters went through the product too; what they got is dropped here)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int m = 16 * mt + 8 * h + g;
-                if (win.owner[m] != adapter || there == 0) continue;
-                const int64_t to = (int64_t)(row0 + m) * c.N + col;
-                float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (c.base) load_columns(f, c.base, c.base_f32, to, there, vec, n);
+                if (left[h] != adapter) continue;
+                left[h] = -1;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f[2 * i] += acc[mt][i][2 * h], f[2 * i + 1] += acc[mt][i][2 * h + 1];
-                store_columns(f, c.y, c.y_f32, to, there, vec, n);
+                for (int i = 0; i < 4; ++i) f[h][2 * i] += acc[i][2 * h], f[h][2 * i + 1] += acc[i][2 * h + 1];
             }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (there > 0 && m0 + 8 * h < c.M && (now[h] >= 0 || copies)) store_columns(f[h], c.y, c.y_f32, (int64_t)(m0 + 8 * h) * c.N + col, there, vec, n);
     }
 }
 
@@ -321,22 +481,25 @@ MXQ_BOUNDS_TU(bounds_take_lora)
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 
-// windows of 64 rows for many rows (a window reads its adapters once), of 16 otherwise
-static int window_tiles(int64_t M) { return M >= 512 ? 4 : 1; }
+// From 512 rows on windows of 32 rows (a window reads its adapters once) and T's fragments made once, by a kernel of their own; below that
+// windows of 16 rows, a CTA per adapter, and every CTA of the expansion makes its own.
+static bool many_rows(int64_t M) { return M >= 512; }
 
 static void lora_plan(LoraCall &c) {
-    const int mt = window_tiles(c.M);
-    const int64_t windows = (c.M + 16 * mt - 1) / (16 * mt);
-    c.slots = mt == 1 ? min(16, min(c.M, c.L)) : 1;
-    // splits of K until every SM has two CTAs (of 8 warps), but at least one step of 32 per warp
-    const int64_t step = 32 * (kShrinkWarps / mt), most = (c.K + step - 1) / step;
-    int64_t want = (2 * (int64_t)sm_count() + windows * c.slots - 1) / (windows * c.slots);
+    const bool many = many_rows(c.M);
+    const int64_t windows = many ? (c.M + 31) / 32 : (c.M + 15) / 16;
+    c.slots = many ? 1 : min(16, min(c.M, c.L));
+    // splits of K as long as the SMs hold the CTAs at once, but at least one step of 32 per warp
+    const int64_t step = 32 * kShrinkWarps, most = (c.K + step - 1) / step;
+    int64_t want = max((int64_t)1, (many ? 1 : 2) * (int64_t)sm_count() / (windows * c.slots));
     if (want > most) want = most;
     if (want > 32) want = 32;
     int64_t len = ((c.K + want - 1) / want + step - 1) / step * step;
     c.split_k = (int32_t)len;
     c.splits = (int32_t)((c.K + len - 1) / len);
 }
+static size_t align256(size_t v) { return (v + 255u) & ~(size_t)255u; }
+static size_t sums_bytes(const LoraCall &c) { return align256((size_t)c.splits * (size_t)c.M * (size_t)c.r * 4); }
 
 static bool lora_shape_ok(int64_t M, int64_t N, int64_t K, int r, int L) {
     return M >= 1 && M <= MXQ_LORA_MAX_M && shape_ok(N, K) && N <= ((int64_t)1 << 31) && K <= ((int64_t)1 << 30) && r >= 8 && r <= 128 && r % 8 == 0 &&
@@ -369,31 +532,46 @@ static bool allow_smem(void (*kernel)(LoraCall), size_t smem) {
     return false;
 }
 
-template <int MT>
+template <int MW, int WM>
 static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
-    const dim3 grid((unsigned)((c.M + 16 * MT - 1) / (16 * MT)), (unsigned)c.slots, (unsigned)c.splits);
-    const size_t smem = (size_t)(kShrinkWarps / MT - 1) * MT * 16 * c.r * 4;
-    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_shrink_kernel<MT, 2> : c.r <= 32 ? lora_shrink_kernel<MT, 4> : c.r <= 64 ? lora_shrink_kernel<MT, 8> : lora_shrink_kernel<MT, 16>;
+    constexpr int kRows = 16 * MW * WM, kSub = kShrinkWarps / WM;
+    const dim3 grid((unsigned)((c.M + kRows - 1) / kRows), (unsigned)c.slots, (unsigned)c.splits);
+    const size_t stage = (size_t)kShrinkWarps * (c.r / 8 + 2 * MW) * 512, parts = (size_t)(kSub - 1) * kRows * c.r * 4;
+    const int steps = (c.split_k + 32 * kSub - 1) / (32 * kSub);
+    LoraCall call = c;
+    call.stages = max(1, min(min(kMostStages, steps), (int)(200 * 1024 / stage)));
+    const size_t smem = max(stage * call.stages, parts);
+    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_shrink_kernel<MW, WM, 2> : c.r <= 32 ? lora_shrink_kernel<MW, WM, 4> : c.r <= 64 ? lora_shrink_kernel<MW, WM, 8> : lora_shrink_kernel<MW, WM, 16>;
     if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
-    return launch_pdl(kernel, grid, kShrinkThreads, smem, stream, c);
+    return launch_pdl(kernel, grid, kShrinkThreads, smem, stream, call);
 }
 
-template <int MT, int WARPS>
 static int expand_launch(const LoraCall &c, cudaStream_t stream) {
-    const dim3 grid((unsigned)((c.N + 32 * WARPS - 1) / (32 * WARPS)), (unsigned)c.slots, (unsigned)((c.M + 16 * MT - 1) / (16 * MT)));
-    const size_t smem = (size_t)MT * ((c.r + 15) / 16) * c.parts * 32 * 16;
-    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_expand_kernel<MT, 1, WARPS> : c.r <= 32 ? lora_expand_kernel<MT, 2, WARPS> : c.r <= 64 ? lora_expand_kernel<MT, 4, WARPS> : lora_expand_kernel<MT, 8, WARPS>;
-    if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
-    return launch_pdl(kernel, grid, 32 * WARPS, smem, stream, c);
+    constexpr int kWarps = 4;
+    const dim3 grid((unsigned)((c.N + 32 * kWarps - 1) / (32 * kWarps)), (unsigned)c.slots, (unsigned)((c.M + 15) / 16));
+    const size_t smem = (size_t)((c.r + 15) / 16) * c.parts * 32 * 16;
+    return launch_pdl(c.r <= 16 ? lora_expand_kernel<1, kWarps> : c.r <= 32 ? lora_expand_kernel<2, kWarps> : c.r <= 64 ? lora_expand_kernel<4, kWarps> : lora_expand_kernel<8, kWarps>,
+                      grid, 32 * kWarps, smem, stream, c);
 }
 
-static int lora_shrink(const LoraCall &c, cudaStream_t stream) { return window_tiles(c.M) == 4 ? shrink_launch<4>(c, stream) : shrink_launch<1>(c, stream); }
+static int expand_many_launch(LoraCall c, cudaStream_t stream) {
+    const int steps = (c.r + 15) / 16, tiles = (c.M + 15) / 16;
+    int rc = launch_pdl(lora_fragments_kernel, dim3((unsigned)(((int64_t)tiles * 16 * steps * 4 + 255) / 256)), 256, 0, stream, c);
+    if (rc != MXQ_OK) return rc;
+    c.tiles = 8;
+    const dim3 grid((unsigned)((c.N + 255) / 256), (unsigned)((tiles + c.tiles - 1) / c.tiles));
+    const size_t smem = (size_t)c.tiles * steps * c.parts * 512;
+    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_expand_many_kernel<1> : c.r <= 32 ? lora_expand_many_kernel<2> : c.r <= 64 ? lora_expand_many_kernel<4> : lora_expand_many_kernel<8>;
+    if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
+    return launch_pdl(kernel, grid, 256, smem, stream, c);
+}
+
+static int lora_shrink(const LoraCall &c, cudaStream_t stream) { return many_rows(c.M) ? shrink_launch<2, 1>(c, stream) : shrink_launch<1, 1>(c, stream); }
 static int lora_expand(LoraCall &c, const void *base, int base_dtype, void *Y, int y_dtype, cudaStream_t stream) {
     c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
-    return window_tiles(c.M) == 4 ? expand_launch<4, 8>(c, stream) : expand_launch<1, 4>(c, stream);
+    c.frag = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c));
+    return many_rows(c.M) ? expand_many_launch(c, stream) : expand_launch(c, stream);
 }
-
-static size_t align256(size_t v) { return (v + 255u) & ~(size_t)255u; }
 
 }  // namespace mxq
 
@@ -405,7 +583,8 @@ size_t mxq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int rank, int a
     mxq::LoraCall c = {};
     c.M = (int32_t)M, c.N = N, c.K = K, c.r = rank, c.L = adapters;
     mxq::lora_plan(c);
-    return (size_t)c.splits * (size_t)M * (size_t)rank * 4;
+    // [partial sums][fragments: three BF16 parts of 16-row tiles]
+    return mxq::sums_bytes(c) + (mxq::many_rows(M) ? (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512 : 0);
 }
 
 int mxq_lora(const void *X_bf16, int64_t M, const mxq_lora_adapters *adapters, const int32_t *ids, int64_t N, int64_t K, const void *base,
