@@ -17,7 +17,6 @@
 
 namespace mxq {
 
-constexpr int kShrinkThreads = 256, kShrinkWarps = 8;
 constexpr int kWindowMost = 64;
 
 struct LoraCall {
@@ -85,16 +84,14 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 }
 
 // ---- T = A x --------------------------------------------------------------------------------------------------------------------
-// grid (windows, slots, splits).  A window has WM * MW tiles of 16 rows; a warp takes MW of them and every (8 / WM)th step of 32 k.  RT: most
-// tiles of 8 ranks.  A step's element order: lane t of a quad holds k = 8t .. 8t+7 of the 32, of rows and of ranks alike.
+// grid (windows, slots, splits).  A window has MW tiles of 16 rows; a warp takes all of them and every WARPSth step of 32 k.  RT: most tiles of 8
+// ranks.  A step's element order: lane t of a quad holds k = 8t .. 8t+7 of the 32, of rows and of ranks alike.
 // Every lane copies its own 16-byte pieces of the next steps into a ring in shared memory (cp.async) and reads back what it copied: the ring
 // holds `stages` steps per warp, no registers are spent on loads in flight, and no warp waits for another one.
-__device__ __forceinline__ void copy16(void *smem, const void *global, bool there) {      // zeros where there is nothing
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void copy16(uint32_t smem, const void *global, bool there) {      // zeros where there is nothing
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(global), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void copy16_shared(void *smem, const void *global) {           // through L1: other warps of the CTA read it too
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
-}
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 constexpr int kMostStages = 4;
 __device__ __forceinline__ void wait_oldest(int stages) {        // of `stages` groups
     if (stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
@@ -103,43 +100,51 @@ __device__ __forceinline__ void wait_oldest(int stages) {        // of `stages` 
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-template <int MW, int WM, int RT>
-__global__ void __launch_bounds__(kShrinkThreads) lora_shrink_kernel(LoraCall c) {
-    constexpr int kSub = kShrinkWarps / WM, kRows = 16 * MW * WM;
-    extern __shared__ uint4 ring[];     // [warps][stages][ranks / 8 + 2 * MW][32 lanes]; then the warps' parts of T, [kSub - 1][kRows][r] floats
+template <int MW, int WARPS, int RT>
+__global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
+    constexpr int kRows = 16 * MW;
+    extern __shared__ uint4 ring[];     // [warps][stages][ranks / 8 + 2 * MW][32 lanes]; then the warps' parts of T, [warps][kRows][r] floats
     __shared__ Window win;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int sub = warp / WM, row0 = blockIdx.x * kRows, m0 = warp % WM * 16 * MW + g;     // this lane's rows: m0 + 8 * j, j < 2 * MW
-    const int64_t k0 = (int64_t)blockIdx.z * c.split_k + 32 * sub, k1 = min(c.K, (int64_t)(blockIdx.z + 1) * c.split_k);
-    const int ranks = c.r / 8, pieces = ranks + 2 * MW, steps = k0 < k1 ? (int)((k1 - k0 + 32 * kSub - 1) / (32 * kSub)) : 0;
+    const int row0 = blockIdx.x * kRows;          // this lane's rows: row0 + g + 8 * j, j < 2 * MW
+    const int64_t k0 = (int64_t)blockIdx.z * c.split_k + 32 * warp, k1 = min(c.K, (int64_t)(blockIdx.z + 1) * c.split_k);
+    const int ranks = c.r / 8, pieces = ranks + 2 * MW, steps = k0 < k1 ? (int)((k1 - k0 + 32 * WARPS - 1) / (32 * WARPS)) : 0;
+    const int64_t stride = 16 * c.K;              // bytes from a row to the eighth after it
     uint4 *mine = ring + warp * c.stages * pieces * 32 + lane;
+    const uint32_t mine_address = shared_address(mine);
     const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2, t_bytes = (size_t)c.splits * c.M * c.r * 4;
     load_window(win, c, row0, kRows);
     __syncthreads();
     bool waited = false;
     for (int at = blockIdx.y; at < win.count; at += c.slots) {
         const int adapter = win.list[at];
-        const uint16_t *wa = c.a + ((int64_t)adapter * c.r + g) * c.K + k0 + 8 * t, *xa = c.x + (int64_t)(row0 + m0) * c.K + k0 + 8 * t;
-        bool own[2 * MW], any = false;
+        bool own[2 * MW];
 #pragma unroll
-        for (int j = 0; j < 2 * MW; ++j) own[j] = win.owner[m0 + 8 * j] == adapter, any |= own[j];
-        const int todo = __any_sync(0xffffffffu, any) ? steps : 0;
-        auto copy_a = [&](int step, int slot) {
-            uint4 *to = mine + slot * pieces * 32;
-            for (int n = 0; n < ranks; ++n) copy16_shared(to + n * 32, MXQ_AT(wa + (int64_t)8 * n * c.K + (int64_t)step * 32 * kSub, 16, c.a, a_bytes));
+        for (int j = 0; j < 2 * MW; ++j) own[j] = win.owner[g + 8 * j] == adapter;
+        // byte addresses of this lane's pieces of the next step to be copied; a row that is not there is not read (its address is the array's own)
+        const uint8_t *wa = reinterpret_cast<const uint8_t *>(c.a + ((int64_t)adapter * c.r + g) * c.K + k0 + 8 * t);
+        const uint8_t *xa = reinterpret_cast<const uint8_t *>(c.x + (int64_t)(row0 + g) * c.K + k0 + 8 * t);
+        auto copy_a = [&](int slot) {
+            const uint32_t to = mine_address + slot * pieces * 512;
+            const uint8_t *from = wa;
+#pragma unroll
+            for (int n = 0; n < RT; ++n, from += stride)
+                if (n < ranks) copy16(to + n * 512, MXQ_AT(from, 16, c.a, a_bytes), true);
+            wa += 64 * WARPS;
         };
-        auto copy_x = [&](int step, int slot) {
-            uint4 *to = mine + (slot * pieces + ranks) * 32;
+        auto copy_x = [&](int slot) {
+            const uint32_t to = mine_address + (slot * pieces + ranks) * 512;
+            const uint8_t *from = xa;
 #pragma unroll
-            for (int j = 0; j < 2 * MW; ++j)     // (a row that is not there is not read: its address is the array's own)
-                copy16(to + j * 32, own[j] ? MXQ_AT(xa + (int64_t)8 * j * c.K + (int64_t)step * 32 * kSub, 16, c.x, x_bytes) : c.x, own[j]);
+            for (int j = 0; j < 2 * MW; ++j, from += stride) copy16(to + j * 512, own[j] ? MXQ_AT(from, 16, c.x, x_bytes) : reinterpret_cast<const uint8_t *>(c.x), own[j]);
+            xa += 64 * WARPS;
         };
         // (the adapters' first steps are on their way before the previous kernel has ended)
-        for (int u = 0; u < c.stages && u < todo; ++u) copy_a(u, u);
+        for (int u = 0; u < c.stages && u < steps; ++u) copy_a(u);
         if (!waited) pdl_wait(), waited = true;
         for (int u = 0; u < c.stages; ++u) {
-            if (u < todo) copy_x(u, u);
+            if (u < steps) copy_x(u);
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
         float acc[MW][RT][4];
@@ -147,7 +152,7 @@ __global__ void __launch_bounds__(kShrinkThreads) lora_shrink_kernel(LoraCall c)
         for (int w = 0; w < MW; ++w)
 #pragma unroll
             for (int n = 0; n < RT; ++n) acc[w][n][0] = acc[w][n][1] = acc[w][n][2] = acc[w][n][3] = 0.f;
-        for (int step = 0, slot = 0; step < todo; ++step) {
+        for (int step = 0, slot = 0; step < steps; ++step) {
             wait_oldest(c.stages);
             const uint4 *from = mine + slot * pieces * 32;
             uint4 x[2 * MW];
@@ -163,41 +168,34 @@ __global__ void __launch_bounds__(kShrinkThreads) lora_shrink_kernel(LoraCall c)
                     mma_bf16(acc[w][n], x[2 * w].z, x[2 * w + 1].z, x[2 * w].w, x[2 * w + 1].w, v.z, v.w);
                 }
             }
-            if (step + c.stages < todo) copy_a(step + c.stages, slot), copy_x(step + c.stages, slot);     // (this lane has read the slot)
+            if (step + c.stages < steps) copy_a(slot), copy_x(slot);     // (this lane has read the slot)
             asm volatile("cp.async.commit_group;" ::: "memory");
             if (++slot == c.stages) slot = 0;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        // the warps' parts of K, added in order; the ring is free for them now
+        // the warps' parts of K, added in order, four ranks of a row per thread; the ring is free for them now
         __syncthreads();
         float *part = reinterpret_cast<float *>(ring);
 #pragma unroll
-        for (int w = 0; w < MW; ++w) {
-            if (sub == 0) break;
+        for (int w = 0; w < MW; ++w)
 #pragma unroll
             for (int n = 0; n < RT; ++n) {
                 if (n >= ranks) break;
-                float *p = part + ((sub - 1) * kRows + m0 + 16 * w) * c.r + 8 * n + 2 * t;
+                float *p = part + (warp * kRows + g + 16 * w) * c.r + 8 * n + 2 * t;
                 *reinterpret_cast<float2 *>(p) = make_float2(acc[w][n][0], acc[w][n][1]);
                 *reinterpret_cast<float2 *>(p + 8 * c.r) = make_float2(acc[w][n][2], acc[w][n][3]);
             }
-        }
         __syncthreads();
-        if (sub == 0 && __any_sync(0xffffffffu, any)) {
+        for (int i = threadIdx.x; i < kRows * ranks * 2; i += 32 * WARPS) {
+            const int row = i / (ranks * 2), rank = 4 * (i - row * ranks * 2);
+            if (win.owner[row] != adapter) continue;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < MW; ++w)
-#pragma unroll
-                for (int n = 0; n < RT; ++n) {
-                    if (n >= ranks) break;
-                    for (int u = 0; u < kSub - 1; ++u) {
-                        const float *p = part + (u * kRows + m0 + 16 * w) * c.r + 8 * n + 2 * t;
-                        const float2 p0 = *reinterpret_cast<const float2 *>(p), p1 = *reinterpret_cast<const float2 *>(p + 8 * c.r);
-                        acc[w][n][0] += p0.x, acc[w][n][1] += p0.y, acc[w][n][2] += p1.x, acc[w][n][3] += p1.y;
-                    }
-                    float *out = c.t + ((int64_t)blockIdx.z * c.M + row0 + m0 + 16 * w) * c.r + 8 * n + 2 * t;
-                    if (own[2 * w]) *reinterpret_cast<float2 *>(MXQ_AT(out, 8, c.t, t_bytes)) = make_float2(acc[w][n][0], acc[w][n][1]);
-                    if (own[2 * w + 1]) *reinterpret_cast<float2 *>(MXQ_AT(out + 8 * (int64_t)c.r, 8, c.t, t_bytes)) = make_float2(acc[w][n][2], acc[w][n][3]);
-                }
+            for (int u = 0; u < WARPS; ++u) {
+                const float4 p = *reinterpret_cast<const float4 *>(part + (u * kRows + row) * c.r + rank);
+                sum.x += p.x, sum.y += p.y, sum.z += p.z, sum.w += p.w;
+            }
+            *reinterpret_cast<float4 *>(MXQ_AT(c.t + ((int64_t)blockIdx.z * c.M + row0 + row) * c.r + rank, 16, c.t, t_bytes)) = sum;
         }
         __syncthreads();
     }
@@ -393,25 +391,17 @@ __global__ void __launch_bounds__(256) lora_fragments_kernel(LoraCall c) {
 }
 
 // grid (blocks of 256 columns, blocks of c.tiles tiles of rows); a warp takes 32 columns, whose B stays in registers while the adapter does, and
-// goes through the tiles; base and ids of the next tile are on their way meanwhile.
-template <int KT>
-__global__ void __launch_bounds__(256) lora_expand_many_kernel(LoraCall c) {
+// goes through the tiles; base and ids of the next tile are on their way meanwhile.  VEC: N is a multiple of 8.
+template <int KT, bool F32, bool VEC>
+__global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
+    constexpr int kParts = F32 ? 3 : 2, kSize = F32 ? 4 : 2;
     extern __shared__ uint4 frag[];      // the rows' fragments of T
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int64_t col0 = ((int64_t)blockIdx.x * 8 + warp) * 32, col = col0 + 8 * t, n = (int64_t)c.M * c.N;
     const int steps = (c.r + 15) / 16, all = (c.M + 15) / 16, tile0 = blockIdx.y * c.tiles, tiles = min(c.tiles, all - tile0);
     const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
-    const bool vec = c.N % 8 == 0, early = c.base && !c.base_f32 && vec && there > 0, copies = c.base != c.y;
-    auto owner = [&](int tile, int h) {
-        const int m = (tile0 + tile) * 16 + 8 * h + g;
-        const int a = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
-        return a >= 0 && a < c.L ? a : -1;
-    };
-    auto base_of = [&](int tile, int h) {        // BF16 in whole vectors; anything else is loaded where it is needed
-        const int m = (tile0 + tile) * 16 + 8 * h + g;
-        return early && m < c.M ? ld_dep_u4(MXQ_AT(c.base + ((int64_t)m * c.N + col) * 2, 16, c.base, n * 2)) : make_uint4(0, 0, 0, 0);
-    };
+    const bool copies = c.base != c.y;
     uint2 w[KT][4];
     auto load = [&](int adapter) {
 #pragma unroll
@@ -420,35 +410,57 @@ __global__ void __launch_bounds__(256) lora_expand_many_kernel(LoraCall c) {
             for (int i = 0; i < 4; ++i)
                 if (s < steps) w[s][i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
     };
-    int own[2] = {owner(0, 0), owner(0, 1)};
-    int current = (int)__reduce_max_sync(0xffffffffu, max(own[0], own[1]));
+    // this lane's rows m, m + 8 of the tile whose ids and base are loaded next; `place` of its columns in base and Y
+    int m = tile0 * 16 + g;
+    int64_t place = (int64_t)m * c.N + col;
+    const int64_t row8 = 8 * c.N;
+    int own[2];
+    Columns base[2];
+    auto load_ids = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int a = m + 8 * h < c.M ? __ldg(MXQ_AT(c.ids + m + 8 * h, 4, c.ids, (size_t)c.M * 4)) : -1;
+            own[h] = a < c.L ? max(a, -1) : -1;
+        }
+    };
+    auto load_base = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            base[h].lo = base[h].hi = make_uint4(0, 0, 0, 0);
+            if (VEC && c.base && there > 0 && m + 8 * h < c.M) {
+                const uint8_t *p = MXQ_AT(c.base + (place + h * row8) * kSize, 8 * kSize, c.base, n * kSize);
+                base[h].lo = ld_dep_u4(p);
+                if (F32) base[h].hi = ld_dep_u4(p + 16);
+            }
+        }
+    };
+    load_ids();
+    int current = __reduce_max_sync(0xffffffffu, max(own[0], own[1]));
     if (current >= 0) load(current);
     pdl_wait();
-    const int pieces = steps * c.parts * 32;
-    const size_t bytes = (size_t)all * pieces * 16;
+    const int pieces = steps * kParts * 32;
     for (int i = threadIdx.x; i < tiles * pieces; i += 256)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(frag + i)), "l"(MXQ_AT(c.frag + (int64_t)tile0 * pieces + i, 16, c.frag, bytes)) : "memory");
-    uint4 base[2] = {base_of(0, 0), base_of(0, 1)};
+        copy16(shared_address(frag + i), MXQ_AT(c.frag + (int64_t)tile0 * pieces + i, 16, c.frag, (size_t)all * pieces * 16), true);
+    load_base();
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     if (col0 >= c.N) return;
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int m0 = (tile0 + tile) * 16 + g;
-        const int now[2] = {own[0], own[1]};
+    const uint4 *q = frag + lane;
+    for (int tile = 0; tile < tiles; ++tile, q += pieces) {
+        const int64_t now = place;
+        const int rows = c.M - m;            // rows m, m + 8 are there if 0, 8 < rows
         float f[2][8];
+        int left[2], none[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            unpack_bf16(f[h], base[h]);
-            if (c.base && !early && there > 0 && m0 + 8 * h < c.M) load_columns(f[h], c.base, c.base_f32, (int64_t)(m0 + 8 * h) * c.N + col, there, vec, n);
+            left[h] = own[h], none[h] = own[h] < 0;
+            unpack_columns(f[h], base[h], F32);
+            if (!VEC && c.base && there > 0 && 8 * h < rows) load_columns(f[h], c.base, F32, now + h * row8, there, false, n);
         }
-        if (tile + 1 < tiles) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) own[h] = owner(tile + 1, h), base[h] = base_of(tile + 1, h);
-        }
-        int left[2] = {now[0], now[1]};
-        while (true) {                       // the tile's adapters, one after the other
-            const int adapter = (int)__reduce_max_sync(0xffffffffu, max(left[0], left[1]));
-            if (adapter < 0) break;
+        m += 16, place += 2 * row8;
+        if (tile + 1 < tiles) load_ids(), load_base();
+        int adapter = __reduce_max_sync(0xffffffffu, max(left[0], left[1]));
+        while (adapter >= 0) {               // the tile's adapters, one after the other
             if (adapter != current) load(adapter), current = adapter;
             float acc[4][4];
 #pragma unroll
@@ -456,24 +468,26 @@ __global__ void __launch_bounds__(256) lora_expand_many_kernel(LoraCall c) {
 #pragma unroll
             for (int s = 0; s < KT; ++s) {
                 if (s >= steps) break;
-                for (int p = 0; p < c.parts; ++p) {
-                    const uint4 q = frag[((tile * steps + s) * c.parts + p) * 32 + lane];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mma_bf16(acc[i], q.x, q.y, q.z, q.w, w[s][i].x, w[s][i].y);
+                for (int p = 0; p < kParts; ++p) {
+                    const uint4 v = q[(s * kParts + p) * 32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma_bf16(acc[i], v.x, v.y, v.z, v.w, w[s][i].x, w[s][i].y);
                 }
             }
             // (rows of other adapters went through the product too; what they got is dropped here)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (left[h] != adapter) continue;
-                left[h] = -1;
+                const bool mine = left[h] == adapter;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f[h][2 * i] += acc[i][2 * h], f[h][2 * i + 1] += acc[i][2 * h + 1];
+                for (int i = 0; i < 4; ++i) f[h][2 * i] = mine ? f[h][2 * i] + acc[i][2 * h] : f[h][2 * i], f[h][2 * i + 1] = mine ? f[h][2 * i + 1] + acc[i][2 * h + 1] : f[h][2 * i + 1];
+                if (mine) left[h] = -1;
             }
+            adapter = __reduce_max_sync(0xffffffffu, max(left[0], left[1]));
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (there > 0 && m0 + 8 * h < c.M && (now[h] >= 0 || copies)) store_columns(f[h], c.y, c.y_f32, (int64_t)(m0 + 8 * h) * c.N + col, there, vec, n);
+            if (there > 0 && 8 * h < rows && (!none[h] || copies)) store_columns(f[h], c.y, F32, now + h * row8, there, VEC, n);
     }
 }
 
@@ -484,13 +498,14 @@ MXQ_BOUNDS_TU(bounds_take_lora)
 // From 512 rows on windows of 32 rows (a window reads its adapters once) and T's fragments made once, by a kernel of their own; below that
 // windows of 16 rows, a CTA per adapter, and every CTA of the expansion makes its own.
 static bool many_rows(int64_t M) { return M >= 512; }
+constexpr int kFewWarps = 8, kManyWarps = 16;     // of a CTA of the shrink (above rank 64 sixteen warps' sums do not fit the registers)
 
 static void lora_plan(LoraCall &c) {
     const bool many = many_rows(c.M);
     const int64_t windows = many ? (c.M + 31) / 32 : (c.M + 15) / 16;
     c.slots = many ? 1 : min(16, min(c.M, c.L));
     // splits of K as long as the SMs hold the CTAs at once, but at least one step of 32 per warp
-    const int64_t step = 32 * kShrinkWarps, most = (c.K + step - 1) / step;
+    const int64_t step = 32 * (many && c.r <= 64 ? kManyWarps : kFewWarps), most = (c.K + step - 1) / step;
     int64_t want = max((int64_t)1, (many ? 1 : 2) * (int64_t)sm_count() / (windows * c.slots));
     if (want > most) want = most;
     if (want > 32) want = 32;
@@ -532,18 +547,18 @@ static bool allow_smem(void (*kernel)(LoraCall), size_t smem) {
     return false;
 }
 
-template <int MW, int WM>
+template <int MW, int WARPS>
 static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
-    constexpr int kRows = 16 * MW * WM, kSub = kShrinkWarps / WM;
+    constexpr int kRows = 16 * MW;
     const dim3 grid((unsigned)((c.M + kRows - 1) / kRows), (unsigned)c.slots, (unsigned)c.splits);
-    const size_t stage = (size_t)kShrinkWarps * (c.r / 8 + 2 * MW) * 512, parts = (size_t)(kSub - 1) * kRows * c.r * 4;
-    const int steps = (c.split_k + 32 * kSub - 1) / (32 * kSub);
+    const size_t stage = (size_t)WARPS * (c.r / 8 + 2 * MW) * 512, parts = (size_t)WARPS * kRows * c.r * 4;
+    const int steps = (c.split_k + 32 * WARPS - 1) / (32 * WARPS);
     LoraCall call = c;
     call.stages = max(1, min(min(kMostStages, steps), (int)(200 * 1024 / stage)));
     const size_t smem = max(stage * call.stages, parts);
-    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_shrink_kernel<MW, WM, 2> : c.r <= 32 ? lora_shrink_kernel<MW, WM, 4> : c.r <= 64 ? lora_shrink_kernel<MW, WM, 8> : lora_shrink_kernel<MW, WM, 16>;
+    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_shrink_kernel<MW, WARPS, 2> : c.r <= 32 ? lora_shrink_kernel<MW, WARPS, 4> : c.r <= 64 ? lora_shrink_kernel<MW, WARPS, 8> : lora_shrink_kernel<MW, WARPS, 16>;
     if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
-    return launch_pdl(kernel, grid, kShrinkThreads, smem, stream, call);
+    return launch_pdl(kernel, grid, 32 * WARPS, smem, stream, call);
 }
 
 static int expand_launch(const LoraCall &c, cudaStream_t stream) {
@@ -554,6 +569,14 @@ static int expand_launch(const LoraCall &c, cudaStream_t stream) {
                       grid, 32 * kWarps, smem, stream, c);
 }
 
+template <bool F32, bool VEC>
+static auto many_kernel_of(int r) -> void (*)(LoraCall) {
+    return r <= 16 ? lora_expand_many_kernel<1, F32, VEC> : r <= 32 ? lora_expand_many_kernel<2, F32, VEC> : r <= 64 ? lora_expand_many_kernel<4, F32, VEC> : lora_expand_many_kernel<8, F32, VEC>;
+}
+static void (*many_kernel(int r, bool f32, bool vec))(LoraCall) {
+    return f32 ? (vec ? many_kernel_of<true, true>(r) : many_kernel_of<true, false>(r)) : (vec ? many_kernel_of<false, true>(r) : many_kernel_of<false, false>(r));
+}
+
 static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     const int steps = (c.r + 15) / 16, tiles = (c.M + 15) / 16;
     int rc = launch_pdl(lora_fragments_kernel, dim3((unsigned)(((int64_t)tiles * 16 * steps * 4 + 255) / 256)), 256, 0, stream, c);
@@ -561,12 +584,14 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     c.tiles = 8;
     const dim3 grid((unsigned)((c.N + 255) / 256), (unsigned)((tiles + c.tiles - 1) / c.tiles));
     const size_t smem = (size_t)c.tiles * steps * c.parts * 512;
-    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_expand_many_kernel<1> : c.r <= 32 ? lora_expand_many_kernel<2> : c.r <= 64 ? lora_expand_many_kernel<4> : lora_expand_many_kernel<8>;
+    void (*const kernel)(LoraCall) = many_kernel(c.r, c.y_f32 != 0, c.N % 8 == 0);
     if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
     return launch_pdl(kernel, grid, 256, smem, stream, c);
 }
 
-static int lora_shrink(const LoraCall &c, cudaStream_t stream) { return many_rows(c.M) ? shrink_launch<2, 1>(c, stream) : shrink_launch<1, 1>(c, stream); }
+static int lora_shrink(const LoraCall &c, cudaStream_t stream) { 
+    return !many_rows(c.M) ? shrink_launch<1, kFewWarps>(c, stream) : c.r <= 64 ? shrink_launch<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps>(c, stream);
+}
 static int lora_expand(LoraCall &c, const void *base, int base_dtype, void *Y, int y_dtype, cudaStream_t stream) {
     c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
     c.frag = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c));
