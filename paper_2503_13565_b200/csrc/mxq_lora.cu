@@ -503,10 +503,11 @@ constexpr int kFewWarps = 8, kManyWarps = 16;     // of a CTA of the shrink (abo
 static void lora_plan(LoraCall &c) {
     const bool many = many_rows(c.M);
     const int64_t windows = many ? (c.M + 31) / 32 : (c.M + 15) / 16;
-    c.slots = many ? 1 : min(16, min(c.M, c.L));
+    // (many rows: a second CTA for the windows in which one adapter's rows end and another's begin; the prompt of 4095 rows: 67 -> us)
+    c.slots = many ? min(2, c.L) : min(16, min(c.M, c.L));
     // splits of K as long as the SMs hold the CTAs at once, but at least one step of 32 per warp
     const int64_t step = 32 * (many && c.r <= 64 ? kManyWarps : kFewWarps), most = (c.K + step - 1) / step;
-    int64_t want = max((int64_t)1, (many ? 1 : 2) * (int64_t)sm_count() / (windows * c.slots));
+    int64_t want = max((int64_t)1, many ? sm_count() / windows : 2 * (int64_t)sm_count() / (windows * c.slots));
     if (want > most) want = most;
     if (want > 32) want = 32;
     int64_t len = ((c.K + want - 1) / want + step - 1) / step * step;
