@@ -789,17 +789,26 @@ def mxq_kv_compact(cache: KVCache, tables: torch.Tensor, lens: torch.Tensor, row
 # ---- what a decoder step needs between its linear layers and its cache --------------------
 
 
-def _rows_of(t: torch.Tensor, what: str):
-    """Pointer and row stride (elements) of a CUDA tensor [M, K] whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda or t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise TypeError("%s must be a CUDA tensor [M, K] with contiguous rows" % what)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+# (These calls take a few microseconds on the GPU, so their host side counts: one function per tensor checks all there is to check,
+# and outputs are made like a tensor that has their shape where there is one, which costs half of an empty one.)
+_DTYPES = {torch.float32: MXQ_F32, torch.bfloat16: MXQ_BF16}
 
 
-def _same(t, shape, what: str):
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be %s" % (what, list(shape)))
-    return t
+def _ptr(t: torch.Tensor, dtype, shape, what: str) -> int:
+    """Address of a contiguous CUDA tensor of this dtype and shape."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        if t.shape != shape:
+            raise ValueError("%s must be %s" % (what, list(shape)))
+        raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (what, dtype))
+    return t.data_ptr()
+
+
+def _float(t: torch.Tensor, shape, what: str):
+    """Address and dtype selector of a contiguous FP32 or BF16 CUDA tensor of this shape."""
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise TypeError("%s must be torch.float32 or torch.bfloat16" % what)
+    return _ptr(t, t.dtype, shape, what), d
 
 
 def mxq_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: torch.Tensor = None, residual_out: torch.Tensor = None,
@@ -808,47 +817,52 @@ def mxq_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residu
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight for rows x [M, K] (FP32 or BF16, a column slice will do).  ``residual_out``
     receives h (``residual`` itself: the stream is updated in place).  Returns y BF16 and / or its MXFP8 pair: y with ``bf16``,
     (codes u8 [M, K], scales u8 [M, K/32]) with ``mxfp8``, (y, codes, scales) with both."""
-    xp, stride = _rows_of(x, "x")
-    m, k = x.shape
-    _same(weight, (k,), "weight")
+    shape, xt = x.shape, _DTYPES.get(x.dtype)
+    m, k = shape
+    stride = k
+    if not x.is_contiguous():
+        stride = x.stride(0) if m > 1 else k
+        if x.stride(1) != 1 or stride < k:
+            raise TypeError("x must be [M, K] with contiguous rows")
+    if xt is None or not x.is_cuda:
+        raise TypeError("x must be a CUDA tensor of dtype torch.float32 or torch.bfloat16")
+    wp, wt = _float(weight, (k,), "weight")
+    rp = rt = op = yp = cp = sp = 0
     if residual is not None:
-        _same(residual, (m, k), "residual")
+        rp, rt = _float(residual, shape, "residual")
     if residual_out is not None:
-        if residual is None or residual_out.dtype != residual.dtype:
+        if residual is None:
             raise TypeError("residual_out needs a residual of its dtype")
-        _same(residual_out, (m, k), "residual_out")
-    bf16, mxfp8 = bf16 or out is not None, mxfp8 or codes is not None or scales is not None
-    if not bf16 and not mxfp8:
+        op = rp if residual_out is residual else _ptr(residual_out, residual.dtype, shape, "residual_out")
+    if out is not None or bf16:
+        if out is None:
+            like = x if xt == MXQ_BF16 and stride == k else residual if rt == MXQ_BF16 and residual is not None else None
+            with _on(stream):
+                out = torch.empty((m, k), dtype=torch.bfloat16, device=x.device) if like is None else torch.empty_like(like)
+        yp = _ptr(out, torch.bfloat16, shape, "out")
+    if mxfp8 or codes is not None or scales is not None:
+        with _on(stream):
+            if codes is None:
+                codes = torch.empty((m, k), dtype=torch.uint8, device=x.device)
+            if scales is None:
+                scales = torch.empty((m, k // 32), dtype=torch.uint8, device=x.device)
+        cp, sp = _ptr(codes, torch.uint8, shape, "codes"), _ptr(scales, torch.uint8, (m, k // 32), "scales")
+    elif out is None:
         raise ValueError("nothing to return: bf16 or mxfp8")
-    with _on(stream):
-        if bf16 and out is None:
-            out = torch.empty((m, k), dtype=torch.bfloat16, device=x.device)
-        if mxfp8 and codes is None:
-            codes = torch.empty((m, k), dtype=torch.uint8, device=x.device)
-        if mxfp8 and scales is None:
-            scales = torch.empty((m, k // 32), dtype=torch.uint8, device=x.device)
-    if bf16:
-        _same(out, (m, k), "out")
-    if mxfp8:
-        _same(codes, (m, k), "codes"), _same(scales, (m, k // 32), "scales")
-    _check(lib().mxq_rmsnorm(xp, _dt(x.dtype), stride, 0 if residual is None else _dev(residual, residual.dtype, "residual"),
-                             0 if residual is None else _dt(residual.dtype), 0 if residual_out is None else _dev(residual_out, residual.dtype, "residual_out"),
-                             _dev(weight, weight.dtype, "weight"), _dt(weight.dtype), eps, m, k, _dev(out, torch.bfloat16, "out") if bf16 else 0,
-                             _dev(codes, torch.uint8, "codes") if mxfp8 else 0, _dev(scales, torch.uint8, "scales") if mxfp8 else 0, _stream(stream)),
-           "mxq_rmsnorm")
-    return (out, codes, scales) if bf16 and mxfp8 else out if bf16 else (codes, scales)
+    _check(lib().mxq_rmsnorm(x.data_ptr(), xt, stride, rp, rt, op, wp, wt, eps, m, k, yp, cp, sp, _stream(stream)), "mxq_rmsnorm")
+    return out if codes is None else (codes, scales) if out is None else (out, codes, scales)
 
 
 def mxq_dequantize_mxfp8(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor = None, out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
     """The values [N, K] that an MXFP8 pair stands for."""
-    n, k = codes.shape
-    _same(scales, (n, k // 32), "scales")
+    shape = codes.shape
+    n, k = shape
     if out is None:
         with _on(stream):
             out = torch.empty((n, k), dtype=out_dtype, device=codes.device)
-    _same(out, (n, k), "out")
-    _check(lib().mxq_dequantize_mxfp8(_dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), n, k, _dev(out, out.dtype, "out"),
-                                      _dt(out.dtype), _stream(stream)), "mxq_dequantize_mxfp8")
+    op, ot = _float(out, shape, "out")
+    _check(lib().mxq_dequantize_mxfp8(_ptr(codes, torch.uint8, shape, "codes"), _ptr(scales, torch.uint8, (n, k // 32), "scales"), n, k, op, ot,
+                                      _stream(stream)), "mxq_dequantize_mxfp8")
     return out
 
 
@@ -867,7 +881,7 @@ class Rope:
         if table.dim() != 2 or style not in ROPE_STYLES:
             raise ValueError("table must be [positions, rotary_dim], style one of %s" % sorted(ROPE_STYLES))
         self.table, self.style = table, style
-        self._struct = _RopeStruct(_dev(table, torch.float32, "table"), table.shape[0], table.shape[1], ROPE_STYLES[style])
+        self._struct = _RopeStruct(_ptr(table, torch.float32, table.shape, "table"), table.shape[0], table.shape[1], ROPE_STYLES[style])
         self.ptr = ctypes.addressof(self._struct)
 
 
@@ -877,9 +891,8 @@ def mxq_rope_table(inv_freq: torch.Tensor, positions: int, amplitude: float = 1.
     if out is None:
         with _on(stream):
             out = torch.empty((positions, rotary), dtype=torch.float32, device=inv_freq.device)
-    _same(out, (positions, rotary), "out")
-    _check(lib().mxq_rope_table(_dev(inv_freq, torch.float64, "inv_freq"), positions, rotary, amplitude, _dev(out, torch.float32, "out"), _stream(stream)),
-           "mxq_rope_table")
+    _check(lib().mxq_rope_table(_ptr(inv_freq, torch.float64, (rotary // 2,), "inv_freq"), positions, rotary, amplitude,
+                                _ptr(out, torch.float32, (positions, rotary), "out"), _stream(stream)), "mxq_rope_table")
     return out
 
 
@@ -900,7 +913,7 @@ def mxq_kv_append_rope(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Ten
         qp, qs = _token_rows(q, shape, "q")
         if q_out is None:
             with _on(stream):
-                q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         op, os_ = _token_rows(q_out, shape, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -923,7 +936,8 @@ class LogitRules:
         if (bias_tokens is None) != (bias_values is None) or (bias_tokens is not None and bias_tokens.shape != bias_values.shape):
             raise ValueError("bias_tokens and bias_values must both be [B, J]")
         self.counts, self.penalties, self.bias_tokens, self.bias_values, self.allowed = counts, penalties, bias_tokens, bias_values, allowed
-        p = [0 if t is None else _dev(t, d, n) for t, d, n in ((counts, torch.int32, "counts"), (penalties, torch.float32, "penalties"),
+        self._fits = None
+        p = [0 if t is None else _ptr(t, d, t.shape, n) for t, d, n in ((counts, torch.int32, "counts"), (penalties, torch.float32, "penalties"),
                                                                (bias_tokens, torch.int32, "bias_tokens"), (bias_values, torch.float32, "bias_values"),
                                                                (allowed, torch.int32, "allowed"))]
         self._struct = _LogitRulesStruct(*p, 0 if bias_tokens is None else bias_tokens.shape[1], 0)
@@ -931,32 +945,37 @@ class LogitRules:
 
     def fit(self, b: int, r: int, v: int) -> int:
         """The struct's address for a call on logits [b, r, v]."""
+        if self._fits == (b, r, v):
+            return self.ptr
         for t, shape, what in ((self.counts, (b, v), "counts"), (self.penalties, (b, 3), "penalties"), (self.allowed, (b, r, (v + 31) // 32), "allowed")):
             if t is not None and t.shape != shape:
                 raise ValueError("%s must be %s" % (what, list(shape)))
         if self.bias_tokens is not None and (self.bias_tokens.dim() != 2 or self.bias_tokens.shape[0] != b):
             raise ValueError("bias_tokens must be [B, J]")
+        self._fits = (b, r, v)
         return self.ptr
 
 
 def _draft(draft, b: int):
     if draft is None:
         return 0, 0
-    if draft.dim() != 2 or draft.shape[0] != b:
+    if draft.dim() != 2:
         raise ValueError("draft must be [B, T]")
-    return _dev(draft, torch.int32, "draft"), draft.shape[1]
+    t = draft.shape[1]
+    return _ptr(draft, torch.int32, (b, t), "draft"), t
 
 
 def mxq_logits_adjust(logits: torch.Tensor, rules: LogitRules, draft: torch.Tensor = None, out: torch.Tensor = None, stream=None) -> torch.Tensor:
     """Logits [B, R, V] after the rules, in their own dtype (``out`` may be ``logits``); row r counts draft[:, :r] as generated."""
-    b, r, v = logits.shape
+    shape = logits.shape
+    b, r, v = shape
     dp, t = _draft(draft, b)
     if out is None:
         with _on(stream):
             out = torch.empty_like(logits)
-    _same(out, (b, r, v), "out")
-    _check(lib().mxq_logits_adjust(_dev(logits, logits.dtype, "logits"), _dt(logits.dtype), b, r, v, dp, t, rules.fit(b, r, v),
-                                   _dev(out, logits.dtype, "out"), _stream(stream)), "mxq_logits_adjust")
+    lp, lt = _float(logits, shape, "logits")
+    _check(lib().mxq_logits_adjust(lp, lt, b, r, v, dp, t, rules.fit(b, r, v), _ptr(out, logits.dtype, shape, "out"), _stream(stream)),
+           "mxq_logits_adjust")
     return out
 
 
@@ -967,20 +986,22 @@ def mxq_greedy_accept_rules_workspace_bytes(b: int, r: int, v: int) -> int:
 def mxq_greedy_accept_rules(logits: torch.Tensor, draft: torch.Tensor, rules: LogitRules, workspace: torch.Tensor = None, stream=None, out=None):
     """mxq_greedy_accept on the logits [B, R, V] after the rules, which are not written -> (verifier [B, R], accept_len [B], next_token [B])
     int32.  ``draft`` [B, T] int32, or None with R = 1: next_token is the argmax.  ``out``: optional triple of tensors to write into."""
-    b, r, v = logits.shape
+    shape = logits.shape
+    b, r, v = shape
     dp, t = _draft(draft, b)
     with _on(stream):
         if workspace is None:
             workspace = new_workspace(mxq_greedy_accept_rules_workspace_bytes(b, r, v), logits.device)
-        if out is None:
-            out = (torch.empty((b, r), dtype=torch.int32, device=logits.device), torch.empty(b, dtype=torch.int32, device=logits.device),
-                   torch.empty(b, dtype=torch.int32, device=logits.device))
+        if out is None:      # (three views of one allocation)
+            ver, n, nxt = torch.empty(b * (r + 2), dtype=torch.int32, device=logits.device).split((b * r, b, b))
+            out = (ver.view(b, r), n, nxt)
     ver, n, nxt = out
-    _same(ver, (b, r), "verifier"), _same(n, (b,), "accept_len"), _same(nxt, (b,), "next_token")
-    _check(lib().mxq_greedy_accept_rules(_dev(logits, logits.dtype, "logits"), _dt(logits.dtype), b, r, v, dp, t, rules.fit(b, r, v),
-                                         _dev(ver, torch.int32, "verifier"), _dev(n, torch.int32, "accept_len"), _dev(nxt, torch.int32, "next_token"),
-                                         _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_greedy_accept_rules")
-    return ver, n, nxt
+    lp, lt = _float(logits, shape, "logits")
+    _check(lib().mxq_greedy_accept_rules(lp, lt, b, r, v, dp, t, rules.fit(b, r, v), _ptr(ver, torch.int32, (b, r), "verifier"),
+                                         _ptr(n, torch.int32, (b,), "accept_len"), _ptr(nxt, torch.int32, (b,), "next_token"),
+                                         _ptr(workspace, torch.uint8, workspace.shape, "workspace"), workspace.numel(), _stream(stream)),
+           "mxq_greedy_accept_rules")
+    return out
 
 
 def mxq_token_counts(counts: torch.Tensor, tokens: torch.Tensor, n: torch.Tensor = None, next_token: torch.Tensor = None, prompt: bool = False,
@@ -988,10 +1009,12 @@ def mxq_token_counts(counts: torch.Tensor, tokens: torch.Tensor, n: torch.Tensor
     """Add the first n[b] (None: all) of tokens [B, L] int32, and next_token [B] if given, to counts int32 [B, V]: as generated, or with
     ``prompt`` marked as prompted.  After a verification: tokens = draft, n = accept_len, next_token."""
     b, v = counts.shape
-    if tokens.dim() != 2 or tokens.shape[0] != b:
+    if tokens.dim() != 2:
         raise ValueError("tokens must be [B, L]")
-    _check(lib().mxq_token_counts(_dev(counts, torch.int32, "counts"), b, v, _dev(tokens, torch.int32, "tokens"), tokens.shape[1],
-                                  _kv_ints(n, (b,), "n"), _kv_ints(next_token, (b,), "next_token"), 1 if prompt else 0, _stream(stream)), "mxq_token_counts")
+    l = tokens.shape[1]
+    _check(lib().mxq_token_counts(_ptr(counts, torch.int32, (b, v), "counts"), b, v, _ptr(tokens, torch.int32, (b, l), "tokens"), l,
+                                  0 if n is None else _ptr(n, torch.int32, (b,), "n"), 0 if next_token is None else _ptr(next_token, torch.int32, (b,), "next_token"),
+                                  1 if prompt else 0, _stream(stream)), "mxq_token_counts")
 
 
 class _LoraStruct(ctypes.Structure):
@@ -1000,12 +1023,12 @@ class _LoraStruct(ctypes.Structure):
 
 def _adapters(a, b, scale, ids, m, k):
     """(struct, ids pointer, N) of adapters a [L, r, K], b [L, N, r] for rows [m, k]."""
-    if a.dim() != 3 or b.dim() != 3 or a.shape[2] != k or b.shape[0] != a.shape[0] or b.shape[2] != a.shape[1]:
+    sa, sb = a.shape, b.shape
+    if len(sa) != 3 or len(sb) != 3 or sa[2] != k or sb[0] != sa[0] or sb[2] != sa[1]:
         raise ValueError("a must be [L, r, K] and b [L, N, r]")
-    if scale is not None:
-        _same(scale, (a.shape[0],), "scale")
-    return (_LoraStruct(_dev(a, torch.bfloat16, "a"), _dev(b, torch.bfloat16, "b"), 0 if scale is None else _dev(scale, torch.float32, "scale"),
-                        a.shape[1], a.shape[0]), _kv_ints(ids, (m,), "ids"), b.shape[1])
+    return (_LoraStruct(_ptr(a, torch.bfloat16, sa, "a"), _ptr(b, torch.bfloat16, sb, "b"),
+                        0 if scale is None else _ptr(scale, torch.float32, (sa[0],), "scale"), sa[1], sa[0]),
+            _ptr(ids, torch.int32, (m,), "ids"), sb[1])
 
 
 def mxq_lora_workspace_bytes(m: int, n: int, k: int, rank: int, adapters: int) -> int:
@@ -1020,14 +1043,12 @@ def mxq_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tenso
     ad, ip, n = _adapters(a, b, scale, ids, m, k)
     with _on(stream):
         if out is None:
-            out = torch.empty((m, n), dtype=out_dtype if base is None else base.dtype, device=x.device)
+            out = torch.empty((m, n), dtype=out_dtype, device=x.device) if base is None else torch.empty_like(base)
         if workspace is None:
             workspace = torch.empty(max(16, mxq_lora_workspace_bytes(m, n, k, ad.rank, ad.count)), dtype=torch.uint8, device=x.device)
-    _same(out, (m, n), "out")
-    if base is not None:
-        _same(base, (m, n), "base")
-    _check(lib().mxq_lora(_dev(x, torch.bfloat16, "x"), m, ctypes.addressof(ad), ip, n, k, 0 if base is None else _dev(base, out.dtype, "base"),
-                          _dev(out, out.dtype, "out"), _dt(out.dtype), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)), "mxq_lora")
+    op, ot = _float(out, (m, n), "out")
+    _check(lib().mxq_lora(_ptr(x, torch.bfloat16, (m, k), "x"), m, ctypes.addressof(ad), ip, n, k, 0 if base is None else _ptr(base, out.dtype, (m, n), "base"),
+                          op, ot, _ptr(workspace, torch.uint8, workspace.shape, "workspace"), workspace.numel(), _stream(stream)), "mxq_lora")
     return out
 
 
@@ -1041,17 +1062,15 @@ def mxq_linear_lora(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, 
     """mxq_linear with the adapters of its rows added (see ``mxq_lora``): X . w^T + scale[i] * b[i] (a[i] x[m])."""
     m, k = x.shape
     ad, ip, n = _adapters(a, b, scale, ids, m, k)
-    if tuple(codes.shape) != (n, k // 2) or tuple(scales.shape) != (n, k // 32):
-        raise ValueError("shape mismatch between X, codes, scales and b")
     with _on(stream):
         if out is None:
             out = torch.empty((m, n), dtype=out_dtype, device=x.device)
         if workspace is None:
             workspace = torch.empty(max(16, mxq_linear_lora_workspace_bytes(m, n, k, ad.rank, ad.count)), dtype=torch.uint8, device=x.device)
-    _same(out, (m, n), "out")
-    _check(lib().mxq_linear_lora(_dev(x, torch.bfloat16, "x"), m, _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), n, k,
-                                 ctypes.addressof(ad), ip, _dev(out, out.dtype, "out"), _dt(out.dtype), _dev(workspace, torch.uint8, "workspace"),
-                                 workspace.numel(), _stream(stream)), "mxq_linear_lora")
+    op, ot = _float(out, (m, n), "out")
+    _check(lib().mxq_linear_lora(_ptr(x, torch.bfloat16, (m, k), "x"), m, _ptr(codes, torch.uint8, (n, k // 2), "codes"),
+                                 _ptr(scales, torch.uint8, (n, k // 32), "scales"), n, k, ctypes.addressof(ad), ip, op, ot,
+                                 _ptr(workspace, torch.uint8, workspace.shape, "workspace"), workspace.numel(), _stream(stream)), "mxq_linear_lora")
     return out
 
 

@@ -82,17 +82,31 @@ __global__ void __launch_bounds__(kRopeThreads) kv_append_rope_kernel(KvView c, 
     const uint32_t lanes = 0xFu << (4 * quad);
     int unit = (int)part * r.rounds * 8 + quad;
 
+    // a decode step's heads are on their way before the row's place is known; a prompt's wait for it, since rows that are not there are not read
     uint4 x[kNb];
     Unit<D> u = rope_unit<D>(r, s, c.heads, row, unit);
+    auto load = [&]() {
 #pragma unroll
-    for (int j = 0; j < kNb; ++j)
-        if (u.kind != 3) x[j] = ld_dep_u4(MXQ_AT(u.src + 32 * j + 8 * q, 16, u.base, u.extent));
+        for (int j = 0; j < kNb; ++j)
+            if (u.kind != 3) x[j] = ld_dep_u4(MXQ_AT(u.src + 32 * j + 8 * q, 16, u.base, u.extent));
+    };
+    if (r.rounds == 1) load();
 
     const int rows = s.nrows(b), place = s.len(b) - rows + i;
     const bool there = i < rows && place >= 0;
+    if (!there) {            // (the whole warp: it has one row)
+        for (int h = unit; h < min(r.q_heads, unit + 8 * r.rounds); h += 8) {
+            uint16_t *dst = r.q_out + (int64_t)row * r.qo_stride + (int64_t)h * D + 8 * q;
+#pragma unroll
+            for (int j = 0; j < kNb; ++j)
+                *reinterpret_cast<uint4 *>(MXQ_AT(dst + 32 * j, 16, r.q_out, (((int64_t)s.B * s.m - 1) * r.qo_stride + (int64_t)r.q_heads * D) * 2)) = make_uint4(0, 0, 0, 0);
+        }
+        return;
+    }
+    if (r.rounds != 1) load();
     const int64_t pos = r.where == nullptr ? place : (int)ld_dep_u32(MXQ_AT(r.where + row, 4, r.where, (size_t)s.B * s.m * 4));
     RowPlace at = {nullptr, 0};
-    if (there) at = row_place<D>(c, s, b, place, 0);
+    at = row_place<D>(c, s, b, place, 0);
     const int half = r.rotary / 2;
     // the angles of this lane's elements: of pairs in the first half of its blocks (kWhole), of each of its blocks (kPairs)
     float cs[kNb / 2 * 8], sn[kNb / 2 * 8];
@@ -123,9 +137,7 @@ __global__ void __launch_bounds__(kRopeThreads) kv_append_rope_kernel(KvView c, 
         unit += 8;
         if (round + 1 < r.rounds) {          // the next heads are on their way meanwhile
             u = rope_unit<D>(r, s, c.heads, row, unit);
-#pragma unroll
-            for (int j = 0; j < kNb; ++j)
-                if (u.kind != 3) x[j] = ld_dep_u4(MXQ_AT(u.src + 32 * j + 8 * q, 16, u.base, u.extent));
+            load();
         }
         if (now.kind == 3) break;            // (quads leave whole)
         if (now.kind != 2) {
@@ -168,7 +180,7 @@ __global__ void __launch_bounds__(kRopeThreads) kv_append_rope_kernel(KvView c, 
             uint16_t *dst = r.q_out + (int64_t)row * r.qo_stride + (int64_t)now.head * D + 8 * q;
 #pragma unroll
             for (int j = 0; j < kNb; ++j)
-                *reinterpret_cast<uint4 *>(MXQ_AT(dst + 32 * j, 16, r.q_out, (((int64_t)s.B * s.m - 1) * r.qo_stride + (int64_t)r.q_heads * D) * 2)) = there ? pack_bf16(f[j]) : make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(MXQ_AT(dst + 32 * j, 16, r.q_out, (((int64_t)s.B * s.m - 1) * r.qo_stride + (int64_t)r.q_heads * D) * 2)) = pack_bf16(f[j]);
             continue;
         }
         uint32_t w[kNb], scale = 0;
