@@ -219,15 +219,15 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
     int r = r0 + from / parts, part = from % parts, first = first_of(b * c.R + r, part);
     Vectors cur, ahead;
     if (from < to) start(cur, b * c.R + r, first);
+    // this thread's entries of the list of biases, then their places in the tables (a second one where two of a row's batches share a token's)
+    int32_t entry[kEntries], second[kEntries];
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) entry[u] = second[u] = -1;
     if (tabled) {
-        int32_t entry_token[kEntries], entry_value[kEntries];
 #pragma unroll
         for (int u = 0; u < kEntries; ++u) {
-            entry_token[u] = -1, entry_value[u] = 0;
-            if (tid + u * kLogitThreads >= c.J) continue;
-            const int64_t at = b * c.J + tid + u * kLogitThreads;
-            entry_token[u] = (int32_t)ld_dep_u32(MXQ_AT(c.bias_tokens + at, 4, c.bias_tokens, c.B * c.J * 4));
-            entry_value[u] = (int32_t)ld_dep_u32(MXQ_AT(c.bias_values + at, 4, c.bias_values, c.B * c.J * 4));
+            if (tid + u * kLogitThreads >= c.J) break;
+            entry[u] = (int32_t)ld_dep_u32(MXQ_AT(c.bias_tokens + b * c.J + tid + u * kLogitThreads, 4, c.bias_tokens, c.B * c.J * 4));
         }
         int32_t proposal = -1;
         if (tid < c.T) proposal = (int32_t)ld_dep_u32(MXQ_AT(c.draft + b * c.T + tid, 4, c.draft, c.B * c.T * 4));
@@ -286,54 +286,19 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
                     if (place >= 0) mark(tab.proposed, place);
                 }
         }
-        bool entries = false;
-        if (c.J > 0) {       // of a token's entries the last one stays
-#pragma unroll 1
-            for (int u = 0; u < 2 * kEntries; ++u) {
-                const int place = place_of(entry_token[0], u & 1);
-                if (place >= 0) {
-                    entries = true;
-                    mark(tab.biased, place);
-                    atomicMax(&tab.bias[place], tid + (u >> 1) * kLogitThreads + 1);
-                }
-                if (u & 1) {                                 // (the entries take their turn in place 0)
-                    const int32_t t = entry_token[0];
 #pragma unroll
-                    for (int i = 0; i + 1 < kEntries; ++i) entry_token[i] = entry_token[i + 1];
-                    entry_token[kEntries - 1] = t;
-                }
+        for (int u = 0; u < kEntries; ++u) {
+            if (tid + u * kLogitThreads >= c.J) break;
+            const int v = entry[u];
+            entry[u] = place_of(v, 0), second[u] = place_of(v, 1);
+            for (int which = 0; which < 2; ++which) {        // of a token's entries the last one stays
+                const int place = which ? second[u] : entry[u];
+                if (place < 0) continue;
+                mark(tab.biased, place);
+                atomicMax(&tab.bias[place], tid + u * kLogitThreads + 1);
             }
         }
-        if (__syncthreads_or(entries)) {
-            uint32_t wins = 0;
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                const int p0 = place_of(entry_token[u], 0), p1 = place_of(entry_token[u], 1), at = p0 >= 0 ? p0 : p1;
-                if (at >= 0 && tab.bias[at] == tid + u * kLogitThreads + 1) wins |= 1u << u;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                if (!(wins >> u & 1)) continue;
-                const int p0 = place_of(entry_token[u], 0), p1 = place_of(entry_token[u], 1);
-                if (p0 >= 0) tab.bias[p0] = entry_value[u];
-                if (p1 >= 0) tab.bias[p1] = entry_value[u];
-            }
-        }
-        // the list of the special tokens, in any order
-        for (int w0 = 32 * warp; w0 < SliceTables::words(places); w0 += kLogitThreads) {
-            uint32_t left = w0 + lane < SliceTables::words(places) ? tab.special[w0 + lane] : 0;
-            int before = __popc(left);
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int n = __shfl_up_sync(0xffffffffu, before, o);
-                if (lane >= o) before += n;
-            }
-            int at = 0;
-            if (lane == 31 && before != 0) at = atomicAdd(&sh.listed, before);
-            at = __shfl_sync(0xffffffffu, at, 31) + before - __popc(left);
-            for (; left; left &= left - 1) tab.list[at++] = (uint16_t)(32 * (w0 + lane) + __ffs(left) - 1);
-        }
+        __syncthreads();
     }
 
     // the stream; accept keeps the best vector of this lane's in the row
@@ -412,9 +377,39 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
         }
         cur = ahead;
     }
-    __syncthreads();         // (the list is there; the stream's stores come before those of the special tokens)
-
     if (tabled) {
+        // the list of the special tokens, in any order
+        for (int w0 = 32 * warp; w0 < SliceTables::words(places); w0 += kLogitThreads) {
+            uint32_t left = w0 + lane < SliceTables::words(places) ? tab.special[w0 + lane] : 0;
+            int before = __popc(left);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int n = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += n;
+            }
+            int at = 0;
+            if (lane == 31 && before != 0) at = atomicAdd(&sh.listed, before);
+            at = __shfl_sync(0xffffffffu, at, 31) + before - __popc(left);
+            for (; left; left &= left - 1) tab.list[at++] = (uint16_t)(32 * (w0 + lane) + __ffs(left) - 1);
+        }
+        // the biases' values in the places of their last entries
+        uint32_t wins = 0;
+#pragma unroll
+        for (int u = 0; u < kEntries; ++u) {
+            const int place = max(entry[u], second[u]);
+            if (place >= 0 && tab.bias[place] == tid + u * kLogitThreads + 1) wins |= 1u << u;
+        }
+        if (__syncthreads_or(wins != 0)) {       // (the list is there; the stream's stores come before those of the special tokens)
+#pragma unroll
+            for (int u = 0; u < kEntries; ++u) {
+                if (!(wins >> u & 1)) continue;
+                const int32_t value = (int32_t)ld_dep_u32(MXQ_AT(c.bias_values + b * c.J + tid + u * kLogitThreads, 4, c.bias_values, c.B * c.J * 4));
+                if (entry[u] >= 0) tab.bias[entry[u]] = value;
+                if (second[u] >= 0) tab.bias[second[u]] = value;
+            }
+            __syncthreads();
+        }
+
         const int listed = sh.listed, pairs = listed * (r1 - r0);
         const float repetition = sh.penalties[0], presence = sh.penalties[1], frequency = sh.penalties[2];
         for (int u0 = tid; u0 < pairs; u0 += kPairs * kLogitThreads) {
