@@ -36,6 +36,7 @@ struct LoraCall {
     int32_t parts;           // BF16 parts of T
     int32_t stages;          // shrink: steps of a warp's ring
     int32_t tiles;           // many rows: tiles of 16 rows per CTA of the expansion
+    int32_t direct;          // many rows, K not split: the shrink writes the fragments itself
 };
 
 struct Window {
@@ -98,6 +99,25 @@ __device__ __forceinline__ void wait_oldest(int stages) {        // of `stages` 
     else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
     else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+// Four ranks 4 q .. 4 q + 3 of a step of a row's T as BF16 parts in the order of the product's first operand, [steps][parts][32 lanes] of a 16-row tile.
+__device__ __forceinline__ void put_parts(uint4 *tile_step, int row, int quarter, float (&v)[4], int parts) {
+    // ranks 4 q + 2 e + {0, 1} of the step, row `row` of the tile: register 2 e + (row >> 3) of lane 4 (row & 7) + q
+    uint32_t *dst = reinterpret_cast<uint32_t *>(tile_step + 4 * (row & 7) + quarter) + (row >> 3);
+    for (int u = 0; u < parts; ++u) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const __nv_bfloat162 part = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+            dst[u * 128 + 2 * e] = *reinterpret_cast<const uint32_t *>(&part);
+            const float2 f = __bfloat1622float2(part);       // (an infinite part leaves nothing)
+            v[2 * e] = isfinite(f.x) ? v[2 * e] - f.x : 0.f, v[2 * e + 1] = isfinite(f.y) ? v[2 * e + 1] - f.y : 0.f;
+        }
+    }
+}
+__device__ __forceinline__ uint4 *fragment(const LoraCall &c, int tile, int step) {
+    const int steps = (c.r + 15) / 16;
+    return MXQ_AT(c.frag + ((int64_t)tile * steps + step) * c.parts * 32, c.parts * 512, c.frag, (size_t)((c.M + 15) / 16) * steps * c.parts * 512);
 }
 
 template <int MW, int WARPS, int RT>
@@ -186,16 +206,24 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
                 *reinterpret_cast<float2 *>(p + 8 * c.r) = make_float2(acc[w][n][2], acc[w][n][3]);
             }
         __syncthreads();
-        for (int i = threadIdx.x; i < kRows * ranks * 2; i += 32 * WARPS) {
-            const int row = i / (ranks * 2), rank = 4 * (i - row * ranks * 2);
+        const int quarters = (c.r + 15) / 16 * 4;     // (a last step of eight ranks is filled with zeros)
+        for (int i = threadIdx.x; i < kRows * quarters; i += 32 * WARPS) {
+            const int row = i / quarters, rank = 4 * (i - row * quarters);
             if (win.owner[row] != adapter) continue;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int u = 0; u < WARPS; ++u) {
+                if (rank >= c.r) break;
                 const float4 p = *reinterpret_cast<const float4 *>(part + (u * kRows + row) * c.r + rank);
                 sum.x += p.x, sum.y += p.y, sum.z += p.z, sum.w += p.w;
             }
-            *reinterpret_cast<float4 *>(MXQ_AT(c.t + ((int64_t)blockIdx.z * c.M + row0 + row) * c.r + rank, 16, c.t, t_bytes)) = sum;
+            if (c.direct) {                      // the whole sum: straight into the fragments
+                const float scale = c.scale ? __ldg(MXQ_AT(c.scale + adapter, 4, c.scale, (size_t)c.L * 4)) : 1.f;
+                float v[4] = {sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale};
+                put_parts(fragment(c, (row0 + row) / 16, rank / 16), (row0 + row) % 16, rank % 16 / 4, v, c.parts);
+            } else if (rank < c.r) {
+                *reinterpret_cast<float4 *>(MXQ_AT(c.t + ((int64_t)blockIdx.z * c.M + row0 + row) * c.r + rank, 16, c.t, t_bytes)) = sum;
+            }
         }
         __syncthreads();
     }
@@ -249,19 +277,6 @@ __device__ __forceinline__ uint2 load_b(const LoraCall &c, int adapter, int64_t 
     return __ldg(reinterpret_cast<const uint2 *>(MXQ_AT(c.b + ((int64_t)adapter * c.N + col) * c.r + 16 * s + 4 * t, 8, c.b, (size_t)c.L * c.N * c.r * 2)));
 }
 
-__device__ __forceinline__ void put_parts(uint4 *tile_step, int row, int quarter, float (&v)[4], int parts) {
-    // ranks 4 q + 2 e + {0, 1} of the step, row `row` of the tile: register 2 e + (row >> 3) of lane 4 (row & 7) + q
-    uint32_t *dst = reinterpret_cast<uint32_t *>(tile_step + 4 * (row & 7) + quarter) + (row >> 3);
-    for (int u = 0; u < parts; ++u) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const __nv_bfloat162 part = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-            dst[u * 128 + 2 * e] = *reinterpret_cast<const uint32_t *>(&part);
-            const float2 f = __bfloat1622float2(part);       // (an infinite part leaves nothing)
-            v[2 * e] = isfinite(f.x) ? v[2 * e] - f.x : 0.f, v[2 * e + 1] = isfinite(f.y) ? v[2 * e + 1] - f.y : 0.f;
-        }
-    }
-}
 // the four ranks' sum over the splits, times the adapter's scale
 __device__ __forceinline__ void sum_splits(float (&v)[4], const LoraCall &c, int m, int rank, int adapter) {
     const size_t t_bytes = (size_t)c.splits * c.M * c.r * 4;
@@ -386,8 +401,7 @@ __global__ void __launch_bounds__(256) lora_fragments_kernel(LoraCall c) {
     const int adapter = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (adapter >= 0 && adapter < c.L && 4 * quarter < c.r) sum_splits(v, c, m, 4 * quarter, adapter);
-    put_parts(MXQ_AT(c.frag + ((int64_t)(m / 16) * (quarters / 4) + quarter / 4) * c.parts * 32, c.parts * 512, c.frag, (size_t)tiles * (quarters / 4) * c.parts * 512),
-              m % 16, quarter % 4, v, c.parts);
+    put_parts(fragment(c, m / 16, quarter / 4), m % 16, quarter % 4, v, c.parts);
 }
 
 // grid (blocks of 256 columns, blocks of c.tiles tiles of rows); a warp takes 32 columns, whose B stays in registers while the adapter does, and
@@ -533,11 +547,15 @@ static int lora_check(const void *X, int64_t M, const mxq_lora_adapters *ad, con
     return MXQ_OK;
 }
 
-static LoraCall lora_call(const void *X, int64_t M, const mxq_lora_adapters *ad, const int32_t *ids, int64_t N, int64_t K, void *workspace) {
+static LoraCall lora_call(const void *X, int64_t M, const mxq_lora_adapters *ad, const int32_t *ids, int64_t N, int64_t K, const void *base, int base_dtype,
+                          void *Y, int y_dtype, void *workspace) {
     LoraCall c = {};
     c.x = (const uint16_t *)X, c.a = (const uint16_t *)ad->A_bf16, c.b = (const uint16_t *)ad->B_bf16, c.scale = ad->scale, c.ids = ids;
     c.t = (float *)workspace, c.N = N, c.K = K, c.M = (int32_t)M, c.r = ad->rank, c.L = ad->count;
+    c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
     lora_plan(c);
+    c.direct = many_rows(M) && c.splits == 1;
+    c.frag = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c));
     return c;
 }
 
@@ -548,7 +566,7 @@ static bool allow_smem(void (*kernel)(LoraCall), size_t smem) {
     return false;
 }
 
-template <int MW, int WARPS>
+template <int MW, int WARPS, int RT>
 static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
     constexpr int kRows = 16 * MW;
     const dim3 grid((unsigned)((c.M + kRows - 1) / kRows), (unsigned)c.slots, (unsigned)c.splits);
@@ -557,9 +575,12 @@ static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
     LoraCall call = c;
     call.stages = max(1, min(min(kMostStages, steps), (int)(200 * 1024 / stage)));
     const size_t smem = max(stage * call.stages, parts);
-    void (*const kernel)(LoraCall) = c.r <= 16 ? lora_shrink_kernel<MW, WARPS, 2> : c.r <= 32 ? lora_shrink_kernel<MW, WARPS, 4> : c.r <= 64 ? lora_shrink_kernel<MW, WARPS, 8> : lora_shrink_kernel<MW, WARPS, 16>;
-    if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
-    return launch_pdl(kernel, grid, 32 * WARPS, smem, stream, call);
+    if (!allow_smem(lora_shrink_kernel<MW, WARPS, RT>, smem)) return MXQ_ERR_CUDA;
+    return launch_pdl(lora_shrink_kernel<MW, WARPS, RT>, grid, 32 * WARPS, smem, stream, call);
+}
+template <int MW, int WARPS>
+static int shrink_by_rank(const LoraCall &c, cudaStream_t stream) {
+    return c.r <= 16 ? shrink_launch<MW, WARPS, 2>(c, stream) : c.r <= 32 ? shrink_launch<MW, WARPS, 4>(c, stream) : shrink_launch<MW, WARPS, 8>(c, stream);
 }
 
 static int expand_launch(const LoraCall &c, cudaStream_t stream) {
@@ -580,8 +601,10 @@ static void (*many_kernel(int r, bool f32, bool vec))(LoraCall) {
 
 static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     const int steps = (c.r + 15) / 16, tiles = (c.M + 15) / 16;
-    int rc = launch_pdl(lora_fragments_kernel, dim3((unsigned)(((int64_t)tiles * 16 * steps * 4 + 255) / 256)), 256, 0, stream, c);
-    if (rc != MXQ_OK) return rc;
+    if (!c.direct) {
+        const int rc = launch_pdl(lora_fragments_kernel, dim3((unsigned)(((int64_t)tiles * 16 * steps * 4 + 255) / 256)), 256, 0, stream, c);
+        if (rc != MXQ_OK) return rc;
+    }
     c.tiles = 8;
     const dim3 grid((unsigned)((c.N + 255) / 256), (unsigned)((tiles + c.tiles - 1) / c.tiles));
     const size_t smem = (size_t)c.tiles * steps * c.parts * 512;
@@ -590,12 +613,11 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     return launch_pdl(kernel, grid, 256, smem, stream, c);
 }
 
-static int lora_shrink(const LoraCall &c, cudaStream_t stream) { 
-    return !many_rows(c.M) ? shrink_launch<1, kFewWarps>(c, stream) : c.r <= 64 ? shrink_launch<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps>(c, stream);
+static int lora_shrink(const LoraCall &c, cudaStream_t stream) {
+    if (many_rows(c.M)) return c.r <= 64 ? shrink_by_rank<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps, 16>(c, stream);
+    return c.r <= 64 ? shrink_by_rank<1, kFewWarps>(c, stream) : shrink_launch<1, kFewWarps, 16>(c, stream);
 }
-static int lora_expand(LoraCall &c, const void *base, int base_dtype, void *Y, int y_dtype, cudaStream_t stream) {
-    c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
-    c.frag = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c));
+static int lora_expand(const LoraCall &c, cudaStream_t stream) {
     return many_rows(c.M) ? expand_many_launch(c, stream) : expand_launch(c, stream);
 }
 
@@ -619,9 +641,9 @@ int mxq_lora(const void *X_bf16, int64_t M, const mxq_lora_adapters *adapters, c
     if (rc != MXQ_OK) return rc;
     if (!mxq::aligned16(base) || !mxq::aligned16(workspace)) return MXQ_ERR_ALIGN;
     if (!workspace || workspace_bytes < mxq_lora_workspace_bytes(M, N, K, adapters->rank, adapters->count)) return MXQ_ERR_WORKSPACE;
-    mxq::LoraCall c = mxq::lora_call(X_bf16, M, adapters, ids, N, K, workspace);
+    const mxq::LoraCall c = mxq::lora_call(X_bf16, M, adapters, ids, N, K, base, y_dtype, Y, y_dtype, workspace);
     rc = mxq::lora_shrink(c, (cudaStream_t)stream);
-    return rc != MXQ_OK ? rc : mxq::lora_expand(c, base, y_dtype, Y, y_dtype, (cudaStream_t)stream);
+    return rc != MXQ_OK ? rc : mxq::lora_expand(c, (cudaStream_t)stream);
 }
 
 // workspace: [T][FP32 sums of the shared layer, for a BF16 Y][mxq_linear's own]
@@ -643,12 +665,12 @@ int mxq_linear_lora(const void *X_bf16, int M, const uint8_t *codes, const uint8
     const size_t t_bytes = mxq::align256(mxq_lora_workspace_bytes(M, N, K, adapters->rank, adapters->count)), sums = mxq::align256((size_t)M * (size_t)N * 4u);
     float *base = y_dtype == MXQ_F32 ? static_cast<float *>(Y) : reinterpret_cast<float *>(ws + t_bytes);
     // T first: the layer's weight stream starts while it is computed, and B is on its way while the layer ends
-    mxq::LoraCall c = mxq::lora_call(X_bf16, M, adapters, ids, N, K, workspace);
+    const mxq::LoraCall c = mxq::lora_call(X_bf16, M, adapters, ids, N, K, base, MXQ_F32, Y, y_dtype, workspace);
     rc = mxq::lora_shrink(c, (cudaStream_t)stream);
     if (rc != MXQ_OK) return rc;
     rc = mxq_linear(X_bf16, M, codes, scales, N, K, base, MXQ_F32, ws + t_bytes + sums, mxq::align256(mxq_linear_workspace_bytes(M, N, K)), stream);
     if (rc != MXQ_OK) return rc;
-    return mxq::lora_expand(c, base, MXQ_F32, Y, y_dtype, (cudaStream_t)stream);
+    return mxq::lora_expand(c, (cudaStream_t)stream);
 }
 
 #pragma GCC visibility pop
