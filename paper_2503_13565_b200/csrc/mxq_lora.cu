@@ -123,15 +123,16 @@ __device__ __forceinline__ uint4 *fragment(const LoraCall &c, int tile, int step
 template <int MW, int WARPS, int RT>
 __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
     constexpr int kRows = 16 * MW;
-    extern __shared__ uint4 ring[];     // [warps][stages][ranks / 8 + 2 * MW][32 lanes]; then the warps' parts of T, [warps][kRows][r] floats
+    extern __shared__ uint4 ring[];     // [warps][stages][RT + 2 * MW][32 lanes]; then the warps' parts of T, [warps][kRows][r] floats
     __shared__ Window win;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int row0 = blockIdx.x * kRows;          // this lane's rows: row0 + g + 8 * j, j < 2 * MW
     const int64_t k0 = (int64_t)blockIdx.z * c.split_k + 32 * warp, k1 = min(c.K, (int64_t)(blockIdx.z + 1) * c.split_k);
-    const int ranks = c.r / 8, pieces = ranks + 2 * MW, steps = k0 < k1 ? (int)((k1 - k0 + 32 * WARPS - 1) / (32 * WARPS)) : 0;
+    constexpr int kPieces = RT + 2 * MW;          // (tiles of ranks that are not there are zeros)
+    const int ranks = c.r / 8, steps = k0 < k1 ? (int)((k1 - k0 + 32 * WARPS - 1) / (32 * WARPS)) : 0;
     const int64_t stride = 16 * c.K;              // bytes from a row to the eighth after it
-    uint4 *mine = ring + warp * c.stages * pieces * 32 + lane;
+    uint4 *mine = ring + warp * c.stages * kPieces * 32 + lane;
     const uint32_t mine_address = shared_address(mine);
     const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2, t_bytes = (size_t)c.splits * c.M * c.r * 4;
     load_window(win, c, row0, kRows);
@@ -146,15 +147,15 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
         const uint8_t *wa = reinterpret_cast<const uint8_t *>(c.a + ((int64_t)adapter * c.r + g) * c.K + k0 + 8 * t);
         const uint8_t *xa = reinterpret_cast<const uint8_t *>(c.x + (int64_t)(row0 + g) * c.K + k0 + 8 * t);
         auto copy_a = [&](int slot) {
-            const uint32_t to = mine_address + slot * pieces * 512;
+            const uint32_t to = mine_address + slot * (kPieces * 512);
             const uint8_t *from = wa;
 #pragma unroll
             for (int n = 0; n < RT; ++n, from += stride)
-                if (n < ranks) copy16(to + n * 512, MXQ_AT(from, 16, c.a, a_bytes), true);
+                copy16(to + n * 512, n < ranks ? MXQ_AT(from, 16, c.a, a_bytes) : reinterpret_cast<const uint8_t *>(c.a), n < ranks);
             wa += 64 * WARPS;
         };
         auto copy_x = [&](int slot) {
-            const uint32_t to = mine_address + (slot * pieces + ranks) * 512;
+            const uint32_t to = mine_address + slot * (kPieces * 512) + RT * 512;
             const uint8_t *from = xa;
 #pragma unroll
             for (int j = 0; j < 2 * MW; ++j, from += stride) copy16(to + j * 512, own[j] ? MXQ_AT(from, 16, c.x, x_bytes) : reinterpret_cast<const uint8_t *>(c.x), own[j]);
@@ -174,13 +175,12 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
             for (int n = 0; n < RT; ++n) acc[w][n][0] = acc[w][n][1] = acc[w][n][2] = acc[w][n][3] = 0.f;
         for (int step = 0, slot = 0; step < steps; ++step) {
             wait_oldest(c.stages);
-            const uint4 *from = mine + slot * pieces * 32;
+            const uint4 *from = mine + slot * (kPieces * 32);
             uint4 x[2 * MW];
 #pragma unroll
-            for (int j = 0; j < 2 * MW; ++j) x[j] = from[(ranks + j) * 32];
+            for (int j = 0; j < 2 * MW; ++j) x[j] = from[(RT + j) * 32];
 #pragma unroll
             for (int n = 0; n < RT; ++n) {
-                if (n >= ranks) break;
                 const uint4 v = from[n * 32];
 #pragma unroll
                 for (int w = 0; w < MW; ++w) {
@@ -570,7 +570,7 @@ template <int MW, int WARPS, int RT>
 static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
     constexpr int kRows = 16 * MW;
     const dim3 grid((unsigned)((c.M + kRows - 1) / kRows), (unsigned)c.slots, (unsigned)c.splits);
-    const size_t stage = (size_t)WARPS * (c.r / 8 + 2 * MW) * 512, parts = (size_t)WARPS * kRows * c.r * 4;
+    const size_t stage = (size_t)WARPS * (RT + 2 * MW) * 512, parts = (size_t)WARPS * kRows * c.r * 4;
     const int steps = (c.split_k + 32 * WARPS - 1) / (32 * WARPS);
     LoraCall call = c;
     call.stages = max(1, min(min(kMostStages, steps), (int)(200 * 1024 / stage)));
