@@ -10,14 +10,14 @@
 // through shared memory first.)  T is FP32 and meets B as a sum of BF16 parts: three for an FP32 Y (all 24 bits), two for a BF16 Y (16 bits: what
 // is lost is 2^-17 of each product, against the 2^-8 of Y's own rounding).
 //
-// A CTA takes a window of 16 or 64 token rows and goes through the adapters that its rows have, one after the other: rows that have
-// another one are left out (zero in the product, not stored).  For up to 16 rows a CTA takes one adapter only (`slots`).
+// A CTA takes a window of token rows and one adapter, or several one after the other: rows that have another one are left out (zero in the
+// product, not stored).
 #include "mxq_device.cuh"
 #include "mxq_host.h"
 
 namespace mxq {
 
-constexpr int kWindowMost = 64;
+constexpr int kWindowMost = 32;
 
 struct LoraCall {
     const uint16_t *x;       // [M][K]
@@ -37,45 +37,101 @@ struct LoraCall {
     int32_t stages;          // shrink: steps of a warp's ring
     int32_t tiles;           // many rows: tiles of 16 rows per CTA of the expansion
     int32_t direct;          // many rows, K not split: the shrink writes the fragments itself
+    int32_t *plan;           // 17 to 511 rows: the segments (see lora_order_kernel), else nullptr
 };
 
 struct Window {
     int32_t owner[kWindowMost];   // adapter of every row, -1: none
+    int32_t row[kWindowMost];     // the rows; -1: none
     int32_t list[kWindowMost];    // its distinct adapters in order of their first row
     int32_t count;
 };
+
+// 17 to 511 rows, the batches of a server: rows sorted by adapter and cut into segments of up to 16 rows of one adapter, so that every
+// adapter is read about once whatever the rows' order.  plan: [0 ..] first place of segment s and, behind the last, M; [kPlanAdapter ..] its
+// adapter, -1: none; [kPlanOrder ..] row at every place; [kPlanCount] segments.
+constexpr int kMostSorted = 512, kPlanAdapter = 1024, kPlanOrder = 2048, kPlanCount = 2560, kPlanBytes = 2561 * 4;
+__global__ void __launch_bounds__(kMostSorted) lora_order_kernel(LoraCall c) {
+    __shared__ uint32_t key[kMostSorted];
+    __shared__ int32_t last[kMostSorted / 32], heads[kMostSorted / 32];
+    const int i = threadIdx.x, warp = i >> 5, lane = i & 31;
+    pdl_wait();              // (and no early trigger: the kernels that follow read the plan ahead of their own waits)
+    uint32_t mine = 0xFFFFFFFFu;
+    if (i < c.M) {
+        const int a = (int)ld_dep_u32(MXQ_AT(c.ids + i, 4, c.ids, (size_t)c.M * 4));
+        mine = (a >= 0 && a < c.L ? (uint32_t)a : (uint32_t)MXQ_LORA_MAX_ADAPTERS) << 9 | i;
+    }
+    for (int size = 2; size <= kMostSorted; size <<= 1) {            // bitonic, over lanes where the partner is in the warp
+        for (int step = size >> 1; step > 0; step >>= 1) {
+            uint32_t other;
+            if (step < 32) {
+                other = __shfl_xor_sync(0xffffffffu, mine, step);
+            } else {
+                __syncthreads();
+                key[i] = mine;
+                __syncthreads();
+                other = key[i ^ step];
+            }
+            mine = ((i & step) == 0) == ((i & size) == 0) ? min(mine, other) : max(mine, other);
+        }
+    }
+    __syncthreads();
+    key[i] = mine;
+    __syncthreads();
+    const bool head = i == 0 || (key[i - 1] >> 9) != (mine >> 9);
+    int start = head ? i : 0;                                        // first place of the adapter's rows: the largest head so far
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int n = __shfl_up_sync(0xffffffffu, start, o);
+        if (lane >= o) start = max(start, n);
+    }
+    if (lane == 31) last[warp] = start;
+    __syncthreads();
+    for (int u = 0; u < warp; ++u) start = max(start, last[u]);
+    const bool cut = i < c.M && (i - start) % 16 == 0;
+    const uint32_t cuts = __ballot_sync(0xffffffffu, cut);
+    if (lane == 0) heads[warp] = __popc(cuts);
+    __syncthreads();
+    int before = __popc(cuts & ((1u << lane) - 1)), all = 0;
+    for (int u = 0; u < kMostSorted / 32; ++u) {
+        if (u < warp) before += heads[u];
+        all += heads[u];
+    }
+    auto at = [&](int place) { return MXQ_AT(c.plan + place, 4, c.plan, kPlanBytes); };
+    if (cut) *at(before) = i, *at(kPlanAdapter + before) = (mine >> 9) == MXQ_LORA_MAX_ADAPTERS ? -1 : (int32_t)(mine >> 9);
+    if (i < c.M) *at(kPlanOrder + i) = (int32_t)(mine & (kMostSorted - 1));
+    if (i == 0) *at(all) = c.M, *at(kPlanCount) = all;
+}
+// segment s as a window of one adapter
+__device__ __forceinline__ void load_segment(int32_t (&owner)[kWindowMost], int32_t (&row)[kWindowMost], int32_t &adapter, const LoraCall &c, int s) {
+    auto at = [&](int place) { return (int)ld_dep_u32(MXQ_AT(c.plan + place, 4, c.plan, kPlanBytes)); };
+    const bool there = s < at(kPlanCount);
+    const int first = there ? at(s) : 0, rows = there ? at(s + 1) - first : 0, lane = threadIdx.x;
+    adapter = there ? at(kPlanAdapter + s) : -1;
+    owner[lane] = lane < rows ? adapter : -1;
+    row[lane] = lane < rows ? at(kPlanOrder + first + lane) : -1;
+}
 
 // filled by warp 0; the caller synchronises.  ids are read ahead of the wait for the previous kernel (they are the caller's, like the
 // weights).
 __device__ __forceinline__ void load_window(Window &w, const LoraCall &c, int row0, int rows) {
     if (threadIdx.x >= 32) return;
     const int lane = threadIdx.x;
-    int o[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = 32 * h + lane;
-        o[h] = -1;
-        if (i < rows && row0 + i < c.M) o[h] = __ldg(MXQ_AT(c.ids + row0 + i, 4, c.ids, (size_t)c.M * 4));
-        if (o[h] < 0 || o[h] >= c.L) o[h] = -1;
-        w.owner[i] = o[h];
+    if (c.plan) {            // (windows are segments then)
+        int adapter;
+        load_segment(w.owner, w.row, adapter, c, row0 / rows);
+        if (lane == 0) w.list[0] = adapter, w.count = adapter >= 0 ? 1 : 0;
+        return;
     }
-    unsigned first = __ballot_sync(0xffffffffu, (__ffs(__match_any_sync(0xffffffffu, o[0])) - 1 == lane) && o[0] >= 0);
-    int n = 0;
-    bool known = false;
-    for (unsigned left = first; left; left &= left - 1) {
-        const int a = __shfl_sync(0xffffffffu, o[0], __ffs(left) - 1);
-        known |= o[1] == a;
-        if (lane == 0) w.list[n] = a;
-        ++n;
-    }
-    const unsigned same = __match_any_sync(0xffffffffu, o[1]);
-    first = __ballot_sync(0xffffffffu, __ffs(same) - 1 == lane && o[1] >= 0 && !known);
-    for (unsigned left = first; left; left &= left - 1) {
-        const int a = __shfl_sync(0xffffffffu, o[1], __ffs(left) - 1);
-        if (lane == 0) w.list[n] = a;
-        ++n;
-    }
-    if (lane == 0) w.count = n;
+    int a = -1;
+    if (lane < rows && row0 + lane < c.M) a = __ldg(MXQ_AT(c.ids + row0 + lane, 4, c.ids, (size_t)c.M * 4));
+    if (a >= c.L) a = -1;
+    w.owner[lane] = max(a, -1);
+    w.row[lane] = lane < rows && row0 + lane < c.M ? row0 + lane : -1;
+    const bool first = __ffs(__match_any_sync(0xffffffffu, a)) - 1 == lane && a >= 0;
+    const unsigned firsts = __ballot_sync(0xffffffffu, first);
+    if (first) w.list[__popc(firsts & ((1u << lane) - 1))] = a;
+    if (lane == 0) w.count = __popc(firsts);
 }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -127,7 +183,6 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
     __shared__ Window win;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.x * kRows;          // this lane's rows: row0 + g + 8 * j, j < 2 * MW
     const int64_t k0 = (int64_t)blockIdx.z * c.split_k + 32 * warp, k1 = min(c.K, (int64_t)(blockIdx.z + 1) * c.split_k);
     constexpr int kPieces = RT + 2 * MW;          // (tiles of ranks that are not there are zeros)
     const int ranks = c.r / 8, steps = k0 < k1 ? (int)((k1 - k0 + 32 * WARPS - 1) / (32 * WARPS)) : 0;
@@ -135,7 +190,7 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
     uint4 *mine = ring + warp * c.stages * kPieces * 32 + lane;
     const uint32_t mine_address = shared_address(mine);
     const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2, t_bytes = (size_t)c.splits * c.M * c.r * 4;
-    load_window(win, c, row0, kRows);
+    load_window(win, c, blockIdx.x * kRows, kRows);      // this lane's rows: places g + 8 * j, j < 2 * MW
     __syncthreads();
     bool waited = false;
     for (int at = blockIdx.y; at < win.count; at += c.slots) {
@@ -145,7 +200,9 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
         for (int j = 0; j < 2 * MW; ++j) own[j] = win.owner[g + 8 * j] == adapter;
         // byte addresses of this lane's pieces of the next step to be copied; a row that is not there is not read (its address is the array's own)
         const uint8_t *wa = reinterpret_cast<const uint8_t *>(c.a + ((int64_t)adapter * c.r + g) * c.K + k0 + 8 * t);
-        const uint8_t *xa = reinterpret_cast<const uint8_t *>(c.x + (int64_t)(row0 + g) * c.K + k0 + 8 * t);
+        const uint8_t *xa[2 * MW];
+#pragma unroll
+        for (int j = 0; j < 2 * MW; ++j) xa[j] = reinterpret_cast<const uint8_t *>(c.x + (own[j] ? (int64_t)win.row[g + 8 * j] * c.K + k0 + 8 * t : 0));
         auto copy_a = [&](int slot) {
             const uint32_t to = mine_address + slot * (kPieces * 512);
             const uint8_t *from = wa;
@@ -156,10 +213,11 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
         };
         auto copy_x = [&](int slot) {
             const uint32_t to = mine_address + slot * (kPieces * 512) + RT * 512;
-            const uint8_t *from = xa;
 #pragma unroll
-            for (int j = 0; j < 2 * MW; ++j, from += stride) copy16(to + j * 512, own[j] ? MXQ_AT(from, 16, c.x, x_bytes) : reinterpret_cast<const uint8_t *>(c.x), own[j]);
-            xa += 64 * WARPS;
+            for (int j = 0; j < 2 * MW; ++j) {
+                copy16(to + j * 512, own[j] ? MXQ_AT(xa[j], 16, c.x, x_bytes) : xa[j], own[j]);
+                if (own[j]) xa[j] += 64 * WARPS;
+            }
         };
         // (the adapters' first steps are on their way before the previous kernel has ended)
         for (int u = 0; u < c.stages && u < steps; ++u) copy_a(u);
@@ -220,9 +278,9 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
             if (c.direct) {                      // the whole sum: straight into the fragments
                 const float scale = c.scale ? __ldg(MXQ_AT(c.scale + adapter, 4, c.scale, (size_t)c.L * 4)) : 1.f;
                 float v[4] = {sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale};
-                put_parts(fragment(c, (row0 + row) / 16, rank / 16), (row0 + row) % 16, rank % 16 / 4, v, c.parts);
+                put_parts(fragment(c, win.row[row] / 16, rank / 16), win.row[row] % 16, rank % 16 / 4, v, c.parts);
             } else if (rank < c.r) {
-                *reinterpret_cast<float4 *>(MXQ_AT(c.t + ((int64_t)blockIdx.z * c.M + row0 + row) * c.r + rank, 16, c.t, t_bytes)) = sum;
+                *reinterpret_cast<float4 *>(MXQ_AT(c.t + ((int64_t)blockIdx.z * c.M + win.row[row]) * c.r + rank, 16, c.t, t_bytes)) = sum;
             }
         }
         __syncthreads();
@@ -323,9 +381,9 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
     __shared__ Window win;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.z * 16, steps = (c.r + 15) / 16;
+    const int steps = (c.r + 15) / 16;
     const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32, col = col0 + 8 * t, n = (int64_t)c.M * c.N;
-    load_window(win, c, row0, 16);
+    load_window(win, c, blockIdx.z * 16, 16);
     __syncthreads();
     const int adapter = (int)blockIdx.y < win.count ? win.list[blockIdx.y] : -2;
     uint2 w[KT][4];                      // this warp's columns of B wait here for T
@@ -339,22 +397,25 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
     // the rows that this CTA stores: its adapter's; the first slot also copies those without one, unless they are there already
     const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
     bool own[2], mine[2];
+    int64_t place[2];                    // of the columns in base and Y
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+        const int row = win.row[8 * h + g];
         own[h] = win.owner[8 * h + g] == adapter;
-        mine[h] = there > 0 && (own[h] || (blockIdx.y == 0 && c.base != c.y && win.owner[8 * h + g] < 0 && row0 + 8 * h + g < c.M));
+        mine[h] = there > 0 && row >= 0 && (own[h] || (blockIdx.y == 0 && c.base != c.y && win.owner[8 * h + g] < 0));
+        place[h] = (int64_t)row * c.N + col;
     }
     pdl_wait();
     const bool vec = c.N % 8 == 0;
     Columns ahead[2];                    // base, on its way while T is made ready
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        if (c.base && vec && mine[h]) ahead[h] = load_ahead(c.base, c.base_f32, (int64_t)(row0 + 8 * h + g) * c.N + col, n);
+        if (c.base && vec && mine[h]) ahead[h] = load_ahead(c.base, c.base_f32, place[h], n);
     if (adapter >= 0) {
         for (int i = threadIdx.x; i < 16 * steps * 4; i += 32 * WARPS) {
             const int quarter = i % (steps * 4), m = i / (steps * 4);       // ranks 4 * quarter .. + 3 of row m
             float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (win.owner[m] == adapter && 4 * quarter < c.r) sum_splits(v, c, row0 + m, 4 * quarter, adapter);
+            if (win.owner[m] == adapter && 4 * quarter < c.r) sum_splits(v, c, win.row[m], 4 * quarter, adapter);
             put_parts(frag + quarter / 4 * c.parts * 32, m, quarter % 4, v, c.parts);
         }
         __syncthreads();
@@ -377,15 +438,14 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (!mine[h]) continue;
-        const int64_t at = (int64_t)(row0 + 8 * h + g) * c.N + col;
         float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (c.base && vec) unpack_columns(f, ahead[h], c.base_f32);
-        else if (c.base) load_columns(f, c.base, c.base_f32, at, there, vec, n);
+        else if (c.base) load_columns(f, c.base, c.base_f32, place[h], there, vec, n);
         if (own[h]) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[2 * i] += acc[i][2 * h], f[2 * i + 1] += acc[i][2 * h + 1];
         }
-        store_columns(f, c.y, c.y_f32, at, there, vec, n);
+        store_columns(f, c.y, c.y_f32, place[h], there, vec, n);
     }
 }
 
@@ -509,21 +569,23 @@ MXQ_BOUNDS_TU(bounds_take_lora)
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 
-// From 512 rows on windows of 32 rows (a window reads its adapters once) and T's fragments made once, by a kernel of their own; below that
-// windows of 16 rows, a CTA per adapter, and every CTA of the expansion makes its own.
-static bool many_rows(int64_t M) { return M >= 512; }
+// Up to 16 rows: one window, a CTA of both kernels for each of its adapters.  Up to 511: sorted into segments (see lora_order_kernel).  More:
+// windows of 32 rows as they come, in a prompt mostly of one adapter, with a second CTA where two meet; T's fragments are made once.
+constexpr int kMostSplits = 16;
 constexpr int kFewWarps = 8, kManyWarps = 16;     // of a CTA of the shrink (above rank 64 sixteen warps' sums do not fit the registers)
+static bool many_rows(int64_t M) { return M >= kMostSorted; }
+static bool few_rows(int64_t M) { return M <= 16; }
+static int64_t most_segments(const LoraCall &c) { return c.M / 16 + min(c.L + 1, c.M); }
 
 static void lora_plan(LoraCall &c) {
-    const bool many = many_rows(c.M);
-    const int64_t windows = many ? (c.M + 31) / 32 : (c.M + 15) / 16;
-    // (many rows: a second CTA for the windows in which one adapter's rows end and another's begin; a prompt of 4095 rows of six adapters: 67 -> 54 us)
-    c.slots = many ? min(2, c.L) : min(16, min(c.M, c.L));
+    const bool few = few_rows(c.M), many = many_rows(c.M);
+    const int64_t sms = sm_count();
+    c.slots = few ? min(c.M, c.L) : many ? min(2, c.L) : 1;
     // splits of K as long as the SMs hold the CTAs at once, but at least one step of 32 per warp
     const int64_t step = 32 * (many && c.r <= 64 ? kManyWarps : kFewWarps), most = (c.K + step - 1) / step;
-    int64_t want = max((int64_t)1, many ? sm_count() / windows : 2 * (int64_t)sm_count() / (windows * c.slots));
+    int64_t want = max((int64_t)1, few ? 2 * sms / c.slots : many ? sms / ((c.M + 31) / 32) : 2 * sms / most_segments(c));
     if (want > most) want = most;
-    if (want > 32) want = 32;
+    if (want > kMostSplits) want = kMostSplits;
     int64_t len = ((c.K + want - 1) / want + step - 1) / step * step;
     c.split_k = (int32_t)len;
     c.splits = (int32_t)((c.K + len - 1) / len);
@@ -555,7 +617,9 @@ static LoraCall lora_call(const void *X, int64_t M, const mxq_lora_adapters *ad,
     c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
     lora_plan(c);
     c.direct = many_rows(M) && c.splits == 1;
-    c.frag = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c));
+    uint8_t *behind = reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c);
+    c.frag = reinterpret_cast<uint4 *>(behind);
+    c.plan = few_rows(M) || many_rows(M) ? nullptr : reinterpret_cast<int32_t *>(behind);
     return c;
 }
 
@@ -569,7 +633,7 @@ static bool allow_smem(void (*kernel)(LoraCall), size_t smem) {
 template <int MW, int WARPS, int RT>
 static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
     constexpr int kRows = 16 * MW;
-    const dim3 grid((unsigned)((c.M + kRows - 1) / kRows), (unsigned)c.slots, (unsigned)c.splits);
+    const dim3 grid((unsigned)(c.plan ? most_segments(c) : (c.M + kRows - 1) / kRows), (unsigned)c.slots, (unsigned)c.splits);
     const size_t stage = (size_t)WARPS * (RT + 2 * MW) * 512, parts = (size_t)WARPS * kRows * c.r * 4;
     const int steps = (c.split_k + 32 * WARPS - 1) / (32 * WARPS);
     LoraCall call = c;
@@ -585,7 +649,7 @@ static int shrink_by_rank(const LoraCall &c, cudaStream_t stream) {
 
 static int expand_launch(const LoraCall &c, cudaStream_t stream) {
     constexpr int kWarps = 4;
-    const dim3 grid((unsigned)((c.N + 32 * kWarps - 1) / (32 * kWarps)), (unsigned)c.slots, (unsigned)((c.M + 15) / 16));
+    const dim3 grid((unsigned)((c.N + 32 * kWarps - 1) / (32 * kWarps)), (unsigned)c.slots, (unsigned)(c.plan ? most_segments(c) : 1));
     const size_t smem = (size_t)((c.r + 15) / 16) * c.parts * 32 * 16;
     return launch_pdl(c.r <= 16 ? lora_expand_kernel<1, kWarps> : c.r <= 32 ? lora_expand_kernel<2, kWarps> : c.r <= 64 ? lora_expand_kernel<4, kWarps> : lora_expand_kernel<8, kWarps>,
                       grid, 32 * kWarps, smem, stream, c);
@@ -615,6 +679,10 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
 
 static int lora_shrink(const LoraCall &c, cudaStream_t stream) {
     if (many_rows(c.M)) return c.r <= 64 ? shrink_by_rank<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps, 16>(c, stream);
+    if (c.plan) {
+        const int rc = launch_pdl(lora_order_kernel, dim3(1), kMostSorted, 0, stream, c);
+        if (rc != MXQ_OK) return rc;
+    }
     return c.r <= 64 ? shrink_by_rank<1, kFewWarps>(c, stream) : shrink_launch<1, kFewWarps, 16>(c, stream);
 }
 static int lora_expand(const LoraCall &c, cudaStream_t stream) {
@@ -631,8 +699,8 @@ size_t mxq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int rank, int a
     mxq::LoraCall c = {};
     c.M = (int32_t)M, c.N = N, c.K = K, c.r = rank, c.L = adapters;
     mxq::lora_plan(c);
-    // [partial sums][fragments: three BF16 parts of 16-row tiles]
-    return mxq::sums_bytes(c) + (mxq::many_rows(M) ? (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512 : 0);
+    // [partial sums][fragments: three BF16 parts of 16-row tiles, or the plan of the segments]
+    return mxq::sums_bytes(c) + (mxq::many_rows(M) ? (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512 : mxq::few_rows(M) ? 0 : (size_t)mxq::kPlanBytes);
 }
 
 int mxq_lora(const void *X_bf16, int64_t M, const mxq_lora_adapters *adapters, const int32_t *ids, int64_t N, int64_t K, const void *base,
