@@ -57,20 +57,30 @@ struct LogitShared {
 // boundaries), so a batch's part of the tables has kVec tokens more than a batch.
 struct SliceTables {
     uint32_t *count;                         // where there are counts
-    int32_t *bias;                           // where there are biases: the last entry of a token, plus 1; then its value's bits
+    uint16_t *bias;                          // where there are biases: the last entry of a token, plus 1
     uint32_t *special, *biased, *proposed;   // bits
     uint16_t *list;                          // places of the special tokens
     __host__ __device__ static int words(int places) { return (places + 31) / 32 + 1; }
     __host__ __device__ static size_t bytes(int places, bool counting, bool biases) {
-        return ((size_t)places * ((counting ? 1 : 0) + (biases ? 1 : 0)) + 3 * words(places)) * 4 + (size_t)places * 2;
+        return (size_t)places * ((counting ? 4 : 0) + (biases ? 2 : 0) + 2) + 3 * words(places) * 4;     // (places is a multiple of 4)
     }
     __device__ SliceTables(uint32_t *at, int places, bool counting, bool biases) {
         count = at, at += counting ? places : 0;
-        bias = reinterpret_cast<int32_t *>(at), at += biases ? places : 0;
+        bias = reinterpret_cast<uint16_t *>(at), at += biases ? places / 2 : 0;
         special = at, biased = special + words(places), proposed = biased + words(places);
         list = reinterpret_cast<uint16_t *>(proposed + words(places));
     }
     __device__ __forceinline__ static uint32_t bits(const uint32_t *w, int place) { return __funnelshift_r(w[place >> 5], w[(place >> 5) + 1], place & 31); }
+    // of a token's entries the last one stays (two places to a word)
+    __device__ __forceinline__ void enter(int place, uint32_t entry) const {
+        uint32_t *word = reinterpret_cast<uint32_t *>(bias) + place / 2, old = *word, seen;
+        const int shift = 16 * (place & 1);
+        do {
+            if ((old >> shift & 0xFFFFu) >= entry) return;
+            seen = old;
+            old = atomicCAS(word, seen, (seen & ~(0xFFFFu << shift)) | entry << shift);
+        } while (old != seen);
+    }
     __device__ __forceinline__ static bool bit(const uint32_t *w, int place) { return w[place >> 5] >> (place & 31) & 1; }
 };
 
@@ -208,7 +218,7 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
     if (tabled) {
         for (int w = tid; w < 3 * SliceTables::words(places); w += kLogitThreads) tab.special[w] = 0;      // (and the two behind it)
         if (c.J > 0)
-            for (int i = tid; i < places; i += kLogitThreads) tab.bias[i] = 0;
+            for (int i = tid; i < places / 2; i += kLogitThreads) reinterpret_cast<uint32_t *>(tab.bias)[i] = 0;
     }
     if (!WRITE && tid <= MXQ_MAX_T) sh.key[tid] = 0;
     if (tid == 0) sh.listed = 0;
@@ -219,13 +229,11 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
     int r = r0 + from / parts, part = from % parts, first = first_of(b * c.R + r, part);
     Vectors cur, ahead;
     if (from < to) start(cur, b * c.R + r, first);
-    // this thread's entries of the list of biases, then their places in the tables (a second one where two of a row's batches share a token's)
-    int32_t entry[kEntries], second[kEntries];
-#pragma unroll
-    for (int u = 0; u < kEntries; ++u) entry[u] = second[u] = -1;
     if (tabled) {
+        int32_t entry[kEntries];
 #pragma unroll
         for (int u = 0; u < kEntries; ++u) {
+            entry[u] = -1;
             if (tid + u * kLogitThreads >= c.J) break;
             entry[u] = (int32_t)ld_dep_u32(MXQ_AT(c.bias_tokens + b * c.J + tid + u * kLogitThreads, 4, c.bias_tokens, c.B * c.J * 4));
         }
@@ -289,13 +297,11 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
 #pragma unroll
         for (int u = 0; u < kEntries; ++u) {
             if (tid + u * kLogitThreads >= c.J) break;
-            const int v = entry[u];
-            entry[u] = place_of(v, 0), second[u] = place_of(v, 1);
-            for (int which = 0; which < 2; ++which) {        // of a token's entries the last one stays
-                const int place = which ? second[u] : entry[u];
+            for (int which = 0; which < 2; ++which) {
+                const int place = place_of(entry[u], which);
                 if (place < 0) continue;
                 mark(tab.biased, place);
-                atomicMax(&tab.bias[place], tid + u * kLogitThreads + 1);
+                tab.enter(place, tid + u * kLogitThreads + 1);
             }
         }
         __syncthreads();
@@ -392,23 +398,7 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
             at = __shfl_sync(0xffffffffu, at, 31) + before - __popc(left);
             for (; left; left &= left - 1) tab.list[at++] = (uint16_t)(32 * (w0 + lane) + __ffs(left) - 1);
         }
-        // the biases' values in the places of their last entries
-        uint32_t wins = 0;
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) {
-            const int place = max(entry[u], second[u]);
-            if (place >= 0 && tab.bias[place] == tid + u * kLogitThreads + 1) wins |= 1u << u;
-        }
-        if (__syncthreads_or(wins != 0)) {       // (the list is there; the stream's stores come before those of the special tokens)
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                if (!(wins >> u & 1)) continue;
-                const int32_t value = (int32_t)ld_dep_u32(MXQ_AT(c.bias_values + b * c.J + tid + u * kLogitThreads, 4, c.bias_values, c.B * c.J * 4));
-                if (entry[u] >= 0) tab.bias[entry[u]] = value;
-                if (second[u] >= 0) tab.bias[second[u]] = value;
-            }
-            __syncthreads();
-        }
+        __syncthreads();     // (the list is there; the stream's stores come before those of the special tokens)
 
         const int listed = sh.listed, pairs = listed * (r1 - r0);
         const float repetition = sh.penalties[0], presence = sh.penalties[1], frequency = sh.penalties[2];
@@ -444,7 +434,7 @@ __global__ void __launch_bounds__(kLogitThreads, kLogitCtas) logit_rules_kernel(
                     if ((count | made) != 0) x[i] = x[i] > 0.f ? __fdiv_rn(x[i], repetition) : __fmul_rn(x[i], repetition);
                     if (made != 0) x[i] = __fsub_rn(__fsub_rn(x[i], __fmul_rn(frequency, (float)made)), presence);
                 }
-                if (SliceTables::bit(tab.biased, place[i])) x[i] = __fadd_rn(x[i], __int_as_float(tab.bias[place[i]]));
+                if (SliceTables::bit(tab.biased, place[i])) x[i] = __fadd_rn(x[i], ld_dep_f32(MXQ_AT(c.bias_values + b * c.J + tab.bias[place[i]] - 1, 4, c.bias_values, c.B * c.J * 4)));
                 if constexpr (WRITE) {
                     const int64_t at = (b * c.R + rank[i]) * c.V + token[i];
                     if constexpr (sizeof(T) == 4) *MXQ_AT(out + at, 4, out, extent) = x[i];
