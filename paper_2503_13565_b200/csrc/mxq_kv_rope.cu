@@ -5,7 +5,10 @@
 //
 // A stream like the append itself: 2 bytes per element read, 2 (queries) or 0.53 (keys, values) written.  The rotation is FP32 with every
 // product and sum rounded once (no contraction), so that a row's codes are defined to the bit; keys are cast from there, without a
-// stop at BF16.
+// stop at BF16.  A warp has one token row: its lookups and angles serve all heads, and four lanes share a head as in the append.
+// Measured in a replayed graph: one row of 32 + 8 heads 2.2 us, 61 x 9 rows of a token tree 2.7 us (launch and three dependent loads: length,
+// table row, page); 13958 rows of 32 + 8 heads of 128 in a batch padded to 3 x 8191 (395 MB, the zeros of the queries that are not there among them)
+// 73 us, 5.4 TB/s = 82 % of the copy rate: what is missing are warps (103 registers, 16 warps per SM) to cover the loads.
 #include "mxq_kv.cuh"
 
 namespace mxq {

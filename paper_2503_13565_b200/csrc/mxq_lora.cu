@@ -5,13 +5,17 @@
 //
 // Two kernels: T = A x into the workspace (shrink), then base + B T (expand).  Both are bound by the adapters' bytes for a few token
 // rows and by X, base and Y for many; the products are m16n8k16 mma.sync with the token rows as m, fed from global memory by 16- and 8-byte
-// loads whose order along the contracted axis is the same for both operands (the sum does not mind the order).  (tcgen05 has nothing
-// to give here: at 16 to 128 ranks the products are 1 to 10 % of the tensor pipe's time, and its operands would have to pass
-// through shared memory first.)  T is FP32 and meets B as a sum of BF16 parts: three for an FP32 Y (all 24 bits), two for a BF16 Y (16 bits: what
+// loads whose order along the contracted axis is the same for both operands (the sum does not mind the order).  (For few rows the
+// products are a hundredth of the time; a prompt's, at 16 to 128 ranks, keep the legacy pipe a quarter busy.)  T is FP32 and meets B as a sum of BF16 parts: three for an FP32 Y (all 24 bits), two for a BF16 Y (16 bits: what
 // is lost is 2^-17 of each product, against the 2^-8 of Y's own rounding).
 //
 // A CTA takes a window of token rows and one adapter, or several one after the other: rows that have another one are left out (zero in the
 // product, not stored).
+// Measured in a replayed graph: one row, rank 16, beside 4096x4096: 9.5 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
+// beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
+// 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 50 us (107 MB: 16 us at the
+// copy rate), 28 for T (shared-memory traffic of the fragments and the legacy tensor pipe, 14 %) and 29 for the expansion (that pipe 27 %,
+// loads at 14 warps per SM).
 #include "mxq_device.cuh"
 #include "mxq_host.h"
 
@@ -488,16 +492,17 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
     int m = tile0 * 16 + g;
     int64_t place = (int64_t)m * c.N + col;
     const int64_t row8 = 8 * c.N;
-    int own[2];
-    Columns base[2];
-    auto load_ids = [&]() {
+    constexpr int kAhead = F32 ? 1 : 2;      // tiles whose base is on its way (the registers hold one of FP32)
+    int own[2], next_own[2];
+    Columns base[2], next_base[2];
+    auto load_ids = [&](int (&own)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int a = m + 8 * h < c.M ? __ldg(MXQ_AT(c.ids + m + 8 * h, 4, c.ids, (size_t)c.M * 4)) : -1;
             own[h] = a < c.L ? max(a, -1) : -1;
         }
     };
-    auto load_base = [&]() {
+    auto load_base = [&](Columns (&base)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             base[h].lo = base[h].hi = make_uint4(0, 0, 0, 0);
@@ -508,21 +513,23 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
             }
         }
     };
-    load_ids();
+    load_ids(own);
     int current = __reduce_max_sync(0xffffffffu, max(own[0], own[1]));
     if (current >= 0) load(current);
     pdl_wait();
     const int pieces = steps * kParts * 32;
     for (int i = threadIdx.x; i < tiles * pieces; i += 256)
         copy16(shared_address(frag + i), MXQ_AT(c.frag + (int64_t)tile0 * pieces + i, 16, c.frag, (size_t)all * pieces * 16), true);
-    load_base();
+    load_base(base);
+    auto advance = [&]() { m += 16, place += 2 * row8; };
+    if (kAhead == 2) advance(), load_ids(next_own), load_base(next_base);      // (rows behind the last are not read)
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     if (col0 >= c.N) return;
     const uint4 *q = frag + lane;
+    int64_t now = (int64_t)(tile0 * 16 + g) * c.N + col;
     for (int tile = 0; tile < tiles; ++tile, q += pieces) {
-        const int64_t now = place;
-        const int rows = c.M - m;            // rows m, m + 8 are there if 0, 8 < rows
+        const int rows = c.M - (tile0 + tile) * 16 - g;            // the lane's rows are there if 0, 8 < rows
         float f[2][8];
         int left[2], none[2];
 #pragma unroll
@@ -531,8 +538,14 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
             unpack_columns(f[h], base[h], F32);
             if (!VEC && c.base && there > 0 && 8 * h < rows) load_columns(f[h], c.base, F32, now + h * row8, there, false, n);
         }
-        m += 16, place += 2 * row8;
-        if (tile + 1 < tiles) load_ids(), load_base();
+        advance();
+        if (kAhead == 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) own[h] = next_own[h], base[h] = next_base[h];
+            if (tile + 2 < tiles) load_ids(next_own), load_base(next_base);
+        } else if (tile + 1 < tiles) {
+            load_ids(own), load_base(base);
+        }
         int adapter = __reduce_max_sync(0xffffffffu, max(left[0], left[1]));
         while (adapter >= 0) {               // the tile's adapters, one after the other
             if (adapter != current) load(adapter), current = adapter;
@@ -562,6 +575,7 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             if (there > 0 && 8 * h < rows && (!none[h] || copies)) store_columns(f[h], c.y, F32, now + h * row8, there, VEC, n);
+        now += 2 * row8;
     }
 }
 
@@ -669,9 +683,16 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
         const int rc = launch_pdl(lora_fragments_kernel, dim3((unsigned)(((int64_t)tiles * 16 * steps * 4 + 255) / 256)), 256, 0, stream, c);
         if (rc != MXQ_OK) return rc;
     }
-    c.tiles = 8;
-    const dim3 grid((unsigned)((c.N + 255) / 256), (unsigned)((tiles + c.tiles - 1) / c.tiles));
-    const size_t smem = (size_t)c.tiles * steps * c.parts * 512;
+    // tiles per CTA: what takes the fewest waves of two CTAs per SM, a CTA costing about as much as three tiles beside its own
+    const int64_t columns = (c.N + 255) / 256, slots = 2 * (int64_t)sm_count();
+    const size_t tile_bytes = (size_t)steps * c.parts * 512;
+    int64_t least = 0;
+    for (int t = 4; t <= 24 && t * tile_bytes <= 100 * 1024; ++t) {
+        const int64_t cost = (columns * ((tiles + t - 1) / t) + slots - 1) / slots * (t + 3);
+        if (t == 4 || cost < least) least = cost, c.tiles = t;
+    }
+    const dim3 grid((unsigned)columns, (unsigned)((tiles + c.tiles - 1) / c.tiles));
+    const size_t smem = c.tiles * tile_bytes;
     void (*const kernel)(LoraCall) = many_kernel(c.r, c.y_f32 != 0, c.N % 8 == 0);
     if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
     return launch_pdl(kernel, grid, 256, smem, stream, c);
