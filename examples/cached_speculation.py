@@ -2,7 +2,7 @@
 
 A small decoder with random weights: per layer q, k, v from one fused MXFP4 projection, attention over the cache, the output
 projection with the residual in its epilogue, a gated feed-forward block; MXFP4 vocabulary projection fused with the
-verification.  (Norms and rotary positions, which a real model applies to the activations between these calls, are left out.)
+verification.  (Norms and rotary positions are left out here; examples/decoder_step.py has them.)
 The draft is the model's first layer; both keep their own cache.  What is shown:
 
   decode    specdec.decode drives both: mxq_kv_resize makes room before a pass and rolls back what was not accepted,
