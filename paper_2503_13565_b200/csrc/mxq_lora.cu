@@ -5,19 +5,22 @@
 //
 // Two kernels: T = A x into the workspace (shrink), then base + B T (expand).  Both are bound by the adapters' bytes for a few token
 // rows and by X, base and Y for many; the products are m16n8k16 mma.sync with the token rows as m, fed from global memory by 16- and 8-byte
-// loads whose order along the contracted axis is the same for both operands (the sum does not mind the order).  (For few rows the
-// products are a hundredth of the time; a prompt's, at 16 to 128 ranks, keep the legacy pipe a quarter busy.)  T is FP32 and meets B as a sum of BF16 parts: three for an FP32 Y (all 24 bits), two for a BF16 Y (16 bits: what
+// loads whose order along the contracted axis is the same for both operands (the sum does not mind the order): for few rows they are a hundredth
+// of the time.  A prompt's T, a matrix product with one short side, takes the tensor memory path instead (lora_shrink_umma_kernel: 50 -> 42 us
+// for the prompt below).
+// T is FP32 and meets B as a sum of BF16 parts: three for an FP32 Y (all 24 bits), two for a BF16 Y (16 bits: what
 // is lost is 2^-17 of each product, against the 2^-8 of Y's own rounding).
 //
 // A CTA takes a window of token rows and one adapter, or several one after the other: rows that have another one are left out (zero in the
 // product, not stored).
-// Measured in a replayed graph: one row, rank 16, beside 4096x4096: 9.5 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
+// Measured in a replayed graph: one row, rank 16, beside 4096x4096: 9.7 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
-// 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 50 us (107 MB: 16 us at the
-// copy rate), 28 for T (shared-memory traffic of the fragments and the legacy tensor pipe, 14 %) and 29 for the expansion (that pipe 27 %,
-// loads at 14 warps per SM).
+// 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 42 us (107 MB: 16 us at the
+// copy rate), the expansion the most of it (base and Y at 14 warps per SM, the legacy tensor pipe 27 % busy).
 #include "mxq_device.cuh"
 #include "mxq_host.h"
+#include "mxq_tcgen05.cuh"
+#include "mxq_tensor_map.h"
 
 namespace mxq {
 
@@ -290,6 +293,153 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
         __syncthreads();
     }
     if (!waited) pdl_wait();
+}
+
+// T = A x of many rows on the tensor memory path (K a multiple of 64): a window of 128 token rows is the first operand of tcgen05.mma (BF16, FP32
+// accumulator in tensor memory), the adapter's ranks the second; the copy engine brings 128 x 64 and ranks x 64 elements per stage, 128-byte swizzled,
+// straight into the operands, so that neither registers nor shared-memory reads stand between memory and the product.  grid (windows, splits,
+// slots: the CTAs that find no adapter come last); warp 0 multiplies, warp 1 copies, warps 2 to 5 take a row per thread from tensor memory to the partial sums.  ranks16: columns of the
+// product (the ranks, up to a multiple of 16: what is behind an adapter's own is computed and dropped).
+constexpr int kUmmaRows = 128, kUmmaK = 64, kUmmaThreads = 192;
+__device__ unsigned int g_lora_status = 0;     // sticky: a bounded wait gave up
+
+__global__ void __launch_bounds__(kUmmaThreads)
+lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap amap, LoraCall c, int ring, int ranks16, int columns) {
+    extern __shared__ uint8_t raw[];
+    __shared__ int32_t owner[kUmmaRows], list[kUmmaRows], count, fail;
+    __shared__ uint32_t holder;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row0 = blockIdx.x * kUmmaRows;
+    const uint32_t stage = kUmmaRows * kUmmaK * 2 + ranks16 * kUmmaK * 2, base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t full0 = base + ring * stage, empty0 = full0 + ring * 8, done = empty0 + ring * 8;
+    const int k0 = blockIdx.y * (c.split_k / kUmmaK), stages = (int)min((int64_t)c.split_k / kUmmaK, c.K / kUmmaK - k0);
+    if (warp == 0) {         // the window's adapters, in ascending order
+        pdl_trigger();
+        uint32_t a[kUmmaRows / 32];
+#pragma unroll
+        for (int j = 0; j < kUmmaRows / 32; ++j) {
+            const int m = row0 + 32 * j + lane;
+            const int id = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
+            a[j] = id >= 0 && id < c.L ? (uint32_t)id : 0xFFFFFFFFu;
+            owner[32 * j + lane] = (int32_t)a[j];
+        }
+        int n = 0;
+        for (;; ++n) {
+            uint32_t least = 0xFFFFFFFFu;
+#pragma unroll
+            for (int j = 0; j < kUmmaRows / 32; ++j) least = min(least, a[j]);
+            least = __reduce_min_sync(0xffffffffu, least);
+            if (least == 0xFFFFFFFFu) break;
+            if (lane == 0) list[n] = (int32_t)least;
+#pragma unroll
+            for (int j = 0; j < kUmmaRows / 32; ++j)
+                if (a[j] == least) a[j] = 0xFFFFFFFFu;
+        }
+        if (lane == 0) count = n;
+    } else if (warp == 1) {
+        for (int b = lane; b < 2 * ring + 1; b += 32) mbar_init(full0 + b * 8, 1u);
+        if (lane == 0) {
+            fail = 0;
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&amap) : "memory");
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if ((int)blockIdx.z >= count) {
+        pdl_wait();
+        return;
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&holder)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&holder);
+    volatile int32_t *failed = &fail;
+
+    int step = 0;            // stages of all passes so far: the ring's state
+    for (int at = blockIdx.z, pass = 0; at < count; at += c.slots, ++pass, step += stages) {
+        const int adapter = list[at];
+        if (warp == 1) {
+            auto copy_a = [&](int i) {
+                const uint32_t slot = (step + i) % ring;
+                mbar_expect_tx(full0 + slot * 8, stage);
+                tma_load_codes(base + slot * stage + kUmmaRows * kUmmaK * 2, &amap, (k0 + i) * kUmmaK, adapter * c.r, full0 + slot * 8);
+            };
+            auto copy_x = [&](int i) {
+                const uint32_t slot = (step + i) % ring;
+                tma_load_codes(base + slot * stage, &xmap, (k0 + i) * kUmmaK, row0, full0 + slot * 8);
+            };
+            int i = 0;
+            if (pass == 0) {         // the adapter's first stages are on their way before the previous kernel has ended; X may be its output
+                const int first = min(ring, stages);
+                if (lane == 0)
+                    for (int u = 0; u < first; ++u) copy_a(u);
+                pdl_wait();
+                if (lane == 0)
+                    for (int u = 0; u < first; ++u) copy_x(u);
+                i = first;
+            }
+            for (; i < stages; ++i) {
+                const int n = step + i;
+                if (n >= ring && !mbar_wait_relaxed(empty0 + n % ring * 8, (n / ring - 1) & 1)) {
+                    if (lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
+                    break;
+                }
+                if (lane == 0) copy_a(i), copy_x(i);
+            }
+        } else if (warp == 0) {
+            // D = F32, A = B = BF16, both K-major, M = 128
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (((uint32_t)ranks16 >> 3) << 17) | ((128u >> 4) << 24);
+            const uint32_t hi = (uint32_t)(smem_desc(0, 16, 1024, 2) >> 32), lo = (uint32_t)smem_desc(base, 16, 1024, 2);
+            for (int i = 0; i < stages; ++i) {
+                const uint32_t n = step + i, slot = n % ring;
+                if (!mbar_wait_relaxed(full0 + slot * 8, (n / ring) & 1)) {
+                    if (lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t x_lo = lo + slot * (stage >> 4), a_lo = x_lo + (kUmmaRows * kUmmaK * 2 >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int j = 0; j < kUmmaK / 16; ++j)   // 16 k: 32 bytes further along both rows
+                        asm volatile(
+                            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                            "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+                            "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+                            ::"r"(tmem), "r"(x_lo + j * 2), "r"(hi), "r"(a_lo + j * 2), "r"(hi), "r"(idesc), "r"((i | j) ? 1u : 0u)
+                            : "memory");
+                    tc_commit(empty0 + slot * 8);
+                }
+                __syncwarp();
+            }
+            if (elect_one()) tc_commit(done);
+            __syncwarp();
+        } else {
+            const int row = 32 * (warp & 3) + lane;
+            if (!mbar_wait_relaxed(done, pass & 1) && lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
+            tc_fence_after();
+            float *out = c.t + ((int64_t)blockIdx.y * c.M + row0 + row) * c.r;
+            const bool mine = owner[row] == adapter, lost = *failed != 0;
+            for (int n = 0; n < ranks16; n += 16) {
+                float d[16];
+                tc_load16(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + n, d);
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    if (!mine || n + j >= c.r) continue;
+                    const float poison = lost ? __uint_as_float(0x7FC00000u) : 0.f;
+                    *reinterpret_cast<float4 *>(MXQ_AT(out + n + j, 16, c.t, (size_t)c.splits * c.M * c.r * 4)) =
+                        make_float4(d[j] + poison, d[j + 1] + poison, d[j + 2] + poison, d[j + 3] + poison);
+                }
+            }
+            tc_fence_before();
+        }
+        __syncthreads();     // the accumulator has been read
+        tc_fence_after();
+    }
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
 }
 
 // ---- base + B T -------------------------------------------------------------------------------------------------------------------
@@ -581,6 +731,14 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
 
 MXQ_BOUNDS_TU(bounds_take_lora)
 
+int lora_take_status(uint32_t *out) {
+    unsigned int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_lora_status, sizeof v) != cudaSuccess) return MXQ_ERR_CUDA;
+    if (v != 0 && cudaMemcpyToSymbol(g_lora_status, &zero, sizeof zero) != cudaSuccess) return MXQ_ERR_CUDA;
+    *out = v;
+    return MXQ_OK;
+}
+
 // ---- host ---------------------------------------------------------------------------------------------------------------
 
 // Up to 16 rows: one window, a CTA of both kernels for each of its adapters.  Up to 511: sorted into segments (see lora_order_kernel).  More:
@@ -589,15 +747,19 @@ constexpr int kMostSplits = 16;
 constexpr int kFewWarps = 8, kManyWarps = 16;     // of a CTA of the shrink (above rank 64 sixteen warps' sums do not fit the registers)
 static bool many_rows(int64_t M) { return M >= kMostSorted; }
 static bool few_rows(int64_t M) { return M <= 16; }
+// The tensor memory path reads a window's 128 rows once for each of its adapters: for adapters of 80 rows and more on average (512 rows of six,
+// 4096 inputs, rank 64: 23 -> 18 us; 1500 rows of twenty, rank 16: 20 -> 24).
+static bool by_umma(const LoraCall &c) { return many_rows(c.M) && c.M >= 80 * (int64_t)c.L && c.K % kUmmaK == 0 && c.K <= 0x3FFFFFFF && tensor_map_available(); }
 static int64_t most_segments(const LoraCall &c) { return c.M / 16 + min(c.L + 1, c.M); }
 
 static void lora_plan(LoraCall &c) {
     const bool few = few_rows(c.M), many = many_rows(c.M);
     const int64_t sms = sm_count();
-    c.slots = few ? min(c.M, c.L) : many ? min(2, c.L) : 1;
-    // splits of K as long as the SMs hold the CTAs at once, but at least one step of 32 per warp
-    const int64_t step = 32 * (many && c.r <= 64 ? kManyWarps : kFewWarps), most = (c.K + step - 1) / step;
-    int64_t want = max((int64_t)1, few ? 2 * sms / c.slots : many ? sms / ((c.M + 31) / 32) : 2 * sms / most_segments(c));
+    const bool umma = by_umma(c);
+    c.slots = few ? min(c.M, c.L) : umma ? min(4, c.L) : many ? min(2, c.L) : 1;
+    // splits of K as long as the SMs hold the CTAs at once, but at least one step of 32 per warp or one stage
+    const int64_t step = umma ? kUmmaK : 32 * (many && c.r <= 64 ? kManyWarps : kFewWarps), most = (c.K + step - 1) / step;
+    int64_t want = max((int64_t)1, few ? 2 * sms / c.slots : umma ? sms / ((c.M + kUmmaRows - 1) / kUmmaRows) : many ? sms / ((c.M + 31) / 32) : 2 * sms / most_segments(c));
     if (want > most) want = most;
     if (want > kMostSplits) want = kMostSplits;
     int64_t len = ((c.K + want - 1) / want + step - 1) / step * step;
@@ -630,7 +792,7 @@ static LoraCall lora_call(const void *X, int64_t M, const mxq_lora_adapters *ad,
     c.t = (float *)workspace, c.N = N, c.K = K, c.M = (int32_t)M, c.r = ad->rank, c.L = ad->count;
     c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
     lora_plan(c);
-    c.direct = many_rows(M) && c.splits == 1;
+    c.direct = many_rows(M) && !by_umma(c) && c.splits == 1;
     uint8_t *behind = reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c);
     c.frag = reinterpret_cast<uint4 *>(behind);
     c.plan = few_rows(M) || many_rows(M) ? nullptr : reinterpret_cast<int32_t *>(behind);
@@ -698,7 +860,23 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     return launch_pdl(kernel, grid, 256, smem, stream, c);
 }
 
+static int shrink_umma_launch(const LoraCall &c, cudaStream_t stream) {
+    const int ranks16 = (c.r + 15) / 16 * 16, columns = ranks16 <= 32 ? 32 : ranks16 <= 64 ? 64 : 128;
+    CUtensorMap xmap, amap;
+    if (!bf16_tensor_map(c.x, c.M, c.K, kUmmaRows, &xmap) || !bf16_tensor_map(c.a, (int64_t)c.L * c.r, c.K, ranks16, &amap)) return MXQ_ERR_CUDA;
+    // a ring that lets two CTAs share an SM where that leaves four stages (the prompt of rank 64: 47 -> 42 us; at rank 128 three stages cost 110 -> 125)
+    const int stage = kUmmaRows * kUmmaK * 2 + ranks16 * kUmmaK * 2, half = 105 * 1024 / stage, ring = min(min(8, c.split_k / kUmmaK), half >= 4 ? half : 200 * 1024 / stage);
+    const size_t smem = 1024 + (size_t)ring * (stage + 16) + 8;
+    if (smem > 40 * 1024 && cudaFuncSetAttribute(lora_shrink_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MXQ_ERR_CUDA;
+    }
+    const dim3 grid((unsigned)((c.M + kUmmaRows - 1) / kUmmaRows), (unsigned)c.splits, (unsigned)c.slots);
+    return launch_pdl(lora_shrink_umma_kernel, grid, kUmmaThreads, smem, stream, xmap, amap, c, ring, ranks16, columns);
+}
+
 static int lora_shrink(const LoraCall &c, cudaStream_t stream) {
+    if (by_umma(c)) return shrink_umma_launch(c, stream);
     if (many_rows(c.M)) return c.r <= 64 ? shrink_by_rank<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps, 16>(c, stream);
     if (c.plan) {
         const int rc = launch_pdl(lora_order_kernel, dim3(1), kMostSorted, 0, stream, c);
