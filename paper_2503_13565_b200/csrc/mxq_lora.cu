@@ -44,7 +44,7 @@ struct LoraCall {
     int32_t stages;          // shrink: steps of a warp's ring
     int32_t tiles;           // many rows: tiles of 16 rows per CTA of the expansion
     int32_t direct;          // many rows, K not split: the shrink writes the fragments itself
-    int32_t *plan;           // 17 to 511 rows: the segments (see lora_order_kernel), else nullptr
+    int32_t *plan;           // segments of sorted rows (see lora_order_kernel), else nullptr
 };
 
 struct Window {
@@ -54,7 +54,7 @@ struct Window {
     int32_t count;
 };
 
-// 17 to 511 rows, the batches of a server: rows sorted by adapter and cut into segments of up to 16 rows of one adapter, so that every
+// 17 to 511 rows of many adapters, the batches of a server: rows sorted by adapter and cut into segments of up to 16 rows of one adapter, so that every
 // adapter is read about once whatever the rows' order.  plan: [0 ..] first place of segment s and, behind the last, M; [kPlanAdapter ..] its
 // adapter, -1: none; [kPlanOrder ..] row at every place; [kPlanCount] segments.
 constexpr int kMostSorted = 512, kPlanAdapter = 1024, kPlanOrder = 2048, kPlanCount = 2560, kPlanBytes = 2561 * 4;
@@ -605,8 +605,9 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
 
 // ---- many rows ------------------------------------------------------------------------------------------------------------------------
 // T's partial sums -> its fragments, [tiles of 16 rows][steps][parts][32 lanes]: once, not for every block of columns.  A thread per row and four ranks.
+// (No early trigger: expansion CTAs that settle beside this kernel's and the shrink's spread unevenly over the SMs.  2000 rows, rank 32, 11008
+// outputs, FP32: 75 us with it, 53 without; 512 rows, rank 64, 4096 outputs: 16.5, 14.7.)
 __global__ void __launch_bounds__(256) lora_fragments_kernel(LoraCall c) {
-    pdl_trigger();
     const int quarters = (c.r + 15) / 16 * 4, tiles = (c.M + 15) / 16;
     const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int m = (int)(n / quarters), quarter = (int)(n - (int64_t)m * quarters);
@@ -741,19 +742,21 @@ int lora_take_status(uint32_t *out) {
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 
-// Up to 16 rows: one window, a CTA of both kernels for each of its adapters.  Up to 511: sorted into segments (see lora_order_kernel).  More:
-// windows of 32 rows as they come, in a prompt mostly of one adapter, with a second CTA where two meet; T's fragments are made once.
+// Up to 16 rows: one window, a CTA of both kernels for each of its adapters.  Up to 511: sorted into segments (see lora_order_kernel).  More, and
+// from 64 rows on with 48 rows and more per adapter: windows of rows as they come, in a prompt mostly of one adapter, with a second CTA where
+// two meet; T's fragments are made once (256 rows of four adapters, rank 128, 11008 outputs: sorted 46 us, so 30; 128 rows of eight, rank 64, 4096
+// outputs: 16, 23).
 constexpr int kMostSplits = 16;
 constexpr int kFewWarps = 8, kManyWarps = 16;     // of a CTA of the shrink (above rank 64 sixteen warps' sums do not fit the registers)
-static bool many_rows(int64_t M) { return M >= kMostSorted; }
+static bool many_rows(const LoraCall &c) { return c.M >= kMostSorted || (c.M >= 64 && c.M >= 48 * (int64_t)c.L); }
 static bool few_rows(int64_t M) { return M <= 16; }
 // The tensor memory path reads a window's 128 rows once for each of its adapters: for adapters of 80 rows and more on average (512 rows of six,
 // 4096 inputs, rank 64: 23 -> 18 us; 1500 rows of twenty, rank 16: 20 -> 24).
-static bool by_umma(const LoraCall &c) { return many_rows(c.M) && c.M >= 80 * (int64_t)c.L && c.K % kUmmaK == 0 && c.K <= 0x3FFFFFFF && tensor_map_available(); }
+static bool by_umma(const LoraCall &c) { return many_rows(c) && c.M >= 80 * (int64_t)c.L && c.K % kUmmaK == 0 && c.K <= 0x3FFFFFFF && tensor_map_available(); }
 static int64_t most_segments(const LoraCall &c) { return c.M / 16 + min(c.L + 1, c.M); }
 
 static void lora_plan(LoraCall &c) {
-    const bool few = few_rows(c.M), many = many_rows(c.M);
+    const bool few = few_rows(c.M), many = many_rows(c);
     const int64_t sms = sm_count();
     const bool umma = by_umma(c);
     c.slots = few ? min(c.M, c.L) : umma ? min(4, c.L) : many ? min(2, c.L) : 1;
@@ -792,10 +795,10 @@ static LoraCall lora_call(const void *X, int64_t M, const mxq_lora_adapters *ad,
     c.t = (float *)workspace, c.N = N, c.K = K, c.M = (int32_t)M, c.r = ad->rank, c.L = ad->count;
     c.base = (const uint8_t *)base, c.y = (uint8_t *)Y, c.base_f32 = base_dtype == MXQ_F32, c.y_f32 = y_dtype == MXQ_F32, c.parts = c.y_f32 ? 3 : 2;
     lora_plan(c);
-    c.direct = many_rows(M) && !by_umma(c) && c.splits == 1;
+    c.direct = many_rows(c) && !by_umma(c) && c.splits == 1;
     uint8_t *behind = reinterpret_cast<uint8_t *>(c.t) + sums_bytes(c);
     c.frag = reinterpret_cast<uint4 *>(behind);
-    c.plan = few_rows(M) || many_rows(M) ? nullptr : reinterpret_cast<int32_t *>(behind);
+    c.plan = few_rows(M) || many_rows(c) ? nullptr : reinterpret_cast<int32_t *>(behind);
     return c;
 }
 
@@ -877,7 +880,7 @@ static int shrink_umma_launch(const LoraCall &c, cudaStream_t stream) {
 
 static int lora_shrink(const LoraCall &c, cudaStream_t stream) {
     if (by_umma(c)) return shrink_umma_launch(c, stream);
-    if (many_rows(c.M)) return c.r <= 64 ? shrink_by_rank<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps, 16>(c, stream);
+    if (many_rows(c)) return c.r <= 64 ? shrink_by_rank<2, kManyWarps>(c, stream) : shrink_launch<2, kFewWarps, 16>(c, stream);
     if (c.plan) {
         const int rc = launch_pdl(lora_order_kernel, dim3(1), kMostSorted, 0, stream, c);
         if (rc != MXQ_OK) return rc;
@@ -885,7 +888,7 @@ static int lora_shrink(const LoraCall &c, cudaStream_t stream) {
     return c.r <= 64 ? shrink_by_rank<1, kFewWarps>(c, stream) : shrink_launch<1, kFewWarps, 16>(c, stream);
 }
 static int lora_expand(const LoraCall &c, cudaStream_t stream) {
-    return many_rows(c.M) ? expand_many_launch(c, stream) : expand_launch(c, stream);
+    return many_rows(c) ? expand_many_launch(c, stream) : expand_launch(c, stream);
 }
 
 }  // namespace mxq
@@ -899,7 +902,7 @@ size_t mxq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int rank, int a
     c.M = (int32_t)M, c.N = N, c.K = K, c.r = rank, c.L = adapters;
     mxq::lora_plan(c);
     // [partial sums][fragments: three BF16 parts of 16-row tiles, or the plan of the segments]
-    return mxq::sums_bytes(c) + (mxq::many_rows(M) ? (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512 : mxq::few_rows(M) ? 0 : (size_t)mxq::kPlanBytes);
+    return mxq::sums_bytes(c) + (mxq::many_rows(c) ? (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512 : mxq::few_rows(M) ? 0 : (size_t)mxq::kPlanBytes);
 }
 
 int mxq_lora(const void *X_bf16, int64_t M, const mxq_lora_adapters *adapters, const int32_t *ids, int64_t N, int64_t K, const void *base,

@@ -38,7 +38,7 @@ def check(got, want, mag, k, r, extra=0.0):
 
 SHAPES = [(1, 4096, 4096, 16, 8), (1, 1, 32, 8, 1), (2, 31, 64, 24, 3), (5, 33, 96, 40, 2), (16, 1025, 4096, 32, 24), (16, 256, 1312, 128, 5), (17, 100, 160, 64, 4),
           (64, 515, 768, 16, 40), (200, 72, 256, 72, 7), (511, 40, 64, 8, 3), (512, 136, 96, 104, 9), (700, 1000, 768, 64, 5), (1030, 33, 416, 16, 70), (513, 64, 64, 128, 2), (600, 40, 448, 24, 20), (2000, 264, 1024, 8, 3),
-          (520, 48, 4096, 72, 5), (3001, 16, 128, 112, 40)]
+          (520, 48, 4096, 72, 5), (3001, 16, 128, 112, 40), (64, 40, 256, 24, 1), (64, 520, 96, 128, 1), (100, 136, 96, 16, 2), (191, 72, 320, 72, 3), (330, 33, 192, 128, 4)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -80,8 +80,8 @@ def test_owners(ids):
 
 
 def test_values_that_are_not_finite_stay_in_their_rows():
-    for m in (12, 600):
-        x, a, b, ids, scale = make(m, 72, 96, 16, 4, seed=3, ids=[i % 4 for i in range(m)])
+    for m, k in ((12, 96), (600, 96), (600, 128), (200, 128)):
+        x, a, b, ids, scale = make(m, 72, k, 16, 4, seed=3, ids=[i % 4 for i in range(m)])
         base = torch.randn(m, 72, device="cuda")
         clean = mxq.mxq_lora(x, a, b, ids, scale=scale, base=base)
         a[1, 3, 5], b[2, 7, 2], x[3, 4], scale[1] = float("inf"), float("nan"), float("nan"), float("inf")
