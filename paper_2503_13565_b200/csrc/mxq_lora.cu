@@ -444,7 +444,12 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
 
 // ---- base + B T -------------------------------------------------------------------------------------------------------------------
 // grid (columns / (32 * warps), slots, windows); a warp takes 32 columns.  Tile i of 8 columns holds, in the product's order, columns
-// 8t + 2i and 8t + 2i + 1 for t = 0..3, so that a lane ends up with eight consecutive columns of its rows.  KT: most steps of 16 ranks.
+// 8t + 2i and 8t + 2i + 1 for t = 0..3, so that a lane ends up with eight consecutive columns of its rows.  Where N is no multiple of 8 and rows
+// start anywhere, base and Y go by the element and the order is the plain one, tile i = columns 8i .. 8i + 7: a lane has columns 2t and 2t + 1 of
+// every tile and four lanes share a sector (4000 x 1025, rank 64, FP32: 42 us with the other order, 28 with this one).  KT: most steps of 16 ranks.
+__device__ __forceinline__ int own_column(bool vec, int t) { return vec ? 8 * t : 2 * t; }         // a lane's first, and from there on:
+__device__ __forceinline__ int element(bool vec, int e) { return vec ? e : 8 * (e >> 1) + (e & 1); }
+__device__ __forceinline__ int b_column(bool vec, int g, int i) { return vec ? 8 * (g >> 1) + 2 * i + (g & 1) : 8 * i + g; }
 __device__ __forceinline__ void load_columns(float (&f)[8], const uint8_t *base, bool f32, int64_t at, int there, bool vec, int64_t n) {
     if (vec) {
         const uint8_t *p = MXQ_AT(base + at * (f32 ? 4 : 2), f32 ? 32 : 16, base, n * (f32 ? 4 : 2));
@@ -461,7 +466,8 @@ __device__ __forceinline__ void load_columns(float (&f)[8], const uint8_t *base,
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         f[e] = 0.f;
-        if (e < there) f[e] = f32 ? ld_dep_f32(MXQ_AT(base + (at + e) * 4, 4, base, n * 4)) : ld_dep_bf16(MXQ_AT(base + (at + e) * 2, 2, base, n * 2));
+        const int o = element(false, e);
+        if (o < there) f[e] = f32 ? ld_dep_f32(MXQ_AT(base + (at + o) * 4, 4, base, n * 4)) : ld_dep_bf16(MXQ_AT(base + (at + o) * 2, 2, base, n * 2));
     }
 }
 __device__ __forceinline__ void store_columns(const float (&f)[8], uint8_t *y, bool f32, int64_t at, int there, bool vec, int64_t n) {
@@ -477,9 +483,10 @@ __device__ __forceinline__ void store_columns(const float (&f)[8], uint8_t *y, b
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (e >= there) continue;
-        if (f32) *reinterpret_cast<float *>(MXQ_AT(y + (at + e) * 4, 4, y, n * 4)) = f[e];
-        else *reinterpret_cast<__nv_bfloat16 *>(MXQ_AT(y + (at + e) * 2, 2, y, n * 2)) = __float2bfloat16_rn(f[e]);
+        const int o = element(false, e);
+        if (o >= there) continue;
+        if (f32) *reinterpret_cast<float *>(MXQ_AT(y + (at + o) * 4, 4, y, n * 4)) = f[e];
+        else *reinterpret_cast<__nv_bfloat16 *>(MXQ_AT(y + (at + o) * 2, 2, y, n * 2)) = __float2bfloat16_rn(f[e]);
     }
 }
 
@@ -536,7 +543,8 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int steps = (c.r + 15) / 16;
-    const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32, col = col0 + 8 * t, n = (int64_t)c.M * c.N;
+    const bool vec = c.N % 8 == 0;
+    const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32, col = col0 + own_column(vec, t), n = (int64_t)c.M * c.N;
     load_window(win, c, blockIdx.z * 16, 16);
     __syncthreads();
     const int adapter = (int)blockIdx.y < win.count ? win.list[blockIdx.y] : -2;
@@ -546,10 +554,10 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
         for (int s = 0; s < KT; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (s < steps) w[s][i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
+                if (s < steps) w[s][i] = load_b(c, adapter, col0 + b_column(vec, g, i), s, t);
     }
     // the rows that this CTA stores: its adapter's; the first slot also copies those without one, unless they are there already
-    const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
+    const int there = (int)max((int64_t)0, min((int64_t)32, c.N - col));
     bool own[2], mine[2];
     int64_t place[2];                    // of the columns in base and Y
 #pragma unroll
@@ -560,7 +568,6 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
         place[h] = (int64_t)row * c.N + col;
     }
     pdl_wait();
-    const bool vec = c.N % 8 == 0;
     Columns ahead[2];                    // base, on its way while T is made ready
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -627,9 +634,9 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
     extern __shared__ uint4 frag[];      // the rows' fragments of T
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t col0 = ((int64_t)blockIdx.x * 8 + warp) * 32, col = col0 + 8 * t, n = (int64_t)c.M * c.N;
+    const int64_t col0 = ((int64_t)blockIdx.x * 8 + warp) * 32, col = col0 + own_column(VEC, t), n = (int64_t)c.M * c.N;
     const int steps = (c.r + 15) / 16, all = (c.M + 15) / 16, tile0 = blockIdx.y * c.tiles, tiles = min(c.tiles, all - tile0);
-    const int there = (int)max((int64_t)0, min((int64_t)8, c.N - col));
+    const int there = (int)max((int64_t)0, min((int64_t)32, c.N - col));
     const bool copies = c.base != c.y;
     uint2 w[KT][4];
     auto load = [&](int adapter) {
@@ -637,7 +644,7 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
         for (int s = 0; s < KT; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (s < steps) w[s][i] = load_b(c, adapter, col0 + 8 * (g >> 1) + 2 * i + (g & 1), s, t);
+                if (s < steps) w[s][i] = load_b(c, adapter, col0 + b_column(VEC, g, i), s, t);
     };
     // this lane's rows m, m + 8 of the tile whose ids and base are loaded next; `place` of its columns in base and Y
     int m = tile0 * 16 + g;
@@ -657,10 +664,20 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             base[h].lo = base[h].hi = make_uint4(0, 0, 0, 0);
-            if (VEC && c.base && there > 0 && m + 8 * h < c.M) {
+            if (!c.base || there <= 0 || m + 8 * h >= c.M) continue;
+            if (VEC) {
                 const uint8_t *p = MXQ_AT(c.base + (place + h * row8) * kSize, 8 * kSize, c.base, n * kSize);
                 base[h].lo = ld_dep_u4(p);
                 if (F32) base[h].hi = ld_dep_u4(p + 16);
+            } else {
+                float f[8];
+                load_columns(f, c.base, F32, place + h * row8, there, false, n);
+                if (F32) {
+                    base[h].lo = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                    base[h].hi = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+                } else {
+                    base[h].lo = pack_bf16(f);       // (exactly: they are BF16)
+                }
             }
         }
     };
@@ -687,7 +704,6 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
         for (int h = 0; h < 2; ++h) {
             left[h] = own[h], none[h] = own[h] < 0;
             unpack_columns(f[h], base[h], F32);
-            if (!VEC && c.base && there > 0 && 8 * h < rows) load_columns(f[h], c.base, F32, now + h * row8, there, false, n);
         }
         advance();
         if (kAhead == 2) {
@@ -866,7 +882,7 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
 static int shrink_umma_launch(const LoraCall &c, cudaStream_t stream) {
     const int ranks16 = (c.r + 15) / 16 * 16, columns = ranks16 <= 32 ? 32 : ranks16 <= 64 ? 64 : 128;
     CUtensorMap xmap, amap;
-    if (!bf16_tensor_map(c.x, c.M, c.K, kUmmaRows, &xmap) || !bf16_tensor_map(c.a, (int64_t)c.L * c.r, c.K, ranks16, &amap)) return MXQ_ERR_CUDA;
+    if (!encode_bf16_tensor_map(c.x, c.M, c.K, kUmmaRows, &xmap) || !encode_bf16_tensor_map(c.a, (int64_t)c.L * c.r, c.K, ranks16, &amap)) return MXQ_ERR_CUDA;
     // a ring that lets two CTAs share an SM where that leaves four stages (the prompt of rank 64: 47 -> 42 us; at rank 128 three stages cost 110 -> 125)
     const int stage = kUmmaRows * kUmmaK * 2 + ranks16 * kUmmaK * 2, half = 105 * 1024 / stage, ring = min(min(8, c.split_k / kUmmaK), half >= 4 ? half : 200 * 1024 / stage);
     const size_t smem = 1024 + (size_t)ring * (stage + 16) + 8;

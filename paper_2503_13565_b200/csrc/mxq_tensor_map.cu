@@ -80,6 +80,21 @@ bool codes_tensor_map(const uint8_t *codes, int64_t N, int64_t K, bool expand_fp
     return true;
 }
 
+bool encode_bf16_tensor_map(const void *base, int64_t rows, int64_t K, int box_rows, CUtensorMap *out) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t gdim[2] = {(cuuint64_t)K, (cuuint64_t)rows};
+    const cuuint64_t gstr[1] = {(cuuint64_t)(K * 2)};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), gdim, gstr, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS && std::getenv("MXQ_DEBUG"))
+        std::fprintf(stderr, "mxq: BF16 tensor map encode failed (%d) for rows=%lld K=%lld\n", (int)r, (long long)rows, (long long)K);
+    return r == CUDA_SUCCESS;
+}
+
 bool bf16_tensor_map(const void *base, int64_t rows, int64_t K, int box_rows, CUtensorMap *out) {
     int dev = 0;
     cudaGetDevice(&dev);
@@ -93,18 +108,7 @@ bool bf16_tensor_map(const void *base, int64_t rows, int64_t K, int box_rows, CU
         *out = slot.map;
         return true;
     }
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t gdim[2] = {(cuuint64_t)K, (cuuint64_t)rows};
-    const cuuint64_t gstr[1] = {(cuuint64_t)(K * 2)};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(&slot.map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), gdim, gstr, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        if (std::getenv("MXQ_DEBUG"))
-            std::fprintf(stderr, "mxq: BF16 tensor map encode failed (%d) for rows=%lld K=%lld\n", (int)r, (long long)rows, (long long)K);
+    if (!encode_bf16_tensor_map(base, rows, K, box_rows, &slot.map)) {
         slot.valid = false;
         return false;
     }

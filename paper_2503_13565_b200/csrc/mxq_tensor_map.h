@@ -19,5 +19,7 @@ bool codes_tensor_map(const uint8_t *codes, int64_t N, int64_t K, bool expand_fp
 // A map over a BF16 matrix [rows][K] (K % 64 == 0, 16-byte aligned base) whose box is box_rows rows x 64 elements
 // (128 bytes), 128-byte swizzled; rows of the box beyond the matrix read as zeros.  Cached like the maps above.
 bool bf16_tensor_map(const void *base, int64_t rows, int64_t K, int box_rows, CUtensorMap *out);
+// The same map made anew: for activations, whose addresses change from call to call.
+bool encode_bf16_tensor_map(const void *base, int64_t rows, int64_t K, int box_rows, CUtensorMap *out);
 
 }  // namespace mxq
