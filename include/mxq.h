@@ -544,6 +544,8 @@ int mxq_token_counts(uint32_t *counts, int64_t B, int64_t V, const int32_t *toke
  *   base [M][N] in Y's type (may be Y itself: added in place, rows without an adapter are then not touched), or NULL: zero
  *   Y [M][N] MXQ_F32, or MXQ_BF16 rounded to nearest even
  *   workspace  device memory, >= the *_workspace_bytes, 16-byte aligned, no initialisation needed; one per stream
+ * adapters and ids are read while the previous call of this library in the stream may still run (see mxq_set_pdl), like the weights of
+ * mxq_linear: that call must not write them.
  * K a multiple of 32, any N, 1 <= M <= MXQ_LORA_MAX_M (mxq_lora) or MXQ_MAX_M.  Sums are FP32; A x meets B with all its bits for an FP32 Y, with 16
  * bits of mantissa for a BF16 Y:
  *     |Y - exact| <= ((K / 16 + 96) * 2^-22 [+ 2^-17, BF16]) * |s_a| sum_r |B_nr| sum_k |A_rk x_k| + 2^-23 |Y| + BF16's rounding.

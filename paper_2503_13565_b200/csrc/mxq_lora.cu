@@ -6,7 +6,7 @@
 // Two kernels: T = A x into the workspace (shrink), then base + B T (expand).  Both are bound by the adapters' bytes for a few token
 // rows and by X, base and Y for many; the products are m16n8k16 mma.sync with the token rows as m, fed from global memory by 16- and 8-byte
 // loads whose order along the contracted axis is the same for both operands (the sum does not mind the order): for few rows they are a hundredth
-// of the time.  A prompt's T, a matrix product with one short side, takes the tensor memory path instead (lora_shrink_umma_kernel: 50 -> 42 us
+// of the time.  A prompt's T, a matrix product with one short side, takes the tensor memory path instead (lora_shrink_umma_kernel: 50 -> 41 us
 // for the prompt below).
 // T is FP32 and meets B as a sum of BF16 parts: three for an FP32 Y (all 24 bits), two for a BF16 Y (16 bits: what
 // is lost is 2^-17 of each product, against the 2^-8 of Y's own rounding).
@@ -15,7 +15,7 @@
 // product, not stored).
 // Measured in a replayed graph: one row, rank 16, beside 4096x4096: 9.7 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
-// 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 42 us (107 MB: 16 us at the
+// 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
 // copy rate), the expansion the most of it (base and Y at 14 warps per SM, the legacy tensor pipe 27 % busy).
 #include "mxq_device.cuh"
 #include "mxq_host.h"
@@ -299,7 +299,8 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
 // accumulator in tensor memory), the adapter's ranks the second; the copy engine brings 128 x 64 and ranks x 64 elements per stage, 128-byte swizzled,
 // straight into the operands, so that neither registers nor shared-memory reads stand between memory and the product.  grid (windows, splits,
 // slots: the CTAs that find no adapter come last); warp 0 multiplies, warp 1 copies, warps 2 to 5 take a row per thread from tensor memory to the partial sums.  ranks16: columns of the
-// product (the ranks, up to a multiple of 16: what is behind an adapter's own is computed and dropped).
+// product (the ranks, up to a multiple of 16: what is behind an adapter's own is computed and dropped).  No early trigger: the kernel behind this
+// one has nothing to do ahead of T, and none that holds tensor memory may settle here while a CTA still waits for its own.
 constexpr int kUmmaRows = 128, kUmmaK = 64, kUmmaThreads = 192;
 __device__ unsigned int g_lora_status = 0;     // sticky: a bounded wait gave up
 
@@ -313,7 +314,6 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
     const uint32_t full0 = base + ring * stage, empty0 = full0 + ring * 8, done = empty0 + ring * 8;
     const int k0 = blockIdx.y * (c.split_k / kUmmaK), stages = (int)min((int64_t)c.split_k / kUmmaK, c.K / kUmmaK - k0);
     if (warp == 0) {         // the window's adapters, in ascending order
-        pdl_trigger();
         uint32_t a[kUmmaRows / 32];
 #pragma unroll
         for (int j = 0; j < kUmmaRows / 32; ++j) {
@@ -349,7 +349,26 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
         pdl_wait();
         return;
     }
-    if (warp == 0) {
+    const int first_stages = min(ring, stages);
+    auto copy_a = [&](int step, int i, int adapter) {
+        const uint32_t slot = (step + i) % ring;
+        mbar_expect_tx(full0 + slot * 8, stage);
+        tma_load_codes(base + slot * stage + kUmmaRows * kUmmaK * 2, &amap, (k0 + i) * kUmmaK, adapter * c.r, full0 + slot * 8);
+    };
+    auto copy_x = [&](int step, int i) {
+        const uint32_t slot = (step + i) % ring;
+        tma_load_codes(base + slot * stage, &xmap, (k0 + i) * kUmmaK, row0, full0 + slot * 8);
+    };
+    // the first adapter's first stages are on their way before the previous kernel has ended; X may be its output.  (All wait here: the bounded
+    // waits below are for this kernel's own steps only.)
+    if (warp == 1 && lane == 0)
+        for (int u = 0; u < first_stages; ++u) copy_a(0, u, list[blockIdx.z]);
+    __syncwarp();
+    pdl_wait();
+    if (warp == 1 && lane == 0)
+        for (int u = 0; u < first_stages; ++u) copy_x(0, u);
+    __syncwarp();
+    if (warp == 0) {         // (behind the wait: the previous kernel's CTAs may still want columns of their own before it)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&holder)), "r"(columns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -362,39 +381,21 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
     int step = 0;            // stages of all passes so far: the ring's state
     for (int at = blockIdx.z, pass = 0; at < count; at += c.slots, ++pass, step += stages) {
         const int adapter = list[at];
+        const bool lost = *failed != 0;          // (an earlier pass gave up: the others give NaN at once)
         if (warp == 1) {
-            auto copy_a = [&](int i) {
-                const uint32_t slot = (step + i) % ring;
-                mbar_expect_tx(full0 + slot * 8, stage);
-                tma_load_codes(base + slot * stage + kUmmaRows * kUmmaK * 2, &amap, (k0 + i) * kUmmaK, adapter * c.r, full0 + slot * 8);
-            };
-            auto copy_x = [&](int i) {
-                const uint32_t slot = (step + i) % ring;
-                tma_load_codes(base + slot * stage, &xmap, (k0 + i) * kUmmaK, row0, full0 + slot * 8);
-            };
-            int i = 0;
-            if (pass == 0) {         // the adapter's first stages are on their way before the previous kernel has ended; X may be its output
-                const int first = min(ring, stages);
-                if (lane == 0)
-                    for (int u = 0; u < first; ++u) copy_a(u);
-                pdl_wait();
-                if (lane == 0)
-                    for (int u = 0; u < first; ++u) copy_x(u);
-                i = first;
-            }
-            for (; i < stages; ++i) {
+            for (int i = pass == 0 ? first_stages : 0; i < stages && !lost; ++i) {
                 const int n = step + i;
                 if (n >= ring && !mbar_wait_relaxed(empty0 + n % ring * 8, (n / ring - 1) & 1)) {
                     if (lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
                     break;
                 }
-                if (lane == 0) copy_a(i), copy_x(i);
+                if (lane == 0) copy_a(step, i, adapter), copy_x(step, i);
             }
         } else if (warp == 0) {
             // D = F32, A = B = BF16, both K-major, M = 128
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (((uint32_t)ranks16 >> 3) << 17) | ((128u >> 4) << 24);
             const uint32_t hi = (uint32_t)(smem_desc(0, 16, 1024, 2) >> 32), lo = (uint32_t)smem_desc(base, 16, 1024, 2);
-            for (int i = 0; i < stages; ++i) {
+            for (int i = 0; i < stages && !lost; ++i) {
                 const uint32_t n = step + i, slot = n % ring;
                 if (!mbar_wait_relaxed(full0 + slot * 8, (n / ring) & 1)) {
                     if (lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
@@ -415,21 +416,21 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
                 }
                 __syncwarp();
             }
-            if (elect_one()) tc_commit(done);
+            if (!lost && elect_one()) tc_commit(done);
             __syncwarp();
         } else {
             const int row = 32 * (warp & 3) + lane;
-            if (!mbar_wait_relaxed(done, pass & 1) && lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
+            if (!lost && !mbar_wait_relaxed(done, pass & 1) && lane == 0) atomicOr(&g_lora_status, 1u), *failed = 1;
             tc_fence_after();
             float *out = c.t + ((int64_t)blockIdx.y * c.M + row0 + row) * c.r;
-            const bool mine = owner[row] == adapter, lost = *failed != 0;
+            const bool mine = owner[row] == adapter, spoilt = *failed != 0;
             for (int n = 0; n < ranks16; n += 16) {
                 float d[16];
                 tc_load16(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + n, d);
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) {
                     if (!mine || n + j >= c.r) continue;
-                    const float poison = lost ? __uint_as_float(0x7FC00000u) : 0.f;
+                    const float poison = spoilt ? __uint_as_float(0x7FC00000u) : 0.f;
                     *reinterpret_cast<float4 *>(MXQ_AT(out + n + j, 16, c.t, (size_t)c.splits * c.M * c.r * 4)) =
                         make_float4(d[j] + poison, d[j + 1] + poison, d[j + 2] + poison, d[j + 3] + poison);
                 }
