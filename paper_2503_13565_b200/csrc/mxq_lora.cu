@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kMostSorted) lora_order_kernel(LoraCall c) {
     __shared__ uint32_t key[kMostSorted];
     __shared__ int32_t last[kMostSorted / 32], heads[kMostSorted / 32];
     const int i = threadIdx.x, warp = i >> 5, lane = i & 31;
-    pdl_wait();              // (and no early trigger: the kernels that follow read the plan ahead of their own waits)
+    pdl_wait();              // (no early trigger: the shrink has nothing to do ahead of the plan)
     uint32_t mine = 0xFFFFFFFFu;
     if (i < c.M) {
         const int a = (int)ld_dep_u32(MXQ_AT(c.ids + i, 4, c.ids, (size_t)c.M * 4));
@@ -109,18 +109,20 @@ __global__ void __launch_bounds__(kMostSorted) lora_order_kernel(LoraCall c) {
     if (i < c.M) *at(kPlanOrder + i) = (int32_t)(mine & (kMostSorted - 1));
     if (i == 0) *at(all) = c.M, *at(kPlanCount) = all;
 }
-// segment s as a window of one adapter
+// Segment s as a window of one adapter.  The plan is an earlier kernel's output, so this comes behind the wait; what is used as an index is
+// held to the call's rows and adapters, as ids are.  (s < most_segments <= 543: all places lie inside the plan.)
 __device__ __forceinline__ void load_segment(int32_t (&owner)[kWindowMost], int32_t (&row)[kWindowMost], int32_t &adapter, const LoraCall &c, int s) {
     auto at = [&](int place) { return (int)ld_dep_u32(MXQ_AT(c.plan + place, 4, c.plan, kPlanBytes)); };
-    const bool there = s < at(kPlanCount);
-    const int first = there ? at(s) : 0, rows = there ? at(s + 1) - first : 0, lane = threadIdx.x;
-    adapter = there ? at(kPlanAdapter + s) : -1;
+    const int lane = threadIdx.x, count = at(kPlanCount), begin = at(s), end = at(s + 1), a = at(kPlanAdapter + s);      // (four loads at once)
+    const bool there = s < count;
+    const int first = there ? min(max(begin, 0), c.M) : 0, rows = there ? min(min(end, c.M) - first, 16) : 0;
+    adapter = there && a < c.L ? max(a, -1) : -1;
     owner[lane] = lane < rows ? adapter : -1;
-    row[lane] = lane < rows ? at(kPlanOrder + first + lane) : -1;
+    row[lane] = lane < rows ? min(max(at(kPlanOrder + first + lane), 0), c.M - 1) : -1;
 }
 
 // filled by warp 0; the caller synchronises.  ids are read ahead of the wait for the previous kernel (they are the caller's, like the
-// weights).
+// weights); a plan is not (see load_segment).
 __device__ __forceinline__ void load_window(Window &w, const LoraCall &c, int row0, int rows) {
     if (threadIdx.x >= 32) return;
     const int lane = threadIdx.x;
@@ -197,9 +199,10 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
     uint4 *mine = ring + warp * c.stages * kPieces * 32 + lane;
     const uint32_t mine_address = shared_address(mine);
     const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2, t_bytes = (size_t)c.splits * c.M * c.r * 4;
+    bool waited = c.plan != nullptr;
+    if (waited) pdl_wait();
     load_window(win, c, blockIdx.x * kRows, kRows);      // this lane's rows: places g + 8 * j, j < 2 * MW
     __syncthreads();
-    bool waited = false;
     for (int at = blockIdx.y; at < win.count; at += c.slots) {
         const int adapter = win.list[at];
         bool own[2 * MW];
@@ -546,6 +549,7 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
     const int steps = (c.r + 15) / 16;
     const bool vec = c.N % 8 == 0;
     const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32, col = col0 + own_column(vec, t), n = (int64_t)c.M * c.N;
+    if (c.plan) pdl_wait();
     load_window(win, c, blockIdx.z * 16, 16);
     __syncthreads();
     const int adapter = (int)blockIdx.y < win.count ? win.list[blockIdx.y] : -2;
@@ -568,7 +572,7 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
         mine[h] = there > 0 && row >= 0 && (own[h] || (blockIdx.y == 0 && c.base != c.y && win.owner[8 * h + g] < 0));
         place[h] = (int64_t)row * c.N + col;
     }
-    pdl_wait();
+    if (!c.plan) pdl_wait();
     Columns ahead[2];                    // base, on its way while T is made ready
 #pragma unroll
     for (int h = 0; h < 2; ++h)
