@@ -461,8 +461,8 @@ int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *table
  * The MXFP8 pair: blocks of 32 along K, one E8M0 scale byte each (as in the MXFP4 pair: 2^(b-127), 0xFF = NaN), E4M3 elements in their
  * natural order: the scale is 2^(floor(log2 max|y|) - 8), never below 2^-127; elements divided by it are rounded to nearest even,
  * magnitudes above 448 clamp to 448.  A block with an Inf or NaN gets scale 0xFF and codes 0.
- * 1 <= M < 2^31, K a multiple of 32 up to MXQ_MAX_NORM_K, eps finite and >= 0.  Bit-reproducible run to run.  `weight` is read before
- * earlier calls of the library in the stream have ended (so are the adapters and ids below): it must not be their output. */
+ * 1 <= M < 2^31, K a multiple of 32 up to MXQ_MAX_NORM_K, eps finite and >= 0.  Bit-reproducible run to run.  `weight` is read while
+ * the kernels before the call may still run (see mxq_set_pdl): no kernel that is still in the stream may write it. */
 #define MXQ_MAX_NORM_K 32768
 int mxq_rmsnorm(const void *X, int x_dtype, int64_t x_stride, const void *residual, int r_dtype, void *residual_out, const void *weight,
                 int w_dtype, float eps, int64_t M, int64_t K, void *Y_bf16, uint8_t *codes, uint8_t *scales, void *stream);
@@ -544,8 +544,8 @@ int mxq_token_counts(uint32_t *counts, int64_t B, int64_t V, const int32_t *toke
  *   base [M][N] in Y's type (may be Y itself: added in place, rows without an adapter are then not touched), or NULL: zero
  *   Y [M][N] MXQ_F32, or MXQ_BF16 rounded to nearest even
  *   workspace  device memory, >= the *_workspace_bytes, 16-byte aligned, no initialisation needed; one per stream
- * adapters and ids are read while the previous call of this library in the stream may still run (see mxq_set_pdl), like the weights of
- * mxq_linear: that call must not write them.
+ * ids, X and base may be what any work before the call in the stream has written.  The adapters' A and B are weights like those of mxq_linear: they
+ * are read while the kernels before the call may still run (see mxq_set_pdl), so no kernel that is still in the stream may write them.
  * K a multiple of 32, any N, 1 <= M <= MXQ_LORA_MAX_M (mxq_lora) or MXQ_MAX_M.  Sums are FP32; A x meets B with all its bits for an FP32 Y, with 16
  * bits of mantissa for a BF16 Y:
  *     |Y - exact| <= ((K / 16 + 96) * 2^-22 [+ 2^-17, BF16]) * |s_a| sum_r |B_nr| sum_k |A_rk x_k| + 2^-23 |Y| + BF16's rounding.

@@ -121,8 +121,15 @@ __device__ __forceinline__ void load_segment(int32_t (&owner)[kWindowMost], int3
     row[lane] = lane < rows ? min(max(at(kPlanOrder + first + lane), 0), c.M - 1) : -1;
 }
 
-// filled by warp 0; the caller synchronises.  ids are read ahead of the wait for the previous kernel (they are the caller's, like the
-// weights); a plan is not (see load_segment).
+// the adapter of row m, -1: none, as there is none behind the last row (no branch: nothing waits for the load here)
+__device__ __forceinline__ int load_id(const LoraCall &c, int m) {
+    const int a = (int)ld_dep_u32(MXQ_AT(c.ids + min(m, c.M - 1), 4, c.ids, (size_t)c.M * 4));
+    return m < c.M && a < c.L ? max(a, -1) : -1;
+}
+// Filled by warp 0; the caller synchronises.  ids are a step's data, which whatever ran before in the stream may have written: a window that is
+// loaded ahead of the wait for the previous kernel is a guess, good for fetching weights early, and is compared with the ids behind the wait
+// (wrong_window) before anything is made of it.  One row beside 4096 x 4096: 9.8 us, 11.6 with nothing done ahead of the wait.  A plan is only read
+// behind it.
 __device__ __forceinline__ void load_window(Window &w, const LoraCall &c, int row0, int rows) {
     if (threadIdx.x >= 32) return;
     const int lane = threadIdx.x;
@@ -133,14 +140,19 @@ __device__ __forceinline__ void load_window(Window &w, const LoraCall &c, int ro
         return;
     }
     int a = -1;
-    if (lane < rows && row0 + lane < c.M) a = __ldg(MXQ_AT(c.ids + row0 + lane, 4, c.ids, (size_t)c.M * 4));
-    if (a >= c.L) a = -1;
-    w.owner[lane] = max(a, -1);
+    if (lane < rows) a = load_id(c, row0 + lane);
+    w.owner[lane] = a;
     w.row[lane] = lane < rows && row0 + lane < c.M ? row0 + lane : -1;
     const bool first = __ffs(__match_any_sync(0xffffffffu, a)) - 1 == lane && a >= 0;
     const unsigned firsts = __ballot_sync(0xffffffffu, first);
     if (first) w.list[__popc(firsts & ((1u << lane) - 1))] = a;
     if (lane == 0) w.count = __popc(firsts);
+}
+
+// A warp's look at the ids behind the wait: `id` loaded early, compared where the result is needed.  All warps of a CTA come to the same answer.
+__device__ __forceinline__ int window_id(const LoraCall &c, int row0, int rows) { return load_id(c, row0 + min((int)(threadIdx.x & 31), rows - 1)); }
+__device__ __forceinline__ bool wrong_window(const Window &w, int id, int rows) {
+    return __any_sync(0xffffffffu, id != w.owner[min((int)(threadIdx.x & 31), rows - 1)]);
 }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -199,11 +211,22 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
     uint4 *mine = ring + warp * c.stages * kPieces * 32 + lane;
     const uint32_t mine_address = shared_address(mine);
     const size_t a_bytes = (size_t)c.L * c.r * c.K * 2, x_bytes = (size_t)c.M * c.K * 2, t_bytes = (size_t)c.splits * c.M * c.r * 4;
-    bool waited = c.plan != nullptr;
-    if (waited) pdl_wait();
+    bool sure = c.plan != nullptr;
+    if (sure) pdl_wait();
     load_window(win, c, blockIdx.x * kRows, kRows);      // this lane's rows: places g + 8 * j, j < 2 * MW
     __syncthreads();
-    for (int at = blockIdx.y; at < win.count; at += c.slots) {
+    int id = -1;
+    auto again = [&]() {
+        __syncthreads();
+        load_window(win, c, blockIdx.x * kRows, kRows);
+        __syncthreads();
+    };
+    if (!sure && (int)blockIdx.y >= win.count) {
+        pdl_wait();
+        sure = true;
+        if (wrong_window(win, window_id(c, blockIdx.x * kRows, kRows), kRows)) again();
+    }
+    for (int at = blockIdx.y; at < win.count;) {
         const int adapter = win.list[at];
         bool own[2 * MW];
 #pragma unroll
@@ -229,13 +252,14 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
                 if (own[j]) xa[j] += 64 * WARPS;
             }
         };
-        // (the adapters' first steps are on their way before the previous kernel has ended)
+        // (the first adapter's first steps are on their way before the previous kernel has ended)
         for (int u = 0; u < c.stages && u < steps; ++u) copy_a(u);
-        if (!waited) pdl_wait(), waited = true;
+        if (!sure) pdl_wait();
         for (int u = 0; u < c.stages; ++u) {
             if (u < steps) copy_x(u);
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
+        if (!sure) id = window_id(c, blockIdx.x * kRows, kRows);
         float acc[MW][RT][4];
 #pragma unroll
         for (int w = 0; w < MW; ++w)
@@ -261,6 +285,13 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
             if (++slot == c.stages) slot = 0;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        if (!sure) {
+            sure = true;
+            if (wrong_window(win, id, kRows)) {
+                again();
+                continue;
+            }
+        }
         // the warps' parts of K, added in order, four ranks of a row per thread; the ring is free for them now
         __syncthreads();
         float *part = reinterpret_cast<float *>(ring);
@@ -294,8 +325,8 @@ __global__ void __launch_bounds__(32 * WARPS) lora_shrink_kernel(LoraCall c) {
             }
         }
         __syncthreads();
+        at += c.slots;
     }
-    if (!waited) pdl_wait();
 }
 
 // T = A x of many rows on the tensor memory path (K a multiple of 64): a window of 128 token rows is the first operand of tcgen05.mma (BF16, FP32
@@ -316,13 +347,13 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
     const uint32_t stage = kUmmaRows * kUmmaK * 2 + ranks16 * kUmmaK * 2, base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t full0 = base + ring * stage, empty0 = full0 + ring * 8, done = empty0 + ring * 8;
     const int k0 = blockIdx.y * (c.split_k / kUmmaK), stages = (int)min((int64_t)c.split_k / kUmmaK, c.K / kUmmaK - k0);
+    pdl_wait();              // (all wait here: the bounded waits below are for this kernel's own steps only)
     if (warp == 0) {         // the window's adapters, in ascending order
         uint32_t a[kUmmaRows / 32];
 #pragma unroll
         for (int j = 0; j < kUmmaRows / 32; ++j) {
             const int m = row0 + 32 * j + lane;
-            const int id = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
-            a[j] = id >= 0 && id < c.L ? (uint32_t)id : 0xFFFFFFFFu;
+            a[j] = (uint32_t)load_id(c, m);      // (-1 is the largest)
             owner[32 * j + lane] = (int32_t)a[j];
         }
         int n = 0;
@@ -348,10 +379,7 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    if ((int)blockIdx.z >= count) {
-        pdl_wait();
-        return;
-    }
+    if ((int)blockIdx.z >= count) return;
     const int first_stages = min(ring, stages);
     auto copy_a = [&](int step, int i, int adapter) {
         const uint32_t slot = (step + i) % ring;
@@ -362,14 +390,8 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
         const uint32_t slot = (step + i) % ring;
         tma_load_codes(base + slot * stage, &xmap, (k0 + i) * kUmmaK, row0, full0 + slot * 8);
     };
-    // the first adapter's first stages are on their way before the previous kernel has ended; X may be its output.  (All wait here: the bounded
-    // waits below are for this kernel's own steps only.)
-    if (warp == 1 && lane == 0)
-        for (int u = 0; u < first_stages; ++u) copy_a(0, u, list[blockIdx.z]);
-    __syncwarp();
-    pdl_wait();
-    if (warp == 1 && lane == 0)
-        for (int u = 0; u < first_stages; ++u) copy_x(0, u);
+    if (warp == 1 && lane == 0)      // the first adapter's first stages
+        for (int u = 0; u < first_stages; ++u) copy_a(0, u, list[blockIdx.z]), copy_x(0, u);
     __syncwarp();
     if (warp == 0) {         // (behind the wait: the previous kernel's CTAs may still want columns of their own before it)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&holder)), "r"(columns) : "memory");
@@ -540,7 +562,7 @@ __device__ __forceinline__ void unpack_columns(float (&f)[8], const Columns &c, 
 }
 
 // few rows: a CTA has one adapter of the window (there are as many slots as a window can have adapters)
-template <int KT, int WARPS>
+template <int KT, int WARPS, bool PLAN>
 __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
     extern __shared__ uint4 frag[];      // [steps][parts][32 lanes]: T as the product's first operand
     __shared__ Window win;
@@ -549,41 +571,49 @@ __global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
     const int steps = (c.r + 15) / 16;
     const bool vec = c.N % 8 == 0;
     const int64_t col0 = ((int64_t)blockIdx.x * WARPS + warp) * 32, col = col0 + own_column(vec, t), n = (int64_t)c.M * c.N;
-    if (c.plan) pdl_wait();
+    if (PLAN) pdl_wait();
     load_window(win, c, blockIdx.z * 16, 16);
     __syncthreads();
-    const int adapter = (int)blockIdx.y < win.count ? win.list[blockIdx.y] : -2;
+    int adapter;
     uint2 w[KT][4];                      // this warp's columns of B wait here for T
-    if (adapter >= 0) {
-#pragma unroll
-        for (int s = 0; s < KT; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (s < steps) w[s][i] = load_b(c, adapter, col0 + b_column(vec, g, i), s, t);
-    }
     // the rows that this CTA stores: its adapter's; the first slot also copies those without one, unless they are there already
     const int there = (int)max((int64_t)0, min((int64_t)32, c.N - col));
     bool own[2], mine[2];
     int64_t place[2];                    // of the columns in base and Y
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int row = win.row[8 * h + g];
-        own[h] = win.owner[8 * h + g] == adapter;
-        mine[h] = there > 0 && row >= 0 && (own[h] || (blockIdx.y == 0 && c.base != c.y && win.owner[8 * h + g] < 0));
-        place[h] = (int64_t)row * c.N + col;
-    }
-    if (!c.plan) pdl_wait();
     Columns ahead[2];                    // base, on its way while T is made ready
+    for (bool sure = PLAN;; sure = true) {           // (a second time where the guess was wrong)
+        adapter = (int)blockIdx.y < win.count ? win.list[blockIdx.y] : -2;
+        if (adapter >= 0) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-        if (c.base && vec && mine[h]) ahead[h] = load_ahead(c.base, c.base_f32, place[h], n);
-    if (adapter >= 0) {
-        for (int i = threadIdx.x; i < 16 * steps * 4; i += 32 * WARPS) {
-            const int quarter = i % (steps * 4), m = i / (steps * 4);       // ranks 4 * quarter .. + 3 of row m
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (win.owner[m] == adapter && 4 * quarter < c.r) sum_splits(v, c, win.row[m], 4 * quarter, adapter);
-            put_parts(frag + quarter / 4 * c.parts * 32, m, quarter % 4, v, c.parts);
+            for (int s = 0; s < KT; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (s < steps) w[s][i] = load_b(c, adapter, col0 + b_column(vec, g, i), s, t);
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = win.row[8 * h + g];
+            own[h] = win.owner[8 * h + g] == adapter;
+            mine[h] = there > 0 && row >= 0 && (own[h] || (blockIdx.y == 0 && c.base != c.y && win.owner[8 * h + g] < 0));
+            place[h] = (int64_t)row * c.N + col;
+        }
+        int id = -1;
+        if (!PLAN) pdl_wait(), id = window_id(c, blockIdx.z * 16, 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (c.base && vec && mine[h]) ahead[h] = load_ahead(c.base, c.base_f32, place[h], n);
+        if (adapter >= 0) {
+            for (int i = threadIdx.x; i < 16 * steps * 4; i += 32 * WARPS) {
+                const int quarter = i % (steps * 4), m = i / (steps * 4);       // ranks 4 * quarter .. + 3 of row m
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+                if (win.owner[m] == adapter && 4 * quarter < c.r) sum_splits(v, c, win.row[m], 4 * quarter, adapter);
+                put_parts(frag + quarter / 4 * c.parts * 32, m, quarter % 4, v, c.parts);
+            }
+        }
+        __syncthreads();
+        if (PLAN || sure || !wrong_window(win, id, 16)) break;
+        __syncthreads();
+        load_window(win, c, blockIdx.z * 16, 16);
         __syncthreads();
     }
     float acc[4][4];
@@ -625,18 +655,20 @@ __global__ void __launch_bounds__(256) lora_fragments_kernel(LoraCall c) {
     const int m = (int)(n / quarters), quarter = (int)(n - (int64_t)m * quarters);
     pdl_wait();
     if (m >= tiles * 16) return;
-    const int adapter = m < c.M ? __ldg(MXQ_AT(c.ids + m, 4, c.ids, (size_t)c.M * 4)) : -1;
+    const int adapter = load_id(c, m);
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (adapter >= 0 && adapter < c.L && 4 * quarter < c.r) sum_splits(v, c, m, 4 * quarter, adapter);
+    if (adapter >= 0 && 4 * quarter < c.r) sum_splits(v, c, m, 4 * quarter, adapter);
     put_parts(fragment(c, m / 16, quarter / 4), m % 16, quarter % 4, v, c.parts);
 }
 
 // grid (blocks of 256 columns, blocks of c.tiles tiles of rows); a warp takes 32 columns, whose B stays in registers while the adapter does, and
-// goes through the tiles; base and ids of the next tile are on their way meanwhile.  VEC: N is a multiple of 8.
+// goes through the tiles; base of the next tile or two is on its way meanwhile.  VEC: N is a multiple of 8.
+constexpr int kMostTiles = 24;
 template <int KT, bool F32, bool VEC>
 __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
     constexpr int kParts = F32 ? 3 : 2, kSize = F32 ? 4 : 2;
     extern __shared__ uint4 frag[];      // the rows' fragments of T
+    __shared__ int32_t owner[kMostTiles * 16];           // ... and their ids
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int64_t col0 = ((int64_t)blockIdx.x * 8 + warp) * 32, col = col0 + own_column(VEC, t), n = (int64_t)c.M * c.N;
@@ -651,20 +683,12 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
             for (int i = 0; i < 4; ++i)
                 if (s < steps) w[s][i] = load_b(c, adapter, col0 + b_column(VEC, g, i), s, t);
     };
-    // this lane's rows m, m + 8 of the tile whose ids and base are loaded next; `place` of its columns in base and Y
+    // this lane's rows m, m + 8 of the tile whose base is loaded next; `place` of its columns in base and Y
     int m = tile0 * 16 + g;
     int64_t place = (int64_t)m * c.N + col;
     const int64_t row8 = 8 * c.N;
     constexpr int kAhead = F32 ? 1 : 2;      // tiles whose base is on its way (the registers hold one of FP32)
-    int own[2], next_own[2];
     Columns base[2], next_base[2];
-    auto load_ids = [&](int (&own)[2]) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int a = m + 8 * h < c.M ? __ldg(MXQ_AT(c.ids + m + 8 * h, 4, c.ids, (size_t)c.M * 4)) : -1;
-            own[h] = a < c.L ? max(a, -1) : -1;
-        }
-    };
     auto load_base = [&](Columns (&base)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -686,16 +710,16 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
             }
         }
     };
-    load_ids(own);
-    int current = __reduce_max_sync(0xffffffffu, max(own[0], own[1]));
+    int current = __reduce_max_sync(0xffffffffu, load_id(c, tile0 * 16 + (lane & 15)));       // whose B is in the registers (a guess: see load_window)
     if (current >= 0) load(current);
     pdl_wait();
+    for (int i = threadIdx.x; i < tiles * 16; i += 256) owner[i] = load_id(c, tile0 * 16 + i);
     const int pieces = steps * kParts * 32;
     for (int i = threadIdx.x; i < tiles * pieces; i += 256)
         copy16(shared_address(frag + i), MXQ_AT(c.frag + (int64_t)tile0 * pieces + i, 16, c.frag, (size_t)all * pieces * 16), true);
     load_base(base);
     auto advance = [&]() { m += 16, place += 2 * row8; };
-    if (kAhead == 2) advance(), load_ids(next_own), load_base(next_base);      // (rows behind the last are not read)
+    if (kAhead == 2) advance(), load_base(next_base);      // (rows behind the last are not read)
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     if (col0 >= c.N) return;
@@ -707,16 +731,16 @@ __global__ void __launch_bounds__(256, 2) lora_expand_many_kernel(LoraCall c) {
         int left[2], none[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            left[h] = own[h], none[h] = own[h] < 0;
+            left[h] = owner[16 * tile + g + 8 * h], none[h] = left[h] < 0;
             unpack_columns(f[h], base[h], F32);
         }
         advance();
         if (kAhead == 2) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) own[h] = next_own[h], base[h] = next_base[h];
-            if (tile + 2 < tiles) load_ids(next_own), load_base(next_base);
+            for (int h = 0; h < 2; ++h) base[h] = next_base[h];
+            if (tile + 2 < tiles) load_base(next_base);
         } else if (tile + 1 < tiles) {
-            load_ids(own), load_base(base);
+            load_base(base);
         }
         int adapter = __reduce_max_sync(0xffffffffu, max(left[0], left[1]));
         while (adapter >= 0) {               // the tile's adapters, one after the other
@@ -847,12 +871,15 @@ static int shrink_by_rank(const LoraCall &c, cudaStream_t stream) {
     return c.r <= 16 ? shrink_launch<MW, WARPS, 2>(c, stream) : c.r <= 32 ? shrink_launch<MW, WARPS, 4>(c, stream) : shrink_launch<MW, WARPS, 8>(c, stream);
 }
 
+template <int WARPS, bool PLAN>
+static void (*few_kernel(int r))(LoraCall) {
+    return r <= 16 ? lora_expand_kernel<1, WARPS, PLAN> : r <= 32 ? lora_expand_kernel<2, WARPS, PLAN> : r <= 64 ? lora_expand_kernel<4, WARPS, PLAN> : lora_expand_kernel<8, WARPS, PLAN>;
+}
 static int expand_launch(const LoraCall &c, cudaStream_t stream) {
     constexpr int kWarps = 4;
     const dim3 grid((unsigned)((c.N + 32 * kWarps - 1) / (32 * kWarps)), (unsigned)c.slots, (unsigned)(c.plan ? most_segments(c) : 1));
     const size_t smem = (size_t)((c.r + 15) / 16) * c.parts * 32 * 16;
-    return launch_pdl(c.r <= 16 ? lora_expand_kernel<1, kWarps> : c.r <= 32 ? lora_expand_kernel<2, kWarps> : c.r <= 64 ? lora_expand_kernel<4, kWarps> : lora_expand_kernel<8, kWarps>,
-                      grid, 32 * kWarps, smem, stream, c);
+    return launch_pdl(c.plan ? few_kernel<kWarps, true>(c.r) : few_kernel<kWarps, false>(c.r), grid, 32 * kWarps, smem, stream, c);
 }
 
 template <bool F32, bool VEC>
@@ -873,7 +900,7 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     const int64_t columns = (c.N + 255) / 256, slots = 2 * (int64_t)sm_count();
     const size_t tile_bytes = (size_t)steps * c.parts * 512;
     int64_t least = 0;
-    for (int t = 4; t <= 24 && t * tile_bytes <= 100 * 1024; ++t) {
+    for (int t = 4; t <= kMostTiles && t * tile_bytes <= 100 * 1024; ++t) {
         const int64_t cost = (columns * ((tiles + t - 1) / t) + slots - 1) / slots * (t + 3);
         if (t == 4 || cost < least) least = cost, c.tiles = t;
     }
