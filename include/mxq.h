@@ -586,10 +586,13 @@ int mxq_linear_lora(const void *X_bf16, int M, const uint8_t *codes, const uint8
  *   store and nothing else.  The refused store is then in mxq_debug_bounds_report.
  * mxq_debug_kv_lost_tile: checked build only (otherwise MXQ_ERR_SHAPE), a test hook for the bounded waits of mxq_kv_attention: its
  *   NEXT call (one-shot) waits for tile `tile` (32 tokens) of sequence 0, kv head 0 without requesting it.  The call still completes
- *   within a few seconds, mxq_linear_device_status reports bit 29, and what the CTAs concerned had still to deliver is NaN.  -1 cancels. */
+ *   within a few seconds, mxq_linear_device_status reports bit 29, and what the CTAs concerned had still to deliver is NaN.  -1 cancels.
+ * mxq_debug_lora_lost_stage: the same for the adapters of many rows (mxq_lora where T is made by tcgen05): the next such call waits for columns
+ *   64 * stage .. of X's rows 0 .. 127 without requesting them; bit 30, and the rows among them whose adapters that CTA has are NaN. */
 int mxq_debug_bounds_report(uint64_t *report);
 int mxq_debug_bounds_selftest(void *stream);
 int mxq_debug_kv_lost_tile(int tile);
+int mxq_debug_lora_lost_stage(int stage);
 
 #ifdef __cplusplus
 }

@@ -13,6 +13,6 @@ from .binding import (MAX_M, MAX_T, MXQ_BF16, MXQ_F32, MxqError, mxq_accept_work
                       new_workspace, status_string, LinearBatch, IndependentBatches, mxq_linear_batch, mxq_set_linear_layout,
                       KVCache, mxq_kv_append, mxq_kv_attention, mxq_kv_attention_workspace_bytes, mxq_kv_compact, mxq_kv_fork,
                       mxq_kv_fork_workspace_bytes, mxq_kv_page_bytes, mxq_kv_read, mxq_kv_resize, mxq_debug_batch_fault, mxq_debug_bounds_report, mxq_debug_bounds_selftest,
-                      mxq_debug_kv_lost_tile, Rope, LogitRules, mxq_rmsnorm, mxq_dequantize_mxfp8, mxq_rope_table, mxq_kv_append_rope,
+                      mxq_debug_kv_lost_tile, mxq_debug_lora_lost_stage, Rope, LogitRules, mxq_rmsnorm, mxq_dequantize_mxfp8, mxq_rope_table, mxq_kv_append_rope,
                       mxq_logits_adjust, mxq_greedy_accept_rules, mxq_greedy_accept_rules_workspace_bytes, mxq_token_counts, mxq_lora,
                       mxq_lora_workspace_bytes, mxq_linear_lora, mxq_linear_lora_workspace_bytes)

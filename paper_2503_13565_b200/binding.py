@@ -122,6 +122,8 @@ def lib() -> ctypes.CDLL:
             L.mxq_kv_compact.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
             L.mxq_debug_kv_lost_tile.restype = i32
             L.mxq_debug_kv_lost_tile.argtypes = [i32]
+            L.mxq_debug_lora_lost_stage.restype = i32
+            L.mxq_debug_lora_lost_stage.argtypes = [i32]
             L.mxq_debug_batch_fault.restype = i32
             L.mxq_debug_batch_fault.argtypes = [i32, ctypes.c_uint]
             L.mxq_rmsnorm.restype = i32
@@ -1099,3 +1101,8 @@ def mxq_debug_batch_fault(unit: int, wait_us: int) -> None:
 def mxq_debug_kv_lost_tile(tile: int) -> None:
     """Test hook, checked build only: the next mxq_kv_attention call waits for a tile that nobody requested (see mxq.h)."""
     _check(lib().mxq_debug_kv_lost_tile(int(tile)), "mxq_debug_kv_lost_tile")
+
+
+def mxq_debug_lora_lost_stage(stage: int) -> None:
+    """Bounds-checked build only: the next mxq_lora whose A x is made by tcgen05 waits for one stage without requesting it (see mxq.h)."""
+    _check(lib().mxq_debug_lora_lost_stage(int(stage)), "mxq_debug_lora_lost_stage")

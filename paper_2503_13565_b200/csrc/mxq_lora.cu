@@ -17,6 +17,8 @@
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
 // 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
 // copy rate), the expansion the most of it (base and Y at 14 warps per SM, the legacy tensor pipe 27 % busy).
+#include <atomic>
+
 #include "mxq_device.cuh"
 #include "mxq_host.h"
 #include "mxq_tcgen05.cuh"
@@ -45,6 +47,7 @@ struct LoraCall {
     int32_t tiles;           // many rows: tiles of 16 rows per CTA of the expansion
     int32_t direct;          // many rows, K not split: the shrink writes the fragments itself
     int32_t *plan;           // segments of sorted rows (see lora_order_kernel), else nullptr
+    int32_t lost_stage;      // test hook: this stage of X is waited for by the first window's first CTA but never requested
 };
 
 struct Window {
@@ -388,6 +391,9 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
     };
     auto copy_x = [&](int step, int i) {
         const uint32_t slot = (step + i) % ring;
+#ifdef MXQ_DEBUG_BOUNDS
+        if (k0 + i == c.lost_stage && blockIdx.x == 0 && blockIdx.z == 0) return;
+#endif
         tma_load_codes(base + slot * stage, &xmap, (k0 + i) * kUmmaK, row0, full0 + slot * 8);
     };
     if (warp == 1 && lane == 0)      // the first adapter's first stages
@@ -404,6 +410,7 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
     volatile int32_t *failed = &fail;
 
     int step = 0;            // stages of all passes so far: the ring's state
+    int issued = first_stages;       // warp 1: stages requested
     for (int at = blockIdx.z, pass = 0; at < count; at += c.slots, ++pass, step += stages) {
         const int adapter = list[at];
         const bool lost = *failed != 0;          // (an earlier pass gave up: the others give NaN at once)
@@ -415,6 +422,7 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
                     break;
                 }
                 if (lane == 0) copy_a(step, i, adapter), copy_x(step, i);
+                issued = n + 1;
             }
         } else if (warp == 0) {
             // D = F32, A = B = BF16, both K-major, M = 128
@@ -465,6 +473,16 @@ lora_shrink_umma_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_c
         __syncthreads();     // the accumulator has been read
         tc_fence_after();
     }
+    // A pass that gave up may have left requests in flight, and the CTA must not end before they have landed: those that are complete are waited for
+    // (one that is not has a second in all), what else there may be is given time.
+    if (warp == 1 && lane == 0 && *failed) {
+        const uint64_t t0 = global_ns();
+        for (int n = max(0, issued - ring); n < issued; ++n)
+            while (!mbar_try_wait(full0 + n % ring * 8, (n / ring) & 1) && global_ns() - t0 < 1000000000ull) __nanosleep(200);
+        const uint64_t t1 = global_ns();
+        while (global_ns() - t1 < 100000ull) __nanosleep(1000);
+    }
+    __syncwarp();
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
 }
 
@@ -911,7 +929,13 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     return launch_pdl(kernel, grid, 256, smem, stream, c);
 }
 
-static int shrink_umma_launch(const LoraCall &c, cudaStream_t stream) {
+// test hook (mxq_debug_lora_lost_stage): consumed by the next launch
+[[maybe_unused]] static std::atomic<int> g_lost_stage{-1};
+
+static int shrink_umma_launch(LoraCall c, cudaStream_t stream) {
+#ifdef MXQ_DEBUG_BOUNDS
+    c.lost_stage = g_lost_stage.exchange(-1, std::memory_order_relaxed);
+#endif
     const int ranks16 = (c.r + 15) / 16 * 16, columns = ranks16 <= 32 ? 32 : ranks16 <= 64 ? 64 : 128;
     CUtensorMap xmap, amap;
     if (!encode_bf16_tensor_map(c.x, c.M, c.K, kUmmaRows, &xmap) || !encode_bf16_tensor_map(c.a, (int64_t)c.L * c.r, c.K, ranks16, &amap)) return MXQ_ERR_CUDA;
@@ -989,6 +1013,16 @@ int mxq_linear_lora(const void *X_bf16, int M, const uint8_t *codes, const uint8
     rc = mxq_linear(X_bf16, M, codes, scales, N, K, base, MXQ_F32, ws + t_bytes + sums, mxq::align256(mxq_linear_workspace_bytes(M, N, K)), stream);
     if (rc != MXQ_OK) return rc;
     return mxq::lora_expand(c, (cudaStream_t)stream);
+}
+
+int mxq_debug_lora_lost_stage(int stage) {
+#ifdef MXQ_DEBUG_BOUNDS
+    mxq::g_lost_stage.store(stage, std::memory_order_relaxed);
+    return MXQ_OK;
+#else
+    (void)stage;
+    return MXQ_ERR_SHAPE;
+#endif
 }
 
 #pragma GCC visibility pop
