@@ -28,6 +28,24 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
+// A map over a matrix of rows, 128-byte swizzled.  The driver's call wants a current context; a host thread that has made no call of the runtime
+// yet has none: its device's is made current then.
+CUresult encode_rows(EncodeTiledFn fn, CUtensorMap *out, CUtensorMapDataType type, const void *base, int64_t width, int64_t rows, int64_t row_bytes,
+                     int box_width, int box_rows) {
+    const cuuint64_t gdim[2] = {(cuuint64_t)width, (cuuint64_t)rows};
+    const cuuint64_t gstr[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)box_width, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    auto encode = [&] {
+        return fn(out, type, 2, const_cast<void *>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    int dev = 0;
+    if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) r = encode();
+    return r;
+}
+
 struct MapSlot {
     int dev;
     const void *ptr;
@@ -57,13 +75,8 @@ bool codes_tensor_map(const uint8_t *codes, int64_t N, int64_t K, bool expand_fp
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     // expanded: dimension 0 counts codes (the type packs two per byte); packed: dimension 0 counts bytes
-    const cuuint64_t gdim[2] = {(cuuint64_t)(expand_fp4 ? K : K / 2), (cuuint64_t)N};
-    const cuuint64_t gstr[1] = {(cuuint64_t)(K / 2)};
-    const cuuint32_t box[2] = {128, 128};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(&slot.map, expand_fp4 ? CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2,
-                          const_cast<uint8_t *>(codes), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const CUresult r = encode_rows(fn, &slot.map, expand_fp4 ? CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B : CU_TENSOR_MAP_DATA_TYPE_UINT8, codes,
+                                   expand_fp4 ? K : K / 2, N, K / 2, 128, 128);
     if (r != CUDA_SUCCESS) {
         if (std::getenv("MXQ_DEBUG"))
             std::fprintf(stderr, "mxq: tensor map encode failed (%d) for N=%lld K=%lld\n", (int)r, (long long)N, (long long)K);
@@ -83,13 +96,7 @@ bool codes_tensor_map(const uint8_t *codes, int64_t N, int64_t K, bool expand_fp
 bool encode_bf16_tensor_map(const void *base, int64_t rows, int64_t K, int box_rows, CUtensorMap *out) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    const cuuint64_t gdim[2] = {(cuuint64_t)K, (cuuint64_t)rows};
-    const cuuint64_t gstr[1] = {(cuuint64_t)(K * 2)};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), gdim, gstr, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const CUresult r = encode_rows(fn, out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, K, rows, K * 2, 64, box_rows);
     if (r != CUDA_SUCCESS && std::getenv("MXQ_DEBUG"))
         std::fprintf(stderr, "mxq: BF16 tensor map encode failed (%d) for rows=%lld K=%lld\n", (int)r, (long long)rows, (long long)K);
     return r == CUDA_SUCCESS;
