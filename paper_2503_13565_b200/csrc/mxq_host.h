@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/mxq.h"
 
 namespace mxq {
@@ -96,6 +98,21 @@ int bounds_take_norm(unsigned long long *out);          // mxq_norm.cu
 int bounds_take_kv_rope(unsigned long long *out);       // mxq_kv_rope.cu
 int bounds_take_logits(unsigned long long *out);        // mxq_logits.cu
 int bounds_take_lora(unsigned long long *out);          // mxq_lora.cu
+
+// Lets a kernel have up to `most` bytes of dynamic shared memory on the current device: its largest launch, once per device (`ready`, one per
+// kernel), and not a call's own size, which another host thread's smaller one would take back between this and the launch.
+template <class Kernel>
+int allow_smem(Kernel *kernel, size_t most, std::atomic<bool> (&ready)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return MXQ_ERR_CUDA;
+    if (ready[dev].load(std::memory_order_relaxed)) return MXQ_OK;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MXQ_ERR_CUDA;
+    }
+    ready[dev].store(true, std::memory_order_relaxed);
+    return MXQ_OK;
+}
 
 // launch with the programmatic-dependent-launch attribute (the kernel waits before it touches memory)
 template <class... P, class... A>

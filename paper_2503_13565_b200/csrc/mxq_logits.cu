@@ -519,6 +519,14 @@ static int check_logits(const void *logits, int dtype, int64_t B, int R, int64_t
     return aligned16(logits) ? MXQ_OK : MXQ_ERR_ALIGN;
 }
 
+constexpr size_t kLogitSmem = 73 * 1024;     // most of a CTA's tables
+template <typename T, bool WRITE, bool MASKED>
+static int rules_launch(const LogitCall &c, int64_t ctas, size_t smem, cudaStream_t stream) {
+    static std::atomic<bool> ready[64];
+    const int rc = allow_smem(logit_rules_kernel<T, WRITE, MASKED>, kLogitSmem, ready);
+    return rc != MXQ_OK ? rc : launch_pdl(logit_rules_kernel<T, WRITE, MASKED>, dim3((unsigned)ctas), kLogitThreads, smem, stream, c);
+}
+
 static int logits_launch(LogitCall &c, const void *logits, int dtype, int64_t B, int R, int64_t V, const int32_t *draft, int T,
                          const mxq_logit_rules *rules, cudaStream_t stream) {
     c.logits = logits, c.draft = draft, c.B = B, c.R = R, c.V = V, c.T = T, c.words = (V + 31) / 32;
@@ -532,7 +540,7 @@ static int logits_launch(LogitCall &c, const void *logits, int dtype, int64_t B,
     c.parts = 0;
     for (int parts = 1; parts <= 32 && parts <= row_batches; ++parts) {
         const size_t smem = SliceTables::bytes((int)(parts * (tokens + vec)), counting, c.J > 0);
-        if (smem > 73 * 1024) break;
+        if (smem > kLogitSmem) break;
         const int64_t slices = (row_batches + parts - 1) / parts;
         const int64_t groups = max((int64_t)1, min(2 * sms / (B * slices), (int64_t)R * parts / kLogitWarps)), rows = (R + groups - 1) / groups;
         const int64_t waves = (B * slices * ((R + rows - 1) / rows) + kLogitCtas * sms - 1) / (kLogitCtas * sms);
@@ -545,16 +553,10 @@ static int logits_launch(LogitCall &c, const void *logits, int dtype, int64_t B,
     const int64_t ctas = B * c.groups * c.slices;
     if (ctas > INT_MAX) return MXQ_ERR_SHAPE;
     const bool f32 = dtype == MXQ_F32, masked = c.allowed != nullptr;
-    void (*const kernel)(LogitCall) =
-        c.out ? (f32 ? (masked ? logit_rules_kernel<float, true, true> : logit_rules_kernel<float, true, false>)
-                     : (masked ? logit_rules_kernel<uint16_t, true, true> : logit_rules_kernel<uint16_t, true, false>))
-              : (f32 ? (masked ? logit_rules_kernel<float, false, true> : logit_rules_kernel<float, false, false>)
-                     : (masked ? logit_rules_kernel<uint16_t, false, true> : logit_rules_kernel<uint16_t, false, false>));
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return MXQ_ERR_CUDA;
-    }
-    return launch_pdl(kernel, dim3((unsigned)ctas), kLogitThreads, smem, stream, c);
+    return c.out ? (f32 ? (masked ? rules_launch<float, true, true>(c, ctas, smem, stream) : rules_launch<float, true, false>(c, ctas, smem, stream))
+                        : (masked ? rules_launch<uint16_t, true, true>(c, ctas, smem, stream) : rules_launch<uint16_t, true, false>(c, ctas, smem, stream)))
+                 : (f32 ? (masked ? rules_launch<float, false, true>(c, ctas, smem, stream) : rules_launch<float, false, false>(c, ctas, smem, stream))
+                        : (masked ? rules_launch<uint16_t, false, true>(c, ctas, smem, stream) : rules_launch<uint16_t, false, false>(c, ctas, smem, stream)));
 }
 
 }  // namespace mxq

@@ -17,8 +17,6 @@
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
 // 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
 // copy rate), the expansion the most of it (base and Y at 14 warps per SM, the legacy tensor pipe 27 % busy).
-#include <atomic>
-
 #include "mxq_device.cuh"
 #include "mxq_host.h"
 #include "mxq_tcgen05.cuh"
@@ -865,12 +863,7 @@ static LoraCall lora_call(const void *X, int64_t M, const mxq_lora_adapters *ad,
     return c;
 }
 
-// (48 KB, less the kernels' static shared memory, need no leave)
-static bool allow_smem(void (*kernel)(LoraCall), size_t smem) {
-    if (smem <= 40 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) == cudaSuccess) return true;
-    (void)cudaGetLastError();
-    return false;
-}
+constexpr size_t kShrinkSmem = 200 * 1024, kExpandSmem = 100 * 1024;      // most of a CTA of the shrink, of the expansion of many rows
 
 template <int MW, int WARPS, int RT>
 static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
@@ -879,9 +872,12 @@ static int shrink_launch(const LoraCall &c, cudaStream_t stream) {
     const size_t stage = (size_t)WARPS * (RT + 2 * MW) * 512, parts = (size_t)WARPS * kRows * c.r * 4;
     const int steps = (c.split_k + 32 * WARPS - 1) / (32 * WARPS);
     LoraCall call = c;
-    call.stages = max(1, min(min(kMostStages, steps), (int)(200 * 1024 / stage)));
+    call.stages = max(1, min(min(kMostStages, steps), (int)(kShrinkSmem / stage)));
     const size_t smem = max(stage * call.stages, parts);
-    if (!allow_smem(lora_shrink_kernel<MW, WARPS, RT>, smem)) return MXQ_ERR_CUDA;
+    static_assert((size_t)WARPS * kRows * 8 * RT * 4 <= kShrinkSmem && (size_t)WARPS * (RT + 2 * MW) * 512 <= kShrinkSmem, "");
+    static std::atomic<bool> ready[64];
+    const int rc = allow_smem(lora_shrink_kernel<MW, WARPS, RT>, kShrinkSmem, ready);
+    if (rc != MXQ_OK) return rc;
     return launch_pdl(lora_shrink_kernel<MW, WARPS, RT>, grid, 32 * WARPS, smem, stream, call);
 }
 template <int MW, int WARPS>
@@ -900,12 +896,16 @@ static int expand_launch(const LoraCall &c, cudaStream_t stream) {
     return launch_pdl(c.plan ? few_kernel<kWarps, true>(c.r) : few_kernel<kWarps, false>(c.r), grid, 32 * kWarps, smem, stream, c);
 }
 
-template <bool F32, bool VEC>
-static auto many_kernel_of(int r) -> void (*)(LoraCall) {
-    return r <= 16 ? lora_expand_many_kernel<1, F32, VEC> : r <= 32 ? lora_expand_many_kernel<2, F32, VEC> : r <= 64 ? lora_expand_many_kernel<4, F32, VEC> : lora_expand_many_kernel<8, F32, VEC>;
+template <int KT, bool F32, bool VEC>
+static int many_launch(const LoraCall &c, dim3 grid, size_t smem, cudaStream_t stream) {
+    static std::atomic<bool> ready[64];
+    const int rc = allow_smem(lora_expand_many_kernel<KT, F32, VEC>, kExpandSmem, ready);
+    return rc != MXQ_OK ? rc : launch_pdl(lora_expand_many_kernel<KT, F32, VEC>, grid, 256, smem, stream, c);
 }
-static void (*many_kernel(int r, bool f32, bool vec))(LoraCall) {
-    return f32 ? (vec ? many_kernel_of<true, true>(r) : many_kernel_of<true, false>(r)) : (vec ? many_kernel_of<false, true>(r) : many_kernel_of<false, false>(r));
+template <bool F32, bool VEC>
+static int many_by_rank(const LoraCall &c, dim3 grid, size_t smem, cudaStream_t stream) {
+    return c.r <= 16 ? many_launch<1, F32, VEC>(c, grid, smem, stream) : c.r <= 32 ? many_launch<2, F32, VEC>(c, grid, smem, stream)
+         : c.r <= 64 ? many_launch<4, F32, VEC>(c, grid, smem, stream) : many_launch<8, F32, VEC>(c, grid, smem, stream);
 }
 
 static int expand_many_launch(LoraCall c, cudaStream_t stream) {
@@ -918,15 +918,15 @@ static int expand_many_launch(LoraCall c, cudaStream_t stream) {
     const int64_t columns = (c.N + 255) / 256, slots = 2 * (int64_t)sm_count();
     const size_t tile_bytes = (size_t)steps * c.parts * 512;
     int64_t least = 0;
-    for (int t = 4; t <= kMostTiles && t * tile_bytes <= 100 * 1024; ++t) {
+    for (int t = 4; t <= kMostTiles && t * tile_bytes <= kExpandSmem; ++t) {
         const int64_t cost = (columns * ((tiles + t - 1) / t) + slots - 1) / slots * (t + 3);
         if (t == 4 || cost < least) least = cost, c.tiles = t;
     }
     const dim3 grid((unsigned)columns, (unsigned)((tiles + c.tiles - 1) / c.tiles));
     const size_t smem = c.tiles * tile_bytes;
-    void (*const kernel)(LoraCall) = many_kernel(c.r, c.y_f32 != 0, c.N % 8 == 0);
-    if (!allow_smem(kernel, smem)) return MXQ_ERR_CUDA;
-    return launch_pdl(kernel, grid, 256, smem, stream, c);
+    const bool vec = c.N % 8 == 0;
+    return c.y_f32 ? (vec ? many_by_rank<true, true>(c, grid, smem, stream) : many_by_rank<true, false>(c, grid, smem, stream))
+                   : (vec ? many_by_rank<false, true>(c, grid, smem, stream) : many_by_rank<false, false>(c, grid, smem, stream));
 }
 
 // test hook (mxq_debug_lora_lost_stage): consumed by the next launch
@@ -940,12 +940,11 @@ static int shrink_umma_launch(LoraCall c, cudaStream_t stream) {
     CUtensorMap xmap, amap;
     if (!encode_bf16_tensor_map(c.x, c.M, c.K, kUmmaRows, &xmap) || !encode_bf16_tensor_map(c.a, (int64_t)c.L * c.r, c.K, ranks16, &amap)) return MXQ_ERR_CUDA;
     // a ring that lets two CTAs share an SM where that leaves four stages (the prompt of rank 64: 47 -> 42 us; at rank 128 three stages cost 110 -> 125)
-    const int stage = kUmmaRows * kUmmaK * 2 + ranks16 * kUmmaK * 2, half = 105 * 1024 / stage, ring = min(min(8, c.split_k / kUmmaK), half >= 4 ? half : 200 * 1024 / stage);
+    const int stage = kUmmaRows * kUmmaK * 2 + ranks16 * kUmmaK * 2, half = 105 * 1024 / stage, ring = min(min(8, c.split_k / kUmmaK), half >= 4 ? half : (int)kShrinkSmem / stage);
     const size_t smem = 1024 + (size_t)ring * (stage + 16) + 8;
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(lora_shrink_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return MXQ_ERR_CUDA;
-    }
+    static std::atomic<bool> ready[64];
+    const int rc = allow_smem(lora_shrink_umma_kernel, 1024 + kShrinkSmem + 8 * 16 + 8, ready);
+    if (rc != MXQ_OK) return rc;
     const dim3 grid((unsigned)((c.M + kUmmaRows - 1) / kUmmaRows), (unsigned)c.splits, (unsigned)c.slots);
     return launch_pdl(lora_shrink_umma_kernel, grid, kUmmaThreads, smem, stream, xmap, amap, c, ring, ranks16, columns);
 }
