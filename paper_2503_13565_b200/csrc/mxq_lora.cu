@@ -577,9 +577,10 @@ __device__ __forceinline__ void unpack_columns(float (&f)[8], const Columns &c, 
     for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
 }
 
-// few rows: a CTA has one adapter of the window (there are as many slots as a window can have adapters)
+// Few rows: a CTA has one adapter of the window (there are as many slots as a window can have adapters).  At least four CTAs per SM (three of 128
+// ranks): left alone the compiler takes 158 registers for rank 32 (16 rows of 13 adapters, 11008 columns, beside the layer: 27.6 us, so 26.3).
 template <int KT, int WARPS, bool PLAN>
-__global__ void __launch_bounds__(32 * WARPS) lora_expand_kernel(LoraCall c) {
+__global__ void __launch_bounds__(32 * WARPS, KT <= 4 ? 4 : 3) lora_expand_kernel(LoraCall c) {
     extern __shared__ uint4 frag[];      // [steps][parts][32 lanes]: T as the product's first operand
     __shared__ Window win;
     pdl_trigger();
