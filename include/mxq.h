@@ -543,7 +543,8 @@ int mxq_token_counts(uint32_t *counts, int64_t B, int64_t V, const int32_t *toke
  *   X_bf16 [M][K] BF16;  ids int32 [M] (device), in any order (rows of one adapter next to one another are fastest)
  *   base [M][N] in Y's type (may be Y itself: added in place, rows without an adapter are then not touched), or NULL: zero
  *   Y [M][N] MXQ_F32, or MXQ_BF16 rounded to nearest even
- *   workspace  device memory, >= the *_workspace_bytes, 16-byte aligned, no initialisation needed; one per stream
+ *   workspace  device memory, >= the *_workspace_bytes, 16-byte aligned, no initialisation needed; one per stream.  The bytes never fall
+ *             where M grows and do not depend on the number of adapters: what the largest batch needs serves all
  * ids, X and base may be what any work before the call in the stream has written.  The adapters' A and B are weights like those of mxq_linear: they
  * are read while the kernels before the call may still run (see mxq_set_pdl), so no kernel that is still in the stream may write them.
  * K a multiple of 32, any N, 1 <= M <= MXQ_LORA_MAX_M (mxq_lora) or MXQ_MAX_M.  Sums are FP32; A x meets B with all its bits for an FP32 Y, with 16

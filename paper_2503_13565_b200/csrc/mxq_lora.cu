@@ -17,6 +17,8 @@
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
 // 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
 // copy rate), the expansion the most of it (base and Y at 14 warps per SM, the legacy tensor pipe 27 % busy).
+#include <algorithm>
+
 #include "mxq_device.cuh"
 #include "mxq_host.h"
 #include "mxq_tcgen05.cuh"
@@ -831,6 +833,12 @@ static void lora_plan(LoraCall &c) {
     c.split_k = (int32_t)len;
     c.splits = (int32_t)((c.K + len - 1) / len);
 }
+// Bound of splits x M: at least one split, at most kMostSplits of one stage each, and more than one only while all windows' (of up to 128 rows) find an SM
+// at once.
+static int64_t most_split_rows(int64_t M, int64_t K) {
+    const int64_t splits = min((int64_t)kMostSplits, (K + kUmmaK - 1) / kUmmaK);
+    return max(M, min(splits * M, (int64_t)kUmmaRows * sm_count()));
+}
 static size_t align256(size_t v) { return (v + 255u) & ~(size_t)255u; }
 static size_t sums_bytes(const LoraCall &c) { return align256((size_t)c.splits * (size_t)c.M * (size_t)c.r * 4); }
 
@@ -970,11 +978,10 @@ extern "C" {
 
 size_t mxq_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int rank, int adapters) {
     if (!mxq::lora_shape_ok(M, N, K, rank, adapters)) return 0;
-    mxq::LoraCall c = {};
-    c.M = (int32_t)M, c.N = N, c.K = K, c.r = rank, c.L = adapters;
-    mxq::lora_plan(c);
-    // [partial sums][fragments: three BF16 parts of 16-row tiles, or the plan of the segments]
-    return mxq::sums_bytes(c) + (mxq::many_rows(c) ? (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512 : mxq::few_rows(M) ? 0 : (size_t)mxq::kPlanBytes);
+    // [partial sums][fragments: three BF16 parts of 16-row tiles, or the plan of the segments].  What a call takes depends on its path and falls where
+    // windows grow; this is a bound for all of them that never falls from M to M + 1, so that the workspace of the largest batch serves all.
+    const size_t fragments = (size_t)((M + 15) / 16) * ((rank + 15) / 16) * 3 * 512;
+    return mxq::align256((size_t)mxq::most_split_rows(M, K) * rank * 4) + (mxq::few_rows(M) ? 0 : std::max(fragments, (size_t)mxq::kPlanBytes));
 }
 
 int mxq_lora(const void *X_bf16, int64_t M, const mxq_lora_adapters *adapters, const int32_t *ids, int64_t N, int64_t K, const void *base,
