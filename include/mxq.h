@@ -452,7 +452,8 @@ int mxq_kv_compact(const mxq_kv_cache *cache, int B, int M, const int32_t *table
 /* ---- what a decoder step needs between its linear layers and its cache --------------------------------------------------------- */
 
 /* Root-mean-square norm with the residual's addition:  h = x + residual,  y = h / sqrt(mean(h^2) + eps) * w,  row by row, all in FP32
- * (the norm is that of the unrounded h; rows whose squares sum to more than FLT_MAX give 0, rows with a NaN NaN).
+ * (the norm is that of the unrounded h, whatever its size: squares that FP32 does not hold are summed in other units.  A row with a NaN is NaN; in
+ * one with an Inf that element is NaN and the others 0; a row of zeros with eps = 0 is NaN).
  *   X [M][K], rows x_stride elements apart (>= K, rows 16-byte aligned), MXQ_F32 or MXQ_BF16 (x_dtype)
  *   residual [M][K] in r_dtype, or NULL;  residual_out [M][K] in r_dtype receives h, or NULL (may be residual itself)
  *   weight [K] in w_dtype

@@ -116,7 +116,43 @@ __global__ void __launch_bounds__(kNormMaxThreads) rmsnorm_kernel(NormCall c) {
     __syncthreads();
     const int warps = threads >> 5;
     sq = warp_sum((threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f);
-    const float scale = 1.0f / sqrtf(sq / (float)c.K + c.eps);
+    float mean = sq / (float)c.K + c.eps;
+    // The rare row (the same for the whole CTA) whose squares overflow, or vanish beside an eps that does not cover them: once more, with h and
+    // eps in units of the power of two at the larger of max |h| and sqrt(eps).  (From 2^-100 on what a sum loses below FP32's least is 2^-35 of it.)
+    if (sq > 3.402823466e38f || (sq < 0x1p-100f && c.eps < 0x1p-100f)) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int ch = threadIdx.x + j * threads;
+            if (ch >= chunks) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(h[j][i]) & 0x7FFFFFFFu);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        __syncthreads();                     // (the sums have been read)
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = __uint_as_float(top);
+        __syncthreads();
+        top = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < warps ? __float_as_uint(part[threadIdx.x & 31]) : 0u);
+        const uint32_t unit = max(top, __float_as_uint(sqrtf(c.eps))) >> 23;
+        if (unit != 0xFFu) {                 // (a row with an Inf stays as it is)
+            // 2^(127 - unit), from the subnormal 2^-127 to 2^126
+            const float to = unit >= 254u ? 0x1p-127f : __uint_as_float((254u - max(unit, 1u)) << 23);
+            sq = 0.f;
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                const int ch = threadIdx.x + j * threads;
+                if (ch >= chunks) continue;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[j][i] *= to, sq = fmaf(h[j][i], h[j][i], sq);
+            }
+            sq = warp_sum(sq);
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sq;
+            __syncthreads();
+            mean = warp_sum((threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f) / (float)c.K + c.eps * to * to;
+        }
+    }
+    const float scale = 1.0f / sqrtf(mean);
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
         const int ch = threadIdx.x + j * threads;
