@@ -13,10 +13,10 @@
 //
 // A CTA takes a window of token rows and one adapter, or several one after the other: rows that have another one are left out (zero in the
 // product, not stored).
-// Measured in a replayed graph: one row, rank 16, beside 4096x4096: 9.7 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
+// Measured in a replayed graph: one row, rank 16, beside 4096x4096: 10.1 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
-// 64 rows of 32 adapters, rank 64, 11008x4096: 34 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
-// copy rate), the expansion the most of it (base and Y at 14 warps per SM, the legacy tensor pipe 27 % busy).
+// 64 rows of 32 adapters, rank 64, 11008x4096: 35 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
+// copy rate), the expansion the most of it: it waits for base at 14 warps per SM, the legacy tensor pipe is 29 % busy.
 #include <algorithm>
 
 #include "mxq_device.cuh"
@@ -809,13 +809,17 @@ int lora_take_status(uint32_t *out) {
 // Up to 16 rows: one window, a CTA of both kernels for each of its adapters.  Up to 511: sorted into segments (see lora_order_kernel).  More, and
 // from 64 rows on with 48 rows and more per adapter: windows of rows as they come, in a prompt mostly of one adapter, with a second CTA where
 // two meet; T's fragments are made once (256 rows of four adapters, rank 128, 11008 outputs: sorted 46 us, so 30; 128 rows of eight, rank 64, 4096
-// outputs: 16, 23).
+// outputs: 16, 23).  What the host knows is the number of adapters that are loaded, not those of the batch: all of these had every loaded adapter among
+// their rows.  Where many more are loaded the way is that of few rows per adapter (400 rows of one adapter, rank 128, 11008 outputs: 22 us of one
+// loaded, 27 of eight, 63 to 69 of nine and more).  From 512 rows on nothing sorts: a tile of 16 rows repeats its product for each adapter that it has
+// (4095 rows of 32 adapters, rank 64, 4096 outputs: 44 us in order, 409 in random order; 512 rows 24, 178).
 constexpr int kMostSplits = 16;
 constexpr int kFewWarps = 8, kManyWarps = 16;     // of a CTA of the shrink (above rank 64 sixteen warps' sums do not fit the registers)
 static bool many_rows(const LoraCall &c) { return c.M >= kMostSorted || (c.M >= 64 && c.M >= 48 * (int64_t)c.L); }
 static bool few_rows(int64_t M) { return M <= 16; }
 // The tensor memory path reads a window's 128 rows once for each of its adapters: for adapters of 80 rows and more on average (512 rows of six,
-// 4096 inputs, rank 64: 23 -> 18 us; 1500 rows of twenty, rank 16: 20 -> 24).
+// 4096 inputs, rank 64: 23 -> 18 us; 1500 rows of twenty, rank 16: 20 -> 24).  By the adapters loaded, as above: 4095 rows of six, rank 64, take 42 us
+// of six loaded and 55 of 52 and more.
 static bool by_umma(const LoraCall &c) { return many_rows(c) && c.M >= 80 * (int64_t)c.L && c.K % kUmmaK == 0 && c.K <= 0x3FFFFFFF && tensor_map_available(); }
 static int64_t most_segments(const LoraCall &c) { return c.M / 16 + min(c.L + 1, c.M); }
 
