@@ -15,8 +15,8 @@
 // a (row, token) pair per thread.  (With the rules inside the stream, a lane's special tokens one after the other, accept over 24 x 8 rows of
 // 128256 took 107 us unrolled, the code leaving the instruction cache, and 37 in a loop, the batches of the frequent tokens last.)
 // Measured in a replayed graph: accept over 24 sequences x 8 rows x 128256 BF16 logits with histories, 200 biases and masks 30 us (65 MB: 10 us at
-// the copy rate), 12 us without rules, which is what mxq_greedy_accept takes; masks add 5 us, biases 3, penalties 9.  Neither memory (1.7 TB/s) nor
-// the issue slots (half of them idle) are full: tables, stream, list and the special tokens come one after the other in a CTA, with barriers between.
+// the copy rate), 12 us without rules, which is what mxq_greedy_accept takes; masks add 5 us, biases 3, penalties 9.  Neither memory (1.9 TB/s) nor
+// the issue slots (45 %) are full: tables, stream, list and the special tokens come one after the other in a CTA, with barriers between.
 // One sequence of 9 x 32000: 6.1 us, a chain of five dependent trips to memory; adjust over 48 x 32001 FP32 logits: 9.2 us (18 MB), the same
 // order of steps for one row.
 #include <limits.h>

@@ -16,7 +16,7 @@
 // Measured in a replayed graph: one row, rank 16, beside 4096x4096: 10.1 us (the 4-bit layer alone 5.8); 16 rows of 13 adapters, rank 32,
 // beside 11008x4096: 26 us (the layer alone 14; the shrink before it and the expansion behind it are a chain of dependent loads each);
 // 64 rows of 32 adapters, rank 64, 11008x4096: 35 us; a prompt of 4095 rows of six adapters, rank 64, 4096x4096: 41 us (107 MB: 16 us at the
-// copy rate), the expansion the most of it: it waits for base at 14 warps per SM, the legacy tensor pipe is 29 % busy.
+// copy rate), the expansion the most of it: it waits for base at 15 warps per SM, the legacy tensor pipe is 29 % busy.
 #include <algorithm>
 
 #include "mxq_device.cuh"

@@ -5,7 +5,7 @@
 //
 // A stream: every input is read once and every output written once; a row stays in the registers of one CTA between the sum of its
 // squares and its scaling.  Measured in a replayed graph (BF16 stream with the residual read and written, BF16 result): 8000 rows of 4096 41.7 us,
-// 6.3 TB/s = 96 % of the copy rate; 8191 rows of 8192 88.5 us (93 %), with the pair beside it 108 us (86 %: the cast's instructions, 63 % of the
+// 6.3 TB/s = 96 % of the copy rate; 8191 rows of 8192 88.5 us (93 %), with the pair beside it 108 us (86 %: the cast's instructions, 61 % of the
 // issue slots, and two CTAs per SM that meet at a barrier each; 104 without the look for rows in other units); one row of 4096 1.5 us, the
 // launch's own time.  All of it is FP32; what is rounded is what is stored (h and y to BF16 where that is their type, y to E4M3).  The norm is that of
 // the unrounded h.
